@@ -14,6 +14,8 @@
  *                                       inference forward runs on the scaled FP4 matrix instruction
  *   attnqat_quantize_mxfp8, attnqat_fwd_infer_mx_fp8pv   the mixed recipe: FP4 Q K^T, FP8 P V
  *   attnqat_kv_cache_*, attnqat_fwd_infer_mx_paged       an FP4 KV cache in pages and the forward over it
+ *   attnqat_page_plan, attnqat_kv_cache_append, attnqat_kv_cache_read, attnqat_fwd_kv4_ragged
+ *                                       a serving step of sequences with different numbers of new positions, over an NVFP4 cache
  *   attnqat_fwd_infer_mx_sparse                          block-sparse attention
  *
  * Conventions shared by every entry point
@@ -401,6 +403,64 @@ int attnqat_debug_fwd_infer_paged(const void* q, int B, int Hq, int Hkv, int Lq,
                                   const void* cache, int num_pages, const int* page_table, int max_pages, const int* kv_lens,
                                   void* o, float* lse, void* workspace, size_t workspace_bytes, void* stream,
                                   int spin_limit, int* wait_expired);
+
+/*
+ * A serving step over the NVFP4 cache whose sequences bring different numbers of new positions (prompts, pieces of prompts, single tokens, drafted
+ * tokens), without a host that knows their lengths: every length, page id and slot is read on the device, so that one captured graph serves
+ * all steps of its sizes.  The new positions of a step are one run of T rows, sequence after sequence; sequence b has rows cu_q[b] .. cu_q[b+1]-1.
+ * A slot is page * 128 + position within the page.  Rows come as [T, heads, d] bf16 with d innermost and any stride per row and per head (in
+ * elements, multiples of 8; pointers 16-byte aligned), such as the views of one projection's output; T = 0 is accepted and does nothing (the plan: no
+ * slots).  At most 65535 sequences of 8192 pages (2^20 positions) each: ATTNQAT_ESHAPE beyond.
+ *
+ * attnqat_page_plan makes page table, slots and positions of a step.  Request b has kv_lens[b] positions and wants new_lens[b] (device int32 [B]):
+ * more (the step's new positions), as many, or fewer (drafted tokens taken back, 0: a request that has ended).  Pages that it needs come out of
+ * the ring free_pages (device int32 [num_free_slots], at least as many places as the cache has pages that the ring may come to hold):
+ * free_state[0] is the place of the first free page, free_state[1] their number, and they follow each other around the ring.  Pages that a request no
+ * longer needs go behind them, in the order of the requests, and may be taken from the next call on.  page_table (device int32
+ * [B, max_pages]) gets the new pages; its other entries stay as they are (those of pages given back, too).
+ * A request is refused, and keeps what it had, if it wants more than max_pages * 128 positions, if its new positions do not end within
+ * the first T of the step, or if the pages that requests 0 .. b ask for are more than were free.
+ * kv_lens_out[b]      new_lens[b], or kv_lens[b] where the request was refused (may be kv_lens itself)
+ * cu_q[B+1]           sums of the new positions that requests ask for (also of refused ones, except those that want more than their row of the
+ *                     page table holds), at most T
+ * slots[T]            int64: where a row's position lies; -1 for rows of refused requests, for rows behind cu_q[B], and where the page table has a
+ *                     negative entry
+ * positions[T]        a row's position in its sequence; 0 behind cu_q[B]
+ * free_state_out[3]   place of the first free page, number of free pages, number of refused requests (may be free_state, then of 3 ints)
+ * free_pages = NULL (num_free_slots 0; free_state and free_state_out unused): the table is complete already, no pages are taken or given back.
+ * Lengths outside [0, max_pages * 128] count as the nearest inside (new_lens above it: refused).  Deterministic.  Workspace:
+ * attnqat_page_plan_workspace_bytes(B), 16-byte aligned.
+ *
+ * attnqat_kv_cache_append quantizes row t of k and v (Hkv heads) into slot slots[t], as attnqat_kv_cache_write does, and writes nothing else.  A slot
+ * outside [0, num_pages * 128) is left out.  Slots must differ from each other: of two rows with one slot either may be found there, block by block.
+ *
+ * attnqat_kv_cache_read is the way back: row t of k and v becomes the values (exact in bf16) that slot slots[t] holds, zeros for a slot outside
+ * the cache.
+ *
+ * attnqat_fwd_kv4_ragged: O = softmax(scale Q K^T + mask) V, K and V being the values that the pages hold: only the cache is in 4 bits.  Q is not
+ * quantized, nor are the probabilities (which are rounded to fp16 for their product with V; scores, sums and O are fp32), as for a
+ * model that was not trained for Alg. 1; attnqat_fwd_infer_paged is Alg. 1.  q [T,Hq,d]; sequence b has kv_lens[b] keys, the last of which belong to
+ * its rows: row i of n sees keys 0 .. kv_lens[b] - n + i with causal != 0, of those the last `window` if window > 0 (causal only), and all keys with
+ * causal = 0.  max_q: no sequence has more rows (rows beyond are left out).  A row without a key gets o = 0, lse = -inf.  o [T,Hq,d] bf16; lse
+ * [T,Hq] fp32 (natural log), may be NULL; rows behind cu_q[B] are left as they are.  o and lse must not lie over q.  scale > 0.
+ * Positions of a page table entry outside [0, num_pages) read as zeros; positions from kv_lens[b] on are never used, whatever their slots
+ * hold.  Workspace: attnqat_kv4_ragged_workspace_bytes(), 16-byte aligned.
+ */
+size_t attnqat_page_plan_workspace_bytes(int B);
+int attnqat_page_plan(const int* kv_lens, const int* new_lens, int B, int* page_table, int max_pages,
+                      int* free_pages, int num_free_slots, const int* free_state, int T,
+                      int* kv_lens_out, int* cu_q, int64_t* slots, int* positions, int* free_state_out,
+                      void* workspace, size_t workspace_bytes, void* stream);
+int attnqat_kv_cache_append(const void* k, int64_t k_token_stride, int64_t k_head_stride, const void* v, int64_t v_token_stride, int64_t v_head_stride,
+                            int T, int Hkv, int d, int dtype, void* cache, int num_pages, const int64_t* slots, void* stream);
+int attnqat_kv_cache_read(const void* cache, int num_pages, const int64_t* slots, int T, int Hkv, int d, int dtype,
+                          void* k, int64_t k_token_stride, int64_t k_head_stride, void* v, int64_t v_token_stride, int64_t v_head_stride, void* stream);
+size_t attnqat_kv4_ragged_workspace_bytes(int T, int B, int Hq, int Hkv, int max_q, int max_pages, int d);
+int attnqat_fwd_kv4_ragged(const void* q, int64_t q_token_stride, int64_t q_head_stride, const int* cu_q, int T, int max_q,
+                           int B, int Hq, int Hkv, int d, int causal, int window, float scale, int dtype,
+                           const void* cache, int num_pages, const int* page_table, int max_pages, const int* kv_lens,
+                           void* o, int64_t o_token_stride, int64_t o_head_stride, float* lse,
+                           void* workspace, size_t workspace_bytes, void* stream);
 
 /*
  * Block-sparse attention (Sec. 5: the paper's datacenter inference kernel supports it): attnqat_fwd_infer_mx with a

@@ -21,7 +21,7 @@ BF16 = 0
 (WS_FWD, WS_FWD_INFER, WS_BWD, WS_FWD_INFER_MX, WS_FWD_MX, WS_BWD_MX, WS_FWD_INFER_MX_FP8PV,
  WS_FWD_INFER_MX_PAGED, WS_FWD_INFER_MX_SPARSE) = 0, 1, 2, 3, 4, 5, 6, 7, 8
 
-_vp, _i, _sz = ctypes.c_void_p, ctypes.c_int, ctypes.c_size_t
+_vp, _i, _sz, _ll, _f = ctypes.c_void_p, ctypes.c_int, ctypes.c_size_t, ctypes.c_int64, ctypes.c_float
 _SIGNATURES = {
     "attnqat_quantize": (_i, [_vp, _i, _i, _i, _i, _i, _vp, _vp, _vp, _vp]),
     "attnqat_fwd": (_i, [_vp, _vp, _vp, _i, _i, _i, _i, _i, _i, _i, _vp, _vp, _vp, _vp, _sz, _vp]),
@@ -51,6 +51,13 @@ _SIGNATURES = {
     "attnqat_paged_workspace_bytes": (_sz, [_i, _i, _i, _i, _i, _i]),
     "attnqat_fwd_infer_paged": (_i, [_vp, _i, _i, _i, _i, _i, _i, _i, _vp, _i, _vp, _i, _vp, _vp, _vp, _vp, _sz, _vp]),
     "attnqat_debug_fwd_infer_paged": (_i, [_vp, _i, _i, _i, _i, _i, _i, _i, _vp, _i, _vp, _i, _vp, _vp, _vp, _vp, _sz, _vp, _i, _vp]),
+    "attnqat_page_plan_workspace_bytes": (_sz, [_i]),
+    "attnqat_page_plan": (_i, [_vp, _vp, _i, _vp, _i, _vp, _i, _vp, _i, _vp, _vp, _vp, _vp, _vp, _vp, _sz, _vp]),
+    "attnqat_kv_cache_append": (_i, [_vp, _ll, _ll, _vp, _ll, _ll, _i, _i, _i, _i, _vp, _i, _vp, _vp]),
+    "attnqat_kv_cache_read": (_i, [_vp, _i, _vp, _i, _i, _i, _i, _vp, _ll, _ll, _vp, _ll, _ll, _vp]),
+    "attnqat_kv4_ragged_workspace_bytes": (_sz, [_i, _i, _i, _i, _i, _i, _i]),
+    "attnqat_fwd_kv4_ragged": (_i, [_vp, _ll, _ll, _vp, _i, _i, _i, _i, _i, _i, _i, _i, _f, _i, _vp, _i, _vp, _i, _vp, _vp, _ll, _ll, _vp,
+                                    _vp, _sz, _vp]),
     "attnqat_fwd_infer_mx_sparse": (_i, [_vp, _vp, _vp, _i, _i, _i, _i, _i, _i, _i, _vp, _vp, _vp, _vp, _sz, _vp]),
     "attnqat_fwd_mx": (_i, [_vp, _vp, _vp, _i, _i, _i, _i, _i, _i, _i, _vp, _vp, _vp, _vp, _sz, _vp]),
     "attnqat_bwd_mx": (_i, [_vp, _vp, _vp, _vp, _vp, _vp, _i, _i, _i, _i, _i, _i, _i,
@@ -255,6 +262,141 @@ def attnqat_fwd_infer_paged(q, cache, num_pages, page_table, kv_lens, Hkv, causa
     _check(lib().attnqat_fwd_infer_paged(_ptr(q), B, Hq, Hkv, Lq, d, int(causal), BF16, _ptr(cache), int(num_pages),
                                          _ptr(page_table), max_pages, _ptr(kv_lens),
                                          _ptr(o), _ptr(lse), _ptr(workspace), workspace.numel(), _stream()))
+    return o, lse
+
+
+def _serve_int(t, name, shape, dtype=torch.int32):
+    if not (t.is_cuda and t.dtype == dtype and t.is_contiguous() and tuple(t.shape) == tuple(shape)):
+        raise AttnQatError(f"{name} must be a contiguous {dtype} CUDA tensor of shape {tuple(shape)}")
+
+
+def _serve_rows(t, name, shape=None):
+    if not (t.is_cuda and t.dtype == torch.bfloat16 and t.dim() == 3 and (t.stride(2) == 1 or t.numel() == 0)
+            and (shape is None or tuple(t.shape) == tuple(shape))):
+        raise AttnQatError(f"{name} must be a bf16 CUDA tensor [T,heads,d]{'' if shape is None else ' of shape ' + str(tuple(shape))}, d innermost")
+    return t.data_ptr(), t.stride(0), t.stride(1)
+
+
+def _serve_cache(cache, num_pages, Hkv, d):
+    if not (cache.is_cuda and cache.dtype == torch.uint8 and cache.is_contiguous()):
+        raise AttnQatError("cache must be a contiguous uint8 CUDA tensor")
+    page = kv_cache_page_bytes_nvfp4(Hkv, d)
+    have = cache.numel() // page if page else 0
+    if num_pages is None:
+        num_pages = have
+    if page and not 0 < num_pages <= have:
+        raise AttnQatError(f"cache has room for {have} pages, not for {num_pages}")
+    return int(num_pages)
+
+
+def _same_device(*tensors):
+    """The kernels run on the current device's current stream."""
+    now = torch.cuda.current_device()
+    if any(t is not None and t.device.index != now for t in tensors):
+        raise AttnQatError(f"all tensors must be on the current device (cuda:{now})")
+
+
+def page_plan_workspace_bytes(B: int) -> int:
+    return lib().attnqat_page_plan_workspace_bytes(B)
+
+
+def attnqat_page_plan(kv_lens, new_lens, page_table, capacity: int, free=None, workspace=None, out=None):
+    """Page table, slots and positions of a serving step.  kv_lens, new_lens int32 [B]: positions that the requests have and want;
+    page_table int32 [B,max_pages], updated in place; ``capacity`` the most new positions of the step; ``free`` = (free_pages int32 [places],
+    free_state int32 [>= 2]: place of the first free page, number of free pages), a ring from which pages are taken (updated in place) and to which they
+    are given back, or None for a table that is complete already.  Returns (kv_lens int32 [B], cu_q int32 [B+1], slots int64 [capacity], positions int32
+    [capacity], free_state int32 [3]: first free place, free pages, refused requests, or None without ``free``).  ``out``: those five; the first and the
+    last may be kv_lens and a free_state of 3."""
+    B, T = kv_lens.numel(), int(capacity)
+    _serve_int(kv_lens, "kv_lens", (B,))
+    _serve_int(new_lens, "new_lens", (B,))
+    if page_table.dim() != 2:
+        raise AttnQatError("page_table must be [B,max_pages]")
+    _serve_int(page_table, "page_table", (B, page_table.shape[1]))
+    if T < 0:
+        raise AttnQatError("capacity must not be negative")
+    ring, state = (None, None) if free is None else free
+    if free is not None:
+        _serve_int(ring, "free_pages", (ring.numel(),))
+        if state.dim() != 1 or state.numel() < 2:
+            raise AttnQatError("free_state must have at least two elements")
+        _serve_int(state, "free_state", (state.numel(),))
+    if out is None:
+        e = lambda n, t=torch.int32: torch.empty(n, dtype=t, device=kv_lens.device)  # noqa: E731
+        out = (e(B), e(B + 1), e(T, torch.int64), e(T), e(3) if free is not None else None)
+    lens, cu, slots, positions, state_out = out
+    _serve_int(lens, "out[0]", (B,))
+    _serve_int(cu, "out[1]", (B + 1,))
+    _serve_int(slots, "out[2]", (T,), torch.int64)
+    _serve_int(positions, "out[3]", (T,))
+    if free is not None:
+        _serve_int(state_out, "out[4]", (3,))
+    _same_device(kv_lens, new_lens, page_table, ring, state, *out, workspace)
+    if workspace is None:
+        workspace = torch.empty(max(page_plan_workspace_bytes(B), 1), dtype=torch.uint8, device=kv_lens.device)
+    _check(lib().attnqat_page_plan(_ptr(kv_lens), _ptr(new_lens), B, _ptr(page_table), page_table.shape[1], _ptr(ring), 0 if ring is None else ring.numel(),
+                                   _ptr(state), T, _ptr(lens), _ptr(cu), _ptr(slots), _ptr(positions), _ptr(state_out) if free is not None else None,
+                                   _ptr(workspace), workspace.numel(), _stream()))
+    return lens, cu, slots, positions, state_out if free is not None else None
+
+
+def attnqat_kv_cache_append(k, v, cache, slots, num_pages=None):
+    """Quantize row t of k, v [T,Hkv,d] bf16 (any stride per row and head) into slot ``slots[t]`` (int64 [T], page * 128 + position within the page; slots
+    outside the cache are left out) of the NVFP4 KV ``cache`` (uint8 CUDA tensor)."""
+    kp, vp = _serve_rows(k, "k"), _serve_rows(v, "v", k.shape)
+    T, Hkv, d = k.shape
+    _serve_int(slots, "slots", (T,), torch.int64)
+    num_pages = _serve_cache(cache, num_pages, Hkv, d)
+    _same_device(k, v, cache, slots)
+    _check(lib().attnqat_kv_cache_append(*kp, *vp, T, Hkv, d, BF16, _ptr(cache), num_pages, _ptr(slots), _stream()))
+
+
+def attnqat_kv_cache_read(cache, slots, Hkv: int, d: int, num_pages=None, out=None):
+    """The values that the NVFP4 KV ``cache`` holds in ``slots`` (int64 [T]; zeros for a slot outside the cache).  Returns (k, v) bf16
+    [T,Hkv,d]; ``out``: those two, of any stride per row and head."""
+    T = slots.numel()
+    _serve_int(slots, "slots", (T,), torch.int64)
+    num_pages = _serve_cache(cache, num_pages, Hkv, d)
+    k, v = out if out is not None else tuple(torch.empty((T, Hkv, d), dtype=torch.bfloat16, device=cache.device) for _ in range(2))
+    kp, vp = _serve_rows(k, "out[0]", (T, Hkv, d)), _serve_rows(v, "out[1]", (T, Hkv, d))
+    _same_device(cache, slots, k, v)
+    _check(lib().attnqat_kv_cache_read(_ptr(cache), num_pages, _ptr(slots), T, Hkv, d, BF16, *kp, *vp, _stream()))
+    return k, v
+
+
+def kv4_ragged_workspace_bytes(T: int, B: int, Hq: int, Hkv: int, max_q: int, max_pages: int, d: int) -> int:
+    return lib().attnqat_kv4_ragged_workspace_bytes(T, B, Hq, Hkv, max_q, max_pages, d)
+
+
+def attnqat_fwd_kv4_ragged(q, cu_q, cache, num_pages, page_table, kv_lens, Hkv: int, causal: bool, max_q=None, window: int = 0, scale=None,
+                           workspace=None, out=None):
+    """Attention over an NVFP4 KV cache, Q and the probabilities not quantized, of sequences with different numbers of queries.  q [T,Hq,d] bf16 (any stride
+    per row and head), rows cu_q[b] .. cu_q[b+1]-1 (int32 [B+1]) being the last positions of sequence b, which has kv_lens[b] keys (int32 [B]) in the
+    pages page_table[b] (int32 [B,max_pages]).  ``max_q``: the most rows of a sequence (default T); ``window`` (causal only): a row sees that many keys at
+    most, its own position included; ``scale``: default 1/sqrt(d).  Returns (o bf16 [T,Hq,d], lse fp32 [T,Hq]); ``out``: those two (lse may be None)."""
+    qp = _serve_rows(q, "q")
+    T, Hq, d = q.shape
+    B = kv_lens.numel()
+    _serve_int(kv_lens, "kv_lens", (B,))
+    _serve_int(cu_q, "cu_q", (B + 1,))
+    if page_table.dim() != 2:
+        raise AttnQatError("page_table must be [B,max_pages]")
+    _serve_int(page_table, "page_table", (B, page_table.shape[1]))
+    num_pages = _serve_cache(cache, num_pages, Hkv, d)
+    if out is None:
+        out = (torch.empty((T, Hq, d), dtype=torch.bfloat16, device=q.device), torch.empty((T, Hq), dtype=torch.float32, device=q.device))
+    o, lse = out
+    op = _serve_rows(o, "out[0]", (T, Hq, d))
+    if lse is not None:
+        _serve_int(lse, "out[1]", (T, Hq), torch.float32)
+    _same_device(q, cu_q, cache, page_table, kv_lens, o, lse, workspace)
+    max_q = max(T, 1) if max_q is None else int(max_q)
+    max_pages = page_table.shape[1]
+    if workspace is None:
+        workspace = torch.empty(max(kv4_ragged_workspace_bytes(T, B, Hq, Hkv, max_q, max_pages, d), 1), dtype=torch.uint8, device=q.device)
+    _check(lib().attnqat_fwd_kv4_ragged(*qp, _ptr(cu_q), T, max_q, B, Hq, Hkv, d, int(causal), int(window),
+                                        1.0 / d ** 0.5 if scale is None else float(scale), BF16, _ptr(cache), num_pages, _ptr(page_table), max_pages,
+                                        _ptr(kv_lens), *op, _ptr(lse), _ptr(workspace), workspace.numel(), _stream()))
     return o, lse
 
 

@@ -567,6 +567,128 @@ int paged_common(const void* q, int B, int Hq, int Hkv, int Lq, int d, int causa
 }
 }  // namespace
 
+namespace {
+// Rows [T, heads, d] as a caller passes them: strides in elements (of an axis of one element any); what is read may repeat rows, what is
+// written may not.
+bool rows_of(const void* p, int64_t token, int64_t head, int T, int heads, int d, bool written, Rows& r)
+{
+    if (T == 1) token = 0;
+    if (heads == 1) head = 0;
+    if (((uintptr_t)p & 15) || token < 0 || head < 0 || token % 8 != 0 || head % 8 != 0) return false;
+    if (token > (1ll << 46) / T || head > (1ll << 46) / heads) return false;                  // (more than any memory)
+    r = Rows{const_cast<void*>(p), (size_t)token, (size_t)head};
+    if (!written) return true;
+    const int64_t across = (int64_t)(heads - 1) * head + d, along = (int64_t)(T - 1) * token + d;
+    return (heads == 1 || head >= d) && (T == 1 || token >= d) && (T == 1 || heads == 1 || token >= across || head >= along);
+}
+size_t rows_extent(const Rows& r, int T, int heads, int d) { return 2 * ((size_t)(T - 1) * r.token + (size_t)(heads - 1) * r.head + d); }
+constexpr int kMaxServeBatch = 65535, kMaxServePages = 1 << 13;      // sequences of a step, pages of a sequence
+}  // namespace
+
+size_t attnqat_page_plan_workspace_bytes(int B) { return B < 1 || B > kMaxServeBatch ? 0 : align_up(page_plan_ws_bytes(B)); }
+
+int attnqat_page_plan(const int* kv_lens, const int* new_lens, int B, int* page_table, int max_pages,
+                      int* free_pages, int num_free_slots, const int* free_state, int T,
+                      int* kv_lens_out, int* cu_q, int64_t* slots, int* positions, int* free_state_out,
+                      void* workspace, size_t workspace_bytes, void* stream)
+{
+    if (!kv_lens || !new_lens || !page_table || !kv_lens_out || !cu_q || B < 1 || max_pages < 1 || T < 0) return ATTNQAT_EINVAL;
+    if (T > 0 && (!slots || !positions)) return ATTNQAT_EINVAL;
+    if (free_pages ? !free_state || !free_state_out || num_free_slots < 1 : num_free_slots != 0) return ATTNQAT_EINVAL;
+    if ((uintptr_t)slots & 7) return ATTNQAT_EINVAL;
+    if (B > kMaxServeBatch || max_pages > kMaxServePages) return ATTNQAT_ESHAPE;
+    if (overlap(cu_q, (size_t)(B + 1) * 4, kv_lens, (size_t)B * 4) || overlap(cu_q, (size_t)(B + 1) * 4, new_lens, (size_t)B * 4)) return ATTNQAT_EINVAL;
+    if (!workspace || ((uintptr_t)workspace & 15) || workspace_bytes < page_plan_ws_bytes(B)) return ATTNQAT_EWORKSPACE;
+    hipStream_t st = (hipStream_t)stream;
+    prof_begin(st);
+    if (launch_page_plan(kv_lens, new_lens, B, page_table, max_pages, free_pages, free_pages ? num_free_slots : 0, free_state, T,
+                         kv_lens_out, cu_q, (long long*)slots, positions, free_state_out, workspace, st)) return ATTNQAT_ELAUNCH;
+    prof_mark("page_plan", st);
+    return ATTNQAT_OK;
+}
+
+namespace {
+int rows_common(const void* k, int64_t k_token, int64_t k_head, const void* v, int64_t v_token, int64_t v_head, int T, int Hkv, int d, int dtype,
+                const void* cache, int num_pages, const int64_t* slots, bool written, Rows& kr, Rows& vr)
+{
+    if (T < 0 || Hkv < 1 || num_pages < 1) return ATTNQAT_EINVAL;
+    if (dtype != ATTNQAT_BF16) return ATTNQAT_EDTYPE;
+    if ((d != 64 && d != 128) || Hkv > 65535) return ATTNQAT_ESHAPE;
+    if (T == 0) return ATTNQAT_OK;
+    if (!k || !v || !cache || !slots || ((uintptr_t)cache & 15) || ((uintptr_t)slots & 7)) return ATTNQAT_EINVAL;
+    if (!rows_of(k, k_token, k_head, T, Hkv, d, written, kr) || !rows_of(v, v_token, v_head, T, Hkv, d, written, vr)) return ATTNQAT_EINVAL;
+    return ATTNQAT_OK;
+}
+}  // namespace
+
+int attnqat_kv_cache_append(const void* k, int64_t k_token_stride, int64_t k_head_stride, const void* v, int64_t v_token_stride, int64_t v_head_stride,
+                            int T, int Hkv, int d, int dtype, void* cache, int num_pages, const int64_t* slots, void* stream)
+{
+    Rows kr, vr;
+    int rc = rows_common(k, k_token_stride, k_head_stride, v, v_token_stride, v_head_stride, T, Hkv, d, dtype, cache, num_pages, slots, false, kr, vr);
+    if (rc || T == 0) return rc;
+    hipStream_t st = (hipStream_t)stream;
+    prof_begin(st);
+    if (launch_kv_append(kr, vr, T, Hkv, d, cache, num_pages, (const long long*)slots, st)) return ATTNQAT_ELAUNCH;
+    prof_mark("kv_cache_append", st);
+    return ATTNQAT_OK;
+}
+
+int attnqat_kv_cache_read(const void* cache, int num_pages, const int64_t* slots, int T, int Hkv, int d, int dtype,
+                          void* k, int64_t k_token_stride, int64_t k_head_stride, void* v, int64_t v_token_stride, int64_t v_head_stride, void* stream)
+{
+    Rows kr, vr;
+    int rc = rows_common(k, k_token_stride, k_head_stride, v, v_token_stride, v_head_stride, T, Hkv, d, dtype, cache, num_pages, slots, true, kr, vr);
+    if (rc || T == 0) return rc;
+    hipStream_t st = (hipStream_t)stream;
+    prof_begin(st);
+    if (launch_kv_read(kr, vr, T, Hkv, d, cache, num_pages, (const long long*)slots, st)) return ATTNQAT_ELAUNCH;
+    prof_mark("kv_cache_read", st);
+    return ATTNQAT_OK;
+}
+
+namespace {
+int ragged_dims(int T, int B, int Hq, int Hkv, int max_q, int max_pages, int d)
+{
+    if (T < 0 || B < 1 || Hq < 1 || Hkv < 1 || max_q < 1 || max_pages < 1) return ATTNQAT_EINVAL;
+    if ((d != 64 && d != 128) || Hq % Hkv != 0 || Hkv > 65535 || B > kMaxServeBatch || max_pages > kMaxServePages) return ATTNQAT_ESHAPE;
+    if ((long long)T * Hq > (1 << 28)) return ATTNQAT_ESHAPE;
+    return ATTNQAT_OK;
+}
+}  // namespace
+
+size_t attnqat_kv4_ragged_workspace_bytes(int T, int B, int Hq, int Hkv, int max_q, int max_pages, int d)
+{
+    if (ragged_dims(T, B, Hq, Hkv, max_q, max_pages, d)) return 0;
+    return ragged_ws_bytes(T, B, Hq, Hkv, max_q, max_pages, d);
+}
+
+int attnqat_fwd_kv4_ragged(const void* q, int64_t q_token_stride, int64_t q_head_stride, const int* cu_q, int T, int max_q,
+                           int B, int Hq, int Hkv, int d, int causal, int window, float scale, int dtype,
+                           const void* cache, int num_pages, const int* page_table, int max_pages, const int* kv_lens,
+                           void* o, int64_t o_token_stride, int64_t o_head_stride, float* lse,
+                           void* workspace, size_t workspace_bytes, void* stream)
+{
+    int rc = ragged_dims(T, B, Hq, Hkv, max_q, max_pages, d);
+    if (rc) return rc;
+    if (dtype != ATTNQAT_BF16) return ATTNQAT_EDTYPE;
+    if (num_pages < 1 || window < 0 || (window > 0 && !causal) || !(scale > 0.0f) || !(scale < INFINITY)) return ATTNQAT_EINVAL;
+    if (T == 0) return ATTNQAT_OK;
+    if (!q || !cu_q || !cache || !page_table || !kv_lens || !o || ((uintptr_t)cache & 15)) return ATTNQAT_EINVAL;
+    Rows qr, out;
+    if (!rows_of(q, q_token_stride, q_head_stride, T, Hq, d, false, qr) || !rows_of(o, o_token_stride, o_head_stride, T, Hq, d, true, out)) return ATTNQAT_EINVAL;
+    const size_t nq = rows_extent(qr, T, Hq, d), no = rows_extent(out, T, Hq, d);
+    if (overlap(q, nq, o, no) || (lse && (overlap(q, nq, lse, (size_t)T * Hq * 4) || overlap(o, no, lse, (size_t)T * Hq * 4)))) return ATTNQAT_EINVAL;
+    if (!workspace || ((uintptr_t)workspace & 15) || workspace_bytes < ragged_ws_bytes(T, B, Hq, Hkv, max_q, max_pages, d)) return ATTNQAT_EWORKSPACE;
+    hipStream_t st = (hipStream_t)stream;
+    prof_begin(st);
+    const RaggedArgs a{(const uint16_t*)q, qr.token, qr.head, cu_q, T, max_q, (const unsigned char*)cache, num_pages, page_table, max_pages, kv_lens,
+                       B, Hq, Hkv, causal != 0, window, scale * 1.4426950408889634f, (uint16_t*)o, out.token, out.head, lse};
+    if (launch_ragged(a, d, workspace, st)) return ATTNQAT_ELAUNCH;
+    prof_mark("fwd_kv4_ragged", st);
+    return ATTNQAT_OK;
+}
+
 size_t attnqat_paged_workspace_bytes(int B, int Hq, int Hkv, int Lq, int max_pages, int d)
 {
     if (check_dims(B, Hq, Hkv, Lq, d, ATTNQAT_BF16) || max_pages < 1 || max_pages > (1 << 13)) return 0;

@@ -68,6 +68,31 @@ size_t nvfp4_page_bytes(int Hkv, int D);
 int launch_kv_page_write(const void* k, const void* v, int Hkv, int n, int D, int pos0,
                          void* cache, int num_pages, const int* page_ids, hipStream_t st);
 
+// A serving step's page table and slot map (serve.hip; arguments as attnqat_page_plan; ring_size 0: no ring).  ws: page_plan_ws_bytes() bytes.
+size_t page_plan_ws_bytes(int B);
+int launch_page_plan(const int* kv_lens, const int* new_lens, int B, int* page_table, int max_pages, int* ring, int ring_size, const int* ring_state,
+                     int T, int* kv_out, int* cu, long long* slots, int* positions, int* state_out, void* ws, hipStream_t st);
+
+// Rows [T, heads, D] bf16 with a stride in elements per token and per head, d innermost.
+struct Rows { void* p; size_t token, head; };
+// The rows of K and V into their slots of the NVFP4 pages, and back.
+int launch_kv_append(const Rows& k, const Rows& v, int T, int Hkv, int D, void* cache, int num_pages, const long long* slots, hipStream_t st);
+int launch_kv_read(const Rows& k, const Rows& v, int T, int Hkv, int D, const void* cache, int num_pages, const long long* slots, hipStream_t st);
+
+// Attention over the NVFP4 pages without any further quantization, sequence b with the queries cu_q[b] .. cu_q[b + 1] - 1 of T (ragged.hip).
+struct RaggedArgs {
+    const uint16_t* q; size_t q_token, q_head;
+    const int* cu_q; int T, max_q;
+    const unsigned char* cache; int num_pages;
+    const int* table; int max_pages; const int* kv_lens;
+    int B, Hq, Hkv, causal, window /* 0: none */;
+    float c;                                     // log2(e) times the factor of the scores
+    uint16_t* o; size_t o_token, o_head;
+    float* lse;                                  // [T, Hq], or null
+};
+size_t ragged_ws_bytes(int T, int B, int Hq, int Hkv, int max_q, int max_pages, int D);
+int launch_ragged(const RaggedArgs& a, int D, void* ws, hipStream_t st);
+
 // Alg. 1 for decode steps over the NVFP4 pages: at most decode_max_rows() query rows per (sequence, kv head), i.e.
 // (Hq / Hkv) * Lq of them; q [B*Hkv, (Hq/Hkv)*Lq, D] (the rows of a kv group are neighbours in [B,Hq,Lq,d]); qh: scratch for
 // phi(Q), [B*Hkv][128][D] fp16.  ws: decode_ws_bytes() bytes.  spin_limit bounds the polls of a chunk waiting for the row maxima

@@ -106,4 +106,15 @@ __device__ __forceinline__ void phi_half_blocks(uint4v& a, uint4v& b)
     }
 }
 
+// The NVFP4 KV cache: a page holds 128 consecutive positions of one sequence for all kv heads; per kv head, in this order,
+// K codes [128][D/2], K scale bytes [128][D/16], V codes [128][D/2], V scale bytes [128][D/16]: the public layout of
+// attnqat_quantize cut into pages.  Blocks run along d, so positions are independent of each other: a sequence grows by
+// writing its new positions only.
+__host__ __device__ inline size_t nvfp4_page_head_bytes(int D) { return (size_t)2 * 128 * (D / 2 + D / 16); }
+// Codes and scale byte of block cb of position l (nullptr for a page id outside the cache).
+__device__ inline const unsigned char* nvfp4_page_part(const unsigned char* cache, int page, int num_pages, int Hkv, int h, int D, int which) {
+    if (page < 0 || page >= num_pages) return nullptr;
+    return cache + ((size_t)page * Hkv + h) * nvfp4_page_head_bytes(D) + (size_t)which * 128 * (D / 2 + D / 16);
+}
+
 }  // namespace aq
