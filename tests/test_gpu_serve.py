@@ -291,6 +291,20 @@ def test_queries_far_from_one(aq, q_scale):
     run_attention(aq, [1, 20], [200, 300], 4, 2, 128, scale=1e-31 if q_scale > 1 else None, seed=3, q_scale=q_scale)
 
 
+def test_nan_stays_in_its_row(aq):
+    for n, G in (([1, 3], 4), ([60, 40], 2)):
+        q, cu, cache, num_pages, table = attention_case(n, [300, 200], 2 * G, 2, 128, 1, tail=0)
+        args = (i32(cu), dev(cache.reshape(-1)), num_pages, dev(table), i32([300, 200]), 2, True)
+        qd = q.cuda()
+        o, lse = aq.attnqat_fwd_kv4_ragged(qd, *args)
+        qn = qd.clone()
+        qn[1, 3, 17] = float("nan")
+        on, ln = aq.attnqat_fwd_kv4_ragged(qn, *args)
+        assert bool(on[1, 3].isnan().all()) and bool(ln[1, 3].isnan())
+        on[1, 3], ln[1, 3] = o[1, 3], lse[1, 3]
+        assert torch.equal(on, o) and torch.equal(ln, lse)
+
+
 def test_rows_beyond_max_q_are_left_out(aq):
     q, cu, cache, num_pages, table = attention_case([5, 2], [300, 20], 4, 2, 64, 1)
     o, lse = torch.full((7, 4, 64), 5.0, dtype=torch.bfloat16, device="cuda"), torch.full((7, 4), 5.0, device="cuda")
