@@ -19,7 +19,7 @@ namespace aq {
 namespace {
 
 constexpr int kFewRows = 32;          // most rows of a (sequence, kv head) that the kernel for few rows takes
-constexpr int kWideRows = 128;        // rows of a tile of the other one
+constexpr int kWideRows = 256;        // rows of a tile of the other one
 
 struct Seq { int first, n, len; };    // first query of the step, number of queries, keys
 __device__ inline Seq seq_of(const RaggedArgs& a, int b)
@@ -36,6 +36,13 @@ __device__ inline void keys_of(const RaggedArgs& a, const Seq& s, int ta, int tb
     hi = max(lo, hi);
 }
 
+// A value that all lanes have, told to the compiler.
+__device__ inline int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
+__device__ inline long long uniform(long long v)
+{
+    return (long long)((unsigned long long)(uint32_t)__builtin_amdgcn_readfirstlane((int)(v >> 32)) << 32 | (uint32_t)__builtin_amdgcn_readfirstlane((int)v));
+}
+
 // The units of work of the kernel for few rows: the pages that the rows of a sequence see, once per kv head, sequence by sequence, head by head, page by
 // page.  Sequences with more rows than `most` have none here.
 struct Few { int rows, first_page, pages; };
@@ -49,39 +56,25 @@ __device__ inline Few few_of(const RaggedArgs& a, int b, int G, int most)
     return Few{rows, lo >> 7, on ? ((hi + 127) >> 7) - (lo >> 7) : 0};
 }
 
-// Sums over a workgroup of 256: inclusive, and of all.
-__device__ inline int wg_scan256(int v, int* red /* [4], LDS */, int& total)
+__device__ inline Seq uniform(const Seq& s) { return Seq{uniform(s.first), uniform(s.n), uniform(s.len)}; }
+__device__ inline Few uniform(const Few& u) { return Few{uniform(u.rows), uniform(u.first_page), uniform(u.pages)}; }
+
+// Sums over a workgroup of W waves: inclusive, and of all.
+template <int W, class T>
+__device__ inline T wg_scan(T v, T* red /* [W], LDS */, T& total)
 {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
 #pragma unroll
-    for (int d = 1; d < 64; d <<= 1) { const int u = __shfl_up(v, d); if (lane >= d) v += u; }
-    __syncthreads();
+    for (int d = 1; d < 64; d <<= 1) { const T u = __shfl_up(v, d); if (lane >= d) v += u; }
+    __syncthreads();                                             // (red of the call before has been read)
     if (lane == 63) red[wave] = v;
     __syncthreads();
-    total = (red[0] + red[1]) + (red[2] + red[3]);
-    return v + (wave > 0 ? red[0] : 0) + (wave > 1 ? red[1] : 0) + (wave > 2 ? red[2] : 0);
-}
-
-// The tile number `item` of the step: sequence by sequence, each with ceil(n G / kWideRows) tiles, none where the kernel for few rows (at most `few`)
-// takes it.  By a workgroup of 256; false behind the last one.
-__device__ inline bool find_tile(const RaggedArgs& a, int G, int few, int item, int& b_out, int& tile_out, int* lds /* [8] */)
-{
-    const int tid = threadIdx.x;
-    if (tid == 0) lds[4] = -1;
-    for (int b0 = 0; b0 < a.B; b0 += 256) {
-        const int b = b0 + tid;
-        const long long rows = b < a.B ? (long long)seq_of(a, b).n * G : 0;
-        const int tiles = rows > few ? (int)((rows + kWideRows - 1) / kWideRows) : 0;
-        int total;
-        const int upto = wg_scan256(tiles, lds, total);
-        if (item < upto && item >= upto - tiles) { lds[4] = b; lds[5] = item - (upto - tiles); }
-        if (item < total) break;
-        item -= total;
-    }
-    __syncthreads();
-    b_out = __builtin_amdgcn_readfirstlane(lds[4]);
-    tile_out = __builtin_amdgcn_readfirstlane(lds[5]);
-    return b_out >= 0;
+    total = 0;
+    T front = 0;
+#pragma unroll
+    for (int w = 0; w < W; ++w) { front += w < wave ? red[w] : T(0); total += red[w]; }
+    total = uniform(total);
+    return v + front;
 }
 
 // Codes and scale bytes of D / 4 values of one key: lane (key cc of 16, group g) holds d = (D/4) g .. + D/4 - 1.
@@ -139,7 +132,7 @@ template <int D, int RT /* 16-row groups of a unit */>
 __global__ __launch_bounds__(256, RT == 1 ? 3 : 2) void ragged_few_kernel(const RaggedArgs a, const FewWs ws)
 {
     constexpr int NS = D / 32, NDT = D / 16, ROWS = 16 * RT;
-    constexpr int RS = 2 * D + 16;                                // bytes per key of the V tile
+    constexpr int RS = 2 * D + 32;                                // bytes per key of the V tile (four keys side by side in other banks)
     constexpr size_t VOFF = (size_t)128 * (D / 2 + D / 16);
     __shared__ __align__(16) unsigned char stage[4 * 32 * RS];     // per wave: V of 32 keys [key][d]; at the end the waves' sums [4][16][D]
     __shared__ float ml[2][4][ROWS];
@@ -155,7 +148,7 @@ __global__ __launch_bounds__(256, RT == 1 ? 3 : 2) void ragged_few_kernel(const 
     int all = 0, total;
     for (int b0 = 0; b0 < a.B; b0 += 256) {
         const int n = b0 + tid < a.B ? few_of(a, b0 + tid, G, ROWS).pages : 0;
-        const int upto = all + wg_scan256(n, red, total);
+        const int upto = all + wg_scan<4>(n, red, total);
         if (blockIdx.x == 0) {
             if (b0 + tid < a.B) ws.front[b0 + tid + 1] = upto;
             if (b0 + tid == 0) ws.front[0] = 0;
@@ -173,21 +166,21 @@ __global__ __launch_bounds__(256, RT == 1 ? 3 : 2) void ragged_few_kernel(const 
         int at = 0;
         for (int b0 = 0; b0 < a.B; b0 += 256) {
             const int n = b0 + tid < a.B ? few_of(a, b0 + tid, G, ROWS).pages : 0;
-            const int upto = at + wg_scan256(n, red, total);
+            const int upto = at + wg_scan<4>(n, red, total);
             if (n > 0 && w < (long long)upto * a.Hkv && w >= (long long)(upto - n) * a.Hkv) { found[0] = b0 + tid; found[1] = upto - n; }
             at += total;
             if (w < (long long)at * a.Hkv) break;
         }
         __syncthreads();
-        b = __builtin_amdgcn_readfirstlane(found[0]);
-        front = __builtin_amdgcn_readfirstlane(found[1]);
+        b = uniform(found[0]);
+        front = uniform(found[1]);
     }
 
     while (w < w_end) {
-        Few u = few_of(a, b, G, ROWS);
-        while (u.pages == 0 && b + 1 < a.B) u = few_of(a, ++b, G, ROWS);          // (there is one: w < work)
+        Few u = uniform(few_of(a, b, G, ROWS));
+        while (u.pages == 0 && b + 1 < a.B) u = uniform(few_of(a, ++b, G, ROWS));          // (there is one: w < work)
         if (u.pages == 0) return;
-        const Seq s = seq_of(a, b);
+        const Seq s = uniform(seq_of(a, b));
         const int in_seq = (int)(w - (long long)front * a.Hkv), h = in_seq / u.pages, off = in_seq % u.pages;
         const int cnt = (int)min((long long)(u.pages - off), w_end - w), rows = u.rows;
         const int groups = RT == 1 ? 1 : (rows + 15) / 16;        // of 16 rows
@@ -428,190 +421,417 @@ __global__ __launch_bounds__(256) void ragged_few_merge_kernel(const RaggedArgs 
     if (d == 0 && a.lse) a.lse[(size_t)(s.first + tk) * a.Hq + hd] = l != 0.0f ? top * 0.6931471805599453f + logf(l) : -INFINITY;
 }
 
-// Many rows (pieces of prompts): bound by the matrix instructions and the softmax between them.  A workgroup takes a tile of 128 rows, 32 to a wave, and
-// walks tiles of 64 keys that its waves unpack together into LDS, K in swizzled rows of fp16, V key by key (padded rows), one tile ahead of the products;
-// the codes of the tile after that are in flight meanwhile.
-template <int D>
-__global__ __launch_bounds__(256, 2) void ragged_wide_kernel(const RaggedArgs a, int most /* rows of a sequence that the kernel for few takes */)
+// The units of work of the kernel for many rows: a tile of kWideRows rows and the tiles of 64 keys that it sees, for every kv head, sequence by sequence,
+// head by head, tile by tile.
+__device__ inline void wide_tile(const RaggedArgs& a, const Seq& s, int G, int tile, int& t0, int& nt)
 {
-    constexpr int ND = D / 16, NB = D / 32, CH = D / 8;           // contraction steps of S, 32-d blocks of O, 16-byte chunks per key
-    constexpr int RS = 2 * D + 16;
+    const int r0 = tile * kWideRows;
+    int lo, hi;
+    keys_of(a, s, r0 / G, (min(r0 + kWideRows, s.n * G) - 1) / G, lo, hi);
+    t0 = lo >> 6;
+    nt = hi > lo ? ((hi + 63) >> 6) - t0 : 0;
+}
+// The key tiles (for one head) of all row tiles of sequence b, a thread each: the lanes of a wave go over the row tiles of one of its sequences after
+// another.  0 where the kernel for few rows takes the sequence.
+__device__ inline long long wide_work(const RaggedArgs& a, int G, int b)
+{
+    const int lane = threadIdx.x & 63;
+    Seq s{0, 0, 0};
+    if (b < a.B) s = seq_of(a, b);
+    const bool on = s.n * G > kFewRows;
+    long long mine = 0;
+    for (unsigned long long left = __builtin_amdgcn_ballot_w64(on); left != 0; left &= left - 1) {
+        const int src = (int)__builtin_ctzll(left);
+        const Seq x{0, __builtin_amdgcn_readlane(s.n, src), __builtin_amdgcn_readlane(s.len, src)};
+        const int tiles = (x.n * G + kWideRows - 1) / kWideRows;
+        long long sum = 0;
+        for (int r = lane; r < tiles; r += 64) { int t0, nt; wide_tile(a, x, G, r, t0, nt); sum += nt; }
+#pragma unroll
+        for (int d = 32; d >= 1; d >>= 1) sum += __shfl_xor(sum, d);
+        if (lane == src) mine = sum;
+    }
+    return mine;
+}
+
+// Where the pages of a workgroup begin: a row tile, its head and how many of its key tiles lie in front.
+struct WideRec { int b, tile, h, off, nt, pad[3]; };
+struct WideWs { long long* quota; WideRec* rec; float* part_o /* [workgroup][2][8 waves][D / 8][64 lanes][4] */; float* part_ml /* [workgroup][2][8][32][2] */; };
+
+// Many rows (pieces of prompts): bound by the matrix instructions and by the softmax between them.  Eight waves have 32 rows each of a tile of 256 and
+// walk tiles of 64 keys together; waves 0 - 3 and 4 - 7 are half an iteration apart, between barriers: while one half computes O += V P and the next
+// tile's S, the other does the softmax and unpacks its half of the keys of a K and a V tile into LDS (K as operands of the matrix instruction, V key by
+// key), so that every SIMD has a wave for either unit.  The work (row tile, key tile) is dealt out evenly as in the kernel for few rows.
+template <int D>
+__global__ __launch_bounds__(512, 2) void ragged_wide_kernel(const RaggedArgs a, const WideWs ws)
+{
+    constexpr int ND = D / 16, NB = D / 32;                       // contraction steps of S, 32-d blocks of O
+    constexpr int RS = 2 * D + 32;                                // bytes per key of the V tile
     constexpr int KB = 64 * 2 * D, VB = 64 * RS;                  // bytes of a tile of K, of V
     constexpr size_t VOFF = (size_t)128 * (D / 2 + D / 16);
     extern __shared__ __align__(256) unsigned char lds[];          // two tiles of K, two of V
-    __shared__ int find[8];
+    __shared__ long long red[8], found_front;
+    __shared__ int found_b;
     const int tid = threadIdx.x, lane = tid & 63, col = lane & 31, half = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int G = a.Hq / a.Hkv, h = blockIdx.y;
-    int b, tile;
-    if (!find_tile(a, G, most, blockIdx.x, b, tile, find)) return;
-    const Seq s = seq_of(a, b);
-    const int rows = s.n * G, r0 = tile * kWideRows;
-    int lo, hi, wlo = 0, whi = 0;                                 // keys that rows of the workgroup, of this wave see
-    keys_of(a, s, r0 / G, (min(r0 + kWideRows, rows) - 1) / G, lo, hi);
-    const int w0 = r0 + 32 * wave, row = min(w0 + col, rows - 1);
-    if (w0 < rows) keys_of(a, s, w0 / G, (min(w0 + 32, rows) - 1) / G, wlo, whi);
-    const int tok = row / G, head = h * G + row % G, pos = s.len - s.n + tok;
-    const int k_first = a.window > 0 ? pos - a.window + 1 : 0, k_last = a.causal ? min(pos, s.len - 1) : s.len - 1;
-    const int see_first = a.window > 0 ? s.len - s.n + (min(w0 + 32, rows) - 1) / G - a.window + 1 : 0;
-    const int see_last = a.causal ? min(s.len - s.n + w0 / G, s.len - 1) : s.len - 1;
+    const bool late = wave >= 4;
+    const int G = a.Hq / a.Hkv;
 
-    // Q: row col, d = 16 i + 8 half .. + 7
-    half8 qreg[ND];
-    float c_row;
-    {
-        uint4v x[ND];
-        float amax = 0.0f;
+    // this workgroup's key tiles [w, w_end) of all units', and where they begin
+    long long all = 0, total;
+    for (int b0 = 0; b0 < a.B; b0 += 512) { (void)wg_scan<8>(wide_work(a, G, b0 + tid), red, total); all += total; }
+    const long long work = all * a.Hkv;
+    long long quota = (work + gridDim.x - 1) / gridDim.x;
+    if (blockIdx.x == 0 && tid == 0) *ws.quota = quota;
+    long long w = (long long)blockIdx.x * quota;
+    const long long w_end = min(w + quota, work);
+    // (also of a workgroup without work: every record is read when the sums are joined)
+    if (tid == 0) ws.rec[blockIdx.x] = WideRec{0, 0, 0, 0, 0, {0, 0, 0}};
+    if (w >= w_end) return;
+    long long front = 0;                                          // key tiles (of one head) of the sequences in front of b
+    for (int b0 = 0; b0 < a.B; b0 += 512) {
+        const long long n = wide_work(a, G, b0 + tid), upto = front + wg_scan<8>(n, red, total);
+        if (n > 0 && w < upto * a.Hkv && w >= (upto - n) * a.Hkv) { found_b = b0 + tid; found_front = upto - n; }
+        front += total;
+        if (w < front * a.Hkv) break;
+    }
+    __syncthreads();
+    int b = uniform(found_b);
+    front = uniform(found_front);
+
+    const uint32_t lds0 = lds_addr_of(lds);
+    const uint32_t v_base = lds0 + 2 * KB + (uint32_t)((4 * half + ((lane & 15) >> 2)) * RS + 32 * ((lane >> 4) & 1) + 8 * (lane & 3));
+    auto phase_end = [&]() __attribute__((always_inline)) {
+        __builtin_amdgcn_sched_barrier(0);
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        __builtin_amdgcn_s_barrier();
+        __builtin_amdgcn_sched_barrier(0);
+    };
+
+    int tile = -1, h = 0, off = 0, t0 = 0, nt = 0;                 // tile < 0: to be looked up
+    Seq s{0, 0, 0};
+    while (w < w_end) {
+        if (tile < 0) {
+            // the row tile of a sequence's work that w lies in
+            if (b >= a.B) return;
+            s = uniform(seq_of(a, b));
+            const int tiles = (s.n * G + kWideRows - 1) / kWideRows;
+            long long per = 0;                                    // key tiles of one head
+            for (int r0 = 0; r0 < tiles; r0 += 64) {
+                int x0, n = 0;
+                if (r0 + lane < tiles) wide_tile(a, s, G, r0 + lane, x0, n);
+                long long v = n;
 #pragma unroll
-        for (int i = 0; i < ND; ++i) {
-            x[i] = *reinterpret_cast<const uint4v*>(a.q + (size_t)(s.first + tok) * a.q_token + (size_t)head * a.q_head + 16 * i + 8 * half);
-#pragma unroll
-            for (int j = 0; j < 4; ++j) amax = fmaxf(amax, fmaxf(fabsf(__uint_as_float(x[i][j] << 16)), fabsf(__uint_as_float(x[i][j] & 0xFFFF0000u))));
-        }
-        amax = lanes_max<32, 32>(amax);
-        float f, inv;
-        row_factor(amax, f, inv);
-#pragma unroll
-        for (int i = 0; i < ND; ++i)
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                qreg[i][2 * j]     = (half_t)(__uint_as_float(x[i][j] << 16) * f);
-                qreg[i][2 * j + 1] = (half_t)(__uint_as_float(x[i][j] & 0xFFFF0000u) * f);
+                for (int d = 32; d >= 1; d >>= 1) v += __shfl_xor(v, d);
+                per += uniform(v);
             }
-        c_row = a.c * inv;
-    }
-
-    floatx16 o[NB];
-    float m = -INFINITY, l = 0.0f;                                 // the maximum in units of the exponent of 2
+            if (per == 0 || s.n * G <= kFewRows) { if (++b >= a.B) return; continue; }
+            const long long in_seq = w - front * a.Hkv;
+            h = (int)(in_seq / per);
+            long long rem = in_seq % per;
+            for (int r0 = 0; r0 < tiles && tile < 0; r0 += 64) {
+                int x0 = 0, n = 0;
+                if (r0 + lane < tiles) wide_tile(a, s, G, r0 + lane, x0, n);
+                int upto = n;
 #pragma unroll
-    for (int i = 0; i < NB; ++i)
-#pragma unroll
-        for (int j = 0; j < 16; ++j) o[i][j] = 0.0f;
-
-    const int t0 = lo >> 6, t1 = (hi + 63) >> 6;                   // tiles of 64 keys
-    const int key = tid >> 2, g = tid & 3;                         // what this thread unpacks: D / 4 values of one key
-    Raw<D> kr, vr;
-    bool live = false;
-    auto load = [&](int t) __attribute__((always_inline)) {
-        t = min(t, t1 - 1);
-        const int page = a.table[(size_t)b * a.max_pages + (t >> 1)];
-        live = page >= 0 && page < a.num_pages;
-        const unsigned char* part = a.cache + ((size_t)(live ? page : 0) * a.Hkv + h) * (2 * VOFF);
-        kr = load_raw<D>(part, (t & 1) * 64 + key, g);
-        vr = load_raw<D>(part + VOFF, (t & 1) * 64 + key, g);
-    };
-    auto unpack = [&](int t, int buf) __attribute__((always_inline)) {
-        const bool on = live && t * 64 + key < s.len;             // (keys behind the end: zeros, whatever the slots hold)
-        const half2v ks = scales_of<D>(kr, on), vs = scales_of<D>(vr, on);
-#pragma unroll
-        for (int j = 0; j < D / 32; ++j) {
-            *reinterpret_cast<half8*>(lds + buf * KB + (key * CH + swz<CH>(key, (D / 32) * g + j)) * 16) = values8<D>(kr, ks, j);
-            *reinterpret_cast<half8*>(lds + 2 * KB + buf * VB + key * RS + (D / 2) * g + 16 * j) = values8<D>(vr, vs, j);
+                for (int d = 1; d < 64; d <<= 1) { const int u = __shfl_up(upto, d); if (lane >= d) upto += u; }
+                const unsigned long long hit = __builtin_amdgcn_ballot_w64(rem < upto && rem >= upto - n);
+                if (hit != 0) {
+                    const int src = (int)__builtin_ctzll(hit);
+                    tile = r0 + src;
+                    off = (int)(rem - (__builtin_amdgcn_readlane(upto, src) - __builtin_amdgcn_readlane(n, src)));
+                    t0 = __builtin_amdgcn_readlane(x0, src); nt = __builtin_amdgcn_readlane(n, src);
+                }
+                rem -= __builtin_amdgcn_readlane(upto, 63);
+            }
+            if (tile < 0) return;                                 // (lengths that change under the launch)
+            if (tid == 0 && w == (long long)blockIdx.x * quota) ws.rec[blockIdx.x] = WideRec{b, tile, h, off, nt, {0, 0, 0}};
         }
-    };
-    const uint32_t k_base = lds_addr_of(lds), v_base = lds_addr_of(lds) + 2 * KB + (uint32_t)((4 * half + ((lane & 15) >> 2)) * RS + 32 * ((lane >> 4) & 1) + 8 * (lane & 3));
+        const int cnt = (int)min((long long)(nt - off), w_end - w), rows = s.n * G, r0 = tile * kWideRows, w0 = r0 + 32 * wave;
+        const bool mine = w0 < rows;                              // this wave has rows
+        const int row = min(w0 + col, rows - 1), tok = row / G, head = h * G + row % G, pos = s.len - s.n + tok;
+        const int k_first = a.window > 0 ? pos - a.window + 1 : 0, k_last = a.causal ? min(pos, s.len - 1) : s.len - 1;
+        const int see_first = a.window > 0 ? s.len - s.n + (min(w0 + 32, rows) - 1) / G - a.window + 1 : 0;      // what all rows of the wave see
+        const int see_last = a.causal ? min(s.len - s.n + w0 / G, s.len - 1) : s.len - 1;
 
-    if (t0 < t1) {
-        load(t0);
-        unpack(t0, 0);
-        load(t0 + 1);
-    }
-    for (int t = t0; t < t1; ++t) {
-        const int buf = (t - t0) & 1;
-        __syncthreads();                                          // this tile is there, and nobody reads the one that is overwritten next
-        if (t + 1 < t1) unpack(t + 1, buf ^ 1);
-        load(t + 2);
-        if (t * 64 >= whi || t * 64 + 63 < wlo) continue;          // (the wave sees none of these keys)
-        floatx16 sc[2];
+        // what this thread unpacks: 32 d of one key, of K (waves 0, 1, 4, 5) or of V; the early waves have the first 32 keys of a tile
+        const int is_v = (wave >> 1) & 1, key = (late ? 32 : 0) + ((tid & 127) >> 2), g = tid & 3;
+        const int first = t0 + off, last = first + cnt - 1;
+        const int* ids = a.table + (size_t)b * a.max_pages;
+        Raw<D> raw;
+        bool raw_on = false;
+        auto load = [&](int t) __attribute__((always_inline)) {
+            t = min(t, last);
+            const int page = ids[t >> 1];
+            const bool live = page >= 0 && page < a.num_pages;
+            raw_on = live && t * 64 + key < s.len;                // (keys behind the end: zeros, whatever the slots hold)
+            raw = load_raw<D>(a.cache + ((size_t)(live ? page : 0) * a.Hkv + h) * (2 * VOFF) + (is_v ? VOFF : 0), (t & 1) * 64 + key, g);
+        };
+        // K: the 16 bytes of d = 16 i + 8 hf .. of a key in place 32 hf + key % 32 of operand (key / 32, i), the places of every second i turned so that
+        // the four threads of a key write to different banks
+        auto unpack = [&](int buf_k, int buf_v) __attribute__((always_inline)) {
+            const half2v sc = scales_of<D>(raw, raw_on);
 #pragma unroll
-        for (int kb = 0; kb < 2; ++kb) {
-#pragma unroll
-            for (int j = 0; j < 16; ++j) sc[kb][j] = 0.0f;
+            for (int j = 0; j < D / 32; ++j) {
+                const int c = (D / 32) * g + j, i = c >> 1;
+                const uint32_t at = is_v ? (uint32_t)(2 * KB + buf_v * VB + key * RS + 16 * c)
+                                         : (uint32_t)(buf_k * KB + (((key >> 5) * ND + i) * 64 + ((32 * (c & 1) + (key & 31)) ^ (4 * ((i >> (D == 128 ? 1 : 0)) & 3)))) * 16);
+                lds_write16_at(lds0 + at, __builtin_bit_cast(uint4v, values8<D>(raw, sc, j)));
+            }
+        };
+
+        // K of the first tile by all: the waves that have V otherwise wait
+        __syncthreads();                                          // (the segment before has read its tiles)
+        if (!is_v) { load(first); unpack(0, 0); }
+        load(is_v ? first : first + 1);
+
+        // Q: row col, d = 16 i + 8 half .. + 7
+        half8 qreg[ND];
+        float c_row;
+        {
+            uint4v x[ND];
+            float amax = 0.0f;
 #pragma unroll
             for (int i = 0; i < ND; ++i) {
-                const uint4v kv = lds_read16_at(k_base + (uint32_t)(buf * KB + ((32 * kb + col) * CH + swz<CH>(32 * kb + col, 2 * i + half)) * 16));
-                sc[kb] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(half8, kv), qreg[i], sc[kb], 0, 0, 0);
+                x[i] = *reinterpret_cast<const uint4v*>(a.q + (size_t)(s.first + tok) * a.q_token + (size_t)head * a.q_head + 16 * i + 8 * half);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) amax = fmaxf(amax, fmaxf(fabsf(__uint_as_float(x[i][j] << 16)), fabsf(__uint_as_float(x[i][j] & 0xFFFF0000u))));
             }
+            amax = lanes_max<32, 32>(amax);
+            float f, inv;
+            row_factor(amax, f, inv);
+#pragma unroll
+            for (int i = 0; i < ND; ++i)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    qreg[i][2 * j]     = (half_t)(__uint_as_float(x[i][j] << 16) * f);
+                    qreg[i][2 * j + 1] = (half_t)(__uint_as_float(x[i][j] & 0xFFFF0000u) * f);
+                }
+            c_row = a.c * inv;
         }
-        if (t * 64 < see_first || t * 64 + 63 > see_last) {
+        floatx16 o[NB], sc[2];
+        float m = -INFINITY, l = 0.0f;                             // the maximum in units of the exponent of 2
+        half8 pt[4];
+#pragma unroll
+        for (int i = 0; i < NB; ++i)
+#pragma unroll
+            for (int j = 0; j < 16; ++j) o[i][j] = 0.0f;
+
+        auto scores = [&](int buf) __attribute__((always_inline)) {
+#pragma unroll
+            for (int kb = 0; kb < 2; ++kb) {
+#pragma unroll
+                for (int j = 0; j < 16; ++j) sc[kb][j] = 0.0f;
+#pragma unroll
+                for (int i = 0; i < ND; ++i) {
+                    const uint4v kv = lds_read16_at(lds0 + (uint32_t)(buf * KB + (kb * ND + i) * 1024) + 16u * (uint32_t)(lane ^ (4 * ((i >> (D == 128 ? 1 : 0)) & 3))));
+                    sc[kb] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(half8, kv), qreg[i], sc[kb], 0, 0, 0);
+                }
+            }
+        };
+        auto vector_phase = [&](int t) __attribute__((always_inline)) {
+            if (t * 64 < see_first || t * 64 + 63 > see_last) {
+#pragma unroll
+                for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+                    for (int j = 0; j < 16; ++j) {
+                        const int k = t * 64 + 32 * kb + (j & 3) + 8 * (j >> 2) + 4 * half;
+                        if (k < k_first || k > k_last) sc[kb][j] = -INFINITY;
+                    }
+            }
+            float mx = -INFINITY;
+#pragma unroll
+            for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+                for (int j = 0; j < 16; ++j) mx = max_nc(mx, sc[kb][j]);
+            mx = lanes_max<32, 32>(mx) * c_row;
+            const float m_new = fmaxf(m, mx), m_at = m_new == -INFINITY ? 0.0f : m_new, alpha = __builtin_amdgcn_exp2f(m - m_at);
+            m = m_new;
+            float add[2] = {0.0f, 0.0f};
 #pragma unroll
             for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
                 for (int j = 0; j < 16; ++j) {
-                    const int k = t * 64 + 32 * kb + (j & 3) + 8 * (j >> 2) + 4 * half;
-                    if (k < k_first || k > k_last) sc[kb][j] = -INFINITY;
+                    const float x = __builtin_amdgcn_exp2f(fmaf(sc[kb][j], c_row, -m_at));
+                    add[j & 1] += x;
+                    pt[2 * kb + (j >> 3)][j & 7] = (half_t)x;
+                }
+            l = fmaf(l, alpha, add[0] + add[1]);
+            if (__builtin_amdgcn_ballot_w64(alpha != 1.0f) != 0) {
+#pragma unroll
+                for (int i = 0; i < NB; ++i) o[i] *= alpha;
+            }
+        };
+        auto values = [&](int buf) __attribute__((always_inline)) {
+#pragma unroll
+            for (int q = 0; q < 4; ++q)
+#pragma unroll
+                for (int i = 0; i < NB; ++i) {
+                    const uint2v x = lds_read_tr16_at(v_base + (uint32_t)(buf * VB + 16 * q * RS + 64 * i)), y = lds_read_tr16_at(v_base + (uint32_t)(buf * VB + (16 * q + 8) * RS + 64 * i));
+                    const uint4v av = {x[0], x[1], y[0], y[1]};
+                    o[i] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(half8, av), pt[q], o[i], 0, 0, 0);
+                }
+        };
+
+        // Half-steps: the early waves are in the vector phase of tile i in half-step 2 i and in its matrix phase in 2 i + 1, the late ones one later.
+        // K(i + 1) and V(i), needed from half-step 2 i + 1 on, take the places of K(i - 1) and V(i - 2), last read in 2 i - 2: the late waves
+        // unpack their half of them in 2 i - 1, the early ones in 2 i.
+        phase_end();
+        if (mine) scores(0);
+        if (late) { unpack(1, 0); load(is_v ? first + 1 : first + 2); phase_end(); }
+        for (int i = 0; i < cnt; ++i) {
+            const int u = late ? i + 1 : i;
+            unpack((u + 1) & 1, u & 1);
+            load(first + (is_v ? u + 1 : u + 2));
+            if (mine) vector_phase(first + i);
+            phase_end();
+            if (mine) {
+                __builtin_amdgcn_s_setprio(1);
+                values(i & 1);
+                scores((i + 1) & 1);
+                __builtin_amdgcn_s_setprio(0);
+            }
+            phase_end();
+        }
+        if (!late) phase_end();
+
+        const bool whole = cnt == nt;
+        if (mine) {
+            l = lanes_sum<32, 32>(l);
+            if (whole) {
+                const float inv = l != 0.0f ? 1.0f / l : 0.0f;
+                if (w0 + col < rows) {
+                    uint16_t* dst = a.o + (size_t)(s.first + tok) * a.o_token + (size_t)head * a.o_head;
+#pragma unroll
+                    for (int i = 0; i < NB; ++i)
+#pragma unroll
+                        for (int j = 0; j < 4; ++j)
+                            *reinterpret_cast<uint2v*>(dst + 32 * i + 8 * j + 4 * half) = uint2v{pack_bf16x2_cvt(o[i][4 * j] * inv, o[i][4 * j + 1] * inv), pack_bf16x2_cvt(o[i][4 * j + 2] * inv, o[i][4 * j + 3] * inv)};
+                    if (half == 0 && a.lse) a.lse[(size_t)(s.first + tok) * a.Hq + head] = l != 0.0f ? m * 0.6931471805599453f + logf(l) : -INFINITY;
+                }
+            } else {
+                const size_t slot = ((size_t)blockIdx.x * 2 + (off == 0 ? 1 : 0)) * 8 + wave;
+#pragma unroll
+                for (int i = 0; i < NB; ++i)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j)
+                        *reinterpret_cast<floatx4*>(ws.part_o + ((slot * (D / 8) + 4 * i + j) * 64 + lane) * 4) = floatx4{o[i][4 * j], o[i][4 * j + 1], o[i][4 * j + 2], o[i][4 * j + 3]};
+                if (half == 0) { ws.part_ml[(slot * 32 + col) * 2] = m; ws.part_ml[(slot * 32 + col) * 2 + 1] = l; }
+            }
+        }
+        // on to the next row tile, head, sequence
+        w += cnt;
+        off = 0;
+        const int tiles = (rows + kWideRows - 1) / kWideRows;
+        nt = 0;
+        while (nt == 0 && ++tile < tiles) wide_tile(a, s, G, tile, t0, nt);
+        if (nt == 0) {                                            // this head is done
+            tile = -1;
+            if (h == a.Hkv - 1) { front = w / a.Hkv; ++b; }       // (w is a multiple of the heads there)
+        }
+    }
+}
+
+// O and lse of the row tiles whose key tiles were shared: a workgroup per place where one workgroup's work ended and another's began, wave of
+// rows and 32 d; of the places within a row tile the first has it.
+template <int D>
+__device__ void wide_merge(const RaggedArgs& a, const WideWs& ws, int place, int part)
+{
+    const long long quota = *ws.quota;
+    if (quota == 0) return;
+    const WideRec r = ws.rec[place];
+    if (r.off == 0 || r.off > quota) return;
+    const Seq s = seq_of(a, r.b);
+    const int G = a.Hq / a.Hkv, rows = s.n * G, wave = part / (D / 32), i = part % (D / 32), lane = threadIdx.x & 63, j = threadIdx.x >> 6;
+    const int col = lane & 31, half = lane >> 5, row = r.tile * kWideRows + 32 * wave + col;
+    if (r.tile * kWideRows + 32 * wave >= rows) return;
+    const int n = 1 + (int)((r.nt - r.off + quota - 1) / quota);
+    float M = -INFINITY, l = 0.0f;
+    floatx4 v = {0.0f, 0.0f, 0.0f, 0.0f};
+    for (int k0 = 0; k0 < n; k0 += 4) {
+        floatx4 po[4];
+        float pm[4], pl[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const int x = min(k0 + k, n - 1);
+            const size_t slot = (x == 0 ? (size_t)(place - 1) * 2 + 1 : (size_t)(place + x - 1) * 2) * 8 + wave;
+            po[k] = *reinterpret_cast<const floatx4*>(ws.part_o + ((slot * (D / 8) + 4 * i + j) * 64 + lane) * 4);
+            pm[k] = k0 + k < n ? ws.part_ml[(slot * 32 + col) * 2] : -INFINITY;
+            pl[k] = ws.part_ml[(slot * 32 + col) * 2 + 1];
+        }
+        const float top = fmaxf(fmaxf(fmaxf(pm[0], pm[1]), fmaxf(pm[2], pm[3])), M), at = top == -INFINITY ? 0.0f : top;
+        const float al = __builtin_amdgcn_exp2f(M - at);
+        M = top; l *= al; v *= al;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) { const float x = __builtin_amdgcn_exp2f(pm[k] - at); l = fmaf(pl[k], x, l); v += po[k] * x; }
+    }
+    if (row >= rows) return;
+    const int tok = row / G, head = r.h * G + row % G;
+    v *= l != 0.0f ? 1.0f / l : 0.0f;
+    *reinterpret_cast<uint2v*>(a.o + (size_t)(s.first + tok) * a.o_token + (size_t)head * a.o_head + 32 * i + 8 * j + 4 * half) =
+        uint2v{pack_bf16x2_cvt(v[0], v[1]), pack_bf16x2_cvt(v[2], v[3])};
+    if (i == 0 && j == 0 && half == 0 && a.lse) a.lse[(size_t)(s.first + tok) * a.Hq + head] = l != 0.0f ? M * 0.6931471805599453f + logf(l) : -INFINITY;
+}
+// (and O = 0, lse = -inf for row tiles, of sequences with many rows, that see no key: they are nobody's work)
+template <int D>
+__global__ __launch_bounds__(256) void ragged_wide_merge_kernel(const RaggedArgs a, const WideWs ws, int places)
+{
+    if ((int)blockIdx.x < places) { if (blockIdx.x > 0) wide_merge<D>(a, ws, blockIdx.x, blockIdx.y); return; }
+    const int G = a.Hq / a.Hkv;
+    for (int b = (int)(blockIdx.x - places) * gridDim.y + blockIdx.y; b < a.B; b += (int)(gridDim.x - places) * gridDim.y) {
+        const Seq s = seq_of(a, b);
+        const int rows = s.n * G;
+        if (rows <= kFewRows) continue;
+        for (int tile = 0; tile * kWideRows < rows; ++tile) {
+            int t0, nt;
+            wide_tile(a, s, G, tile, t0, nt);
+            if (nt > 0) break;                                    // (the ones behind it see keys as well)
+            const int r1 = min((tile + 1) * kWideRows, rows);
+            for (int h = 0; h < a.Hkv; ++h)
+                for (int e = threadIdx.x; e < (r1 - tile * kWideRows) * (D / 8); e += 256) {
+                    const int row = tile * kWideRows + e / (D / 8), d = e % (D / 8) * 8, head = h * G + row % G;
+                    *reinterpret_cast<uint4v*>(a.o + (size_t)(s.first + row / G) * a.o_token + (size_t)head * a.o_head + d) = uint4v{0u, 0u, 0u, 0u};
+                    if (d == 0 && a.lse) a.lse[(size_t)(s.first + row / G) * a.Hq + head] = -INFINITY;
                 }
         }
-        float mx = -INFINITY;
-#pragma unroll
-        for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-            for (int j = 0; j < 16; ++j) mx = max_nc(mx, sc[kb][j]);
-        mx = lanes_max<32, 32>(mx) * c_row;
-        const float m_new = fmaxf(m, mx), m_at = m_new == -INFINITY ? 0.0f : m_new, alpha = __builtin_amdgcn_exp2f(m - m_at);
-        m = m_new;
-        float add = 0.0f;
-        half8 pt[4];
-#pragma unroll
-        for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-            for (int j = 0; j < 16; ++j) {
-                const float x = __builtin_amdgcn_exp2f(fmaf(sc[kb][j], c_row, -m_at));
-                add += x;
-                pt[2 * kb + (j >> 3)][j & 7] = (half_t)x;
-            }
-        l = fmaf(l, alpha, add);
-        if (__builtin_amdgcn_ballot_w64(alpha != 1.0f) != 0) {
-#pragma unroll
-            for (int i = 0; i < NB; ++i) o[i] *= alpha;
-        }
-#pragma unroll
-        for (int q = 0; q < 4; ++q)
-#pragma unroll
-            for (int i = 0; i < NB; ++i) {
-                const uint2v x = lds_read_tr16_at(v_base + (uint32_t)(buf * VB + 16 * q * RS + 64 * i)), y = lds_read_tr16_at(v_base + (uint32_t)(buf * VB + (16 * q + 8) * RS + 64 * i));
-                const uint4v av = {x[0], x[1], y[0], y[1]};
-                o[i] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(half8, av), pt[q], o[i], 0, 0, 0);
-            }
     }
-    if (w0 + col >= rows) return;
-    l = lanes_sum<32, 32>(l);
-    const float inv = l != 0.0f ? 1.0f / l : 0.0f;
-    uint16_t* dst = a.o + (size_t)(s.first + tok) * a.o_token + (size_t)head * a.o_head;
-#pragma unroll
-    for (int i = 0; i < NB; ++i)
-#pragma unroll
-        for (int j = 0; j < 4; ++j)
-            *reinterpret_cast<uint2v*>(dst + 32 * i + 8 * j + 4 * half) = uint2v{pack_bf16x2_cvt(o[i][4 * j] * inv, o[i][4 * j + 1] * inv), pack_bf16x2_cvt(o[i][4 * j + 2] * inv, o[i][4 * j + 3] * inv)};
-    if (half == 0 && a.lse) a.lse[(size_t)(s.first + tok) * a.Hq + head] = l != 0.0f ? m * 0.6931471805599453f + logf(l) : -INFINITY;
 }
 
 inline size_t up256(size_t x) { return (x + 255) / 256 * 256; }
 
 // Which kernels a step may need: the host knows only how many rows a sequence has at most.
-struct RaggedPlan { int few_groups; bool wide; int few_wgs; };
+struct RaggedPlan { int few_groups, few_wgs, wide_wgs /* 0: no sequence has that many rows */; };
 inline RaggedPlan plan_of(int T, int B, int Hq, int Hkv, int max_q, int max_pages, int cus)
 {
-    const long long rows = (long long)(max_q < T ? max_q : T) * (Hq / Hkv), units = (long long)B * Hkv * max_pages;
+    const long long most = (long long)(max_q < T ? max_q : T) * (Hq / Hkv), rows = (long long)T * (Hq / Hkv);
     RaggedPlan p;
-    p.few_groups = rows <= 16 ? 1 : 2;
-    p.wide = rows > kFewRows;
-    const long long wgs = (long long)cus * (p.few_groups == 1 ? 3 : 2);
+    p.few_groups = most <= 16 ? 1 : 2;
+    const long long units = (long long)B * Hkv * max_pages, wgs = (long long)cus * (p.few_groups == 1 ? 3 : 2);
     p.few_wgs = (int)(units < wgs ? units : wgs);
+    p.wide_wgs = 0;
+    if (most > kFewRows) {
+        const long long tiles = ((long long)B + rows / kWideRows) * Hkv * max_pages * 2, wide = cus;
+        p.wide_wgs = (int)(tiles < wide ? tiles : wide);
+    }
     return p;
 }
-inline FewWs carve_few(void* ws, const RaggedPlan& p, int B, int D, size_t& bytes)
+struct RaggedWs { FewWs few; WideWs wide; size_t bytes; };
+inline RaggedWs carve_ragged(void* ws, const RaggedPlan& p, int B, int D)
 {
     unsigned char* base = (unsigned char*)ws;
     size_t off = 0;
     auto take = [&](size_t n) { unsigned char* r = base + off; off += up256(n); return r; };
-    const size_t rows = (size_t)p.few_wgs * 2 * 16 * p.few_groups;
-    FewWs w;
-    w.quota = (int*)take(4);
-    w.front = (int*)take(((size_t)B + 1) * 4);
-    w.part_o = (float*)take(rows * D * 4);
-    w.part_ml = (float*)take(rows * 8);
-    bytes = off;
+    const size_t rows = (size_t)p.few_wgs * 2 * 16 * p.few_groups, wide = (size_t)p.wide_wgs * 2 * kWideRows;
+    RaggedWs w;
+    w.few.quota = (int*)take(4);
+    w.few.front = (int*)take(((size_t)B + 1) * 4);
+    w.wide.quota = (long long*)take(8);
+    w.wide.rec = (WideRec*)take(p.wide_wgs * sizeof(WideRec));
+    // (the two kinds of partial sums follow each other: both launches' are there until they are joined)
+    w.few.part_o = (float*)take(rows * D * 4);
+    w.few.part_ml = (float*)take(rows * 8);
+    w.wide.part_o = (float*)take(wide * D * 4);
+    w.wide.part_ml = (float*)take(wide * 8);
+    w.bytes = off;
     return w;
 }
 
@@ -626,14 +846,14 @@ int launch_few(const RaggedArgs& a, const RaggedPlan& p, const FewWs& w, hipStre
 }
 
 template <int D>
-int launch_wide(const RaggedArgs& a, hipStream_t st)
+int launch_wide(const RaggedArgs& a, const RaggedPlan& p, const WideWs& w, hipStream_t st)
 {
-    constexpr int bytes = 2 * 64 * (2 * D + 2 * D + 16);
+    constexpr int bytes = 2 * 64 * (2 * D + 2 * D + 32);
     static unsigned long long done = 0;
     if (!ensure_dynamic_lds((const void*)ragged_wide_kernel<D>, bytes, done)) return -1;
-    const int G = a.Hq / a.Hkv;
-    const dim3 grid((unsigned)(a.B + (long long)a.T * G / kWideRows), a.Hkv);
-    hipLaunchKernelGGL((ragged_wide_kernel<D>), grid, dim3(256), bytes, st, a, kFewRows);
+    hipLaunchKernelGGL((ragged_wide_kernel<D>), dim3(p.wide_wgs), dim3(512), bytes, st, a, w);
+    if (hipGetLastError() != hipSuccess) return -1;
+    hipLaunchKernelGGL((ragged_wide_merge_kernel<D>), dim3(p.wide_wgs + 8, D / 4), dim3(256), 0, st, a, w, p.wide_wgs);
     return hipGetLastError() == hipSuccess ? 0 : -1;
 }
 
@@ -641,19 +861,16 @@ int launch_wide(const RaggedArgs& a, hipStream_t st)
 
 size_t ragged_ws_bytes(int T, int B, int Hq, int Hkv, int max_q, int max_pages, int D)
 {
-    size_t bytes;
-    carve_few(nullptr, plan_of(T, B, Hq, Hkv, max_q, max_pages, kChipCus), B, D, bytes);
-    return bytes;
+    return carve_ragged(nullptr, plan_of(T, B, Hq, Hkv, max_q, max_pages, kChipCus), B, D).bytes;
 }
 
 int launch_ragged(const RaggedArgs& a, int D, void* ws, hipStream_t st)
 {
     const RaggedPlan p = plan_of(a.T, a.B, a.Hq, a.Hkv, a.max_q, a.max_pages, kChipCus);
-    size_t bytes;
-    const FewWs w = carve_few(ws, p, a.B, D, bytes);
-    int rc = D == 128 ? (p.few_groups == 1 ? launch_few<128, 1>(a, p, w, st) : launch_few<128, 2>(a, p, w, st))
-                      : (p.few_groups == 1 ? launch_few<64, 1>(a, p, w, st) : launch_few<64, 2>(a, p, w, st));
-    if (!rc && p.wide) rc = D == 128 ? launch_wide<128>(a, st) : launch_wide<64>(a, st);
+    const RaggedWs w = carve_ragged(ws, p, a.B, D);
+    int rc = D == 128 ? (p.few_groups == 1 ? launch_few<128, 1>(a, p, w.few, st) : launch_few<128, 2>(a, p, w.few, st))
+                      : (p.few_groups == 1 ? launch_few<64, 1>(a, p, w.few, st) : launch_few<64, 2>(a, p, w.few, st));
+    if (!rc && p.wide_wgs > 0) rc = D == 128 ? launch_wide<128>(a, p, w.wide, st) : launch_wide<64>(a, p, w.wide, st);
     return rc;
 }
 
