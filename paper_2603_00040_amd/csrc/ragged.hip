@@ -14,11 +14,18 @@
 #include "kernels.hpp"
 #include "nvfp4.hpp"
 
+#include <type_traits>
+
 namespace aq {
 
 namespace {
 
 constexpr int kFewRows = 32;          // most rows of a (sequence, kv head) that the kernel for few rows takes
+// The reference that a row's exponents are taken against, in powers of two, follows its running maximum only when that is more than this above it: a row's
+// largest probability so far is then up to 2^8 (as fp16 as good as 1), and most tiles need no rescaling of O: some row of 32 has a new maximum
+// in most of the first fifty tiles.
+constexpr float kSlack = 8.0f;
+constexpr int kWideStart = 3;         // (10 000 cycles against 4 000 for a tile of keys of 128 d)
 constexpr int kWideRows = 256;        // rows of a tile of the other one
 
 struct Seq { int first, n, len; };    // first query of the step, number of queries, keys
@@ -77,7 +84,8 @@ __device__ inline T wg_scan(T v, T* red /* [W], LDS */, T& total)
     return v + front;
 }
 
-// Codes and scale bytes of D / 4 values of one key: lane (key cc of 16, group g) holds d = (D/4) g .. + D/4 - 1.
+// Codes and scale bytes of D / 4 values of one key: lane (key cc of 16, group g) holds d = (D/4) g .. + D/4 - 1.  (The scale bytes as the dword that they
+// lie in: of a narrower load the compiler makes the widening an instruction of its own, which waits for the load wherever it puts it.)
 template <int D> struct Raw { uint32_t w[D / 32]; uint32_t sc; };
 template <int D>
 __device__ inline Raw<D> load_raw(const unsigned char* part /* K or V part of a page's head */, int key, int g)
@@ -86,17 +94,21 @@ __device__ inline Raw<D> load_raw(const unsigned char* part /* K or V part of a 
     if constexpr (D == 128) {
         const uint4v c = *reinterpret_cast<const uint4v*>(part + key * 64 + 16 * g);
         r.w[0] = c[0]; r.w[1] = c[1]; r.w[2] = c[2]; r.w[3] = c[3];
-        r.sc = *reinterpret_cast<const uint16_t*>(part + 128 * 64 + key * 8 + 2 * g);
+        r.sc = *reinterpret_cast<const uint32_t*>(part + 128 * 64 + key * 8 + 4 * (g >> 1));
     } else {
         const uint2v c = *reinterpret_cast<const uint2v*>(part + key * 32 + 8 * g);
         r.w[0] = c[0]; r.w[1] = c[1];
-        r.sc = part[128 * 32 + key * 4 + g];
+        r.sc = *reinterpret_cast<const uint32_t*>(part + 128 * 32 + key * 4);
     }
     return r;
 }
 // The block scales of those values as an fp16 pair (one for D = 64).  Not live: 0, whatever the bytes are (a stale scale byte may be NaN).
 template <int D>
-__device__ inline half2v scales_of(const Raw<D>& r, bool live) { return __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(live ? r.sc : 0u, 1.0f, false); }
+__device__ inline half2v scales_of(const Raw<D>& r, int g, bool live)
+{
+    const uint32_t sc = r.sc >> (D == 128 ? 16 * (g & 1) : 8 * g);
+    return __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(live ? sc : 0u, 1.0f, false);
+}
 // Values 8 s .. 8 s + 7 of the lane's as fp16.
 template <int D>
 __device__ inline half8 values8(const Raw<D>& r, half2v sc, int s)
@@ -132,7 +144,7 @@ template <int D, int RT /* 16-row groups of a unit */>
 __global__ __launch_bounds__(256, RT == 1 ? 3 : 2) void ragged_few_kernel(const RaggedArgs a, const FewWs ws)
 {
     constexpr int NS = D / 32, NDT = D / 16, ROWS = 16 * RT;
-    constexpr int RS = 2 * D + 32;                                // bytes per key of the V tile (four keys side by side in other banks)
+    constexpr int RS = 2 * D + 32;                                // bytes per key of the V tile (eight keys side by side in other banks)
     constexpr size_t VOFF = (size_t)128 * (D / 2 + D / 16);
     __shared__ __align__(16) unsigned char stage[4 * 32 * RS];     // per wave: V of 32 keys [key][d]; at the end the waves' sums [4][16][D]
     __shared__ float ml[2][4][ROWS];
@@ -142,7 +154,8 @@ __global__ __launch_bounds__(256, RT == 1 ? 3 : 2) void ragged_few_kernel(const 
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int G = a.Hq / a.Hkv;
     unsigned char* stg = stage + wave * (32 * RS);
-    const uint32_t tr_base = lds_addr_of(stg) + (uint32_t)((4 * g + (cc >> 2)) * RS + 8 * (cc & 3));
+    // (the two 16-byte pieces of every 32 change places in keys 4 - 7 of 8: a store serves eight lanes, eight keys, at a time on 32 banks)
+    const uint32_t tr_base = lds_addr_of(stg) + (uint32_t)((4 * g + (cc >> 2)) * RS + 8 * ((cc & 3) ^ (2 * (g & 1))));
 
     // this workgroup's pages [w, w_end) of all units', and the sequence that the first of them belongs to
     int all = 0, total;
@@ -249,7 +262,7 @@ __global__ __launch_bounds__(256, RT == 1 ? 3 : 2) void ragged_few_kernel(const 
             floatx4 sc[RT][2];
 #pragma unroll
             for (int blk = 0; blk < 2; ++blk) {
-                const half2v ks = scales_of<D>(t.k[blk], t.live);
+                const half2v ks = scales_of<D>(t.k[blk], g, t.live);
 #pragma unroll
                 for (int rt = 0; rt < RT; ++rt) sc[rt][blk] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
@@ -263,9 +276,9 @@ __global__ __launch_bounds__(256, RT == 1 ? 3 : 2) void ragged_few_kernel(const 
             __builtin_amdgcn_wave_barrier();
 #pragma unroll
             for (int blk = 0; blk < 2; ++blk) {
-                const half2v vs = scales_of<D>(t.v[blk], t.live && kt + 16 * blk + cc < s.len);
+                const half2v vs = scales_of<D>(t.v[blk], g, t.live && kt + 16 * blk + cc < s.len);
 #pragma unroll
-                for (int j = 0; j < NS; ++j) *reinterpret_cast<half8*>(stg + (16 * blk + cc) * RS + (D / 2) * g + 16 * j) = values8<D>(t.v[blk], vs, j);
+                for (int j = 0; j < NS; ++j) *reinterpret_cast<half8*>(stg + (16 * blk + cc) * RS + (D / 2) * g + 16 * (j ^ ((cc >> 2) & 1))) = values8<D>(t.v[blk], vs, j);
             }
             __builtin_amdgcn_wave_barrier();
             half8 pt[RT];
@@ -282,8 +295,14 @@ __global__ __launch_bounds__(256, RT == 1 ? 3 : 2) void ragged_few_kernel(const 
                 float mx = max_nc(max_nc(max_nc(sc[rt][0][0], sc[rt][0][1]), max_nc(sc[rt][0][2], sc[rt][0][3])),
                                   max_nc(max_nc(sc[rt][1][0], sc[rt][1][1]), max_nc(sc[rt][1][2], sc[rt][1][3])));
                 mx = lanes_max<16, 32>(mx) * c_row[rt];
-                const float m_new = fmaxf(m[rt], mx), m_at = m_new == -INFINITY ? 0.0f : m_new, alpha = __builtin_amdgcn_exp2f(m[rt] - m_at);
-                m[rt] = m_new;
+                if (__builtin_amdgcn_ballot_w64(mx > m[rt] + kSlack) != 0) {
+                    const float m_new = fmaxf(m[rt], mx), alpha = __builtin_amdgcn_exp2f(m[rt] - (m_new == -INFINITY ? 0.0f : m_new));
+                    m[rt] = m_new;
+                    l[rt] *= alpha;
+#pragma unroll
+                    for (int dt = 0; dt < NDT; ++dt) o[rt][dt] *= alpha;
+                }
+                const float m_at = m[rt] == -INFINITY ? 0.0f : m[rt];
                 float add = 0.0f;
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {
@@ -291,11 +310,7 @@ __global__ __launch_bounds__(256, RT == 1 ? 3 : 2) void ragged_few_kernel(const 
                     add += x;
                     pt[rt][j] = (half_t)x;
                 }
-                l[rt] = fmaf(l[rt], alpha, add);
-                if (__builtin_amdgcn_ballot_w64(alpha != 1.0f) != 0) {
-#pragma unroll
-                    for (int dt = 0; dt < NDT; ++dt) o[rt][dt] *= alpha;
-                }
+                l[rt] += add;
             }
 #pragma unroll
             for (int dt = 0; dt < NDT; ++dt) {
@@ -422,14 +437,15 @@ __global__ __launch_bounds__(256) void ragged_few_merge_kernel(const RaggedArgs 
 }
 
 // The units of work of the kernel for many rows: a tile of kWideRows rows and the tiles of 64 keys that it sees, for every kv head, sequence by sequence,
-// head by head, tile by tile.
+// head by head, tile by tile.  What a row tile costs besides (its rows of Q, the first tiles of K and V, the result) counts as kWideStart
+// tiles of keys in front of its own.
 __device__ inline void wide_tile(const RaggedArgs& a, const Seq& s, int G, int tile, int& t0, int& nt)
 {
     const int r0 = tile * kWideRows;
     int lo, hi;
     keys_of(a, s, r0 / G, (min(r0 + kWideRows, s.n * G) - 1) / G, lo, hi);
     t0 = lo >> 6;
-    nt = hi > lo ? ((hi + 63) >> 6) - t0 : 0;
+    nt = hi > lo ? ((hi + 63) >> 6) - t0 + kWideStart : 0;
 }
 // The key tiles (for one head) of all row tiles of sequence b, a thread each: the lanes of a wave go over the row tiles of one of its sequences after
 // another.  0 where the kernel for few rows takes the sequence.
@@ -465,8 +481,9 @@ template <int D>
 __global__ __launch_bounds__(512, 2) void ragged_wide_kernel(const RaggedArgs a, const WideWs ws)
 {
     constexpr int ND = D / 16, NB = D / 32;                       // contraction steps of S, 32-d blocks of O
-    constexpr int RS = 2 * D + 32;                                // bytes per key of the V tile
+    constexpr int RS = 2 * D + 64;                                // bytes per key of the V tile: the 64 bytes of four keys that are read together in other banks
     constexpr int KB = 64 * 2 * D, VB = 64 * RS;                  // bytes of a tile of K, of V
+    constexpr bool kInProducts = D == 64;
     constexpr size_t VOFF = (size_t)128 * (D / 2 + D / 16);
     extern __shared__ __align__(256) unsigned char lds[];          // two tiles of K, two of V
     __shared__ long long red[8], found_front;
@@ -499,7 +516,9 @@ __global__ __launch_bounds__(512, 2) void ragged_wide_kernel(const RaggedArgs a,
     front = uniform(found_front);
 
     const uint32_t lds0 = lds_addr_of(lds);
-    const uint32_t v_base = lds0 + 2 * KB + (uint32_t)((4 * half + ((lane & 15) >> 2)) * RS + 32 * ((lane >> 4) & 1) + 8 * (lane & 3));
+    // (key 4 half + r of 16, r = (lane & 15) / 4; for the order of the 16-byte pieces of a key see unpack)
+    const int r4 = (lane & 15) >> 2;
+    const uint32_t v_base = lds0 + 2 * KB + (uint32_t)((4 * half + r4) * RS + 16 * ((2 * ((lane >> 4) & 1) + ((lane & 3) >> 1)) ^ ((D == 128 ? 2 : 1) * (r4 & 1))) + 8 * (lane & 1));
     auto phase_end = [&]() __attribute__((always_inline)) {
         __builtin_amdgcn_sched_barrier(0);
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
@@ -508,6 +527,7 @@ __global__ __launch_bounds__(512, 2) void ragged_wide_kernel(const RaggedArgs a,
     };
 
     int tile = -1, h = 0, off = 0, t0 = 0, nt = 0;                 // tile < 0: to be looked up
+    int id_lane = 0, id_b = -1, id_first = 0;                      // lane i: the id of page id_first + i of sequence id_b, -1: outside the cache
     Seq s{0, 0, 0};
     while (w < w_end) {
         if (tile < 0) {
@@ -546,7 +566,11 @@ __global__ __launch_bounds__(512, 2) void ragged_wide_kernel(const RaggedArgs a,
             if (tile < 0) return;                                 // (lengths that change under the launch)
             if (tid == 0 && w == (long long)blockIdx.x * quota) ws.rec[blockIdx.x] = WideRec{b, tile, h, off, nt, {0, 0, 0}};
         }
-        const int cnt = (int)min((long long)(nt - off), w_end - w), rows = s.n * G, r0 = tile * kWideRows, w0 = r0 + 32 * wave;
+        const int units = (int)min((long long)(nt - off), w_end - w);      // of work, the start included
+        const int keys = nt - kWideStart, at = max(off - kWideStart, 0), cnt = min(off + units - kWideStart, keys) - at;      // tiles of keys: all of them, where this workgroup begins, how many
+        w += units;
+        if (cnt <= 0) { off += units; continue; }                 // (the start alone: w is at this workgroup's end)
+        const int rows = s.n * G, r0 = tile * kWideRows, w0 = r0 + 32 * wave;
         const bool mine = w0 < rows;                              // this wave has rows
         const int row = min(w0 + col, rows - 1), tok = row / G, head = h * G + row % G, pos = s.len - s.n + tok;
         const int k_first = a.window > 0 ? pos - a.window + 1 : 0, k_last = a.causal ? min(pos, s.len - 1) : s.len - 1;
@@ -555,47 +579,87 @@ __global__ __launch_bounds__(512, 2) void ragged_wide_kernel(const RaggedArgs a,
 
         // what this thread unpacks: 32 d of one key, of K (waves 0, 1, 4, 5) or of V; the early waves have the first 32 keys of a tile
         const int is_v = (wave >> 1) & 1, key = (late ? 32 : 0) + ((tid & 127) >> 2), g = tid & 3;
-        const int first = t0 + off, last = first + cnt - 1;
+        const int first = t0 + at, last = first + cnt - 1;
         const int* ids = a.table + (size_t)b * a.max_pages;
+        const unsigned char* part0 = a.cache + (size_t)h * (2 * VOFF) + (is_v ? VOFF : 0);      // of page 0
+        const size_t page_bytes = (size_t)a.Hkv * (2 * VOFF);
+        const uint32_t code_at = (uint32_t)(key * (D / 2) + (D / 8) * g), scale_at = (uint32_t)(128 * (D / 2) + key * (D / 16) + (D == 128 ? 4 * (g >> 1) : 0));
         Raw<D> raw;
         bool raw_on = false;
-        auto load = [&](int t) __attribute__((always_inline)) {
-            t = min(t, last);
-            const int page = ids[t >> 1];
-            const bool live = page >= 0 && page < a.num_pages;
-            raw_on = live && t * 64 + key < s.len;                // (keys behind the end: zeros, whatever the slots hold)
-            raw = load_raw<D>(a.cache + ((size_t)(live ? page : 0) * a.Hkv + h) * (2 * VOFF) + (is_v ? VOFF : 0), (t & 1) * 64 + key, g);
-        };
-        // K: the 16 bytes of d = 16 i + 8 hf .. of a key in place 32 hf + key % 32 of operand (key / 32, i), the places of every second i turned so that
-        // the four threads of a key write to different banks
-        auto unpack = [&](int buf_k, int buf_v) __attribute__((always_inline)) {
-            const half2v sc = scales_of<D>(raw, raw_on);
-#pragma unroll
-            for (int j = 0; j < D / 32; ++j) {
-                const int c = (D / 32) * g + j, i = c >> 1;
-                const uint32_t at = is_v ? (uint32_t)(2 * KB + buf_v * VB + key * RS + 16 * c)
-                                         : (uint32_t)(buf_k * KB + (((key >> 5) * ND + i) * 64 + ((32 * (c & 1) + (key & 31)) ^ (4 * ((i >> (D == 128 ? 1 : 0)) & 3)))) * 16);
-                lds_write16_at(lds0 + at, __builtin_bit_cast(uint4v, values8<D>(raw, sc, j)));
+        auto page_at = [&](int t) __attribute__((always_inline)) {
+            const int p = t >> 1;
+            if (b != id_b || p < id_first || p >= id_first + 64) {      // 64 page ids at a time, waited for here and not at every use
+                id_b = b; id_first = p;
+                id_lane = ids[min(p + lane, a.max_pages - 1)];
+                id_lane = id_lane >= 0 && id_lane < a.num_pages ? id_lane : -1;
+                asm volatile("" : "+v"(id_lane));
             }
+            return __builtin_amdgcn_readlane(id_lane, p - id_first);
+        };
+        auto load_to = [&](Raw<D>& r, bool& on, int t) __attribute__((always_inline)) {
+            t = min(t, last);
+            const int page = page_at(t);
+            on = t * 64 + key < (page >= 0 ? s.len : 0);          // (keys behind the end: zeros, whatever the slots hold)
+            const unsigned char* part = part0 + (size_t)(uint32_t)max(page, 0) * page_bytes + (t & 1) * 64 * (D / 2);
+            const unsigned char* part_s = part - (t & 1) * (64 * (D / 2) - 64 * (D / 16));
+            if constexpr (D == 128) {
+                const uint4v c = *reinterpret_cast<const uint4v*>(part + code_at);
+                r.w[0] = c[0]; r.w[1] = c[1]; r.w[2] = c[2]; r.w[3] = c[3];
+            } else {
+                const uint2v c = *reinterpret_cast<const uint2v*>(part + code_at);
+                r.w[0] = c[0]; r.w[1] = c[1];
+            }
+            r.sc = *reinterpret_cast<const uint32_t*>(part_s + scale_at);
+        };
+        auto load = [&](int t) __attribute__((always_inline)) { load_to(raw, raw_on, t); };
+        // K: the 16 bytes of d = 16 i + 8 hf .. of a key in place 32 hf + key % 32 of operand (key / 32, i).  V: key after key.  A store serves eight lanes at
+        // a time, the four pieces j of two keys, on 32 banks: the places of K's operands are turned by the piece, the 16-byte pieces of V's
+        // keys by the key and the piece, so that they are eight different places of 16 bytes of 128.
+        uint32_t place[D / 32];
+#pragma unroll
+        for (int j = 0; j < D / 32; ++j) {
+            const int c = (D / 32) * g + j, i = c >> 1;
+            place[j] = lds0 + (is_v ? (uint32_t)(2 * KB + key * RS + 16 * (D == 128 ? c ^ (2 * (key & 1)) ^ (g >> 1) : c ^ (key & 1)))
+                                    : (uint32_t)((((key >> 5) * ND + i) * 64 + ((32 * (c & 1) + (key & 31)) ^ (2 * ((i >> (D == 128 ? 1 : 0)) & 3)))) * 16));
+        }
+        // (in D / 8 parts, so that they can stand between products: part 4 j + x makes values 8 j + 2 x, + 1, the last of four stores them)
+        struct Unpack { half2v sc; uint32_t buf; uint4v v; };
+        auto unpack_part = [&](Unpack& p, const Raw<D>& raw, bool raw_on, int part, int buf_k, int buf_v) __attribute__((always_inline)) {
+            const int j = part >> 2, x = part & 3;
+            if (part == 0) { p.sc = scales_of<D>(raw, g, raw_on); p.buf = is_v ? (uint32_t)(buf_v * VB) : (uint32_t)(buf_k * KB); }
+            const half_t sv = (D == 128 && j >= 2) ? p.sc[1] : p.sc[0];
+            const half2v sc2 = {sv, sv};
+            if (x == 0) p.v[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(raw.w[j], 1.0f, 0) * sc2);
+            if (x == 1) p.v[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(raw.w[j], 1.0f, 1) * sc2);
+            if (x == 2) p.v[2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(raw.w[j], 1.0f, 2) * sc2);
+            if (x == 3) { p.v[3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(raw.w[j], 1.0f, 3) * sc2); lds_write16_at(place[j] + p.buf, p.v); }
+        };
+        auto unpack = [&](const Raw<D>& raw, bool raw_on, int buf_k, int buf_v) __attribute__((always_inline)) {
+            Unpack p;
+#pragma unroll
+            for (int part = 0; part < D / 8; ++part) unpack_part(p, raw, raw_on, part, buf_k, buf_v);
         };
 
-        // K of the first tile by all: the waves that have V otherwise wait
-        __syncthreads();                                          // (the segment before has read its tiles)
-        if (!is_v) { load(first); unpack(0, 0); }
-        load(is_v ? first : first + 1);
+        // what a segment needs from memory first, asked for at once: Q, the first tile of V, the first two of K
+        uint4v x[ND];
+#pragma unroll
+        for (int i = 0; i < ND; ++i)
+            x[i] = *reinterpret_cast<const uint4v*>(a.q + (size_t)(s.first + tok) * a.q_token + (size_t)head * a.q_head + 16 * i + 8 * half);
+        Raw<D> raw0, raw1;
+        bool on0, on1;
+        load_to(raw0, on0, first);
+        load_to(raw1, on1, first + 1);
+        if (is_v) { raw = raw1; raw_on = on1; } else load(first + 2);
 
         // Q: row col, d = 16 i + 8 half .. + 7
         half8 qreg[ND];
         float c_row;
         {
-            uint4v x[ND];
             float amax = 0.0f;
 #pragma unroll
-            for (int i = 0; i < ND; ++i) {
-                x[i] = *reinterpret_cast<const uint4v*>(a.q + (size_t)(s.first + tok) * a.q_token + (size_t)head * a.q_head + 16 * i + 8 * half);
+            for (int i = 0; i < ND; ++i)
 #pragma unroll
                 for (int j = 0; j < 4; ++j) amax = fmaxf(amax, fmaxf(fabsf(__uint_as_float(x[i][j] << 16)), fabsf(__uint_as_float(x[i][j] & 0xFFFF0000u))));
-            }
             amax = lanes_max<32, 32>(amax);
             float f, inv;
             row_factor(amax, f, inv);
@@ -608,6 +672,9 @@ __global__ __launch_bounds__(512, 2) void ragged_wide_kernel(const RaggedArgs a,
                 }
             c_row = a.c * inv;
         }
+        __syncthreads();                                          // (the segment before has read its tiles)
+        unpack(raw0, on0, 0, 0);
+        if (!is_v) unpack(raw1, on1, 1, 0);
         floatx16 o[NB], sc[2];
         float m = -INFINITY, l = 0.0f;                             // the maximum in units of the exponent of 2
         half8 pt[4];
@@ -616,17 +683,48 @@ __global__ __launch_bounds__(512, 2) void ragged_wide_kernel(const RaggedArgs a,
 #pragma unroll
             for (int j = 0; j < 16; ++j) o[i][j] = 0.0f;
 
-        auto scores = [&](int buf) __attribute__((always_inline)) {
+        // The products of a matrix phase in one run, each operand requested kAhead products before its own: a wave issues in order, and the trip to LDS
+        // is as long as four products.  First (t >= 0) O += V P of a tile, group of 16 keys by group, then S of the next.
+        constexpr int kAhead = 6, NV = 4 * NB, NK = 2 * ND;
+        uint32_t k_base[4];
 #pragma unroll
-            for (int kb = 0; kb < 2; ++kb) {
+        for (int x = 0; x < 4; ++x) k_base[x] = lds0 + 16u * (uint32_t)(lane ^ (2 * x));
+        auto products = [&](auto with_values, int buf_v, int buf_k, int next) __attribute__((always_inline)) {
+            constexpr int N0 = decltype(with_values)::value ? 0 : NV, N = NV + NK;
+            const uint32_t vb[2] = {v_base + (uint32_t)(buf_v * VB), (v_base ^ 16u) + (uint32_t)(buf_v * VB)};
+            uint32_t kb4[4];
 #pragma unroll
-                for (int j = 0; j < 16; ++j) sc[kb][j] = 0.0f;
-#pragma unroll
-                for (int i = 0; i < ND; ++i) {
-                    const uint4v kv = lds_read16_at(lds0 + (uint32_t)(buf * KB + (kb * ND + i) * 1024) + 16u * (uint32_t)(lane ^ (4 * ((i >> (D == 128 ? 1 : 0)) & 3))));
-                    sc[kb] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(half8, kv), qreg[i], sc[kb], 0, 0, 0);
+            for (int x = 0; x < 4; ++x) kb4[x] = k_base[x] + (uint32_t)(buf_k * KB);
+            half8 ring[kAhead];
+            Unpack up;
+            auto operand = [&](int n) __attribute__((always_inline)) {
+                if (n < NV) {
+                    const uint32_t at = vb[(n % NB) >> 1] + (uint32_t)((n / NB) * 16 * RS + 64 * (n % NB));
+                    const uint2v x = lds_read_tr16_at(at), y = lds_read_tr16_at(at + 8 * RS);
+                    return __builtin_bit_cast(half8, uint4v{x[0], x[1], y[0], y[1]});
                 }
+                const int i = (n - NV) >> 1, kb = (n - NV) & 1;
+                return __builtin_bit_cast(half8, lds_read16_at(kb4[(i >> (D == 128 ? 1 : 0)) & 3] + (uint32_t)((kb * ND + i) * 1024)));
+            };
+#pragma unroll
+            for (int n = N0; n < N0 + kAhead; ++n) ring[n % kAhead] = operand(n);
+#pragma unroll
+            for (int n = N0; n < N; ++n) {
+                __builtin_amdgcn_sched_barrier(0);
+                if (n < NV) o[n % NB] = __builtin_amdgcn_mfma_f32_32x32x16_f16(ring[n % kAhead], pt[n / NB], o[n % NB], 0, 0, 0);
+                else {
+                    const int i = (n - NV) >> 1, kb = (n - NV) & 1;
+                    if (i == 0) {
+#pragma unroll
+                        for (int j = 0; j < 16; ++j) sc[kb][j] = 0.0f;
+                    }
+                    sc[kb] = __builtin_amdgcn_mfma_f32_32x32x16_f16(ring[n % kAhead], qreg[i], sc[kb], 0, 0, 0);
+                }
+                if (n + kAhead < N) ring[n % kAhead] = operand(n + kAhead);
+                if (kInProducts && N0 == 0 && n >= 2 && n - 2 < D / 8) unpack_part(up, raw, raw_on, n - 2, buf_v, buf_k);
+                if (kInProducts && N0 == 0 && n == 2 + D / 8) load(next);
             }
+            __builtin_amdgcn_sched_barrier(0);
         };
         auto vector_phase = [&](int t) __attribute__((always_inline)) {
             if (t * 64 < see_first || t * 64 + 63 > see_last) {
@@ -644,8 +742,14 @@ __global__ __launch_bounds__(512, 2) void ragged_wide_kernel(const RaggedArgs a,
 #pragma unroll
                 for (int j = 0; j < 16; ++j) mx = max_nc(mx, sc[kb][j]);
             mx = lanes_max<32, 32>(mx) * c_row;
-            const float m_new = fmaxf(m, mx), m_at = m_new == -INFINITY ? 0.0f : m_new, alpha = __builtin_amdgcn_exp2f(m - m_at);
-            m = m_new;
+            if (__builtin_amdgcn_ballot_w64(mx > m + kSlack) != 0) {
+                const float m_new = fmaxf(m, mx), alpha = __builtin_amdgcn_exp2f(m - (m_new == -INFINITY ? 0.0f : m_new));
+                m = m_new;
+                l *= alpha;
+#pragma unroll
+                for (int i = 0; i < NB; ++i) o[i] *= alpha;
+            }
+            const float m_at = m == -INFINITY ? 0.0f : m;
             float add[2] = {0.0f, 0.0f};
 #pragma unroll
             for (int kb = 0; kb < 2; ++kb)
@@ -655,46 +759,32 @@ __global__ __launch_bounds__(512, 2) void ragged_wide_kernel(const RaggedArgs a,
                     add[j & 1] += x;
                     pt[2 * kb + (j >> 3)][j & 7] = (half_t)x;
                 }
-            l = fmaf(l, alpha, add[0] + add[1]);
-            if (__builtin_amdgcn_ballot_w64(alpha != 1.0f) != 0) {
-#pragma unroll
-                for (int i = 0; i < NB; ++i) o[i] *= alpha;
-            }
+            l += add[0] + add[1];
         };
-        auto values = [&](int buf) __attribute__((always_inline)) {
-#pragma unroll
-            for (int q = 0; q < 4; ++q)
-#pragma unroll
-                for (int i = 0; i < NB; ++i) {
-                    const uint2v x = lds_read_tr16_at(v_base + (uint32_t)(buf * VB + 16 * q * RS + 64 * i)), y = lds_read_tr16_at(v_base + (uint32_t)(buf * VB + (16 * q + 8) * RS + 64 * i));
-                    const uint4v av = {x[0], x[1], y[0], y[1]};
-                    o[i] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(half8, av), pt[q], o[i], 0, 0, 0);
-                }
-        };
-
         // Half-steps: the early waves are in the vector phase of tile i in half-step 2 i and in its matrix phase in 2 i + 1, the late ones one later.
-        // K(i + 1) and V(i), needed from half-step 2 i + 1 on, take the places of K(i - 1) and V(i - 2), last read in 2 i - 2: the late waves
-        // unpack their half of them in 2 i - 1, the early ones in 2 i.
+        // K(i + 2) and V(i + 1), needed from half-step 2 i + 3 on, take the places of K(i) and V(i - 1), last read in 2 i: a wave unpacks its share of
+        // them in 2 i + 1 or 2 i + 2, the one of its two phases that is the shorter: of heads of 64 the matrix phase, between the products, of heads
+        // of 128 the vector phase.
         phase_end();
-        if (mine) scores(0);
-        if (late) { unpack(1, 0); load(is_v ? first + 1 : first + 2); phase_end(); }
+        if (mine) products(std::false_type{}, 0, 0, 0);
+        if (late) phase_end();
         for (int i = 0; i < cnt; ++i) {
-            const int u = late ? i + 1 : i;
-            unpack((u + 1) & 1, u & 1);
-            load(first + (is_v ? u + 1 : u + 2));
-            if (mine) vector_phase(first + i);
-            phase_end();
-            if (mine) {
-                __builtin_amdgcn_s_setprio(1);
-                values(i & 1);
-                scores((i + 1) & 1);
-                __builtin_amdgcn_s_setprio(0);
+            if constexpr (!kInProducts) {
+                __builtin_amdgcn_s_setprio(1);                    // (the longer of the two phases)
+                const int u = late ? i + 1 : i;
+                if (u > 0) { unpack(raw, raw_on, (u + 1) & 1, u & 1); load(first + (is_v ? u + 1 : u + 2)); }
             }
+            if (mine) vector_phase(first + i);
+            if constexpr (!kInProducts) __builtin_amdgcn_s_setprio(0);
+            phase_end();
+            const int next = first + i + (is_v ? 2 : 3);
+            if (mine) products(std::true_type{}, i & 1, (i + 1) & 1, next);
+            else if (kInProducts) { unpack(raw, raw_on, i & 1, (i + 1) & 1); load(next); }
             phase_end();
         }
         if (!late) phase_end();
 
-        const bool whole = cnt == nt;
+        const bool whole = cnt == keys;
         if (mine) {
             l = lanes_sum<32, 32>(l);
             if (whole) {
@@ -709,7 +799,7 @@ __global__ __launch_bounds__(512, 2) void ragged_wide_kernel(const RaggedArgs a,
                     if (half == 0 && a.lse) a.lse[(size_t)(s.first + tok) * a.Hq + head] = l != 0.0f ? m * 0.6931471805599453f + logf(l) : -INFINITY;
                 }
             } else {
-                const size_t slot = ((size_t)blockIdx.x * 2 + (off == 0 ? 1 : 0)) * 8 + wave;
+                const size_t slot = ((size_t)blockIdx.x * 2 + (at == 0 ? 1 : 0)) * 8 + wave;
 #pragma unroll
                 for (int i = 0; i < NB; ++i)
 #pragma unroll
@@ -719,7 +809,6 @@ __global__ __launch_bounds__(512, 2) void ragged_wide_kernel(const RaggedArgs a,
             }
         }
         // on to the next row tile, head, sequence
-        w += cnt;
         off = 0;
         const int tiles = (rows + kWideRows - 1) / kWideRows;
         nt = 0;
@@ -739,7 +828,7 @@ __device__ void wide_merge(const RaggedArgs& a, const WideWs& ws, int place, int
     const long long quota = *ws.quota;
     if (quota == 0) return;
     const WideRec r = ws.rec[place];
-    if (r.off == 0 || r.off > quota) return;
+    if (r.off <= kWideStart || r.off - quota > kWideStart) return;      // it begins there, or has begun two workgroups ago
     const Seq s = seq_of(a, r.b);
     const int G = a.Hq / a.Hkv, rows = s.n * G, wave = part / (D / 32), i = part % (D / 32), lane = threadIdx.x & 63, j = threadIdx.x >> 6;
     const int col = lane & 31, half = lane >> 5, row = r.tile * kWideRows + 32 * wave + col;
@@ -848,7 +937,7 @@ int launch_few(const RaggedArgs& a, const RaggedPlan& p, const FewWs& w, hipStre
 template <int D>
 int launch_wide(const RaggedArgs& a, const RaggedPlan& p, const WideWs& w, hipStream_t st)
 {
-    constexpr int bytes = 2 * 64 * (2 * D + 2 * D + 32);
+    constexpr int bytes = 2 * 64 * (2 * D + 2 * D + 64);
     static unsigned long long done = 0;
     if (!ensure_dynamic_lds((const void*)ragged_wide_kernel<D>, bytes, done)) return -1;
     hipLaunchKernelGGL((ragged_wide_kernel<D>), dim3(p.wide_wgs), dim3(512), bytes, st, a, w);
