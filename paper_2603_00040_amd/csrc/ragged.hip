@@ -66,13 +66,24 @@ __device__ inline Few few_of(const RaggedArgs& a, int b, int G, int most)
 __device__ inline Seq uniform(const Seq& s) { return Seq{uniform(s.first), uniform(s.n), uniform(s.len)}; }
 __device__ inline Few uniform(const Few& u) { return Few{uniform(u.rows), uniform(u.first_page), uniform(u.pages)}; }
 
-// Sums over a workgroup of W waves: inclusive, and of all.
+// Inclusive sums over the lanes of a wave, by DPP (a step through LDS is a hundred cycles, and the start of a step is all such sums), and over a
+// workgroup of W waves, with the sum of all.  64 bits: values below 2^40.
+__device__ inline int lane_scan(int v)
+{
+#define AQ_ADD(CTRL, ROWS) v += __builtin_amdgcn_update_dpp(0, v, CTRL, ROWS, 0xF, false)
+    AQ_ADD(0x111, 0xF); AQ_ADD(0x112, 0xF); AQ_ADD(0x114, 0xF); AQ_ADD(0x118, 0xF);      // within a row of 16 lanes
+    AQ_ADD(0x142, 0xA); AQ_ADD(0x143, 0xC);                                              // the last lane of a row into the next, of the lower half into the upper
+#undef AQ_ADD
+    return v;
+}
+__device__ inline long long lane_scan(long long v) { return (long long)lane_scan((int)(v & 0xFFFF)) + ((long long)lane_scan((int)(v >> 16)) << 16); }
+__device__ inline int lane_total(int v) { return __builtin_amdgcn_readlane(lane_scan(v), 63); }
+__device__ inline long long lane_total(long long v) { return (long long)lane_total((int)(v & 0xFFFF)) + ((long long)lane_total((int)(v >> 16)) << 16); }
 template <int W, class T>
 __device__ inline T wg_scan(T v, T* red /* [W], LDS */, T& total)
 {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) { const T u = __shfl_up(v, d); if (lane >= d) v += u; }
+    v = lane_scan(v);
     __syncthreads();                                             // (red of the call before has been read)
     if (lane == 63) red[wave] = v;
     __syncthreads();
@@ -158,12 +169,12 @@ __global__ __launch_bounds__(256, RT == 1 ? 3 : 2) void ragged_few_kernel(const 
     const uint32_t tr_base = lds_addr_of(stg) + (uint32_t)((4 * g + (cc >> 2)) * RS + 8 * ((cc & 3) ^ (2 * (g & 1))));
 
     // this workgroup's pages [w, w_end) of all units', and the sequence that the first of them belongs to
-    int all = 0, total;
+    int all = 0, total, n_b = 0, upto_b = 0;
     for (int b0 = 0; b0 < a.B; b0 += 256) {
-        const int n = b0 + tid < a.B ? few_of(a, b0 + tid, G, ROWS).pages : 0;
-        const int upto = all + wg_scan<4>(n, red, total);
+        n_b = b0 + tid < a.B ? few_of(a, b0 + tid, G, ROWS).pages : 0;
+        upto_b = all + wg_scan<4>(n_b, red, total);
         if (blockIdx.x == 0) {
-            if (b0 + tid < a.B) ws.front[b0 + tid + 1] = upto;
+            if (b0 + tid < a.B) ws.front[b0 + tid + 1] = upto_b;
             if (b0 + tid == 0) ws.front[0] = 0;
         }
         all += total;
@@ -174,20 +185,17 @@ __global__ __launch_bounds__(256, RT == 1 ? 3 : 2) void ragged_few_kernel(const 
     long long w = (long long)blockIdx.x * quota;
     const long long w_end = min(w + quota, work);
     if (w >= w_end) return;
-    int b = 0, front = 0;
-    {
-        int at = 0;
-        for (int b0 = 0; b0 < a.B; b0 += 256) {
-            const int n = b0 + tid < a.B ? few_of(a, b0 + tid, G, ROWS).pages : 0;
-            const int upto = at + wg_scan<4>(n, red, total);
-            if (n > 0 && w < (long long)upto * a.Hkv && w >= (long long)(upto - n) * a.Hkv) { found[0] = b0 + tid; found[1] = upto - n; }
+    for (int b0 = 0, at = 0; ; b0 += 256) {
+        if (a.B > 256) {                                          // (up to 256 sequences: as found above)
+            n_b = b0 + tid < a.B ? few_of(a, b0 + tid, G, ROWS).pages : 0;
+            upto_b = at + wg_scan<4>(n_b, red, total);
             at += total;
-            if (w < (long long)at * a.Hkv) break;
         }
-        __syncthreads();
-        b = uniform(found[0]);
-        front = uniform(found[1]);
+        if (n_b > 0 && w < (long long)upto_b * a.Hkv && w >= (long long)(upto_b - n_b) * a.Hkv) { found[0] = b0 + tid; found[1] = upto_b - n_b; }
+        if (a.B <= 256 || w < (long long)at * a.Hkv || b0 + 256 >= a.B) break;
     }
+    __syncthreads();
+    int b = uniform(found[0]), front = uniform(found[1]);
 
     while (w < w_end) {
         Few u = uniform(few_of(a, b, G, ROWS));
@@ -462,8 +470,7 @@ __device__ inline long long wide_work(const RaggedArgs& a, int G, int b)
         const int tiles = (x.n * G + kWideRows - 1) / kWideRows;
         long long sum = 0;
         for (int r = lane; r < tiles; r += 64) { int t0, nt; wide_tile(a, x, G, r, t0, nt); sum += nt; }
-#pragma unroll
-        for (int d = 32; d >= 1; d >>= 1) sum += __shfl_xor(sum, d);
+        sum = lane_total(sum);
         if (lane == src) mine = sum;
     }
     return mine;
@@ -486,7 +493,7 @@ __global__ __launch_bounds__(512, 2) void ragged_wide_kernel(const RaggedArgs a,
     constexpr bool kInProducts = D == 64;
     constexpr size_t VOFF = (size_t)128 * (D / 2 + D / 16);
     extern __shared__ __align__(256) unsigned char lds[];          // two tiles of K, two of V
-    __shared__ long long red[8], found_front;
+    __shared__ long long red[8], found_front, found_per;
     __shared__ int found_b;
     const int tid = threadIdx.x, lane = tid & 63, col = lane & 31, half = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -494,8 +501,12 @@ __global__ __launch_bounds__(512, 2) void ragged_wide_kernel(const RaggedArgs a,
     const int G = a.Hq / a.Hkv;
 
     // this workgroup's key tiles [w, w_end) of all units', and where they begin
-    long long all = 0, total;
-    for (int b0 = 0; b0 < a.B; b0 += 512) { (void)wg_scan<8>(wide_work(a, G, b0 + tid), red, total); all += total; }
+    long long all = 0, total, n_b = 0, upto_b = 0;
+    for (int b0 = 0; b0 < a.B; b0 += 512) {
+        n_b = wide_work(a, G, b0 + tid);
+        upto_b = all + wg_scan<8>(n_b, red, total);
+        all += total;
+    }
     const long long work = all * a.Hkv;
     long long quota = (work + gridDim.x - 1) / gridDim.x;
     if (blockIdx.x == 0 && tid == 0) *ws.quota = quota;
@@ -505,15 +516,19 @@ __global__ __launch_bounds__(512, 2) void ragged_wide_kernel(const RaggedArgs a,
     if (tid == 0) ws.rec[blockIdx.x] = WideRec{0, 0, 0, 0, 0, {0, 0, 0}};
     if (w >= w_end) return;
     long long front = 0;                                          // key tiles (of one head) of the sequences in front of b
-    for (int b0 = 0; b0 < a.B; b0 += 512) {
-        const long long n = wide_work(a, G, b0 + tid), upto = front + wg_scan<8>(n, red, total);
-        if (n > 0 && w < upto * a.Hkv && w >= (upto - n) * a.Hkv) { found_b = b0 + tid; found_front = upto - n; }
-        front += total;
-        if (w < front * a.Hkv) break;
+    for (int b0 = 0; ; b0 += 512) {
+        if (a.B > 512) {                                          // (up to 512 sequences: as found above)
+            n_b = wide_work(a, G, b0 + tid);
+            upto_b = front + wg_scan<8>(n_b, red, total);
+            front += total;
+        }
+        if (n_b > 0 && w < upto_b * a.Hkv && w >= (upto_b - n_b) * a.Hkv) { found_b = b0 + tid; found_front = upto_b - n_b; found_per = n_b; }
+        if (a.B <= 512 || w < front * a.Hkv || b0 + 512 >= a.B) break;
     }
     __syncthreads();
     int b = uniform(found_b);
     front = uniform(found_front);
+    long long per = uniform(found_per);                           // key tiles of one head of sequence b; 0: to be counted
 
     const uint32_t lds0 = lds_addr_of(lds);
     // (key 4 half + r of 16, r = (lane & 15) / 4; for the order of the 16-byte pieces of a key see unpack)
@@ -535,25 +550,21 @@ __global__ __launch_bounds__(512, 2) void ragged_wide_kernel(const RaggedArgs a,
             if (b >= a.B) return;
             s = uniform(seq_of(a, b));
             const int tiles = (s.n * G + kWideRows - 1) / kWideRows;
-            long long per = 0;                                    // key tiles of one head
-            for (int r0 = 0; r0 < tiles; r0 += 64) {
-                int x0, n = 0;
-                if (r0 + lane < tiles) wide_tile(a, s, G, r0 + lane, x0, n);
-                long long v = n;
-#pragma unroll
-                for (int d = 32; d >= 1; d >>= 1) v += __shfl_xor(v, d);
-                per += uniform(v);
+            if (per == 0 && s.n * G > kFewRows) {
+                for (int r0 = 0; r0 < tiles; r0 += 64) {
+                    int x0, n = 0;
+                    if (r0 + lane < tiles) wide_tile(a, s, G, r0 + lane, x0, n);
+                    per += lane_total(n);                         // (64 row tiles of at most 2^14 key tiles)
+                }
             }
-            if (per == 0 || s.n * G <= kFewRows) { if (++b >= a.B) return; continue; }
+            if (per == 0) { ++b; continue; }                      // (a sequence of the other kernel, or without a key)
             const long long in_seq = w - front * a.Hkv;
             h = (int)(in_seq / per);
             long long rem = in_seq % per;
             for (int r0 = 0; r0 < tiles && tile < 0; r0 += 64) {
                 int x0 = 0, n = 0;
                 if (r0 + lane < tiles) wide_tile(a, s, G, r0 + lane, x0, n);
-                int upto = n;
-#pragma unroll
-                for (int d = 1; d < 64; d <<= 1) { const int u = __shfl_up(upto, d); if (lane >= d) upto += u; }
+                const int upto = lane_scan(n);
                 const unsigned long long hit = __builtin_amdgcn_ballot_w64(rem < upto && rem >= upto - n);
                 if (hit != 0) {
                     const int src = (int)__builtin_ctzll(hit);
@@ -815,7 +826,7 @@ __global__ __launch_bounds__(512, 2) void ragged_wide_kernel(const RaggedArgs a,
         while (nt == 0 && ++tile < tiles) wide_tile(a, s, G, tile, t0, nt);
         if (nt == 0) {                                            // this head is done
             tile = -1;
-            if (h == a.Hkv - 1) { front = w / a.Hkv; ++b; }       // (w is a multiple of the heads there)
+            if (h == a.Hkv - 1) { front += per; per = 0; ++b; }
         }
     }
 }
