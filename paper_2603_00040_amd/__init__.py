@@ -120,6 +120,10 @@ def _stream():
     return _raw_stream(torch.cuda.current_device())
 
 
+def _stream_on(dev):
+    return torch.cuda.current_stream(dev).cuda_stream if _raw_stream is None else _raw_stream(dev)
+
+
 def _dev_bf16(t, name):
     if not (t.is_cuda and t.dtype == torch.bfloat16 and t.is_contiguous() and t.dim() == 4):
         raise AttnQatError(f"{name} must be a contiguous 4-d bf16 CUDA tensor [B,H,L,d]")
@@ -265,35 +269,33 @@ def attnqat_fwd_infer_paged(q, cache, num_pages, page_table, kv_lens, Hkv, causa
     return o, lse
 
 
-def _serve_int(t, name, shape, dtype=torch.int32):
-    if not (t.is_cuda and t.dtype == dtype and t.is_contiguous() and tuple(t.shape) == tuple(shape)):
-        raise AttnQatError(f"{name} must be a contiguous {dtype} CUDA tensor of shape {tuple(shape)}")
+# The calls of a serving step.  The smallest of them take a few microseconds, of which the checks of their arguments are a good part: what is
+# expected is asked for in one expression, and only where that fails is it found out which tensor it was.
+_BF, _I32, _I64, _U8, _F32 = torch.bfloat16, torch.int32, torch.int64, torch.uint8, torch.float32
+_current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
 
 
-def _serve_rows(t, name, shape=None):
-    if not (t.is_cuda and t.dtype == torch.bfloat16 and t.dim() == 3 and (t.stride(2) == 1 or t.numel() == 0)
-            and (shape is None or tuple(t.shape) == tuple(shape))):
-        raise AttnQatError(f"{name} must be a bf16 CUDA tensor [T,heads,d]{'' if shape is None else ' of shape ' + str(tuple(shape))}, d innermost")
-    return t.data_ptr(), t.stride(0), t.stride(1)
-
-
-def _serve_cache(cache, num_pages, Hkv, d):
-    if not (cache.is_cuda and cache.dtype == torch.uint8 and cache.is_contiguous()):
+def _serve_refuse(ints, rows=(), cache=None):
+    """Names the tensor that is not as it should be: ``ints`` (name, tensor, shape, dtype), ``rows`` (name, tensor, shape)."""
+    for name, t, shape, dtype in ints:
+        if not (t.is_cuda and t.dtype is dtype and t.is_contiguous() and t.shape == shape):
+            raise AttnQatError(f"{name} must be a contiguous {dtype} CUDA tensor of shape {shape}")
+    for name, t, shape in rows:
+        if not (t.is_cuda and t.dtype is _BF and t.dim() == 3 and t.shape == shape and (t.stride(2) == 1 or t.numel() == 0)):
+            raise AttnQatError(f"{name} must be a bf16 CUDA tensor [T,heads,d] of shape {tuple(shape)}, d innermost")
+    if cache is not None and not (cache.is_cuda and cache.dtype is _U8 and cache.is_contiguous()):
         raise AttnQatError("cache must be a contiguous uint8 CUDA tensor")
-    page = kv_cache_page_bytes_nvfp4(Hkv, d)
-    have = cache.numel() // page if page else 0
+    raise AttnQatError(f"all tensors must be on the current device (cuda:{_current_device()})")
+
+
+def _serve_pages(cache, num_pages, Hkv, d):
+    page = Hkv * d * 144                          # (2 parts of 128 positions of d / 2 + d / 16 bytes; the library refuses other d)
+    have = cache.numel() // page if page > 0 else 0
     if num_pages is None:
-        num_pages = have
-    if page and not 0 < num_pages <= have:
+        return have
+    if not 0 < num_pages <= have:
         raise AttnQatError(f"cache has room for {have} pages, not for {num_pages}")
     return int(num_pages)
-
-
-def _same_device(*tensors):
-    """The kernels run on the current device's current stream."""
-    now = torch.cuda.current_device()
-    if any(t is not None and t.device.index != now for t in tensors):
-        raise AttnQatError(f"all tensors must be on the current device (cuda:{now})")
 
 
 def page_plan_workspace_bytes(B: int) -> int:
@@ -303,64 +305,81 @@ def page_plan_workspace_bytes(B: int) -> int:
 def attnqat_page_plan(kv_lens, new_lens, page_table, capacity: int, free=None, workspace=None, out=None):
     """Page table, slots and positions of a serving step.  kv_lens, new_lens int32 [B]: positions that the requests have and want;
     page_table int32 [B,max_pages], updated in place; ``capacity`` the most new positions of the step; ``free`` = (free_pages int32 [places],
-    free_state int32 [>= 2]: place of the first free page, number of free pages), a ring from which pages are taken (updated in place) and to which they
-    are given back, or None for a table that is complete already.  Returns (kv_lens int32 [B], cu_q int32 [B+1], slots int64 [capacity], positions int32
-    [capacity], free_state int32 [3]: first free place, free pages, refused requests, or None without ``free``).  ``out``: those five; the first and the
-    last may be kv_lens and a free_state of 3."""
-    B, T = kv_lens.numel(), int(capacity)
-    _serve_int(kv_lens, "kv_lens", (B,))
-    _serve_int(new_lens, "new_lens", (B,))
+    free_state int32 [>= 2]: place of the first free page, number of free pages), a ring from which pages are taken and to which they are given
+    back (updated in place), or None for a table that is complete already.  Returns (kv_lens int32 [B], cu_q int32 [B+1], slots int64 [capacity],
+    positions int32 [capacity], free_state int32 [3]: first free place, free pages, refused requests, or None without ``free``).  ``out``: those
+    five; the first and the last may be kv_lens and a free_state of 3."""
+    B, T, dev = kv_lens.numel(), int(capacity), kv_lens.get_device()
     if page_table.dim() != 2:
         raise AttnQatError("page_table must be [B,max_pages]")
-    _serve_int(page_table, "page_table", (B, page_table.shape[1]))
     if T < 0:
         raise AttnQatError("capacity must not be negative")
+    most = page_table.shape[1]
     ring, state = (None, None) if free is None else free
-    if free is not None:
-        _serve_int(ring, "free_pages", (ring.numel(),))
-        if state.dim() != 1 or state.numel() < 2:
-            raise AttnQatError("free_state must have at least two elements")
-        _serve_int(state, "free_state", (state.numel(),))
     if out is None:
-        e = lambda n, t=torch.int32: torch.empty(n, dtype=t, device=kv_lens.device)  # noqa: E731
-        out = (e(B), e(B + 1), e(T, torch.int64), e(T), e(3) if free is not None else None)
+        e = lambda n, t=_I32: torch.empty(n, dtype=t, device=kv_lens.device)  # noqa: E731
+        out = (e(B), e(B + 1), e(T, _I64), e(T), e(3) if free is not None else None)
     lens, cu, slots, positions, state_out = out
-    _serve_int(lens, "out[0]", (B,))
-    _serve_int(cu, "out[1]", (B + 1,))
-    _serve_int(slots, "out[2]", (T,), torch.int64)
-    _serve_int(positions, "out[3]", (T,))
-    if free is not None:
-        _serve_int(state_out, "out[4]", (3,))
-    _same_device(kv_lens, new_lens, page_table, ring, state, *out, workspace)
+    if not (dev == _current_device() == new_lens.get_device() == page_table.get_device() == lens.get_device() == cu.get_device() == slots.get_device() == positions.get_device()
+            and kv_lens.dtype is new_lens.dtype is page_table.dtype is lens.dtype is cu.dtype is positions.dtype is _I32 and slots.dtype is _I64
+            and kv_lens.shape == new_lens.shape == lens.shape == (B,) and cu.shape == (B + 1,) and slots.shape == positions.shape == (T,) and page_table.shape[0] == B
+            and kv_lens.is_contiguous() and new_lens.is_contiguous() and page_table.is_contiguous() and lens.is_contiguous() and cu.is_contiguous()
+            and slots.is_contiguous() and positions.is_contiguous()):
+        _serve_refuse([("kv_lens", kv_lens, (B,), _I32), ("new_lens", new_lens, (B,), _I32), ("page_table", page_table, (B, most), _I32), ("out[0]", lens, (B,), _I32),
+                       ("out[1]", cu, (B + 1,), _I32), ("out[2]", slots, (T,), _I64), ("out[3]", positions, (T,), _I32)])
+    if free is None:
+        places, state_out = 0, None
+        pr = ps = po = None
+    else:
+        places = ring.numel()
+        if not (dev == ring.get_device() == state.get_device() == state_out.get_device() and ring.dtype is state.dtype is state_out.dtype is _I32 and ring.dim() == state.dim() == 1
+                and state.numel() >= 2 and state_out.shape == (3,) and ring.is_contiguous() and state.is_contiguous() and state_out.is_contiguous()):
+            _serve_refuse([("free_pages", ring, (places,), _I32), ("free_state", state, (max(2, state.numel()),), _I32), ("out[4]", state_out, (3,), _I32)])
+        pr, ps, po = ring.data_ptr(), state.data_ptr(), state_out.data_ptr()
     if workspace is None:
-        workspace = torch.empty(max(page_plan_workspace_bytes(B), 1), dtype=torch.uint8, device=kv_lens.device)
-    _check(lib().attnqat_page_plan(_ptr(kv_lens), _ptr(new_lens), B, _ptr(page_table), page_table.shape[1], _ptr(ring), 0 if ring is None else ring.numel(),
-                                   _ptr(state), T, _ptr(lens), _ptr(cu), _ptr(slots), _ptr(positions), _ptr(state_out) if free is not None else None,
-                                   _ptr(workspace), workspace.numel(), _stream()))
-    return lens, cu, slots, positions, state_out if free is not None else None
+        workspace = torch.empty(max(page_plan_workspace_bytes(B), 1), dtype=_U8, device=kv_lens.device)
+    elif workspace.get_device() != dev:
+        raise AttnQatError("workspace must be on the device of the other tensors")
+    rc = (_lib or lib()).attnqat_page_plan(kv_lens.data_ptr(), new_lens.data_ptr(), B, page_table.data_ptr(), most, pr, places, ps, T, lens.data_ptr(), cu.data_ptr(),
+                                           slots.data_ptr(), positions.data_ptr(), po, workspace.data_ptr(), workspace.nbytes, _stream_on(dev))
+    if rc:
+        _check(rc)
+    return lens, cu, slots, positions, state_out
 
 
 def attnqat_kv_cache_append(k, v, cache, slots, num_pages=None):
     """Quantize row t of k, v [T,Hkv,d] bf16 (any stride per row and head) into slot ``slots[t]`` (int64 [T], page * 128 + position within the page; slots
     outside the cache are left out) of the NVFP4 KV ``cache`` (uint8 CUDA tensor)."""
-    kp, vp = _serve_rows(k, "k"), _serve_rows(v, "v", k.shape)
-    T, Hkv, d = k.shape
-    _serve_int(slots, "slots", (T,), torch.int64)
-    num_pages = _serve_cache(cache, num_pages, Hkv, d)
-    _same_device(k, v, cache, slots)
-    _check(lib().attnqat_kv_cache_append(*kp, *vp, T, Hkv, d, BF16, _ptr(cache), num_pages, _ptr(slots), _stream()))
+    shape, dev = k.shape, k.get_device()
+    if not (len(shape) == 3 and v.shape == shape and k.dtype is v.dtype is _BF and slots.dtype is _I64 and slots.shape == shape[:1] and cache.dtype is _U8
+            and dev == _current_device() == v.get_device() == cache.get_device() == slots.get_device() and cache.is_contiguous() and slots.is_contiguous()):
+        _serve_refuse([("slots", slots, tuple(shape[:1]), _I64)], [("k", k, shape), ("v", v, shape)], cache)
+    T, Hkv, d = shape
+    (kt, kh, k1), (vt, vh, v1) = k.stride(), v.stride()
+    if not k1 == v1 == 1 and k.numel() > 0:
+        _serve_refuse([], [("k", k, shape), ("v", v, shape)])
+    rc = (_lib or lib()).attnqat_kv_cache_append(k.data_ptr(), kt, kh, v.data_ptr(), vt, vh, T, Hkv, d, BF16, cache.data_ptr(), _serve_pages(cache, num_pages, Hkv, d),
+                                                 slots.data_ptr(), _stream_on(dev))
+    if rc:
+        _check(rc)
 
 
 def attnqat_kv_cache_read(cache, slots, Hkv: int, d: int, num_pages=None, out=None):
     """The values that the NVFP4 KV ``cache`` holds in ``slots`` (int64 [T]; zeros for a slot outside the cache).  Returns (k, v) bf16
     [T,Hkv,d]; ``out``: those two, of any stride per row and head."""
-    T = slots.numel()
-    _serve_int(slots, "slots", (T,), torch.int64)
-    num_pages = _serve_cache(cache, num_pages, Hkv, d)
-    k, v = out if out is not None else tuple(torch.empty((T, Hkv, d), dtype=torch.bfloat16, device=cache.device) for _ in range(2))
-    kp, vp = _serve_rows(k, "out[0]", (T, Hkv, d)), _serve_rows(v, "out[1]", (T, Hkv, d))
-    _same_device(cache, slots, k, v)
-    _check(lib().attnqat_kv_cache_read(_ptr(cache), num_pages, _ptr(slots), T, Hkv, d, BF16, *kp, *vp, _stream()))
+    T, dev = slots.numel(), slots.get_device()
+    shape = (T, Hkv, d)
+    k, v = out if out is not None else tuple(torch.empty(shape, dtype=_BF, device=cache.device) for _ in range(2))
+    if not (k.shape == v.shape == shape and k.dtype is v.dtype is _BF and slots.dtype is _I64 and slots.dim() == 1 and cache.dtype is _U8
+            and dev == _current_device() == k.get_device() == v.get_device() == cache.get_device() and cache.is_contiguous() and slots.is_contiguous()):
+        _serve_refuse([("slots", slots, (T,), _I64)], [("out[0]", k, shape), ("out[1]", v, shape)], cache)
+    (kt, kh, k1), (vt, vh, v1) = k.stride(), v.stride()
+    if not k1 == v1 == 1 and k.numel() > 0:
+        _serve_refuse([], [("out[0]", k, shape), ("out[1]", v, shape)])
+    rc = (_lib or lib()).attnqat_kv_cache_read(cache.data_ptr(), _serve_pages(cache, num_pages, Hkv, d), slots.data_ptr(), T, Hkv, d, BF16, k.data_ptr(), kt, kh,
+                                               v.data_ptr(), vt, vh, _stream_on(dev))
+    if rc:
+        _check(rc)
     return k, v
 
 
@@ -374,29 +393,32 @@ def attnqat_fwd_kv4_ragged(q, cu_q, cache, num_pages, page_table, kv_lens, Hkv: 
     per row and head), rows cu_q[b] .. cu_q[b+1]-1 (int32 [B+1]) being the last positions of sequence b, which has kv_lens[b] keys (int32 [B]) in the
     pages page_table[b] (int32 [B,max_pages]).  ``max_q``: the most rows of a sequence (default T); ``window`` (causal only): a row sees that many keys at
     most, its own position included; ``scale``: default 1/sqrt(d).  Returns (o bf16 [T,Hq,d], lse fp32 [T,Hq]); ``out``: those two (lse may be None)."""
-    qp = _serve_rows(q, "q")
-    T, Hq, d = q.shape
-    B = kv_lens.numel()
-    _serve_int(kv_lens, "kv_lens", (B,))
-    _serve_int(cu_q, "cu_q", (B + 1,))
-    if page_table.dim() != 2:
-        raise AttnQatError("page_table must be [B,max_pages]")
-    _serve_int(page_table, "page_table", (B, page_table.shape[1]))
-    num_pages = _serve_cache(cache, num_pages, Hkv, d)
-    if out is None:
-        out = (torch.empty((T, Hq, d), dtype=torch.bfloat16, device=q.device), torch.empty((T, Hq), dtype=torch.float32, device=q.device))
-    o, lse = out
-    op = _serve_rows(o, "out[0]", (T, Hq, d))
-    if lse is not None:
-        _serve_int(lse, "out[1]", (T, Hq), torch.float32)
-    _same_device(q, cu_q, cache, page_table, kv_lens, o, lse, workspace)
+    shape, dev, B = q.shape, q.get_device(), kv_lens.numel()
+    if len(shape) != 3 or page_table.dim() != 2:
+        raise AttnQatError("q must be [T,Hq,d] and page_table [B,max_pages]")
+    T, Hq, d = shape
+    most = page_table.shape[1]
+    o, lse = out if out is not None else (torch.empty(shape, dtype=_BF, device=q.device), torch.empty((T, Hq), dtype=_F32, device=q.device))
+    if not (q.dtype is o.dtype is _BF and o.shape == shape and kv_lens.dtype is cu_q.dtype is page_table.dtype is _I32 and cache.dtype is _U8
+            and kv_lens.shape == (B,) and cu_q.shape == (B + 1,) and page_table.shape[0] == B
+            and dev == _current_device() == o.get_device() == cu_q.get_device() == cache.get_device() == page_table.get_device() == kv_lens.get_device()
+            and cache.is_contiguous() and cu_q.is_contiguous() and page_table.is_contiguous() and kv_lens.is_contiguous()
+            and (lse is None or (lse.dtype is _F32 and lse.shape == (T, Hq) and lse.get_device() == dev and lse.is_contiguous()))):
+        _serve_refuse([("kv_lens", kv_lens, (B,), _I32), ("cu_q", cu_q, (B + 1,), _I32), ("page_table", page_table, (B, most), _I32)]
+                      + ([] if lse is None else [("out[1]", lse, (T, Hq), _F32)]), [("q", q, shape), ("out[0]", o, shape)], cache)
+    (qt, qh, q1), (ot, oh, o1) = q.stride(), o.stride()
+    if not q1 == o1 == 1 and q.numel() > 0:
+        _serve_refuse([], [("q", q, shape), ("out[0]", o, shape)])
     max_q = max(T, 1) if max_q is None else int(max_q)
-    max_pages = page_table.shape[1]
     if workspace is None:
-        workspace = torch.empty(max(kv4_ragged_workspace_bytes(T, B, Hq, Hkv, max_q, max_pages, d), 1), dtype=torch.uint8, device=q.device)
-    _check(lib().attnqat_fwd_kv4_ragged(*qp, _ptr(cu_q), T, max_q, B, Hq, Hkv, d, int(causal), int(window),
-                                        1.0 / d ** 0.5 if scale is None else float(scale), BF16, _ptr(cache), num_pages, _ptr(page_table), max_pages,
-                                        _ptr(kv_lens), *op, _ptr(lse), _ptr(workspace), workspace.numel(), _stream()))
+        workspace = torch.empty(max(kv4_ragged_workspace_bytes(T, B, Hq, Hkv, max_q, most, d), 1), dtype=_U8, device=q.device)
+    elif workspace.get_device() != dev:
+        raise AttnQatError("workspace must be on the device of the other tensors")
+    rc = (_lib or lib()).attnqat_fwd_kv4_ragged(q.data_ptr(), qt, qh, cu_q.data_ptr(), T, max_q, B, Hq, Hkv, d, int(causal), int(window), d ** -0.5 if scale is None else scale, BF16,
+                                                cache.data_ptr(), _serve_pages(cache, num_pages, Hkv, d), page_table.data_ptr(), most, kv_lens.data_ptr(),
+                                                o.data_ptr(), ot, oh, None if lse is None else lse.data_ptr(), workspace.data_ptr(), workspace.nbytes, _stream_on(dev))
+    if rc:
+        _check(rc)
     return o, lse
 
 

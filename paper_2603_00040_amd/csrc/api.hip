@@ -597,12 +597,26 @@ int attnqat_page_plan(const int* kv_lens, const int* new_lens, int B, int* page_
     if (free_pages ? !free_state || !free_state_out || num_free_slots < 1 : num_free_slots != 0) return ATTNQAT_EINVAL;
     if ((uintptr_t)slots & 7) return ATTNQAT_EINVAL;
     if (B > kMaxServeBatch || max_pages > kMaxServePages) return ATTNQAT_ESHAPE;
-    if (overlap(cu_q, (size_t)(B + 1) * 4, kv_lens, (size_t)B * 4) || overlap(cu_q, (size_t)(B + 1) * 4, new_lens, (size_t)B * 4)) return ATTNQAT_EINVAL;
+    // kv_lens_out may be kv_lens and free_state_out free_state; what else is written lies over nothing that is read
+    const size_t nb = (size_t)B * 4;
+    struct Range { const void* p; size_t n; };
+    const Range in[5] = {{kv_lens, nb}, {new_lens, nb}, {free_state, free_pages ? 8u : 0u}, {page_table, nb * max_pages}, {free_pages, (size_t)num_free_slots * 4}};
+    const Range out[5] = {{kv_lens_out, nb}, {free_state_out, free_pages ? 12u : 0u}, {cu_q, nb + 4}, {slots, (size_t)T * 8}, {positions, (size_t)T * 4}};
+    bool in_place = false;
+    for (int o = 0; o < 5; ++o) {
+        for (int i = 0; i < 5; ++i)
+            if (out[o].n && in[i].n && overlap(out[o].p, out[o].n, in[i].p, in[i].n)) {
+                if (out[o].p != in[i].p || !((o == 0 && i == 0) || (o == 1 && i == 2))) return ATTNQAT_EINVAL;
+                in_place = true;
+            }
+        for (int x = 0; x < o; ++x)
+            if (out[o].n && out[x].n && overlap(out[o].p, out[o].n, out[x].p, out[x].n)) return ATTNQAT_EINVAL;
+    }
     if (!workspace || ((uintptr_t)workspace & 15) || workspace_bytes < page_plan_ws_bytes(B)) return ATTNQAT_EWORKSPACE;
     hipStream_t st = (hipStream_t)stream;
     prof_begin(st);
     if (launch_page_plan(kv_lens, new_lens, B, page_table, max_pages, free_pages, free_pages ? num_free_slots : 0, free_state, T,
-                         kv_lens_out, cu_q, (long long*)slots, positions, free_state_out, workspace, st)) return ATTNQAT_ELAUNCH;
+                         kv_lens_out, cu_q, (long long*)slots, positions, free_state_out, in_place, workspace, st)) return ATTNQAT_ELAUNCH;
     prof_mark("page_plan", st);
     return ATTNQAT_OK;
 }

@@ -174,6 +174,42 @@ template <int FROM, int TO> __device__ __forceinline__ float lanes_sum(float x) 
 template <int N>
 __device__ __forceinline__ uint32_t lane_down(uint32_t x) { return __builtin_amdgcn_update_dpp(0u, x, 0x100 + N, 0xF, 0xF, true); }
 
+// A value that all lanes have, told to the compiler.
+__device__ inline int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
+__device__ inline long long uniform(long long v)
+{
+    return (long long)((unsigned long long)(uint32_t)__builtin_amdgcn_readfirstlane((int)(v >> 32)) << 32 | (uint32_t)__builtin_amdgcn_readfirstlane((int)v));
+}
+
+// Inclusive sums over the lanes of a wave, by DPP (a step through LDS is a hundred cycles, and the start of a step is all such sums), and over a
+// workgroup of W waves, with the sum of all.  64 bits: values below 2^40.
+__device__ inline int lane_scan(int v)
+{
+#define AQ_ADD(CTRL, ROWS) v += __builtin_amdgcn_update_dpp(0, v, CTRL, ROWS, 0xF, false)
+    AQ_ADD(0x111, 0xF); AQ_ADD(0x112, 0xF); AQ_ADD(0x114, 0xF); AQ_ADD(0x118, 0xF);      // within a row of 16 lanes
+    AQ_ADD(0x142, 0xA); AQ_ADD(0x143, 0xC);                                              // the last lane of a row into the next, of the lower half into the upper
+#undef AQ_ADD
+    return v;
+}
+__device__ inline long long lane_scan(long long v) { return (long long)lane_scan((int)(v & 0xFFFF)) + ((long long)lane_scan((int)(v >> 16)) << 16); }
+__device__ inline int lane_total(int v) { return __builtin_amdgcn_readlane(lane_scan(v), 63); }
+__device__ inline long long lane_total(long long v) { return (long long)lane_total((int)(v & 0xFFFF)) + ((long long)lane_total((int)(v >> 16)) << 16); }
+template <int W, class T>
+__device__ inline T wg_scan(T v, T* red /* [W], LDS */, T& total)
+{
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    v = lane_scan(v);
+    __syncthreads();                                             // (red of the call before has been read)
+    if (lane == 63) red[wave] = v;
+    __syncthreads();
+    total = 0;
+    T front = 0;
+#pragma unroll
+    for (int w = 0; w < W; ++w) { front += w < wave ? red[w] : T(0); total += red[w]; }
+    total = uniform(total);
+    return v + front;
+}
+
 // Whatever a free register holds: the first operand of a conversion that replaces part of a register whose rest is never read, or is
 // replaced by the conversions that follow.  A zero, or a register that is still needed, costs a move.
 __device__ inline uint32_t any_register() {

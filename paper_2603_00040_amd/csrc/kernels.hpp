@@ -71,7 +71,8 @@ int launch_kv_page_write(const void* k, const void* v, int Hkv, int n, int D, in
 // A serving step's page table and slot map (serve.hip; arguments as attnqat_page_plan; ring_size 0: no ring).  ws: page_plan_ws_bytes() bytes.
 size_t page_plan_ws_bytes(int B);
 int launch_page_plan(const int* kv_lens, const int* new_lens, int B, int* page_table, int max_pages, int* ring, int ring_size, const int* ring_state,
-                     int T, int* kv_out, int* cu, long long* slots, int* positions, int* state_out, void* ws, hipStream_t st);
+                     int T, int* kv_out, int* cu, long long* slots, int* positions, int* state_out, bool in_place /* an output lies over an input */,
+                     void* ws, hipStream_t st);
 
 // Rows [T, heads, D] bf16 with a stride in elements per token and per head, d innermost.
 struct Rows { void* p; size_t token, head; };

@@ -43,13 +43,6 @@ __device__ inline void keys_of(const RaggedArgs& a, const Seq& s, int ta, int tb
     hi = max(lo, hi);
 }
 
-// A value that all lanes have, told to the compiler.
-__device__ inline int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
-__device__ inline long long uniform(long long v)
-{
-    return (long long)((unsigned long long)(uint32_t)__builtin_amdgcn_readfirstlane((int)(v >> 32)) << 32 | (uint32_t)__builtin_amdgcn_readfirstlane((int)v));
-}
-
 // The units of work of the kernel for few rows: the pages that the rows of a sequence see, once per kv head, sequence by sequence, head by head, page by
 // page.  Sequences with more rows than `most` have none here.
 struct Few { int rows, first_page, pages; };
@@ -63,37 +56,8 @@ __device__ inline Few few_of(const RaggedArgs& a, int b, int G, int most)
     return Few{rows, lo >> 7, on ? ((hi + 127) >> 7) - (lo >> 7) : 0};
 }
 
-__device__ inline Seq uniform(const Seq& s) { return Seq{uniform(s.first), uniform(s.n), uniform(s.len)}; }
-__device__ inline Few uniform(const Few& u) { return Few{uniform(u.rows), uniform(u.first_page), uniform(u.pages)}; }
-
-// Inclusive sums over the lanes of a wave, by DPP (a step through LDS is a hundred cycles, and the start of a step is all such sums), and over a
-// workgroup of W waves, with the sum of all.  64 bits: values below 2^40.
-__device__ inline int lane_scan(int v)
-{
-#define AQ_ADD(CTRL, ROWS) v += __builtin_amdgcn_update_dpp(0, v, CTRL, ROWS, 0xF, false)
-    AQ_ADD(0x111, 0xF); AQ_ADD(0x112, 0xF); AQ_ADD(0x114, 0xF); AQ_ADD(0x118, 0xF);      // within a row of 16 lanes
-    AQ_ADD(0x142, 0xA); AQ_ADD(0x143, 0xC);                                              // the last lane of a row into the next, of the lower half into the upper
-#undef AQ_ADD
-    return v;
-}
-__device__ inline long long lane_scan(long long v) { return (long long)lane_scan((int)(v & 0xFFFF)) + ((long long)lane_scan((int)(v >> 16)) << 16); }
-__device__ inline int lane_total(int v) { return __builtin_amdgcn_readlane(lane_scan(v), 63); }
-__device__ inline long long lane_total(long long v) { return (long long)lane_total((int)(v & 0xFFFF)) + ((long long)lane_total((int)(v >> 16)) << 16); }
-template <int W, class T>
-__device__ inline T wg_scan(T v, T* red /* [W], LDS */, T& total)
-{
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    v = lane_scan(v);
-    __syncthreads();                                             // (red of the call before has been read)
-    if (lane == 63) red[wave] = v;
-    __syncthreads();
-    total = 0;
-    T front = 0;
-#pragma unroll
-    for (int w = 0; w < W; ++w) { front += w < wave ? red[w] : T(0); total += red[w]; }
-    total = uniform(total);
-    return v + front;
-}
+__device__ inline Seq uniform_seq(const Seq& s) { return Seq{uniform(s.first), uniform(s.n), uniform(s.len)}; }
+__device__ inline Few uniform_few(const Few& u) { return Few{uniform(u.rows), uniform(u.first_page), uniform(u.pages)}; }
 
 // Codes and scale bytes of D / 4 values of one key: lane (key cc of 16, group g) holds d = (D/4) g .. + D/4 - 1.  (The scale bytes as the dword that they
 // lie in: of a narrower load the compiler makes the widening an instruction of its own, which waits for the load wherever it puts it.)
@@ -198,10 +162,10 @@ __global__ __launch_bounds__(256, RT == 1 ? 3 : 2) void ragged_few_kernel(const 
     int b = uniform(found[0]), front = uniform(found[1]);
 
     while (w < w_end) {
-        Few u = uniform(few_of(a, b, G, ROWS));
-        while (u.pages == 0 && b + 1 < a.B) u = uniform(few_of(a, ++b, G, ROWS));          // (there is one: w < work)
+        Few u = uniform_few(few_of(a, b, G, ROWS));
+        while (u.pages == 0 && b + 1 < a.B) u = uniform_few(few_of(a, ++b, G, ROWS));          // (there is one: w < work)
         if (u.pages == 0) return;
-        const Seq s = uniform(seq_of(a, b));
+        const Seq s = uniform_seq(seq_of(a, b));
         const int in_seq = (int)(w - (long long)front * a.Hkv), h = in_seq / u.pages, off = in_seq % u.pages;
         const int cnt = (int)min((long long)(u.pages - off), w_end - w), rows = u.rows;
         const int groups = RT == 1 ? 1 : (rows + 15) / 16;        // of 16 rows
@@ -548,7 +512,7 @@ __global__ __launch_bounds__(512, 2) void ragged_wide_kernel(const RaggedArgs a,
         if (tile < 0) {
             // the row tile of a sequence's work that w lies in
             if (b >= a.B) return;
-            s = uniform(seq_of(a, b));
+            s = uniform_seq(seq_of(a, b));
             const int tiles = (s.n * G + kWideRows - 1) / kWideRows;
             if (per == 0 && s.n * G > kFewRows) {
                 for (int r0 = 0; r0 < tiles; r0 += 64) {

@@ -17,77 +17,55 @@ struct PlanHead { int tail, unused[3]; };
 
 __device__ inline int pages_of(int positions) { return (positions + 127) >> 7; }
 
-// Inclusive sums over a workgroup of 1024 threads, and the sums over all of it.
-template <class T>
-__device__ inline T wg_scan(T v, T* red /* [16], LDS */, T& total)
+// Who gets what, by a workgroup of 1024: of request b (a thread each) what the rest of the plan needs; sums of the requests in front in `in`, which moves on.
+// A request is served if it fits its row of the page table, its new positions end within the step's capacity T, and the pages asked for up to and
+// including it are free; pages given back by this step are for the next one.  The sums run over refused requests too, so that nobody
+// waits for a decision: refused for want of pages are then all that ask for any from the first such on, and the pages that are taken are a prefix
+// of those asked for.  (64 bits for the positions: what is asked for is not limited by T.)
+struct PlanArgs {
+    const int *kv_lens, *new_lens; int B;
+    int* page_table; int max_pages;
+    int* ring; int ring_size /* 0: no ring, the table is complete */; const int* ring_state;
+    int T;
+    int *kv_out, *cu; long long* slots; int *positions, *state_out;
+};
+struct PlanSums { long long grown; int needed, given; };
+struct PlanRing { int head, count; };
+__device__ inline PlanRing plan_ring(const PlanArgs& a)
 {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
-        const T a = __shfl_up(v, d);
-        if (lane >= d) v += a;
-    }
-    __syncthreads();                                             // (red of the call before has been read)
-    if (lane == 63) red[wave] = v;
-    __syncthreads();
-    T front = 0;
-    total = 0;
-#pragma unroll
-    for (int w = 0; w < 16; ++w) {
-        front += w < wave ? red[w] : T(0);
-        total += red[w];
-    }
-    return v + front;
+    if (a.ring_size == 0) return PlanRing{0, 0};
+    return PlanRing{min(max(a.ring_state[0], 0), a.ring_size - 1), min(max(a.ring_state[1], 0), a.ring_size)};
 }
-
-// One workgroup: who gets what.  A request is served if it fits its row of the page table, its new positions end within the step's capacity
-// T, and the pages asked for up to and including it are free; pages given back by this step are for the next one.  The sums run over
-// refused requests too, so that nobody waits for a decision: refused for want of pages are then all that ask for any from the first such on,
-// and the pages that are taken are a prefix of those asked for.  (64 bits for the positions: what is asked for is not limited by T.)
-__global__ __launch_bounds__(1024) void plan_scan_kernel(const int* kv_lens, const int* new_lens, int B, int max_pages, const int* ring_state,
-                                                         int ring_size /* 0: no ring, the table is complete */, int T, int* kv_out,
-                                                         int* __restrict__ cu, int* state_out, PlanHead* __restrict__ hd, PlanItem* __restrict__ items)
+__device__ inline PlanItem plan_request(const PlanArgs& a, const PlanRing& r, int b, PlanSums& in, int& cu_end, int& kv_new, int& taken /* LDS */, int& refused /* LDS */,
+                                        long long* red_l /* [16], LDS */, int* red_i /* [16], LDS */)
 {
-    __shared__ long long red_l[16];
-    __shared__ int red_i[16], taken, refused;
-    const int tid = threadIdx.x;
-    const bool ring = ring_size > 0;
-    const int head = ring ? min(max(ring_state[0], 0), ring_size - 1) : 0, count = ring ? min(max(ring_state[1], 0), ring_size) : 0;
-    if (tid == 0) { taken = 0; refused = 0; cu[0] = 0; }
-    long long grown = 0, total_l;
-    int needed = 0, given = 0, total;
-    for (int b0 = 0; b0 < B; b0 += 1024) {
-        const int b = b0 + tid;
-        const bool on = b < B;
-        const int old = on ? min(max(kv_lens[b], 0), max_pages * 128) : 0, want = on ? max(new_lens[b], 0) : 0;
-        const bool bad = want > max_pages * 128;
-        const int grow = bad ? 0 : max(want - old, 0), give = ring && !bad ? max(pages_of(old) - pages_of(want), 0) : 0;
-        const long long end = grown + wg_scan<long long>(grow, red_l, total_l);
-        grown += total_l;
-        const bool late = grow > 0 && end > T;
-        const int need = !ring || bad || late ? 0 : max(pages_of(want) - pages_of(old), 0);
-        const int upto = needed + wg_scan(need, red_i, total);
-        needed += total;
-        const int give_end = given + wg_scan(give, red_i, total);
-        given += total;
-        const bool ok = !bad && !late && (need == 0 || upto <= count);
-        if (on) {
-            cu[b + 1] = (int)min(end, (long long)T);
-            kv_out[b] = ok ? want : old;
-            items[b] = PlanItem{old, ok ? (ring ? (int)(((long long)head + upto - need) % ring_size) : 0) : -1, give, give_end - give};
-            if (need > 0 && ok) atomicMax(&taken, upto);
-            if (!ok) atomicAdd(&refused, 1);
-        }
-    }
-    __syncthreads();
-    if (tid == 0) {
-        hd->tail = ring ? (int)(((long long)head + count) % ring_size) : 0;
-        if (state_out) {
-            state_out[0] = ring ? (int)(((long long)head + taken) % ring_size) : 0;
-            state_out[1] = (int)min((long long)count - taken + given, (long long)ring_size);
-            state_out[2] = refused;
-        }
-    }
+    const bool on = b < a.B, ring = a.ring_size > 0;
+    const int old = on ? min(max(a.kv_lens[b], 0), a.max_pages * 128) : 0, want = on ? max(a.new_lens[b], 0) : 0;
+    const bool bad = want > a.max_pages * 128;
+    const int grow = bad ? 0 : max(want - old, 0), give = ring && !bad ? max(pages_of(old) - pages_of(want), 0) : 0;
+    long long total_l;
+    const long long end = in.grown + wg_scan<16>((long long)grow, red_l, total_l);
+    in.grown += total_l;
+    const bool late = grow > 0 && end > a.T;
+    const int need = !ring || bad || late ? 0 : max(pages_of(want) - pages_of(old), 0);
+    int total;
+    const int upto = in.needed + wg_scan<16>(need, red_i, total);
+    in.needed += total;
+    const int give_end = in.given + wg_scan<16>(give, red_i, total);
+    in.given += total;
+    const bool ok = !bad && !late && (need == 0 || upto <= r.count);
+    cu_end = (int)min(end, (long long)a.T);
+    kv_new = ok ? want : old;
+    if (on && need > 0 && ok) atomicMax(&taken, upto);
+    if (on && !ok) atomicAdd(&refused, 1);
+    return PlanItem{old, ok ? (ring ? (int)(((long long)r.head + upto - need) % a.ring_size) : 0) : -1, give, give_end - give};
+}
+__device__ inline void plan_state(const PlanArgs& a, const PlanRing& r, const PlanSums& in, int taken, int refused)
+{
+    if (!a.state_out) return;
+    a.state_out[0] = a.ring_size > 0 ? (int)(((long long)r.head + taken) % a.ring_size) : 0;
+    a.state_out[1] = (int)min((long long)r.count - taken + in.given, (long long)a.ring_size);
+    a.state_out[2] = refused;
 }
 
 // The request of position t of the step: the last b with cu[b] <= t (t < cu[B]).
@@ -100,50 +78,100 @@ __device__ inline int request_of(const int* cu, int B, int t)
     }
     return lo;
 }
-
-// Slots and positions of the step's tokens, a thread each; the token that begins a new page writes it into the table (every new page begins with
-// one).  The last workgroups: pages that are given back, a wave for 64 requests, its lanes over the pages of one request after another.  What
-// is read of the ring and what is written to it do not meet: free pages and pages given back together are no more than the ring has places.
-__global__ __launch_bounds__(256) void plan_fill_kernel(const int* __restrict__ cu, int B, int* page_table, int max_pages, int* ring,
-                                                        int ring_size, int T, int token_wgs, const PlanHead* __restrict__ hd,
-                                                        const PlanItem* __restrict__ items, long long* __restrict__ slots, int* __restrict__ positions)
+// Slot and position of row t of the step, which is position pos of request b (b < 0: of none).  The row that begins a new page writes it into the
+// table (every new page begins with one).
+__device__ inline void plan_row(const PlanArgs& a, int t, int b, int pos, int old_len, int take)
 {
-    const int tid = threadIdx.x;
-    if ((int)blockIdx.x < token_wgs) {
-        const int t = (int)blockIdx.x * 256 + tid;
-        if (t >= T) return;
-        long long slot = -1;
-        int pos = 0;
-        if (t < cu[B]) {
-            const int b = request_of(cu, B, t);
-            const PlanItem it = items[b];
-            pos = it.old_len + (t - cu[b]);
-            if (it.take >= 0) {
-                const int j = pos >> 7, fresh = j - pages_of(it.old_len);          // < max_pages: the request fits its row
-                int* entry = page_table + (size_t)b * max_pages + j;
-                int page;
-                if (ring_size > 0 && fresh >= 0) {
-                    page = ring[((long long)it.take + fresh) % ring_size];
-                    if ((pos & 127) == 0) *entry = page;
-                } else page = *entry;
-                if (page >= 0) slot = (long long)page * 128 + (pos & 127);
-            }
-        }
-        slots[t] = slot;
-        positions[t] = pos;
-        return;
+    long long slot = -1;
+    if (b >= 0 && take >= 0) {
+        const int j = pos >> 7, fresh = j - pages_of(old_len);    // j < max_pages: the request fits its row
+        int* entry = a.page_table + (size_t)b * a.max_pages + j;
+        int page;
+        if (a.ring_size > 0 && fresh >= 0) {
+            page = a.ring[((long long)take + fresh) % a.ring_size];
+            if ((pos & 127) == 0) *entry = page;
+        } else page = *entry;
+        if (page >= 0) slot = (long long)page * 128 + (pos & 127);
     }
-    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
-    const int b0 = (((int)blockIdx.x - token_wgs) * 4 + wave) * 64, b = b0 + lane;
-    const PlanItem it = b < B ? items[b] : PlanItem{0, 0, 0, 0};
-    const int tail = hd->tail;
+    a.slots[t] = slot;
+    a.positions[t] = b >= 0 ? pos : 0;
+}
+// Pages that 64 requests from b0 on give back, by a wave: its lanes over the pages of one request after another.  What is read of the ring and what is
+// written to it do not meet: free pages and pages given back together are no more than the ring has places.
+__device__ inline void plan_give(const PlanArgs& a, const PlanItem& it /* of request b0 + lane */, int b0, int tail)
+{
+    const int lane = threadIdx.x & 63;
     for (unsigned long long m = __builtin_amdgcn_ballot_w64(it.give > 0); m != 0; m &= m - 1) {
         const int src = (int)__builtin_ctzll(m);
         const int give = __builtin_amdgcn_readlane(it.give, src), first = __builtin_amdgcn_readlane(it.first_give, src);
         const int kept = pages_of(__builtin_amdgcn_readlane(it.old_len, src)) - give;
         for (int j = lane; j < give; j += 64)
-            ring[((long long)tail + first + j) % ring_size] = page_table[(size_t)(b0 + src) * max_pages + kept + j];
+            a.ring[((long long)tail + first + j) % a.ring_size] = a.page_table[(size_t)(b0 + src) * a.max_pages + kept + j];
     }
+}
+
+// Up to 1024 requests: one launch, in which every workgroup makes out for itself who gets what and then does its share of the rows.  (Two launches, as
+// below, take as long on the GPU, but the second one costs the host its 3 us, which is what a step waits for.)
+constexpr int kPlanOne = 1024;
+constexpr int kPlanOneWg = 4096;      // rows that one workgroup does alone: then nobody else reads what it writes
+__global__ __launch_bounds__(1024) void plan_one_kernel(const PlanArgs a)
+{
+    __shared__ long long red_l[16];
+    __shared__ int red_i[16], taken, refused, cu_s[kPlanOne + 1], old_s[kPlanOne], take_s[kPlanOne];
+    const int tid = threadIdx.x;
+    const PlanRing r = plan_ring(a);
+    if (tid == 0) { taken = 0; refused = 0; cu_s[0] = 0; }
+    PlanSums in{0, 0, 0};
+    int cu_end, kv_new;
+    const PlanItem it = plan_request(a, r, tid, in, cu_end, kv_new, taken, refused, red_l, red_i);
+    cu_s[tid + 1] = cu_end; old_s[tid] = it.old_len; take_s[tid] = it.take;
+    __syncthreads();                                              // (every input but the ring and the table has been read: outputs may lie over them)
+    if (blockIdx.x == 0) {
+        if (tid < a.B) { a.kv_out[tid] = kv_new; a.cu[tid + 1] = cu_end; }
+        if (tid == 0) { a.cu[0] = 0; plan_state(a, r, in, taken, refused); }
+        if (a.ring_size > 0) plan_give(a, it, tid & ~63, (int)(((long long)r.head + r.count) % a.ring_size));
+    }
+    for (int t = (int)blockIdx.x * 1024 + tid; t < a.T; t += (int)gridDim.x * 1024) {
+        int b = -1, pos = 0;
+        if (t < cu_s[a.B]) { b = request_of(cu_s, a.B, t); pos = old_s[b] + (t - cu_s[b]); }
+        plan_row(a, t, b, pos, b >= 0 ? old_s[b] : 0, b >= 0 ? take_s[b] : -1);
+    }
+}
+
+// More requests, or outputs that lie over inputs that other workgroups would still read: one workgroup makes out who gets what, a second launch does the rows.
+__global__ __launch_bounds__(1024) void plan_scan_kernel(const PlanArgs a, PlanHead* __restrict__ hd, PlanItem* __restrict__ items)
+{
+    __shared__ long long red_l[16];
+    __shared__ int red_i[16], taken, refused;
+    const int tid = threadIdx.x;
+    const PlanRing r = plan_ring(a);
+    if (tid == 0) { taken = 0; refused = 0; a.cu[0] = 0; }
+    PlanSums in{0, 0, 0};
+    for (int b0 = 0; b0 < a.B; b0 += 1024) {
+        int cu_end, kv_new;
+        const PlanItem it = plan_request(a, r, b0 + tid, in, cu_end, kv_new, taken, refused, red_l, red_i);
+        if (b0 + tid < a.B) { a.cu[b0 + tid + 1] = cu_end; a.kv_out[b0 + tid] = kv_new; items[b0 + tid] = it; }
+    }
+    __syncthreads();
+    if (tid == 0) {
+        hd->tail = a.ring_size > 0 ? (int)(((long long)r.head + r.count) % a.ring_size) : 0;
+        plan_state(a, r, in, taken, refused);
+    }
+}
+__global__ __launch_bounds__(256) void plan_fill_kernel(const PlanArgs a, int row_wgs, const PlanHead* __restrict__ hd, const PlanItem* __restrict__ items)
+{
+    const int tid = threadIdx.x;
+    if ((int)blockIdx.x < row_wgs) {
+        const int t = (int)blockIdx.x * 256 + tid;
+        if (t >= a.T) return;
+        if (t >= a.cu[a.B]) { plan_row(a, t, -1, 0, 0, -1); return; }
+        const int b = request_of(a.cu, a.B, t);
+        const PlanItem it = items[b];
+        plan_row(a, t, b, it.old_len + (t - a.cu[b]), it.old_len, it.take);
+        return;
+    }
+    const int b0 = (((int)blockIdx.x - row_wgs) * 4 + (tid >> 6)) * 64, b = b0 + (tid & 63);
+    plan_give(a, b < a.B ? items[b] : PlanItem{0, 0, 0, 0}, b0, hd->tail);
 }
 
 // A row (token, kv head) of K or V has D / 16 blocks; a thread takes one block of one row, neighbouring threads the blocks of a row and
@@ -213,15 +241,21 @@ __global__ __launch_bounds__(256) void read_kernel(uint16_t* __restrict__ k, uin
 size_t page_plan_ws_bytes(int B) { return sizeof(PlanHead) + (size_t)B * sizeof(PlanItem); }
 
 int launch_page_plan(const int* kv_lens, const int* new_lens, int B, int* page_table, int max_pages, int* ring, int ring_size, const int* ring_state,
-                     int T, int* kv_out, int* cu, long long* slots, int* positions, int* state_out, void* ws, hipStream_t st)
+                     int T, int* kv_out, int* cu, long long* slots, int* positions, int* state_out, bool in_place, void* ws, hipStream_t st)
 {
+    const PlanArgs a{kv_lens, new_lens, B, page_table, max_pages, ring, ring_size, ring_state, T, kv_out, cu, slots, positions, state_out};
+    const int wgs = T <= kPlanOneWg ? 1 : (T + 1023) / 1024;
+    if (B <= kPlanOne && (wgs == 1 || !in_place)) {
+        hipLaunchKernelGGL(plan_one_kernel, dim3(wgs < 256 ? wgs : 256), dim3(1024), 0, st, a);
+        return hipGetLastError() == hipSuccess ? 0 : -1;
+    }
     PlanHead* hd = (PlanHead*)ws;
     PlanItem* items = (PlanItem*)(hd + 1);
-    hipLaunchKernelGGL(plan_scan_kernel, dim3(1), dim3(1024), 0, st, kv_lens, new_lens, B, max_pages, ring_state, ring_size, T, kv_out, cu, state_out, hd, items);
+    hipLaunchKernelGGL(plan_scan_kernel, dim3(1), dim3(1024), 0, st, a, hd, items);
     if (hipGetLastError() != hipSuccess) return -1;
-    const int token_wgs = (T + 255) / 256, give_wgs = ring_size > 0 ? (B + 255) / 256 : 0;
-    if (token_wgs + give_wgs > 0)
-        hipLaunchKernelGGL(plan_fill_kernel, dim3(token_wgs + give_wgs), dim3(256), 0, st, cu, B, page_table, max_pages, ring, ring_size, T, token_wgs, hd, items, slots, positions);
+    const int row_wgs = (T + 255) / 256, give_wgs = ring_size > 0 ? (B + 255) / 256 : 0;
+    if (row_wgs + give_wgs > 0)
+        hipLaunchKernelGGL(plan_fill_kernel, dim3(row_wgs + give_wgs), dim3(256), 0, st, a, row_wgs, hd, items);
     return hipGetLastError() == hipSuccess ? 0 : -1;
 }
 

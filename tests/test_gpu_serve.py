@@ -412,3 +412,23 @@ def test_binding_refuses(aq):
                  (lens, lens, i32([[0], [1]]), 4, (i32([0]), i32([0])))):
         with pytest.raises(aq.AttnQatError):
             aq.attnqat_page_plan(*args)
+
+
+@pytest.mark.parametrize("B,T", [(30, 4096), (30, 4097), (1024, 6000), (1025, 6000), (200, 9000)])
+@pytest.mark.parametrize("in_place", [False, True])
+def test_plan_in_place_and_beside(aq, B, T, in_place):
+    """The results do not depend on where they go, whichever launches the sizes take."""
+    rng = np.random.default_rng(B + T)
+    old, want, table, ring, state, _ = _plan_case(B, rng, 40, 2 * T // B, 0.9)
+    t_ref, r_ref = table.copy(), ring.copy()
+    ref = S.plan(old, want, t_ref, r_ref, state, T)
+    lens, st, t_dev, r_dev = i32(old), i32(list(state) + [7]), dev(table), dev(ring)
+    out = None
+    if in_place:
+        out = (lens, torch.empty(B + 1, dtype=torch.int32, device="cuda"), torch.empty(T, dtype=torch.int64, device="cuda"), torch.empty(T, dtype=torch.int32, device="cuda"), st)
+    got = aq.attnqat_page_plan(lens, i32(want), t_dev, T, free=(r_dev, st), out=out)
+    for g, r in zip(got, ref):
+        assert np.array_equal(g.cpu().numpy(), r)
+    assert np.array_equal(t_dev.cpu().numpy(), t_ref) and np.array_equal(r_dev.cpu().numpy(), r_ref)
+    if not in_place:
+        assert np.array_equal(lens.cpu().numpy(), old) and np.array_equal(st.cpu().numpy()[:2], state)
