@@ -444,7 +444,7 @@ int attnqat_debug_fwd_infer_paged(const void* q, int B, int Hq, int Hkv, int Lq,
  * causal = 0.  max_q: no sequence has more rows (rows beyond are left out).  A row without a key gets o = 0, lse = -inf.  o [T,Hq,d] bf16; lse
  * [T,Hq] fp32 (natural log), may be NULL; rows behind cu_q[B] are left as they are.  o and lse must not lie over q.  scale > 0.
  * Positions of a page table entry outside [0, num_pages) read as zeros; positions from kv_lens[b] on are never used, whatever their slots
- * hold.  Workspace: attnqat_kv4_ragged_workspace_bytes(), 16-byte aligned.
+ * hold.  At most 2^28 rows of heads (T Hq) and 2^24 (sequence, kv head)s.  Workspace: attnqat_kv4_ragged_workspace_bytes(), 16-byte aligned.
  */
 size_t attnqat_page_plan_workspace_bytes(int B);
 int attnqat_page_plan(const int* kv_lens, const int* new_lens, int B, int* page_table, int max_pages,

@@ -666,7 +666,7 @@ int ragged_dims(int T, int B, int Hq, int Hkv, int max_q, int max_pages, int d)
 {
     if (T < 0 || B < 1 || Hq < 1 || Hkv < 1 || max_q < 1 || max_pages < 1) return ATTNQAT_EINVAL;
     if ((d != 64 && d != 128) || Hq % Hkv != 0 || Hkv > 65535 || B > kMaxServeBatch || max_pages > kMaxServePages) return ATTNQAT_ESHAPE;
-    if ((long long)T * Hq > (1 << 28)) return ATTNQAT_ESHAPE;
+    if ((long long)T * Hq > (1 << 28) || (long long)B * Hkv > (1 << 24)) return ATTNQAT_ESHAPE;
     return ATTNQAT_OK;
 }
 }  // namespace

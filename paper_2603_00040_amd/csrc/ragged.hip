@@ -44,20 +44,20 @@ __device__ inline void keys_of(const RaggedArgs& a, const Seq& s, int ta, int tb
 }
 
 // The units of work of the kernel for few rows: the pages that the rows of a sequence see, once per kv head, sequence by sequence, head by head, page by
-// page.  Sequences with more rows than `most` have none here.
-struct Few { int rows, first_page, pages; };
-__device__ inline Few few_of(const RaggedArgs& a, int b, int G, int most)
+// page.  What a (sequence, kv head) costs besides (its rows of Q, the first trip to its pages, the result) counts as kFewStart pages in
+// front of its own.  Sequences with more rows than `most` have no units here.
+template <int D> constexpr int kFewStart = D == 64 ? 3 : 2;      // (6 000 cycles, against 2 000 and 3 200 for a page)
+struct Few { int rows, first_page, pages, units; };
+template <int D>
+__device__ inline Few few_of(const RaggedArgs& a, const Seq& s, int G, int most)
 {
-    const Seq s = seq_of(a, b);
     const int rows = s.n <= most ? s.n * G : most + 1;
     int lo, hi;
     keys_of(a, s, 0, s.n - 1, lo, hi);
-    const bool on = rows > 0 && rows <= most && hi > lo;
-    return Few{rows, lo >> 7, on ? ((hi + 127) >> 7) - (lo >> 7) : 0};
+    const int pages = rows > 0 && rows <= most && hi > lo ? ((hi + 127) >> 7) - (lo >> 7) : 0;
+    return Few{rows, lo >> 7, pages, pages > 0 ? pages + kFewStart<D> : 0};
 }
-
 __device__ inline Seq uniform_seq(const Seq& s) { return Seq{uniform(s.first), uniform(s.n), uniform(s.len)}; }
-__device__ inline Few uniform_few(const Few& u) { return Few{uniform(u.rows), uniform(u.first_page), uniform(u.pages)}; }
 
 // Codes and scale bytes of D / 4 values of one key: lane (key cc of 16, group g) holds d = (D/4) g .. + D/4 - 1.  (The scale bytes as the dword that they
 // lie in: of a narrower load the compiler makes the widening an instruction of its own, which waits for the load wherever it puts it.)
@@ -119,11 +119,12 @@ template <int D, int RT /* 16-row groups of a unit */>
 __global__ __launch_bounds__(256, RT == 1 ? 3 : 2) void ragged_few_kernel(const RaggedArgs a, const FewWs ws)
 {
     constexpr int NS = D / 32, NDT = D / 16, ROWS = 16 * RT;
+    constexpr int SETS = D == 64 ? 4 : RT == 1 ? 2 : 3;           // pages in registers, the present one included (heads of 64: half the bytes each)
     constexpr int RS = 2 * D + 32;                                // bytes per key of the V tile (eight keys side by side in other banks)
     constexpr size_t VOFF = (size_t)128 * (D / 2 + D / 16);
     __shared__ __align__(16) unsigned char stage[4 * 32 * RS];     // per wave: V of 32 keys [key][d]; at the end the waves' sums [4][16][D]
     __shared__ float ml[2][4][ROWS];
-    __shared__ int red[4], found[2];
+    __shared__ int red[4], found[5];
 
     const int tid = threadIdx.x, lane = tid & 63, cc = lane & 15, g = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -132,10 +133,12 @@ __global__ __launch_bounds__(256, RT == 1 ? 3 : 2) void ragged_few_kernel(const 
     // (the two 16-byte pieces of every 32 change places in keys 4 - 7 of 8: a store serves eight lanes, eight keys, at a time on 32 banks)
     const uint32_t tr_base = lds_addr_of(stg) + (uint32_t)((4 * g + (cc >> 2)) * RS + 8 * ((cc & 3) ^ (2 * (g & 1))));
 
-    // this workgroup's pages [w, w_end) of all units', and the sequence that the first of them belongs to
+    // this workgroup's units [w, w_end) of all, and the sequence that the first of them belongs to
     int all = 0, total, n_b = 0, upto_b = 0;
+    Seq s_b{0, 0, 0};
     for (int b0 = 0; b0 < a.B; b0 += 256) {
-        n_b = b0 + tid < a.B ? few_of(a, b0 + tid, G, ROWS).pages : 0;
+        s_b = b0 + tid < a.B ? seq_of(a, b0 + tid) : Seq{0, 0, 0};
+        n_b = few_of<D>(a, s_b, G, ROWS).units;
         upto_b = all + wg_scan<4>(n_b, red, total);
         if (blockIdx.x == 0) {
             if (b0 + tid < a.B) ws.front[b0 + tid + 1] = upto_b;
@@ -151,42 +154,80 @@ __global__ __launch_bounds__(256, RT == 1 ? 3 : 2) void ragged_few_kernel(const 
     if (w >= w_end) return;
     for (int b0 = 0, at = 0; ; b0 += 256) {
         if (a.B > 256) {                                          // (up to 256 sequences: as found above)
-            n_b = b0 + tid < a.B ? few_of(a, b0 + tid, G, ROWS).pages : 0;
+            s_b = b0 + tid < a.B ? seq_of(a, b0 + tid) : Seq{0, 0, 0};
+            n_b = few_of<D>(a, s_b, G, ROWS).units;
             upto_b = at + wg_scan<4>(n_b, red, total);
             at += total;
         }
-        if (n_b > 0 && w < (long long)upto_b * a.Hkv && w >= (long long)(upto_b - n_b) * a.Hkv) { found[0] = b0 + tid; found[1] = upto_b - n_b; }
+        if (n_b > 0 && w < (long long)upto_b * a.Hkv && w >= (long long)(upto_b - n_b) * a.Hkv) {
+            found[0] = b0 + tid; found[1] = upto_b - n_b; found[2] = s_b.first; found[3] = s_b.n; found[4] = s_b.len;
+        }
         if (a.B <= 256 || w < (long long)at * a.Hkv || b0 + 256 >= a.B) break;
     }
     __syncthreads();
     int b = uniform(found[0]), front = uniform(found[1]);
+    Seq s{uniform(found[2]), uniform(found[3]), uniform(found[4])};
+    Few u = few_of<D>(a, s, G, ROWS);
+    int h, off;                                                   // the head, and the units of it in front of w
+    {
+        const int in_seq = (int)(w - (long long)front * a.Hkv);
+        h = in_seq / u.units; off = in_seq % u.units;
+    }
 
     while (w < w_end) {
-        Few u = uniform_few(few_of(a, b, G, ROWS));
-        while (u.pages == 0 && b + 1 < a.B) u = uniform_few(few_of(a, ++b, G, ROWS));          // (there is one: w < work)
-        if (u.pages == 0) return;
-        const Seq s = uniform_seq(seq_of(a, b));
-        const int in_seq = (int)(w - (long long)front * a.Hkv), h = in_seq / u.pages, off = in_seq % u.pages;
-        const int cnt = (int)min((long long)(u.pages - off), w_end - w), rows = u.rows;
+        const int units = (int)min((long long)(u.units - off), w_end - w);
+        const int at = max(off - kFewStart<D>, 0), cnt = min(off + units - kFewStart<D>, u.pages) - at, rows = u.rows;      // pages: where this workgroup begins, how many
+        w += units;
+        if (cnt <= 0) break;                                      // (the start alone: w is at this workgroup's end)
         const int groups = RT == 1 ? 1 : (rows + 15) / 16;        // of 16 rows
+        const int first = u.first_page + at;
+        const int* ids = a.table + (size_t)b * a.max_pages + first;
 
-        // Q: row cc of a group of 16, d = (D/4) g + 8 s .. + 7
-        half8 qreg[RT][NS];
-        float c_row[RT];
+        // what a segment needs from memory first, asked for at once: page ids (64 at a time: lane x has that of page id_end - 64 + x) and Q
+        int id_lane = ids[min(lane, cnt - 1)], id_end = 64;
+        uint4v x[RT][NS];
         int k_first[RT], k_last[RT];                              // keys that this lane's rows see
 #pragma unroll
         for (int rt = 0; rt < RT; ++rt) {
             const int row = min(16 * rt + cc, rows - 1), tok = row / G, head = h * G + row % G, pos = s.len - s.n + tok;
             k_first[rt] = a.window > 0 ? pos - a.window + 1 : 0;
             k_last[rt] = a.causal ? min(pos, s.len - 1) : s.len - 1;
-            uint4v x[NS];
+#pragma unroll
+            for (int i = 0; i < NS; ++i)
+                x[rt][i] = *reinterpret_cast<const uint4v*>(a.q + (size_t)(s.first + tok) * a.q_token + (size_t)head * a.q_head + (D / 4) * g + 8 * i);
+        }
+        asm volatile("" : "+v"(id_lane));                         // (waited for here and not at every use)
+
+        struct Tile { Raw<D> k[2], v[2]; bool live; };
+        auto load = [&](Tile& t, int i) __attribute__((always_inline)) {
+            if (i >= id_end) {
+                id_lane = ids[min(id_end + lane, cnt - 1)];
+                asm volatile("" : "+v"(id_lane));
+                id_end += 64;
+            }
+            const int page = __builtin_amdgcn_readlane(id_lane, i - (id_end - 64));
+            t.live = page >= 0 && page < a.num_pages;
+            const unsigned char* part = a.cache + ((size_t)(t.live ? page : 0) * a.Hkv + h) * (2 * VOFF);
+#pragma unroll
+            for (int blk = 0; blk < 2; ++blk) t.k[blk] = load_raw<D>(part, 32 * wave + 16 * blk + cc, g);
+#pragma unroll
+            for (int blk = 0; blk < 2; ++blk) t.v[blk] = load_raw<D>(part + VOFF, 32 * wave + 16 * blk + cc, g);
+        };
+        // (sets of registers by name, and requests that depend on nothing: rotated by copies the compiler waits for everything in flight)
+        Tile t[SETS];
+#pragma unroll
+        for (int i = 0; i + 1 < SETS; ++i) load(t[i], min(i, cnt - 1));
+
+        // Q: row cc of a group of 16, d = (D/4) g + 8 s .. + 7
+        half8 qreg[RT][NS];
+        float c_row[RT];
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt) {
             float amax = 0.0f;
 #pragma unroll
-            for (int i = 0; i < NS; ++i) {
-                x[i] = *reinterpret_cast<const uint4v*>(a.q + (size_t)(s.first + tok) * a.q_token + (size_t)head * a.q_head + (D / 4) * g + 8 * i);
+            for (int i = 0; i < NS; ++i)
 #pragma unroll
-                for (int j = 0; j < 4; ++j) amax = fmaxf(amax, fmaxf(fabsf(__uint_as_float(x[i][j] << 16)), fabsf(__uint_as_float(x[i][j] & 0xFFFF0000u))));
-            }
+                for (int j = 0; j < 4; ++j) amax = fmaxf(amax, fmaxf(fabsf(__uint_as_float(x[rt][i][j] << 16)), fabsf(__uint_as_float(x[rt][i][j] & 0xFFFF0000u))));
             amax = lanes_max<16, 32>(amax);
             float f, inv;
             row_factor(amax, f, inv);
@@ -194,8 +235,8 @@ __global__ __launch_bounds__(256, RT == 1 ? 3 : 2) void ragged_few_kernel(const 
             for (int i = 0; i < NS; ++i)
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
-                    qreg[rt][i][2 * j]     = (half_t)(__uint_as_float(x[i][j] << 16) * f);
-                    qreg[rt][i][2 * j + 1] = (half_t)(__uint_as_float(x[i][j] & 0xFFFF0000u) * f);
+                    qreg[rt][i][2 * j]     = (half_t)(__uint_as_float(x[rt][i][j] << 16) * f);
+                    qreg[rt][i][2 * j + 1] = (half_t)(__uint_as_float(x[rt][i][j] & 0xFFFF0000u) * f);
                 }
             c_row[rt] = a.c * inv;
         }
@@ -210,24 +251,6 @@ __global__ __launch_bounds__(256, RT == 1 ? 3 : 2) void ragged_few_kernel(const 
 #pragma unroll
             for (int dt = 0; dt < NDT; ++dt) o[rt][dt] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
         }
-        const int first = u.first_page + off;
-        const int* ids = a.table + (size_t)b * a.max_pages + first;
-        int id_lane = 0;
-
-        struct Tile { Raw<D> k[2], v[2]; bool live; };
-        auto load = [&](Tile& t, int i) __attribute__((always_inline)) {
-            if ((i & 63) == 0) {                                  // 64 page ids at a time, waited for here and not at every use
-                id_lane = ids[min(i + lane, cnt - 1)];
-                asm volatile("" : "+v"(id_lane));
-            }
-            const int page = __builtin_amdgcn_readlane(id_lane, i & 63);
-            t.live = page >= 0 && page < a.num_pages;
-            const unsigned char* part = a.cache + ((size_t)(t.live ? page : 0) * a.Hkv + h) * (2 * VOFF);
-#pragma unroll
-            for (int blk = 0; blk < 2; ++blk) t.k[blk] = load_raw<D>(part, 32 * wave + 16 * blk + cc, g);
-#pragma unroll
-            for (int blk = 0; blk < 2; ++blk) t.v[blk] = load_raw<D>(part + VOFF, 32 * wave + 16 * blk + cc, g);
-        };
         auto step = [&](const Tile& t, int i) __attribute__((always_inline)) {
             const int kt = (first + i) * 128 + 32 * wave;
             const bool masked = kt < see_first || kt + 31 > see_last;
@@ -292,20 +315,18 @@ __global__ __launch_bounds__(256, RT == 1 ? 3 : 2) void ragged_few_kernel(const 
                 for (int rt = 0; rt < RT; ++rt) if (rt < groups) o[rt][dt] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(half8, av), pt[rt], o[rt][dt], 0, 0, 0);
             }
         };
-        // (two sets of registers by name, and requests that depend on nothing: rotated by copies the compiler waits for everything in flight)
-        Tile ta, tb;
-        load(ta, 0);
-        for (int i = 0; i < cnt; i += 2) {
-            load(tb, min(i + 1, cnt - 1));
-            step(ta, i);
-            if (i + 1 >= cnt) break;
-            load(ta, min(i + 2, cnt - 1));
-            step(tb, i + 1);
+        for (int i = 0; i < cnt; i += SETS) {
+#pragma unroll
+            for (int x = 0; x < SETS; ++x) {
+                if (x > 0 && i + x >= cnt) break;
+                load(t[(x + SETS - 1) % SETS], min(i + x + SETS - 1, cnt - 1));
+                step(t[x], i + x);
+            }
         }
 
         // the four waves' sums, in units of their common maximum
         const bool whole = cnt == u.pages;
-        const size_t slot = (size_t)blockIdx.x * 2 + (off == 0 ? 1 : 0);
+        const size_t slot = (size_t)blockIdx.x * 2 + (at == 0 ? 1 : 0);
         float* sums = reinterpret_cast<float*>(stage);
 #pragma unroll
         for (int rt = 0; rt < RT; ++rt) {
@@ -344,24 +365,32 @@ __global__ __launch_bounds__(256, RT == 1 ? 3 : 2) void ragged_few_kernel(const 
             }
             __syncthreads();
         }
-        w += cnt;
-        if (off + cnt == u.pages && h == a.Hkv - 1) { front += u.pages; ++b; }
+        // on to the next head, sequence (there is one while w < w_end; a sequence of the other kernel, or without a key, has no units)
+        off = 0;
+        if (++h == a.Hkv) {
+            h = 0;
+            do {
+                if (++b >= a.B) return;
+                s = uniform_seq(seq_of(a, b));
+                u = few_of<D>(a, s, G, ROWS);
+            } while (w < w_end && u.units == 0);
+        }
     }
 }
 
 // O and lse of the units whose pages were shared, and of rows that see no key: a workgroup per unit and row, whose groups of D / 4 threads take the
 // partial sums in turn.
 template <int D, int ROWS>
-__global__ __launch_bounds__(256) void ragged_few_merge_kernel(const RaggedArgs a, const FewWs ws)
+__device__ void few_merge(const RaggedArgs& a, const FewWs& ws, int unit, int r)
 {
     constexpr int NG = 256 / (D / 4);
     __shared__ __align__(16) float acc[NG][D];
     __shared__ float ml[NG][2];
-    const int G = a.Hq / a.Hkv, b = blockIdx.x / a.Hkv, h = blockIdx.x % a.Hkv, r = blockIdx.y;
+    const int G = a.Hq / a.Hkv, b = unit / a.Hkv, h = unit % a.Hkv;
     const int tid = threadIdx.x, grp = tid / (D / 4), d = tid % (D / 4) * 4;
-    const Few u = few_of(a, b, G, ROWS);
-    if (r >= u.rows || u.rows > ROWS) return;
     const Seq s = seq_of(a, b);
+    const Few u = few_of<D>(a, s, G, ROWS);
+    if (r >= u.rows || u.rows > ROWS) return;
     const int tk = r / G, hd = h * G + r % G;
     uint16_t* dst = a.o + (size_t)(s.first + tk) * a.o_token + (size_t)hd * a.o_head;
     if (u.pages == 0) {
@@ -370,7 +399,7 @@ __global__ __launch_bounds__(256) void ragged_few_merge_kernel(const RaggedArgs 
         return;
     }
     const int quota = *ws.quota;
-    const long long w0 = (long long)ws.front[b] * a.Hkv + (long long)h * u.pages, w1 = w0 + u.pages - 1;
+    const long long w0 = (long long)ws.front[b] * a.Hkv + (long long)h * u.units + kFewStart<D>, w1 = w0 + u.pages - 1;
     const int f = (int)(w0 / quota), n = (int)(w1 / quota) - f + 1;
     if (n < 2) return;
     float M = -INFINITY, l = 0.0f;
@@ -800,6 +829,7 @@ __global__ __launch_bounds__(512, 2) void ragged_wide_kernel(const RaggedArgs a,
 template <int D>
 __device__ void wide_merge(const RaggedArgs& a, const WideWs& ws, int place, int part)
 {
+    if (place == 0) return;                                       // (nothing in front of the first)
     const long long quota = *ws.quota;
     if (quota == 0) return;
     const WideRec r = ws.rec[place];
@@ -835,13 +865,12 @@ __device__ void wide_merge(const RaggedArgs& a, const WideWs& ws, int place, int
         uint2v{pack_bf16x2_cvt(v[0], v[1]), pack_bf16x2_cvt(v[2], v[3])};
     if (i == 0 && j == 0 && half == 0 && a.lse) a.lse[(size_t)(s.first + tok) * a.Hq + head] = l != 0.0f ? M * 0.6931471805599453f + logf(l) : -INFINITY;
 }
-// (and O = 0, lse = -inf for row tiles, of sequences with many rows, that see no key: they are nobody's work)
+// O = 0, lse = -inf for row tiles, of sequences with many rows, that see no key: they are nobody's work.  One of n workgroups.
 template <int D>
-__global__ __launch_bounds__(256) void ragged_wide_merge_kernel(const RaggedArgs a, const WideWs ws, int places)
+__device__ void wide_empty(const RaggedArgs& a, int which, int n)
 {
-    if ((int)blockIdx.x < places) { if (blockIdx.x > 0) wide_merge<D>(a, ws, blockIdx.x, blockIdx.y); return; }
     const int G = a.Hq / a.Hkv;
-    for (int b = (int)(blockIdx.x - places) * gridDim.y + blockIdx.y; b < a.B; b += (int)(gridDim.x - places) * gridDim.y) {
+    for (int b = which; b < a.B; b += n) {
         const Seq s = seq_of(a, b);
         const int rows = s.n * G;
         if (rows <= kFewRows) continue;
@@ -859,21 +888,33 @@ __global__ __launch_bounds__(256) void ragged_wide_merge_kernel(const RaggedArgs
         }
     }
 }
+// The last launch of a step: what the others left to be joined.
+constexpr int kEmptyWgs = 64;
+template <int D, int ROWS>
+__global__ __launch_bounds__(256) void ragged_merge_kernel(const RaggedArgs a, const FewWs few, int few_rows, const WideWs wide, int places)
+{
+    int x = (int)blockIdx.x;
+    const int few_wgs = a.B * a.Hkv * few_rows;
+    if (x < few_wgs) { few_merge<D, ROWS>(a, few, x / few_rows, x % few_rows); return; }
+    x -= few_wgs;
+    if (x < places * (D / 4)) { wide_merge<D>(a, wide, x / (D / 4), x % (D / 4)); return; }
+    wide_empty<D>(a, x - places * (D / 4), kEmptyWgs);
+}
 
 inline size_t up256(size_t x) { return (x + 255) / 256 * 256; }
 
 // Which kernels a step may need: the host knows only how many rows a sequence has at most.
 struct RaggedPlan { int few_groups, few_wgs, wide_wgs /* 0: no sequence has that many rows */; };
-inline RaggedPlan plan_of(int T, int B, int Hq, int Hkv, int max_q, int max_pages, int cus)
+inline RaggedPlan plan_of(int T, int B, int Hq, int Hkv, int max_q, int max_pages, int D, int cus)
 {
     const long long most = (long long)(max_q < T ? max_q : T) * (Hq / Hkv), rows = (long long)T * (Hq / Hkv);
     RaggedPlan p;
     p.few_groups = most <= 16 ? 1 : 2;
-    const long long units = (long long)B * Hkv * max_pages, wgs = (long long)cus * (p.few_groups == 1 ? 3 : 2);
+    const long long units = (long long)B * Hkv * (max_pages + (D == 64 ? kFewStart<64> : kFewStart<128>)), wgs = (long long)cus * (p.few_groups == 1 ? 3 : 2);
     p.few_wgs = (int)(units < wgs ? units : wgs);
     p.wide_wgs = 0;
     if (most > kFewRows) {
-        const long long tiles = ((long long)B + rows / kWideRows) * Hkv * max_pages * 2, wide = cus;
+        const long long tiles = ((long long)B + rows / kWideRows) * Hkv * (max_pages * 2 + kWideStart), wide = cus;
         p.wide_wgs = (int)(tiles < wide ? tiles : wide);
     }
     return p;
@@ -900,24 +941,20 @@ inline RaggedWs carve_ragged(void* ws, const RaggedPlan& p, int B, int D)
 }
 
 template <int D, int RT>
-int launch_few(const RaggedArgs& a, const RaggedPlan& p, const FewWs& w, hipStream_t st)
+int launch_ragged_of(const RaggedArgs& a, const RaggedPlan& p, const RaggedWs& w, hipStream_t st)
 {
-    hipLaunchKernelGGL((ragged_few_kernel<D, RT>), dim3(p.few_wgs), dim3(256), 0, st, a, w);
+    hipLaunchKernelGGL((ragged_few_kernel<D, RT>), dim3(p.few_wgs), dim3(256), 0, st, a, w.few);
     if (hipGetLastError() != hipSuccess) return -1;
-    const int rows = (a.max_q < a.T ? a.max_q : a.T) * (a.Hq / a.Hkv);                        // (the host has checked that T Hq fits)
-    hipLaunchKernelGGL((ragged_few_merge_kernel<D, 16 * RT>), dim3(a.B * a.Hkv, rows < 16 * RT ? rows : 16 * RT), dim3(256), 0, st, a, w);
-    return hipGetLastError() == hipSuccess ? 0 : -1;
-}
-
-template <int D>
-int launch_wide(const RaggedArgs& a, const RaggedPlan& p, const WideWs& w, hipStream_t st)
-{
-    constexpr int bytes = 2 * 64 * (2 * D + 2 * D + 64);
-    static unsigned long long done = 0;
-    if (!ensure_dynamic_lds((const void*)ragged_wide_kernel<D>, bytes, done)) return -1;
-    hipLaunchKernelGGL((ragged_wide_kernel<D>), dim3(p.wide_wgs), dim3(512), bytes, st, a, w);
-    if (hipGetLastError() != hipSuccess) return -1;
-    hipLaunchKernelGGL((ragged_wide_merge_kernel<D>), dim3(p.wide_wgs + 8, D / 4), dim3(256), 0, st, a, w, p.wide_wgs);
+    if (p.wide_wgs > 0) {
+        constexpr int bytes = 2 * 64 * (2 * D + 2 * D + 64);
+        static unsigned long long done = 0;
+        if (!ensure_dynamic_lds((const void*)ragged_wide_kernel<D>, bytes, done)) return -1;
+        hipLaunchKernelGGL((ragged_wide_kernel<D>), dim3(p.wide_wgs), dim3(512), bytes, st, a, w.wide);
+        if (hipGetLastError() != hipSuccess) return -1;
+    }
+    const int rows = (a.max_q < a.T ? a.max_q : a.T) * (a.Hq / a.Hkv), few_rows = rows < 16 * RT ? rows : 16 * RT;      // (the host has checked that T Hq fits)
+    const int wgs = a.B * a.Hkv * few_rows + (p.wide_wgs > 0 ? p.wide_wgs * (D / 4) + kEmptyWgs : 0);
+    hipLaunchKernelGGL((ragged_merge_kernel<D, 16 * RT>), dim3(wgs), dim3(256), 0, st, a, w.few, few_rows, w.wide, p.wide_wgs);
     return hipGetLastError() == hipSuccess ? 0 : -1;
 }
 
@@ -925,17 +962,15 @@ int launch_wide(const RaggedArgs& a, const RaggedPlan& p, const WideWs& w, hipSt
 
 size_t ragged_ws_bytes(int T, int B, int Hq, int Hkv, int max_q, int max_pages, int D)
 {
-    return carve_ragged(nullptr, plan_of(T, B, Hq, Hkv, max_q, max_pages, kChipCus), B, D).bytes;
+    return carve_ragged(nullptr, plan_of(T, B, Hq, Hkv, max_q, max_pages, D, kChipCus), B, D).bytes;
 }
 
 int launch_ragged(const RaggedArgs& a, int D, void* ws, hipStream_t st)
 {
-    const RaggedPlan p = plan_of(a.T, a.B, a.Hq, a.Hkv, a.max_q, a.max_pages, kChipCus);
+    const RaggedPlan p = plan_of(a.T, a.B, a.Hq, a.Hkv, a.max_q, a.max_pages, D, kChipCus);
     const RaggedWs w = carve_ragged(ws, p, a.B, D);
-    int rc = D == 128 ? (p.few_groups == 1 ? launch_few<128, 1>(a, p, w.few, st) : launch_few<128, 2>(a, p, w.few, st))
-                      : (p.few_groups == 1 ? launch_few<64, 1>(a, p, w.few, st) : launch_few<64, 2>(a, p, w.few, st));
-    if (!rc && p.wide_wgs > 0) rc = D == 128 ? launch_wide<128>(a, p, w.wide, st) : launch_wide<64>(a, p, w.wide, st);
-    return rc;
+    return D == 128 ? (p.few_groups == 1 ? launch_ragged_of<128, 1>(a, p, w, st) : launch_ragged_of<128, 2>(a, p, w, st))
+                    : (p.few_groups == 1 ? launch_ragged_of<64, 1>(a, p, w, st) : launch_ragged_of<64, 2>(a, p, w, st));
 }
 
 }  // namespace aq
