@@ -378,63 +378,70 @@ __global__ __launch_bounds__(256, RT == 1 ? 3 : 2) void ragged_few_kernel(const 
     }
 }
 
-// O and lse of the units whose pages were shared, and of rows that see no key: a workgroup per unit and row, whose groups of D / 4 threads take the
-// partial sums in turn.
+// O and lse of a unit whose pages were shared, and of rows that see no key, by a workgroup: groups of D / 4 threads have a row each, or, while there are
+// fewer rows than groups, several groups share the partial sums of a row.
 template <int D, int ROWS>
-__device__ void few_merge(const RaggedArgs& a, const FewWs& ws, int unit, int r)
+__device__ void few_merge(const RaggedArgs& a, const FewWs& ws, int unit)
 {
     constexpr int NG = 256 / (D / 4);
     __shared__ __align__(16) float acc[NG][D];
     __shared__ float ml[NG][2];
     const int G = a.Hq / a.Hkv, b = unit / a.Hkv, h = unit % a.Hkv;
     const int tid = threadIdx.x, grp = tid / (D / 4), d = tid % (D / 4) * 4;
+    const int quota = *ws.quota, front = ws.front[b];             // (beside the lengths, not behind them)
     const Seq s = seq_of(a, b);
     const Few u = few_of<D>(a, s, G, ROWS);
-    if (r >= u.rows || u.rows > ROWS) return;
-    const int tk = r / G, hd = h * G + r % G;
-    uint16_t* dst = a.o + (size_t)(s.first + tk) * a.o_token + (size_t)hd * a.o_head;
-    if (u.pages == 0) {
-        if (grp == 0) *reinterpret_cast<uint2v*>(dst + d) = uint2v{0u, 0u};
-        if (tid == 0 && a.lse) a.lse[(size_t)(s.first + tk) * a.Hq + hd] = -INFINITY;
-        return;
+    if (u.rows == 0 || u.rows > ROWS) return;
+    int f = 0, n = 0;                                             // the first workgroup that had pages of it, how many had
+    if (u.pages > 0) {
+        const long long w0 = (long long)front * a.Hkv + (long long)h * u.units + kFewStart<D>, w1 = w0 + u.pages - 1;
+        f = (int)(w0 / quota); n = (int)(w1 / quota) - f + 1;
+        if (n < 2) return;
     }
-    const int quota = *ws.quota;
-    const long long w0 = (long long)ws.front[b] * a.Hkv + (long long)h * u.units + kFewStart<D>, w1 = w0 + u.pages - 1;
-    const int f = (int)(w0 / quota), n = (int)(w1 / quota) - f + 1;
-    if (n < 2) return;
-    float M = -INFINITY, l = 0.0f;
-    floatx4 v = {0.0f, 0.0f, 0.0f, 0.0f};
-    for (int i0 = grp; i0 < n; i0 += 4 * NG) {                      // four at a time: one trip to memory
-        floatx4 po[4];
-        float pm[4], pl[4];
+    int per = NG;                                                 // groups to a row
+    while (per > 1 && (NG / per) < u.rows) per >>= 1;
+    for (int r0 = 0; r0 < u.rows; r0 += NG / per) {
+        const int r = r0 + grp / per;
+        const bool on = r < u.rows;
+        float M = -INFINITY, l = 0.0f;
+        floatx4 v = {0.0f, 0.0f, 0.0f, 0.0f};
+        if (on) {
+            for (int i0 = grp % per; i0 < n; i0 += 4 * per) {      // four at a time: one trip to memory
+                floatx4 po[4];
+                float pm[4], pl[4];
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            const int i = min(i0 + k * NG, n - 1);
-            const size_t at = ((size_t)(f + i) * 2 + (i == 0 ? 1 : 0)) * ROWS + r;
-            po[k] = *reinterpret_cast<const floatx4*>(ws.part_o + at * D + d);
-            pm[k] = i0 + k * NG < n ? ws.part_ml[at * 2] : -INFINITY;
-            pl[k] = ws.part_ml[at * 2 + 1];
+                for (int k = 0; k < 4; ++k) {
+                    const int i = min(i0 + k * per, n - 1);
+                    const size_t at = ((size_t)(f + i) * 2 + (i == 0 ? 1 : 0)) * ROWS + r;
+                    po[k] = *reinterpret_cast<const floatx4*>(ws.part_o + at * D + d);
+                    pm[k] = i0 + k * per < n ? ws.part_ml[at * 2] : -INFINITY;
+                    pl[k] = ws.part_ml[at * 2 + 1];
+                }
+                const float top = fmaxf(fmaxf(fmaxf(pm[0], pm[1]), fmaxf(pm[2], pm[3])), M), at = top == -INFINITY ? 0.0f : top;
+                const float al = __builtin_amdgcn_exp2f(M - at);
+                M = top; l *= al; v *= al;
+#pragma unroll
+                for (int k = 0; k < 4; ++k) { const float x = __builtin_amdgcn_exp2f(pm[k] - at); l = fmaf(pl[k], x, l); v += po[k] * x; }
+            }
         }
-        const float top = fmaxf(fmaxf(fmaxf(pm[0], pm[1]), fmaxf(pm[2], pm[3])), M), at = top == -INFINITY ? 0.0f : top;
-        const float al = __builtin_amdgcn_exp2f(M - at);
-        M = top; l *= al; v *= al;
-#pragma unroll
-        for (int k = 0; k < 4; ++k) { const float x = __builtin_amdgcn_exp2f(pm[k] - at); l = fmaf(pl[k], x, l); v += po[k] * x; }
+        if (per > 1) {                                            // (then one round is all)
+            *reinterpret_cast<floatx4*>(&acc[grp][d]) = v;
+            if (d == 0) { ml[grp][0] = M; ml[grp][1] = l; }
+            __syncthreads();
+            if (grp % per != 0 || !on) return;
+            float top = -INFINITY;
+            for (int k = 0; k < per; ++k) top = fmaxf(top, ml[grp + k][0]);
+            const float at = top == -INFINITY ? 0.0f : top;
+            l = 0.0f; v = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
+            for (int k = 0; k < per; ++k) { const float x = __builtin_amdgcn_exp2f(ml[grp + k][0] - at); l = fmaf(ml[grp + k][1], x, l); v += *reinterpret_cast<const floatx4*>(&acc[grp + k][d]) * x; }
+            M = top;
+        }
+        if (!on) continue;
+        const int tk = r / G, hd = h * G + r % G;
+        v *= l != 0.0f ? 1.0f / l : 0.0f;
+        *reinterpret_cast<uint2v*>(a.o + (size_t)(s.first + tk) * a.o_token + (size_t)hd * a.o_head + d) = uint2v{pack_bf16x2_cvt(v[0], v[1]), pack_bf16x2_cvt(v[2], v[3])};
+        if (d == 0 && a.lse) a.lse[(size_t)(s.first + tk) * a.Hq + hd] = l != 0.0f ? M * 0.6931471805599453f + logf(l) : -INFINITY;
     }
-    *reinterpret_cast<floatx4*>(&acc[grp][d]) = v;
-    if (d == 0) { ml[grp][0] = M; ml[grp][1] = l; }
-    __syncthreads();
-    if (grp != 0) return;
-    float top = -INFINITY;
-#pragma unroll
-    for (int k = 0; k < NG; ++k) top = fmaxf(top, ml[k][0]);
-    const float at = top == -INFINITY ? 0.0f : top;
-    l = 0.0f; v = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-    for (int k = 0; k < NG; ++k) { const float x = __builtin_amdgcn_exp2f(ml[k][0] - at); l = fmaf(ml[k][1], x, l); v += *reinterpret_cast<const floatx4*>(&acc[k][d]) * x; }
-    v *= l != 0.0f ? 1.0f / l : 0.0f;
-    *reinterpret_cast<uint2v*>(dst + d) = uint2v{pack_bf16x2_cvt(v[0], v[1]), pack_bf16x2_cvt(v[2], v[3])};
-    if (d == 0 && a.lse) a.lse[(size_t)(s.first + tk) * a.Hq + hd] = l != 0.0f ? top * 0.6931471805599453f + logf(l) : -INFINITY;
 }
 
 // The units of work of the kernel for many rows: a tile of kWideRows rows and the tiles of 64 keys that it sees, for every kv head, sequence by sequence,
@@ -824,46 +831,52 @@ __global__ __launch_bounds__(512, 2) void ragged_wide_kernel(const RaggedArgs a,
     }
 }
 
-// O and lse of the row tiles whose key tiles were shared: a workgroup per place where one workgroup's work ended and another's began, wave of
-// rows and 32 d; of the places within a row tile the first has it.
+// O and lse of the row tiles whose key tiles were shared: a workgroup per place where one workgroup's work ended and another's began, and 32 rows; of the
+// places within a row tile the first has it.
 template <int D>
-__device__ void wide_merge(const RaggedArgs& a, const WideWs& ws, int place, int part)
+__device__ void wide_merge(const RaggedArgs& a, const WideWs& ws, int place, int wave)
 {
+    constexpr int NB = D / 32;
     if (place == 0) return;                                       // (nothing in front of the first)
     const long long quota = *ws.quota;
-    if (quota == 0) return;
     const WideRec r = ws.rec[place];
-    if (r.off <= kWideStart || r.off - quota > kWideStart) return;      // it begins there, or has begun two workgroups ago
+    if (quota == 0 || r.off <= kWideStart || r.off - quota > kWideStart) return;      // it begins there, or has begun two workgroups ago
     const Seq s = seq_of(a, r.b);
-    const int G = a.Hq / a.Hkv, rows = s.n * G, wave = part / (D / 32), i = part % (D / 32), lane = threadIdx.x & 63, j = threadIdx.x >> 6;
+    const int G = a.Hq / a.Hkv, rows = s.n * G, lane = threadIdx.x & 63, j = threadIdx.x >> 6;
     const int col = lane & 31, half = lane >> 5, row = r.tile * kWideRows + 32 * wave + col;
     if (r.tile * kWideRows + 32 * wave >= rows) return;
     const int n = 1 + (int)((r.nt - r.off + quota - 1) / quota);
     float M = -INFINITY, l = 0.0f;
-    floatx4 v = {0.0f, 0.0f, 0.0f, 0.0f};
-    for (int k0 = 0; k0 < n; k0 += 4) {
-        floatx4 po[4];
-        float pm[4], pl[4];
+    floatx4 v[NB] = {};
+    for (int k0 = 0; k0 < n; k0 += 2) {
+        floatx4 po[2][NB];
+        float pm[2], pl[2];
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
+        for (int k = 0; k < 2; ++k) {
             const int x = min(k0 + k, n - 1);
             const size_t slot = (x == 0 ? (size_t)(place - 1) * 2 + 1 : (size_t)(place + x - 1) * 2) * 8 + wave;
-            po[k] = *reinterpret_cast<const floatx4*>(ws.part_o + ((slot * (D / 8) + 4 * i + j) * 64 + lane) * 4);
+#pragma unroll
+            for (int i = 0; i < NB; ++i) po[k][i] = *reinterpret_cast<const floatx4*>(ws.part_o + ((slot * (D / 8) + 4 * i + j) * 64 + lane) * 4);
             pm[k] = k0 + k < n ? ws.part_ml[(slot * 32 + col) * 2] : -INFINITY;
             pl[k] = ws.part_ml[(slot * 32 + col) * 2 + 1];
         }
-        const float top = fmaxf(fmaxf(fmaxf(pm[0], pm[1]), fmaxf(pm[2], pm[3])), M), at = top == -INFINITY ? 0.0f : top;
-        const float al = __builtin_amdgcn_exp2f(M - at);
-        M = top; l *= al; v *= al;
+        const float top = fmaxf(fmaxf(pm[0], pm[1]), M), at = top == -INFINITY ? 0.0f : top;
+        const float f0 = __builtin_amdgcn_exp2f(M - at), f1 = __builtin_amdgcn_exp2f(pm[0] - at), f2 = __builtin_amdgcn_exp2f(pm[1] - at);
+        M = top;
+        l = l * f0 + pl[0] * f1 + pl[1] * f2;
 #pragma unroll
-        for (int k = 0; k < 4; ++k) { const float x = __builtin_amdgcn_exp2f(pm[k] - at); l = fmaf(pl[k], x, l); v += po[k] * x; }
+        for (int i = 0; i < NB; ++i) v[i] = v[i] * f0 + po[0][i] * f1 + po[1][i] * f2;
     }
     if (row >= rows) return;
     const int tok = row / G, head = r.h * G + row % G;
-    v *= l != 0.0f ? 1.0f / l : 0.0f;
-    *reinterpret_cast<uint2v*>(a.o + (size_t)(s.first + tok) * a.o_token + (size_t)head * a.o_head + 32 * i + 8 * j + 4 * half) =
-        uint2v{pack_bf16x2_cvt(v[0], v[1]), pack_bf16x2_cvt(v[2], v[3])};
-    if (i == 0 && j == 0 && half == 0 && a.lse) a.lse[(size_t)(s.first + tok) * a.Hq + head] = l != 0.0f ? M * 0.6931471805599453f + logf(l) : -INFINITY;
+    const float inv = l != 0.0f ? 1.0f / l : 0.0f;
+    uint16_t* dst = a.o + (size_t)(s.first + tok) * a.o_token + (size_t)head * a.o_head + 8 * j + 4 * half;
+#pragma unroll
+    for (int i = 0; i < NB; ++i) {
+        const floatx4 y = v[i] * inv;
+        *reinterpret_cast<uint2v*>(dst + 32 * i) = uint2v{pack_bf16x2_cvt(y[0], y[1]), pack_bf16x2_cvt(y[2], y[3])};
+    }
+    if (j == 0 && half == 0 && a.lse) a.lse[(size_t)(s.first + tok) * a.Hq + head] = l != 0.0f ? M * 0.6931471805599453f + logf(l) : -INFINITY;
 }
 // O = 0, lse = -inf for row tiles, of sequences with many rows, that see no key: they are nobody's work.  One of n workgroups.
 template <int D>
@@ -891,14 +904,13 @@ __device__ void wide_empty(const RaggedArgs& a, int which, int n)
 // The last launch of a step: what the others left to be joined.
 constexpr int kEmptyWgs = 64;
 template <int D, int ROWS>
-__global__ __launch_bounds__(256) void ragged_merge_kernel(const RaggedArgs a, const FewWs few, int few_rows, const WideWs wide, int places)
+__global__ __launch_bounds__(256) void ragged_merge_kernel(const RaggedArgs a, const FewWs few, const WideWs wide, int places)
 {
     int x = (int)blockIdx.x;
-    const int few_wgs = a.B * a.Hkv * few_rows;
-    if (x < few_wgs) { few_merge<D, ROWS>(a, few, x / few_rows, x % few_rows); return; }
-    x -= few_wgs;
-    if (x < places * (D / 4)) { wide_merge<D>(a, wide, x / (D / 4), x % (D / 4)); return; }
-    wide_empty<D>(a, x - places * (D / 4), kEmptyWgs);
+    if (x < 8 * places) { wide_merge<D>(a, wide, x / 8, x % 8); return; }
+    x -= 8 * places;
+    if (x < a.B * a.Hkv) { few_merge<D, ROWS>(a, few, x); return; }
+    wide_empty<D>(a, x - a.B * a.Hkv, kEmptyWgs);
 }
 
 inline size_t up256(size_t x) { return (x + 255) / 256 * 256; }
@@ -952,9 +964,8 @@ int launch_ragged_of(const RaggedArgs& a, const RaggedPlan& p, const RaggedWs& w
         hipLaunchKernelGGL((ragged_wide_kernel<D>), dim3(p.wide_wgs), dim3(512), bytes, st, a, w.wide);
         if (hipGetLastError() != hipSuccess) return -1;
     }
-    const int rows = (a.max_q < a.T ? a.max_q : a.T) * (a.Hq / a.Hkv), few_rows = rows < 16 * RT ? rows : 16 * RT;      // (the host has checked that T Hq fits)
-    const int wgs = a.B * a.Hkv * few_rows + (p.wide_wgs > 0 ? p.wide_wgs * (D / 4) + kEmptyWgs : 0);
-    hipLaunchKernelGGL((ragged_merge_kernel<D, 16 * RT>), dim3(wgs), dim3(256), 0, st, a, w.few, few_rows, w.wide, p.wide_wgs);
+    const int wgs = a.B * a.Hkv + (p.wide_wgs > 0 ? p.wide_wgs * 8 + kEmptyWgs : 0);
+    hipLaunchKernelGGL((ragged_merge_kernel<D, 16 * RT>), dim3(wgs), dim3(256), 0, st, a, w.few, w.wide, p.wide_wgs);
     return hipGetLastError() == hipSuccess ? 0 : -1;
 }
 
