@@ -435,7 +435,7 @@ int attnqat_debug_fwd_infer_paged(const void* q, int B, int Hq, int Hkv, int Lq,
  * outside [0, num_pages * 128) is left out.  Slots must differ from each other: of two rows with one slot either may be found there, block by block.
  *
  * attnqat_kv_cache_read is the way back: row t of k and v becomes the values (exact in bf16) that slot slots[t] holds, zeros for a slot outside
- * the cache.
+ * the cache.  (Both: at most 2^30 rows of heads, T Hkv.)
  *
  * attnqat_fwd_kv4_ragged: O = softmax(scale Q K^T + mask) V, K and V being the values that the pages hold: only the cache is in 4 bits.  Q is not
  * quantized, nor are the probabilities (which are rounded to fp16 for their product with V; scores, sums and O are fp32), as for a

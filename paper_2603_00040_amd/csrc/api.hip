@@ -627,7 +627,7 @@ int rows_common(const void* k, int64_t k_token, int64_t k_head, const void* v, i
 {
     if (T < 0 || Hkv < 1 || num_pages < 1) return ATTNQAT_EINVAL;
     if (dtype != ATTNQAT_BF16) return ATTNQAT_EDTYPE;
-    if ((d != 64 && d != 128) || Hkv > 65535) return ATTNQAT_ESHAPE;
+    if ((d != 64 && d != 128) || (long long)T * Hkv > (1 << 30)) return ATTNQAT_ESHAPE;
     if (T == 0) return ATTNQAT_OK;
     if (!k || !v || !cache || !slots || ((uintptr_t)cache & 15) || ((uintptr_t)slots & 7)) return ATTNQAT_EINVAL;
     if (!rows_of(k, k_token, k_head, T, Hkv, d, written, kr) || !rows_of(v, v_token, v_head, T, Hkv, d, written, vr)) return ATTNQAT_EINVAL;

@@ -174,65 +174,91 @@ __global__ __launch_bounds__(256) void plan_fill_kernel(const PlanArgs a, int ro
     plan_give(a, b < a.B ? items[b] : PlanItem{0, 0, 0, 0}, b0, hd->tail);
 }
 
-// A row (token, kv head) of K or V has D / 16 blocks; a thread takes one block of one row, neighbouring threads the blocks of a row and
-// then the rows of the next tokens, whose slots in a page mostly follow each other.
+// A row (token, kv head) of K or V is D / 16 blocks; a thread takes a block of kAppendRows rows, which are under way at once.  Rows are taken token by
+// token, all heads of a token after each other: they lie side by side in memory.
+constexpr int kAppendRows = 2;
 template <int D>
 __global__ __launch_bounds__(256) void append_kernel(const uint16_t* __restrict__ k, const uint16_t* __restrict__ v, size_t k_token, size_t k_head,
                                                      size_t v_token, size_t v_head, int T, int Hkv, unsigned char* __restrict__ cache, int num_pages,
                                                      const long long* __restrict__ slots)
 {
-    constexpr int nb = D / 16;
-    const int h = blockIdx.y, which = blockIdx.z, cb = threadIdx.x % nb;
-    const int t = (int)blockIdx.x * (256 / nb) + threadIdx.x / nb, tc = min(t, T - 1);
-    const long long slot = slots[tc];
-    const uint4v* src = reinterpret_cast<const uint4v*>((which ? v : k) + (size_t)tc * (which ? v_token : k_token) + (size_t)h * (which ? v_head : k_head) + cb * 16);
-    const uint4v a = src[0], b = src[1];
-    float val[16];
+    constexpr int nb = D / 16, per = 256 / nb;                    // threads to a row, rows at a time
+    const int which = blockIdx.y, c = threadIdx.x % nb, r0 = (int)blockIdx.x * (per * kAppendRows) + threadIdx.x / nb, rows = T * Hkv;
+    const uint16_t* src = (which ? v : k) + 16 * c;
+    const size_t token = which ? v_token : k_token, head = which ? v_head : k_head;
+    uint4v x[kAppendRows][2];
+    long long slot[kAppendRows];
+    int h[kAppendRows];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        val[2 * i]         = __uint_as_float(a[i] << 16);
-        val[2 * i + 1]     = __uint_as_float(a[i] & 0xFFFF0000u);
-        val[8 + 2 * i]     = __uint_as_float(b[i] << 16);
-        val[8 + 2 * i + 1] = __uint_as_float(b[i] & 0xFFFF0000u);
+    for (int i = 0; i < kAppendRows; ++i) {
+        const int r = min(r0 + i * per, rows - 1), t = r / Hkv;
+        h[i] = r % Hkv;
+        const uint4v* p = reinterpret_cast<const uint4v*>(src + (size_t)t * token + (size_t)h[i] * head);
+        x[i][0] = p[0]; x[i][1] = p[1];
+        slot[i] = slots[t];
     }
-    const Nv16 q = phi_block16_bf16(val);
-    // the scale bytes of four neighbouring blocks of a row as one dword
-    uint32_t sb = q.sc & 0xFFu;
-    sb |= lane_down<1>(sb) << 8;
-    sb |= lane_down<2>(sb) << 16;
-    if (t >= T || slot < 0 || slot >= (long long)num_pages * 128) return;
-    unsigned char* part = cache + ((size_t)(slot >> 7) * Hkv + h) * nvfp4_page_head_bytes(D) + (which ? 128 * (D / 2 + nb) : 0);
-    const int off = (int)(slot & 127);
-    uint2v c2; c2[0] = q.clo; c2[1] = q.chi;
-    *reinterpret_cast<uint2v*>(part + off * (D / 2) + cb * 8) = c2;
-    if ((cb & 3) == 0) *reinterpret_cast<uint32_t*>(part + 128 * (D / 2) + off * nb + cb) = sb;
+#pragma unroll
+    for (int i = 0; i < kAppendRows; ++i) {
+        float val[16];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            val[2 * j]     = __uint_as_float(x[i][j >> 2][j & 3] << 16);
+            val[2 * j + 1] = __uint_as_float(x[i][j >> 2][j & 3] & 0xFFFF0000u);
+        }
+        const Nv16 q = phi_block16_bf16(val);
+        // the scale bytes of four neighbouring blocks of a row as one dword
+        uint32_t sb = q.sc & 0xFFu;
+        sb |= lane_down<1>(sb) << 8;
+        sb |= lane_down<2>(sb) << 16;
+        if (r0 + i * per >= rows || slot[i] < 0 || slot[i] >= (long long)num_pages * 128) continue;
+        unsigned char* part = cache + ((size_t)(slot[i] >> 7) * Hkv + h[i]) * nvfp4_page_head_bytes(D) + (which ? 128 * (D / 2 + nb) : 0);
+        const int off = (int)(slot[i] & 127);
+        uint2v c2; c2[0] = q.clo; c2[1] = q.chi;
+        *reinterpret_cast<uint2v*>(part + off * (D / 2) + c * 8) = c2;
+        if ((c & 3) == 0) *reinterpret_cast<uint32_t*>(part + 128 * (D / 2) + off * nb + c) = sb;
+    }
 }
 
-// The same way back; a slot outside the cache reads as zeros.  (A value has at most 6 significant bits: exact in bf16.)
+// The same way back; a slot outside the cache reads as zeros.  (A value has at most 6 significant bits: exact in bf16.)  Bound by what it writes: a thread
+// makes 8 values, so that a wave stores 1 KiB in one piece per instruction, and has kReadRows rows under way at once.
+constexpr int kReadRows = 4;
 template <int D>
 __global__ __launch_bounds__(256) void read_kernel(uint16_t* __restrict__ k, uint16_t* __restrict__ v, size_t k_token, size_t k_head, size_t v_token,
                                                    size_t v_head, int T, int Hkv, const unsigned char* __restrict__ cache, int num_pages,
                                                    const long long* __restrict__ slots)
 {
-    constexpr int nb = D / 16;
-    const int h = blockIdx.y, which = blockIdx.z, cb = threadIdx.x % nb;
-    const int t = (int)blockIdx.x * (256 / nb) + threadIdx.x / nb;
-    if (t >= T) return;
-    const long long slot = slots[t];
-    float x[16] = {};
-    if (slot >= 0 && slot < (long long)num_pages * 128) {
-        const unsigned char* part = cache + ((size_t)(slot >> 7) * Hkv + h) * nvfp4_page_head_bytes(D) + (which ? 128 * (D / 2 + nb) : 0);
-        const int off = (int)(slot & 127);
-        const uint2v c = *reinterpret_cast<const uint2v*>(part + off * (D / 2) + cb * 8);
-        dequant_block16(nv16_of(c[0], c[1], part[128 * (D / 2) + off * nb + cb]), x);
+    constexpr int nt = D / 8, per = 256 / nt;                     // threads to a row, rows at a time
+    const int which = blockIdx.y, c = threadIdx.x % nt, r0 = (int)blockIdx.x * (per * kReadRows) + threadIdx.x / nt, rows = T * Hkv;
+    long long slot[kReadRows];
+    uint32_t codes[kReadRows], sc[kReadRows];
+    int t[kReadRows], h[kReadRows];
+#pragma unroll
+    for (int i = 0; i < kReadRows; ++i) {
+        const int r = min(r0 + i * per, rows - 1);
+        t[i] = r / Hkv; h[i] = r % Hkv;
+        slot[i] = slots[t[i]];
     }
-    uint4v* dst = reinterpret_cast<uint4v*>((which ? v : k) + (size_t)t * (which ? v_token : k_token) + (size_t)h * (which ? v_head : k_head) + cb * 16);
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
+    for (int i = 0; i < kReadRows; ++i) {
+        const bool in = slot[i] >= 0 && slot[i] < (long long)num_pages * 128;
+        const long long at = in ? slot[i] : 0;
+        const unsigned char* part = cache + ((size_t)(at >> 7) * Hkv + h[i]) * nvfp4_page_head_bytes(D) + (which ? 128 * (D / 2 + D / 16) : 0);
+        const int off = (int)(at & 127);
+        codes[i] = *reinterpret_cast<const uint32_t*>(part + off * (D / 2) + 4 * c);
+        sc[i] = part[128 * (D / 2) + off * (D / 16) + (c >> 1)];
+        if (!in) { codes[i] = 0; sc[i] = 0; }
+    }
+    uint16_t* dst = (which ? v : k) + 8 * c;
+    const size_t token = which ? v_token : k_token, head = which ? v_head : k_head;
+#pragma unroll
+    for (int i = 0; i < kReadRows; ++i) {
+        typedef float float2v __attribute__((ext_vector_type(2)));
+        const float f = __builtin_amdgcn_cvt_scalef32_f32_fp8(sc[i], 1.0f, 0);
         uint4v w;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) w[j] = pack_bf16x2_cvt(x[8 * i + 2 * j], x[8 * i + 2 * j + 1]);
-        dst[i] = w;
+#define AQ_VALUES(J) { const float2v x = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes[i], 1.0f, J); w[J] = pack_bf16x2_cvt(x[0] * f, x[1] * f); }
+        AQ_VALUES(0) AQ_VALUES(1) AQ_VALUES(2) AQ_VALUES(3)
+#undef AQ_VALUES
+        if (r0 + i * per < rows) *reinterpret_cast<uint4v*>(dst + (size_t)t[i] * token + (size_t)h[i] * head) = w;
     }
 }
 
@@ -261,8 +287,8 @@ int launch_page_plan(const int* kv_lens, const int* new_lens, int B, int* page_t
 
 int launch_kv_append(const Rows& k, const Rows& v, int T, int Hkv, int D, void* cache, int num_pages, const long long* slots, hipStream_t st)
 {
-    const int per = 256 / (D / 16);
-    const dim3 grid((T + per - 1) / per, Hkv, 2);
+    const int per = 256 / (D / 16) * kAppendRows;
+    const dim3 grid((T * Hkv + per - 1) / per, 2);
     if (D == 128) hipLaunchKernelGGL((append_kernel<128>), grid, dim3(256), 0, st, (const uint16_t*)k.p, (const uint16_t*)v.p, k.token, k.head, v.token, v.head, T, Hkv, (unsigned char*)cache, num_pages, slots);
     else          hipLaunchKernelGGL((append_kernel<64>), grid, dim3(256), 0, st, (const uint16_t*)k.p, (const uint16_t*)v.p, k.token, k.head, v.token, v.head, T, Hkv, (unsigned char*)cache, num_pages, slots);
     return hipGetLastError() == hipSuccess ? 0 : -1;
@@ -270,8 +296,8 @@ int launch_kv_append(const Rows& k, const Rows& v, int T, int Hkv, int D, void* 
 
 int launch_kv_read(const Rows& k, const Rows& v, int T, int Hkv, int D, const void* cache, int num_pages, const long long* slots, hipStream_t st)
 {
-    const int per = 256 / (D / 16);
-    const dim3 grid((T + per - 1) / per, Hkv, 2);
+    const int per = 256 / (D / 8) * kReadRows;
+    const dim3 grid((T * Hkv + per - 1) / per, 2);
     if (D == 128) hipLaunchKernelGGL((read_kernel<128>), grid, dim3(256), 0, st, (uint16_t*)k.p, (uint16_t*)v.p, k.token, k.head, v.token, v.head, T, Hkv, (const unsigned char*)cache, num_pages, slots);
     else          hipLaunchKernelGGL((read_kernel<64>), grid, dim3(256), 0, st, (uint16_t*)k.p, (uint16_t*)v.p, k.token, k.head, v.token, v.head, T, Hkv, (const unsigned char*)cache, num_pages, slots);
     return hipGetLastError() == hipSuccess ? 0 : -1;

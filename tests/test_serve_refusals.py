@@ -34,7 +34,7 @@ def _append(**kw):
 
 @pytest.mark.parametrize("kw,code", [
     (dict(k=None), aq.EINVAL), (dict(v=None), aq.EINVAL), (dict(cache=None), aq.EINVAL), (dict(slots=None), aq.EINVAL), (dict(pages=0), aq.EINVAL), (dict(Hkv=0), aq.EINVAL),
-    (dict(T=-1), aq.EINVAL), (dict(dtype=1), aq.EDTYPE), (dict(d=96), aq.ESHAPE), (dict(Hkv=65536), aq.ESHAPE), (dict(k=P + 8), aq.EINVAL), (dict(v=P + 2), aq.EINVAL),
+    (dict(T=-1), aq.EINVAL), (dict(dtype=1), aq.EDTYPE), (dict(d=96), aq.ESHAPE), (dict(Hkv=1 << 29), aq.ESHAPE), (dict(T=(1 << 27) + 1), aq.ESHAPE), (dict(k=P + 8), aq.EINVAL), (dict(v=P + 2), aq.EINVAL),
     (dict(cache=3 * P + 8), aq.EINVAL), (dict(slots=4 * P + 4), aq.EINVAL), (dict(kt=1028), aq.EINVAL), (dict(vh=132), aq.EINVAL), (dict(kt=-1024), aq.EINVAL),
     (dict(vt=1 << 60), aq.EINVAL), (dict(kh=1 << 60), aq.EINVAL)])
 def test_append_and_read(kw, code):
