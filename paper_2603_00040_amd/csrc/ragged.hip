@@ -20,12 +20,15 @@ namespace aq {
 
 namespace {
 
-constexpr int kFewRows = 32;          // most rows of a (sequence, kv head) that the kernel for few rows takes
+// Most rows of a (sequence, kv head) that the kernel for few rows takes, in tiles of 16 or 32 that read the keys each for itself; more go to the one that has
+// tiles of 256.  Few -> many, 16 sequences of 4096 keys, 8 kv heads of 128: 48 rows 56 against 78 us, 80 rows 76 against 79, 128 rows 84 against 87;
+// 4 of 16 000 keys: 40 rows 59 against 75, 120 rows 91 against 81.
+constexpr int kFewRows = 96;
 // The reference that a row's exponents are taken against, in powers of two, follows its running maximum only when that is more than this above it: a row's
 // largest probability so far is then up to 2^8 (as fp16 as good as 1), and most tiles need no rescaling of O: some row of 32 has a new maximum
 // in most of the first fifty tiles.
 constexpr float kSlack = 8.0f;
-constexpr int kWideStart = 3;         // (10 000 cycles against 4 000 for a tile of keys of 128 d)
+constexpr int kWideStart = 5;         // (20 000 cycles against 4 000 for a tile of keys of 128 d)
 constexpr int kWideRows = 256;        // rows of a tile of the other one
 
 struct Seq { int first, n, len; };    // first query of the step, number of queries, keys
@@ -43,20 +46,21 @@ __device__ inline void keys_of(const RaggedArgs& a, const Seq& s, int ta, int tb
     hi = max(lo, hi);
 }
 
-// The units of work of the kernel for few rows: the pages that the rows of a sequence see, once per kv head, sequence by sequence, head by head, page by
-// page.  What a (sequence, kv head) costs besides (its rows of Q, the first trip to its pages, the result) counts as kFewStart pages in
-// front of its own.  Sequences with more rows than `most` have no units here.
+// The units of work of the kernel for few rows: the pages that the rows of a sequence see, once per kv head and tile of rows, sequence by sequence, head by
+// head, tile by tile, page by page.  What a tile costs besides (its rows of Q, the first trip to its pages, the result) counts as kFewStart pages in
+// front of its own.  Sequences with more rows than kFewRows have no units here.
 template <int D> constexpr int kFewStart = D == 64 ? 3 : 2;      // (6 000 cycles, against 2 000 and 3 200 for a page)
-struct Few { int rows, first_page, pages, units; };
-template <int D>
-__device__ inline Few few_of(const RaggedArgs& a, const Seq& s, int G, int most)
+struct Few { int rows, tiles /* of ROWS rows */, first_page, pages, units /* of a tile */; };
+template <int D, int ROWS>
+__device__ inline Few few_of(const RaggedArgs& a, const Seq& s, int G)
 {
-    const int rows = s.n <= most ? s.n * G : most + 1;
+    const int rows = s.n * G;
     int lo, hi;
     keys_of(a, s, 0, s.n - 1, lo, hi);
-    const int pages = rows > 0 && rows <= most && hi > lo ? ((hi + 127) >> 7) - (lo >> 7) : 0;
-    return Few{rows, lo >> 7, pages, pages > 0 ? pages + kFewStart<D> : 0};
+    const int pages = rows > 0 && rows <= kFewRows && hi > lo ? ((hi + 127) >> 7) - (lo >> 7) : 0;
+    return Few{rows, (rows + ROWS - 1) / ROWS, lo >> 7, pages, pages > 0 ? pages + kFewStart<D> : 0};
 }
+__device__ inline int few_units(const Few& u) { return u.tiles * u.units; }      // of a head
 __device__ inline Seq uniform_seq(const Seq& s) { return Seq{uniform(s.first), uniform(s.n), uniform(s.len)}; }
 
 // Codes and scale bytes of D / 4 values of one key: lane (key cc of 16, group g) holds d = (D/4) g .. + D/4 - 1.  (The scale bytes as the dword that they
@@ -138,7 +142,7 @@ __global__ __launch_bounds__(256, RT == 1 ? 3 : 2) void ragged_few_kernel(const 
     Seq s_b{0, 0, 0};
     for (int b0 = 0; b0 < a.B; b0 += 256) {
         s_b = b0 + tid < a.B ? seq_of(a, b0 + tid) : Seq{0, 0, 0};
-        n_b = few_of<D>(a, s_b, G, ROWS).units;
+        n_b = few_units(few_of<D, ROWS>(a, s_b, G));
         upto_b = all + wg_scan<4>(n_b, red, total);
         if (blockIdx.x == 0) {
             if (b0 + tid < a.B) ws.front[b0 + tid + 1] = upto_b;
@@ -155,7 +159,7 @@ __global__ __launch_bounds__(256, RT == 1 ? 3 : 2) void ragged_few_kernel(const 
     for (int b0 = 0, at = 0; ; b0 += 256) {
         if (a.B > 256) {                                          // (up to 256 sequences: as found above)
             s_b = b0 + tid < a.B ? seq_of(a, b0 + tid) : Seq{0, 0, 0};
-            n_b = few_of<D>(a, s_b, G, ROWS).units;
+            n_b = few_units(few_of<D, ROWS>(a, s_b, G));
             upto_b = at + wg_scan<4>(n_b, red, total);
             at += total;
         }
@@ -167,16 +171,17 @@ __global__ __launch_bounds__(256, RT == 1 ? 3 : 2) void ragged_few_kernel(const 
     __syncthreads();
     int b = uniform(found[0]), front = uniform(found[1]);
     Seq s{uniform(found[2]), uniform(found[3]), uniform(found[4])};
-    Few u = few_of<D>(a, s, G, ROWS);
-    int h, off;                                                   // the head, and the units of it in front of w
+    Few u = few_of<D, ROWS>(a, s, G);
+    int ht, off;                                                  // head and tile (head * tiles + tile), and its units in front of w
     {
-        const int in_seq = (int)(w - (long long)front * a.Hkv);
-        h = in_seq / u.units; off = in_seq % u.units;
+        const long long in_seq = w - (long long)front * a.Hkv;
+        ht = (int)(in_seq / u.units); off = (int)(in_seq % u.units);
     }
 
     while (w < w_end) {
         const int units = (int)min((long long)(u.units - off), w_end - w);
-        const int at = max(off - kFewStart<D>, 0), cnt = min(off + units - kFewStart<D>, u.pages) - at, rows = u.rows;      // pages: where this workgroup begins, how many
+        const int at = max(off - kFewStart<D>, 0), cnt = min(off + units - kFewStart<D>, u.pages) - at;      // pages: where this workgroup begins, how many
+        const int h = ht / u.tiles, r0 = ht % u.tiles * ROWS, rows = min(u.rows - r0, ROWS);
         w += units;
         if (cnt <= 0) break;                                      // (the start alone: w is at this workgroup's end)
         const int groups = RT == 1 ? 1 : (rows + 15) / 16;        // of 16 rows
@@ -189,7 +194,7 @@ __global__ __launch_bounds__(256, RT == 1 ? 3 : 2) void ragged_few_kernel(const 
         int k_first[RT], k_last[RT];                              // keys that this lane's rows see
 #pragma unroll
         for (int rt = 0; rt < RT; ++rt) {
-            const int row = min(16 * rt + cc, rows - 1), tok = row / G, head = h * G + row % G, pos = s.len - s.n + tok;
+            const int row = r0 + min(16 * rt + cc, rows - 1), tok = row / G, head = h * G + row % G, pos = s.len - s.n + tok;
             k_first[rt] = a.window > 0 ? pos - a.window + 1 : 0;
             k_last[rt] = a.causal ? min(pos, s.len - 1) : s.len - 1;
 #pragma unroll
@@ -241,7 +246,7 @@ __global__ __launch_bounds__(256, RT == 1 ? 3 : 2) void ragged_few_kernel(const 
             c_row[rt] = a.c * inv;
         }
         // keys that every row sees: a page inside [see_first, see_last] needs no mask
-        const int see_first = a.window > 0 ? s.len - a.window : 0, see_last = a.causal ? s.len - s.n : s.len - 1;
+        const int see_first = a.window > 0 ? s.len - s.n + (r0 + rows - 1) / G - a.window + 1 : 0, see_last = a.causal ? min(s.len - s.n + r0 / G, s.len - 1) : s.len - 1;
 
         floatx4 o[RT][NDT];
         float m[RT], l[RT];                                       // the maximum in units of the exponent of 2
@@ -353,7 +358,7 @@ __global__ __launch_bounds__(256, RT == 1 ? 3 : 2) void ragged_few_kernel(const 
                     v += *reinterpret_cast<const floatx4*>(sums + (x * 16 + q) * D + d);
                 }
                 if (whole) {
-                    const int tk = rr / G, hd = h * G + rr % G;
+                    const int tk = (r0 + rr) / G, hd = h * G + (r0 + rr) % G;
                     v *= lt != 0.0f ? 1.0f / lt : 0.0f;
                     const uint2v y = {pack_bf16x2_cvt(v[0], v[1]), pack_bf16x2_cvt(v[2], v[3])};
                     *reinterpret_cast<uint2v*>(a.o + (size_t)(s.first + tk) * a.o_token + (size_t)hd * a.o_head + d) = y;
@@ -367,12 +372,12 @@ __global__ __launch_bounds__(256, RT == 1 ? 3 : 2) void ragged_few_kernel(const 
         }
         // on to the next head, sequence (there is one while w < w_end; a sequence of the other kernel, or without a key, has no units)
         off = 0;
-        if (++h == a.Hkv) {
-            h = 0;
+        if (++ht == a.Hkv * u.tiles) {
+            ht = 0;
             do {
                 if (++b >= a.B) return;
                 s = uniform_seq(seq_of(a, b));
-                u = few_of<D>(a, s, G, ROWS);
+                u = few_of<D, ROWS>(a, s, G);
             } while (w < w_end && u.units == 0);
         }
     }
@@ -381,28 +386,29 @@ __global__ __launch_bounds__(256, RT == 1 ? 3 : 2) void ragged_few_kernel(const 
 // O and lse of a unit whose pages were shared, and of rows that see no key, by a workgroup: groups of D / 4 threads have a row each, or, while there are
 // fewer rows than groups, several groups share the partial sums of a row.
 template <int D, int ROWS>
-__device__ void few_merge(const RaggedArgs& a, const FewWs& ws, int unit)
+__device__ void few_merge(const RaggedArgs& a, const FewWs& ws, int unit, int tiles /* of a sequence at most */)
 {
     constexpr int NG = 256 / (D / 4);
     __shared__ __align__(16) float acc[NG][D];
     __shared__ float ml[NG][2];
-    const int G = a.Hq / a.Hkv, b = unit / a.Hkv, h = unit % a.Hkv;
+    const int G = a.Hq / a.Hkv, tile = unit % tiles, b = unit / tiles / a.Hkv, h = unit / tiles % a.Hkv;
     const int tid = threadIdx.x, grp = tid / (D / 4), d = tid % (D / 4) * 4;
     const int quota = *ws.quota, front = ws.front[b];             // (beside the lengths, not behind them)
     const Seq s = seq_of(a, b);
-    const Few u = few_of<D>(a, s, G, ROWS);
-    if (u.rows == 0 || u.rows > ROWS) return;
+    const Few u = few_of<D, ROWS>(a, s, G);
+    if (u.rows > kFewRows || tile >= u.tiles) return;
+    const int first_row = tile * ROWS, rows = min(u.rows - first_row, ROWS);
     int f = 0, n = 0;                                             // the first workgroup that had pages of it, how many had
     if (u.pages > 0) {
-        const long long w0 = (long long)front * a.Hkv + (long long)h * u.units + kFewStart<D>, w1 = w0 + u.pages - 1;
+        const long long w0 = (long long)front * a.Hkv + (long long)(h * u.tiles + tile) * u.units + kFewStart<D>, w1 = w0 + u.pages - 1;
         f = (int)(w0 / quota); n = (int)(w1 / quota) - f + 1;
         if (n < 2) return;
     }
     int per = NG;                                                 // groups to a row
-    while (per > 1 && (NG / per) < u.rows) per >>= 1;
-    for (int r0 = 0; r0 < u.rows; r0 += NG / per) {
+    while (per > 1 && (NG / per) < rows) per >>= 1;
+    for (int r0 = 0; r0 < rows; r0 += NG / per) {
         const int r = r0 + grp / per;
-        const bool on = r < u.rows;
+        const bool on = r < rows;
         float M = -INFINITY, l = 0.0f;
         floatx4 v = {0.0f, 0.0f, 0.0f, 0.0f};
         if (on) {
@@ -437,7 +443,7 @@ __device__ void few_merge(const RaggedArgs& a, const FewWs& ws, int unit)
             M = top;
         }
         if (!on) continue;
-        const int tk = r / G, hd = h * G + r % G;
+        const int tk = (first_row + r) / G, hd = h * G + (first_row + r) % G;
         v *= l != 0.0f ? 1.0f / l : 0.0f;
         *reinterpret_cast<uint2v*>(a.o + (size_t)(s.first + tk) * a.o_token + (size_t)hd * a.o_head + d) = uint2v{pack_bf16x2_cvt(v[0], v[1]), pack_bf16x2_cvt(v[2], v[3])};
         if (d == 0 && a.lse) a.lse[(size_t)(s.first + tk) * a.Hq + hd] = l != 0.0f ? M * 0.6931471805599453f + logf(l) : -INFINITY;
@@ -490,7 +496,6 @@ __global__ __launch_bounds__(512, 2) void ragged_wide_kernel(const RaggedArgs a,
     constexpr int ND = D / 16, NB = D / 32;                       // contraction steps of S, 32-d blocks of O
     constexpr int RS = 2 * D + 64;                                // bytes per key of the V tile: the 64 bytes of four keys that are read together in other banks
     constexpr int KB = 64 * 2 * D, VB = 64 * RS;                  // bytes of a tile of K, of V
-    constexpr bool kInProducts = D == 64;
     constexpr size_t VOFF = (size_t)128 * (D / 2 + D / 16);
     extern __shared__ __align__(256) unsigned char lds[];          // two tiles of K, two of V
     __shared__ long long red[8], found_front, found_per;
@@ -732,8 +737,8 @@ __global__ __launch_bounds__(512, 2) void ragged_wide_kernel(const RaggedArgs a,
                     sc[kb] = __builtin_amdgcn_mfma_f32_32x32x16_f16(ring[n % kAhead], qreg[i], sc[kb], 0, 0, 0);
                 }
                 if (n + kAhead < N) ring[n % kAhead] = operand(n + kAhead);
-                if (kInProducts && N0 == 0 && n >= 2 && n - 2 < D / 8) unpack_part(up, raw, raw_on, n - 2, buf_v, buf_k);
-                if (kInProducts && N0 == 0 && n == 2 + D / 8) load(next);
+                if (N0 == 0 && n >= 2 && n - 2 < D / 8) unpack_part(up, raw, raw_on, n - 2, buf_v, buf_k);
+                if (N0 == 0 && n == 2 + D / 8) load(next);
             }
             __builtin_amdgcn_sched_barrier(0);
         };
@@ -773,24 +778,20 @@ __global__ __launch_bounds__(512, 2) void ragged_wide_kernel(const RaggedArgs a,
             l += add[0] + add[1];
         };
         // Half-steps: the early waves are in the vector phase of tile i in half-step 2 i and in its matrix phase in 2 i + 1, the late ones one later.
-        // K(i + 2) and V(i + 1), needed from half-step 2 i + 3 on, take the places of K(i) and V(i - 1), last read in 2 i: a wave unpacks its share of
-        // them in 2 i + 1 or 2 i + 2, the one of its two phases that is the shorter: of heads of 64 the matrix phase, between the products, of heads
-        // of 128 the vector phase.
+        // K(i + 2) and V(i + 1), needed from half-step 2 i + 3 on, take the places of K(i) and V(i - 1), last read in 2 i: every wave unpacks its share of
+        // them in its matrix phase, 2 i + 1 or 2 i + 2, between the products, which leave the vector unit idle three quarters of the time.  (In the
+        // vector phase, with that phase at the higher priority: heads of 128 the same within 3 %, heads of 64 20 % slower.)
         phase_end();
         if (mine) products(std::false_type{}, 0, 0, 0);
         if (late) phase_end();
         for (int i = 0; i < cnt; ++i) {
-            if constexpr (!kInProducts) {
-                __builtin_amdgcn_s_setprio(1);                    // (the longer of the two phases)
-                const int u = late ? i + 1 : i;
-                if (u > 0) { unpack(raw, raw_on, (u + 1) & 1, u & 1); load(first + (is_v ? u + 1 : u + 2)); }
-            }
             if (mine) vector_phase(first + i);
-            if constexpr (!kInProducts) __builtin_amdgcn_s_setprio(0);
             phase_end();
             const int next = first + i + (is_v ? 2 : 3);
+            __builtin_amdgcn_s_setprio(1);                        // (the longer of the two phases)
             if (mine) products(std::true_type{}, i & 1, (i + 1) & 1, next);
-            else if (kInProducts) { unpack(raw, raw_on, i & 1, (i + 1) & 1); load(next); }
+            else { unpack(raw, raw_on, i & 1, (i + 1) & 1); load(next); }
+            __builtin_amdgcn_s_setprio(0);
             phase_end();
         }
         if (!late) phase_end();
@@ -904,25 +905,26 @@ __device__ void wide_empty(const RaggedArgs& a, int which, int n)
 // The last launch of a step: what the others left to be joined.
 constexpr int kEmptyWgs = 64;
 template <int D, int ROWS>
-__global__ __launch_bounds__(256) void ragged_merge_kernel(const RaggedArgs a, const FewWs few, const WideWs wide, int places)
+__global__ __launch_bounds__(256) void ragged_merge_kernel(const RaggedArgs a, const FewWs few, int tiles, const WideWs wide, int places)
 {
     int x = (int)blockIdx.x;
     if (x < 8 * places) { wide_merge<D>(a, wide, x / 8, x % 8); return; }
     x -= 8 * places;
-    if (x < a.B * a.Hkv) { few_merge<D, ROWS>(a, few, x); return; }
-    wide_empty<D>(a, x - a.B * a.Hkv, kEmptyWgs);
+    if (x < a.B * a.Hkv * tiles) { few_merge<D, ROWS>(a, few, x, tiles); return; }
+    wide_empty<D>(a, x - a.B * a.Hkv * tiles, kEmptyWgs);
 }
 
 inline size_t up256(size_t x) { return (x + 255) / 256 * 256; }
 
 // Which kernels a step may need: the host knows only how many rows a sequence has at most.
-struct RaggedPlan { int few_groups, few_wgs, wide_wgs /* 0: no sequence has that many rows */; };
+struct RaggedPlan { int few_groups, few_tiles, few_wgs, wide_wgs /* 0: no sequence has that many rows */; };
 inline RaggedPlan plan_of(int T, int B, int Hq, int Hkv, int max_q, int max_pages, int D, int cus)
 {
     const long long most = (long long)(max_q < T ? max_q : T) * (Hq / Hkv), rows = (long long)T * (Hq / Hkv);
     RaggedPlan p;
     p.few_groups = most <= 16 ? 1 : 2;
-    const long long units = (long long)B * Hkv * (max_pages + (D == 64 ? kFewStart<64> : kFewStart<128>)), wgs = (long long)cus * (p.few_groups == 1 ? 3 : 2);
+    p.few_tiles = (int)(((most < kFewRows ? most : kFewRows) + 16 * p.few_groups - 1) / (16 * p.few_groups));
+    const long long units = (long long)B * Hkv * p.few_tiles * (max_pages + (D == 64 ? kFewStart<64> : kFewStart<128>)), wgs = (long long)cus * (p.few_groups == 1 ? 3 : 2);
     p.few_wgs = (int)(units < wgs ? units : wgs);
     p.wide_wgs = 0;
     if (most > kFewRows) {
@@ -964,8 +966,8 @@ int launch_ragged_of(const RaggedArgs& a, const RaggedPlan& p, const RaggedWs& w
         hipLaunchKernelGGL((ragged_wide_kernel<D>), dim3(p.wide_wgs), dim3(512), bytes, st, a, w.wide);
         if (hipGetLastError() != hipSuccess) return -1;
     }
-    const int wgs = a.B * a.Hkv + (p.wide_wgs > 0 ? p.wide_wgs * 8 + kEmptyWgs : 0);
-    hipLaunchKernelGGL((ragged_merge_kernel<D, 16 * RT>), dim3(wgs), dim3(256), 0, st, a, w.few, w.wide, p.wide_wgs);
+    const int wgs = a.B * a.Hkv * p.few_tiles + (p.wide_wgs > 0 ? p.wide_wgs * 8 + kEmptyWgs : 0);
+    hipLaunchKernelGGL((ragged_merge_kernel<D, 16 * RT>), dim3(wgs), dim3(256), 0, st, a, w.few, p.few_tiles, w.wide, p.wide_wgs);
     return hipGetLastError() == hipSuccess ? 0 : -1;
 }
 
