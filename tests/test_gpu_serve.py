@@ -432,3 +432,94 @@ def test_plan_in_place_and_beside(aq, B, T, in_place):
     assert np.array_equal(t_dev.cpu().numpy(), t_ref) and np.array_equal(r_dev.cpu().numpy(), r_ref)
     if not in_place:
         assert np.array_equal(lens.cpu().numpy(), old) and np.array_equal(st.cpu().numpy()[:2], state)
+
+
+def test_many_sequences(aq):
+    """More sequences than a workgroup has threads, some of them with enough rows for the kernel of many, some empty."""
+    rng = np.random.default_rng(31)
+    for B in (300, 700):
+        kv = [int(x) for x in rng.integers(0, 260, B)]
+        n = [min(k, int(rng.choice([0, 1, 1, 1, 2]))) for k in kv]
+        for b in (3, B // 2, B - 1):
+            kv[b], n[b] = 200, 150
+        run_attention(aq, n, kv, 2, 1, 64, seed=B)
+
+
+@pytest.mark.parametrize("n,kv", [([1], [20000]), ([1, 5], [9000, 17001]), ([150], [17001]), ([60, 1], [8193, 16385])])
+@pytest.mark.parametrize("window", [0, 9000])
+def test_long_sequences(aq, n, kv, window):
+    """More pages than a wave has lanes."""
+    run_attention(aq, n, kv, 4, 1, 64, window=window, seed=kv[0])
+
+
+def test_offsets_beyond_32_bits(aq):
+    Hkv, d = 8, 128
+    page = aq.kv_cache_page_bytes_nvfp4(Hkv, d)
+    num = (5 << 30) // page
+    cache = torch.zeros(num * page, dtype=torch.uint8, device="cuda")
+    rng = np.random.default_rng(6)
+    kv, n = [200, 150], [1, 60]
+    table = np.array([[num - 1, 3], [num - 2, num - 3]], np.int32)
+    pos = [np.arange(k) for k in kv]
+    slots = np.concatenate([table[b, p // 128].astype(np.int64) * 128 + p % 128 for b, p in enumerate(pos)])
+    x = S.bf16(rng.standard_normal((2, sum(kv), Hkv, d)))
+    aq.attnqat_kv_cache_append(x[0].cuda(), x[1].cuda(), cache, dev(slots))
+    k, v = aq.attnqat_kv_cache_read(cache, dev(slots), Hkv, d)
+    want = [S.value(*S.phi(x[i].double().numpy())) for i in range(2)]
+    assert np.array_equal(k.double().cpu().numpy(), want[0]) and np.array_equal(v.double().cpu().numpy(), want[1])
+    q = S.bf16(rng.standard_normal((61, 16, d)))
+    o, lse = aq.attnqat_fwd_kv4_ragged(q.cuda(), i32([0, 1, 61]), cache, num, dev(table), i32(kv), Hkv, True)
+    used = sorted(set(table.reshape(-1)))
+    small = cache.view(num, -1)[torch.tensor(used, device="cuda")].cpu().numpy().reshape(len(used), Hkv, 2, -1)      # the reference: those pages alone
+    table_s = np.array([[used.index(t) for t in row] for row in table], np.int32)
+    check_attention(o, lse, S.attend(q.double().numpy(), [0, 1, 61], small, table_s, kv, Hkv, True, 0, d ** -0.5))
+
+
+def test_nothing_to_do_leaves_the_outputs(aq):
+    q, cu, cache, num_pages, table = attention_case([3, 2], [30, 20], 4, 2, 64, 1, tail=0)
+    o, lse = torch.full((5, 4, 64), 5.0, dtype=torch.bfloat16, device="cuda"), torch.full((5, 4), 5.0, device="cuda")
+    aq.attnqat_fwd_kv4_ragged(q.cuda(), i32([0, 0, 0]), dev(cache.reshape(-1)), num_pages, dev(table), i32([30, 20]), 2, True, out=(o, lse))
+    assert bool((o == 5.0).all()) and bool((lse == 5.0).all())
+
+
+def test_offsets_out_of_order_stay_inside(aq):
+    """cu_q that does not rise or leaves [0, T], lengths beyond the table: clamped, nothing outside the tensors is touched."""
+    q, cu, cache, num_pages, table = attention_case([3, 2, 4], [30, 20, 128], 4, 2, 64, 1, tail=0)
+    for c, lens in (([-5, 4, 2, 400], [30, 20, 128]), ([0, 3, 5, 9], [-7, 1 << 30, 1 << 20])):
+        o = torch.full((11, 4, 64), 5.0, dtype=torch.bfloat16, device="cuda")
+        aq.attnqat_fwd_kv4_ragged(q.cuda(), i32(c), dev(cache.reshape(-1)), num_pages, dev(np.clip(table, 0, num_pages - 1)), i32(lens), 2, True, out=(o[1:10], None))
+        torch.cuda.synchronize()
+        assert bool((o[0] == 5.0).all()) and bool((o[10] == 5.0).all())
+
+
+@pytest.mark.parametrize("n,kv,window", [([1, 1, 4], [3000, 40, 900], 0), ([300, 1, 20], [700, 500, 60], 0), ([300, 1, 20], [700, 500, 60], 64)])
+def test_same_bits_again_on_another_stream_and_in_a_graph(aq, n, kv, window):
+    q, cu, cache, num_pages, table = attention_case(n, kv, 8, 2, 128, 5, tail=0)
+    args = (q.cuda(), i32(cu), dev(cache.reshape(-1)), num_pages, dev(table), i32(kv), 2, True)
+    ws = torch.empty(aq.kv4_ragged_workspace_bytes(q.shape[0], len(n), 8, 2, max(n), table.shape[1], 128), dtype=torch.uint8, device="cuda")
+    o, lse = aq.attnqat_fwd_kv4_ragged(*args, max_q=max(n), window=window)
+    ws.random_(0, 256)                                           # (what lies in the workspace does not matter)
+    out = tuple(torch.empty_like(t) for t in (o, lse))
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        aq.attnqat_fwd_kv4_ragged(*args, max_q=max(n), window=window, workspace=ws, out=out)
+    side.synchronize()
+    assert torch.equal(out[0], o) and torch.equal(out[1], lse)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        aq.attnqat_fwd_kv4_ragged(*args, max_q=max(n), window=window, workspace=ws, out=out)
+    for _ in range(3):
+        out[0].zero_(), out[1].zero_(), ws.random_(0, 256)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out[0], o) and torch.equal(out[1], lse)
+
+
+def test_one_row_of_a_batch_does_not_depend_on_padding_rows(aq):
+    """A step captured for more rows than it has: same results as without the rows behind."""
+    q, cu, cache, num_pages, table = attention_case([1, 2], [300, 200], 4, 2, 128, 5, tail=30)
+    args = (i32(cu), dev(cache.reshape(-1)), num_pages, dev(table), i32([300, 200]), 2, True)
+    o, lse = aq.attnqat_fwd_kv4_ragged(q.cuda(), *args, max_q=2)
+    o3, lse3 = aq.attnqat_fwd_kv4_ragged(q[:3].cuda(), *args, max_q=2)
+    assert torch.equal(o[:3], o3) and torch.equal(lse[:3], lse3)
