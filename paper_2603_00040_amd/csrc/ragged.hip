@@ -123,10 +123,10 @@ template <int D, int RT /* 16-row groups of a unit */>
 __global__ __launch_bounds__(256, RT == 1 ? 3 : 2) void ragged_few_kernel(const RaggedArgs a, const FewWs ws)
 {
     constexpr int NS = D / 32, NDT = D / 16, ROWS = 16 * RT;
-    constexpr int SETS = D == 64 ? 4 : RT == 1 ? 2 : 3;           // pages in registers, the present one included (heads of 64: half the bytes each)
+    constexpr int SETS = D == 64 ? 3 : 2;           // pages in registers, the present one included (heads of 64: half the bytes each)
     constexpr int RS = 2 * D + 32;                                // bytes per key of the V tile (eight keys side by side in other banks)
     constexpr size_t VOFF = (size_t)128 * (D / 2 + D / 16);
-    __shared__ __align__(16) unsigned char stage[4 * 32 * RS];     // per wave: V of 32 keys [key][d]; at the end the waves' sums [4][16][D]
+    __shared__ __align__(16) unsigned char stage[4 * 32 * RS];     // per wave: V of 32 keys [key][d]; at the end the waves' sums [4][16][D + 4]
     __shared__ float ml[2][4][ROWS];
     __shared__ int red[4], found[5];
 
@@ -184,7 +184,6 @@ __global__ __launch_bounds__(256, RT == 1 ? 3 : 2) void ragged_few_kernel(const 
         const int h = ht / u.tiles, r0 = ht % u.tiles * ROWS, rows = min(u.rows - r0, ROWS);
         w += units;
         if (cnt <= 0) break;                                      // (the start alone: w is at this workgroup's end)
-        const int groups = RT == 1 ? 1 : (rows + 15) / 16;        // of 16 rows
         const int first = u.first_page + at;
         const int* ids = a.table + (size_t)b * a.max_pages + first;
 
@@ -256,20 +255,21 @@ __global__ __launch_bounds__(256, RT == 1 ? 3 : 2) void ragged_few_kernel(const 
 #pragma unroll
             for (int dt = 0; dt < NDT; ++dt) o[rt][dt] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
         }
-        auto step = [&](const Tile& t, int i) __attribute__((always_inline)) {
+        auto step = [&](auto groups, const Tile& t, int i) __attribute__((always_inline)) {
+            constexpr int N = decltype(groups)::value;            // groups of 16 rows that there are
             const int kt = (first + i) * 128 + 32 * wave;
             const bool masked = kt < see_first || kt + 31 > see_last;
-            floatx4 sc[RT][2];
+            floatx4 sc[N][2];
 #pragma unroll
             for (int blk = 0; blk < 2; ++blk) {
                 const half2v ks = scales_of<D>(t.k[blk], g, t.live);
 #pragma unroll
-                for (int rt = 0; rt < RT; ++rt) sc[rt][blk] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
+                for (int rt = 0; rt < N; ++rt) sc[rt][blk] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
                 for (int j = 0; j < NS; ++j) {
                     const half8 kv = values8<D>(t.k[blk], ks, j);
 #pragma unroll
-                    for (int rt = 0; rt < RT; ++rt) if (rt < groups) sc[rt][blk] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kv, qreg[rt][j], sc[rt][blk], 0, 0, 0);
+                    for (int rt = 0; rt < N; ++rt) sc[rt][blk] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kv, qreg[rt][j], sc[rt][blk], 0, 0, 0);
                 }
             }
             // V through LDS: written key by key, read back with four keys of one d in a lane
@@ -281,10 +281,9 @@ __global__ __launch_bounds__(256, RT == 1 ? 3 : 2) void ragged_few_kernel(const 
                 for (int j = 0; j < NS; ++j) *reinterpret_cast<half8*>(stg + (16 * blk + cc) * RS + (D / 2) * g + 16 * (j ^ ((cc >> 2) & 1))) = values8<D>(t.v[blk], vs, j);
             }
             __builtin_amdgcn_wave_barrier();
-            half8 pt[RT];
+            half8 pt[N];
 #pragma unroll
-            for (int rt = 0; rt < RT; ++rt) {
-                if (rt >= groups) break;
+            for (int rt = 0; rt < N; ++rt) {
                 if (masked) {
 #pragma unroll
                     for (int j = 0; j < 8; ++j) {
@@ -317,21 +316,28 @@ __global__ __launch_bounds__(256, RT == 1 ? 3 : 2) void ragged_few_kernel(const 
                 const uint2v x = lds_read_tr16_at(tr_base + 32 * dt), y = lds_read_tr16_at(tr_base + 32 * dt + 16 * RS);
                 const uint4v av = {x[0], x[1], y[0], y[1]};
 #pragma unroll
-                for (int rt = 0; rt < RT; ++rt) if (rt < groups) o[rt][dt] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(half8, av), pt[rt], o[rt][dt], 0, 0, 0);
+                for (int rt = 0; rt < N; ++rt) o[rt][dt] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(half8, av), pt[rt], o[rt][dt], 0, 0, 0);
             }
         };
-        for (int i = 0; i < cnt; i += SETS) {
+        // (a loop for either number of groups: asked at every product, the products stand alone between branches)
+        auto walk = [&](auto groups) __attribute__((always_inline)) {
+            for (int i = 0; i < cnt; i += SETS) {
 #pragma unroll
-            for (int x = 0; x < SETS; ++x) {
-                if (x > 0 && i + x >= cnt) break;
-                load(t[(x + SETS - 1) % SETS], min(i + x + SETS - 1, cnt - 1));
-                step(t[x], i + x);
+                for (int x = 0; x < SETS; ++x) {
+                    if (x > 0 && i + x >= cnt) break;
+                    load(t[(x + SETS - 1) % SETS], min(i + x + SETS - 1, cnt - 1));
+                    step(groups, t[x], i + x);
+                }
             }
-        }
+        };
+        if (RT == 1 || rows <= 16) walk(std::integral_constant<int, 1>{});
+        else walk(std::integral_constant<int, RT>{});
 
         // the four waves' sums, in units of their common maximum
         const bool whole = cnt == u.pages;
         const size_t slot = (size_t)blockIdx.x * 2 + (at == 0 ? 1 : 0);
+        constexpr int SS = D + 4;                                 // floats per row of the sums (16 rows are written side by side)
+        static_assert(4 * 16 * SS * 4 <= 4 * 32 * RS);
         float* sums = reinterpret_cast<float*>(stage);
 #pragma unroll
         for (int rt = 0; rt < RT; ++rt) {
@@ -345,7 +351,7 @@ __global__ __launch_bounds__(256, RT == 1 ? 3 : 2) void ragged_few_kernel(const 
             const int r = 16 * rt + cc;
             const float top = fmaxf(fmaxf(ml[0][0][r], ml[0][1][r]), fmaxf(ml[0][2][r], ml[0][3][r])), f = __builtin_amdgcn_exp2f(m[rt] - (top == -INFINITY ? 0.0f : top));
 #pragma unroll
-            for (int dt = 0; dt < NDT; ++dt) *reinterpret_cast<floatx4*>(sums + (wave * 16 + cc) * D + 16 * dt + 4 * g) = o[rt][dt] * f;
+            for (int dt = 0; dt < NDT; ++dt) *reinterpret_cast<floatx4*>(sums + (wave * 16 + cc) * SS + 16 * dt + 4 * g) = o[rt][dt] * f;
             __syncthreads();
             for (int e = tid; e < min(16, rows - 16 * rt) * (D / 4); e += 256) {
                 const int q = e / (D / 4), d = e % (D / 4) * 4, rr = 16 * rt + q;
@@ -355,7 +361,7 @@ __global__ __launch_bounds__(256, RT == 1 ? 3 : 2) void ragged_few_kernel(const 
 #pragma unroll
                 for (int x = 0; x < 4; ++x) {
                     lt += ml[1][x][rr] * __builtin_amdgcn_exp2f(ml[0][x][rr] - at);
-                    v += *reinterpret_cast<const floatx4*>(sums + (x * 16 + q) * D + d);
+                    v += *reinterpret_cast<const floatx4*>(sums + (x * 16 + q) * SS + d);
                 }
                 if (whole) {
                     const int tk = (r0 + rr) / G, hd = h * G + (r0 + rr) % G;
