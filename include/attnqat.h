@@ -410,7 +410,8 @@ int attnqat_debug_fwd_infer_paged(const void* q, int B, int Hq, int Hkv, int Lq,
  * all steps of its sizes.  The new positions of a step are one run of T rows, sequence after sequence; sequence b has rows cu_q[b] .. cu_q[b+1]-1.
  * A slot is page * 128 + position within the page.  Rows come as [T, heads, d] bf16 with d innermost and any stride per row and per head (in
  * elements, multiples of 8; pointers 16-byte aligned), such as the views of one projection's output; T = 0 is accepted and does nothing (the plan: no
- * slots).  At most 65535 sequences of 8192 pages (2^20 positions) each: ATTNQAT_ESHAPE beyond.
+ * slots).  At most 65535 sequences of 8192 pages (2^20 positions) each and 2^29 rows: ATTNQAT_ESHAPE beyond.  What a call reads on the device must
+ * not change before its work there is done, and calls that may run at once take workspaces of their own.
  *
  * attnqat_page_plan makes page table, slots and positions of a step.  Request b has kv_lens[b] positions and wants new_lens[b] (device int32 [B]):
  * more (the step's new positions), as many, or fewer (drafted tokens taken back, 0: a request that has ended).  Pages that it needs come out of
@@ -435,16 +436,16 @@ int attnqat_debug_fwd_infer_paged(const void* q, int B, int Hq, int Hkv, int Lq,
  * outside [0, num_pages * 128) is left out.  Slots must differ from each other: of two rows with one slot either may be found there, block by block.
  *
  * attnqat_kv_cache_read is the way back: row t of k and v becomes the values (exact in bf16) that slot slots[t] holds, zeros for a slot outside
- * the cache.  (Both: at most 2^30 rows of heads, T Hkv.)
+ * the cache.  k and v must not lie over each other.  (Both: at most 2^29 rows of heads, T Hkv.)
  *
  * attnqat_fwd_kv4_ragged: O = softmax(scale Q K^T + mask) V, K and V being the values that the pages hold: only the cache is in 4 bits.  Q is not
  * quantized, nor are the probabilities (which are rounded to fp16 for their product with V; scores, sums and O are fp32), as for a
  * model that was not trained for Alg. 1; attnqat_fwd_infer_paged is Alg. 1.  q [T,Hq,d]; sequence b has kv_lens[b] keys, the last of which belong to
  * its rows: row i of n sees keys 0 .. kv_lens[b] - n + i with causal != 0, of those the last `window` if window > 0 (causal only), and all keys with
- * causal = 0.  max_q: no sequence has more rows (rows beyond are left out).  A row without a key gets o = 0, lse = -inf.  o [T,Hq,d] bf16; lse
+ * causal = 0.  max_q: no sequence has more rows (of one that has, the first max_q are computed as if there were no others).  A row without a key gets o = 0, lse = -inf.  o [T,Hq,d] bf16; lse
  * [T,Hq] fp32 (natural log), may be NULL; rows behind cu_q[B] are left as they are.  o and lse must not lie over q.  scale > 0.
  * Positions of a page table entry outside [0, num_pages) read as zeros; positions from kv_lens[b] on are never used, whatever their slots
- * hold.  At most 2^28 rows of heads (T Hq) and 2^24 (sequence, kv head)s.  Workspace: attnqat_kv4_ragged_workspace_bytes(), 16-byte aligned.
+ * hold.  At most 2^28 rows of heads (T Hq) and 2^22 (sequence, kv head)s.  Workspace: attnqat_kv4_ragged_workspace_bytes(), 16-byte aligned.
  */
 size_t attnqat_page_plan_workspace_bytes(int B);
 int attnqat_page_plan(const int* kv_lens, const int* new_lens, int B, int* page_table, int max_pages,

@@ -583,6 +583,7 @@ bool rows_of(const void* p, int64_t token, int64_t head, int T, int heads, int d
 }
 size_t rows_extent(const Rows& r, int T, int heads, int d) { return 2 * ((size_t)(T - 1) * r.token + (size_t)(heads - 1) * r.head + d); }
 constexpr int kMaxServeBatch = 65535, kMaxServePages = 1 << 13;      // sequences of a step, pages of a sequence
+constexpr int kMaxServeRows = 1 << 29;                               // (with the threads that a row takes, less than the 2^32 of a launch)
 }  // namespace
 
 size_t attnqat_page_plan_workspace_bytes(int B) { return B < 1 || B > kMaxServeBatch ? 0 : align_up(page_plan_ws_bytes(B)); }
@@ -596,12 +597,13 @@ int attnqat_page_plan(const int* kv_lens, const int* new_lens, int B, int* page_
     if (T > 0 && (!slots || !positions)) return ATTNQAT_EINVAL;
     if (free_pages ? !free_state || !free_state_out || num_free_slots < 1 : num_free_slots != 0) return ATTNQAT_EINVAL;
     if ((uintptr_t)slots & 7) return ATTNQAT_EINVAL;
-    if (B > kMaxServeBatch || max_pages > kMaxServePages) return ATTNQAT_ESHAPE;
-    // kv_lens_out may be kv_lens and free_state_out free_state; what else is written lies over nothing that is read
+    if (B > kMaxServeBatch || max_pages > kMaxServePages || T > kMaxServeRows) return ATTNQAT_ESHAPE;
+    // kv_lens_out may be kv_lens and free_state_out free_state; what else is written lies over nothing else
     const size_t nb = (size_t)B * 4;
     struct Range { const void* p; size_t n; };
     const Range in[5] = {{kv_lens, nb}, {new_lens, nb}, {free_state, free_pages ? 8u : 0u}, {page_table, nb * max_pages}, {free_pages, (size_t)num_free_slots * 4}};
     const Range out[5] = {{kv_lens_out, nb}, {free_state_out, free_pages ? 12u : 0u}, {cu_q, nb + 4}, {slots, (size_t)T * 8}, {positions, (size_t)T * 4}};
+    if (free_pages && overlap(in[3].p, in[3].n, in[4].p, in[4].n)) return ATTNQAT_EINVAL;
     bool in_place = false;
     for (int o = 0; o < 5; ++o) {
         for (int i = 0; i < 5; ++i)
@@ -627,7 +629,7 @@ int rows_common(const void* k, int64_t k_token, int64_t k_head, const void* v, i
 {
     if (T < 0 || Hkv < 1 || num_pages < 1) return ATTNQAT_EINVAL;
     if (dtype != ATTNQAT_BF16) return ATTNQAT_EDTYPE;
-    if ((d != 64 && d != 128) || (long long)T * Hkv > (1 << 30)) return ATTNQAT_ESHAPE;
+    if ((d != 64 && d != 128) || (long long)T * Hkv > kMaxServeRows) return ATTNQAT_ESHAPE;
     if (T == 0) return ATTNQAT_OK;
     if (!k || !v || !cache || !slots || ((uintptr_t)cache & 15) || ((uintptr_t)slots & 7)) return ATTNQAT_EINVAL;
     if (!rows_of(k, k_token, k_head, T, Hkv, d, written, kr) || !rows_of(v, v_token, v_head, T, Hkv, d, written, vr)) return ATTNQAT_EINVAL;
@@ -666,7 +668,7 @@ int ragged_dims(int T, int B, int Hq, int Hkv, int max_q, int max_pages, int d)
 {
     if (T < 0 || B < 1 || Hq < 1 || Hkv < 1 || max_q < 1 || max_pages < 1) return ATTNQAT_EINVAL;
     if ((d != 64 && d != 128) || Hq % Hkv != 0 || Hkv > 65535 || B > kMaxServeBatch || max_pages > kMaxServePages) return ATTNQAT_ESHAPE;
-    if ((long long)T * Hq > (1 << 28) || (long long)B * Hkv > (1 << 24)) return ATTNQAT_ESHAPE;
+    if ((long long)T * Hq > (1 << 28) || (long long)B * Hkv > (1 << 22)) return ATTNQAT_ESHAPE;
     return ATTNQAT_OK;
 }
 }  // namespace

@@ -8,7 +8,7 @@
 //
 // Numbers: a cached value has at most 6 significant bits and lies in [2^-10, 2688], exact in fp16.  A row of Q, bf16, is multiplied by the power of
 // two that brings its largest element to [2^14, 2^15) and is exact in fp16 but for elements 2^-28 of the largest and less, which lose
-// what lies below 2^-39 of the largest.  Scores, maxima, sums and O are fp32.  P is rounded to fp16 (11 bits, P <= 1) for the product with V: a
+// what lies below 2^-39 of the largest.  Scores, maxima, sums and O are fp32.  P is rounded to fp16 (11 bits, P <= 2^8, see kSlack) for the product with V: a
 // relative 2^-12 per probability, an eighth of what rounding the output to bf16 costs; the sum that divides O is of the unrounded ones.
 #include "common.hpp"
 #include "kernels.hpp"
@@ -103,7 +103,9 @@ __device__ inline half8 values8(const Raw<D>& r, half2v sc, int s)
     return __builtin_bit_cast(half8, v);
 }
 
-// The power of two that brings a row's largest magnitude to [2^14, 2^15), and its inverse (magnitudes below 2^-112 count as that).
+// The power of two that brings a row's largest magnitude to [2^14, 2^15), and its inverse (magnitudes below 2^-112 count as that).  The factor of the
+// scores times the inverse is kept a normal number: where it would be less, scores differ by less than 2^-90, but a masked one times 0 would be a NaN.
+constexpr float kLeastFactor = 0x1p-126f;
 __device__ inline void row_factor(float amax, float& f, float& inv)
 {
     const uint32_t e = max(__float_as_uint(amax) >> 23, 15u);
@@ -242,7 +244,7 @@ __global__ __launch_bounds__(256, RT == 1 ? 3 : 2) void ragged_few_kernel(const 
                     qreg[rt][i][2 * j]     = (half_t)(__uint_as_float(x[rt][i][j] << 16) * f);
                     qreg[rt][i][2 * j + 1] = (half_t)(__uint_as_float(x[rt][i][j] & 0xFFFF0000u) * f);
                 }
-            c_row[rt] = a.c * inv;
+            c_row[rt] = fmaxf(a.c * inv, kLeastFactor);
         }
         // keys that every row sees: a page inside [see_first, see_last] needs no mask
         const int see_first = a.window > 0 ? s.len - s.n + (r0 + rows - 1) / G - a.window + 1 : 0, see_last = a.causal ? min(s.len - s.n + r0 / G, s.len - 1) : s.len - 1;
@@ -692,7 +694,7 @@ __global__ __launch_bounds__(512, 2) void ragged_wide_kernel(const RaggedArgs a,
                     qreg[i][2 * j]     = (half_t)(__uint_as_float(x[i][j] << 16) * f);
                     qreg[i][2 * j + 1] = (half_t)(__uint_as_float(x[i][j] & 0xFFFF0000u) * f);
                 }
-            c_row = a.c * inv;
+            c_row = fmaxf(a.c * inv, kLeastFactor);
         }
         __syncthreads();                                          // (the segment before has read its tiles)
         unpack(raw0, on0, 0, 0);

@@ -291,6 +291,16 @@ def test_queries_far_from_one(aq, q_scale):
     run_attention(aq, [1, 20], [200, 300], 4, 2, 128, scale=1e-31 if q_scale > 1 else None, seed=3, q_scale=q_scale)
 
 
+@pytest.mark.parametrize("scale", [1e-44, 1e-20, None])
+@pytest.mark.parametrize("causal", [True, False])
+def test_queries_of_zeros_and_least_factors(aq, scale, causal):
+    """Even probabilities over the keys that a row sees: the factor of the scores may lie below the least number, masked keys stay masked."""
+    for n, kv in (([1, 20], [200, 300]), ([70, 90], [200, 90])):
+        for q_scale in (0.0, 1e-3):
+            run_attention(aq, n, kv, 4, 2, 128, causal, scale=scale, seed=3, q_scale=q_scale)
+            run_attention(aq, n, kv, 4, 2, 64, causal, scale=scale, seed=3, q_scale=q_scale)
+
+
 def test_nan_stays_in_its_row(aq):
     for n, G in (([1, 3], 4), ([60, 40], 2)):
         q, cu, cache, num_pages, table = attention_case(n, [300, 200], 2 * G, 2, 128, 1, tail=0)

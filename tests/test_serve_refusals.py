@@ -78,3 +78,13 @@ def test_size_queries():
     assert aq.kv4_ragged_workspace_bytes(0, 1, 8, 2, 1, 1, 128) > 0
     for bad in ((-1, 1, 8, 2, 1, 1, 128), (4, 0, 8, 2, 1, 1, 128), (4, 1, 8, 3, 1, 1, 128), (4, 1, 8, 2, 0, 1, 128), (4, 1, 8, 2, 1, 9000, 128), (4, 1, 8, 2, 1, 1, 80)):
         assert aq.kv4_ragged_workspace_bytes(*bad) == 0
+
+
+def test_more_than_a_launch_holds():
+    assert _plan(T=(1 << 29) + 1) == aq.ESHAPE
+    assert _append(T=(1 << 26) + 1) == (aq.ESHAPE, aq.ESHAPE)
+    assert _attend(B=65535, Hq=128, Hkv=128) == aq.ESHAPE and aq.kv4_ragged_workspace_bytes(4, 65535, 128, 128, 1, 1, 128) == 0
+
+
+def test_plan_refuses_a_ring_that_lies_over_the_table():
+    assert _plan(ring=3 * P + 64) == aq.EINVAL
