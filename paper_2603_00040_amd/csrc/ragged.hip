@@ -606,35 +606,39 @@ __global__ __launch_bounds__(512, 2) void ragged_wide_kernel(const RaggedArgs a,
         const int first = t0 + at, last = first + cnt - 1;
         const int* ids = a.table + (size_t)b * a.max_pages;
         const unsigned char* part0 = a.cache + (size_t)h * (2 * VOFF) + (is_v ? VOFF : 0);      // of page 0
-        const size_t page_bytes = (size_t)a.Hkv * (2 * VOFF);
+        const uint32_t page_bytes = (uint32_t)a.Hkv * (uint32_t)(2 * VOFF);      // (at most 65535 heads of 18 KiB)
         const uint32_t code_at = (uint32_t)(key * (D / 2) + (D / 8) * g), scale_at = (uint32_t)(128 * (D / 2) + key * (D / 16) + (D == 128 ? 4 * (g >> 1) : 0));
+        if (b != id_b) { id_b = b; id_first = 1 << 30; }          // (none of them)
         Raw<D> raw;
         bool raw_on = false;
-        auto page_at = [&](int t) __attribute__((always_inline)) {
+        // Where tile t lies, and how many positions of its page and sequence there are from its first on (none: a page outside the cache)
+        struct Place { const unsigned char* page; uint32_t odd; int have; };
+        auto place_of = [&](int t) __attribute__((always_inline)) {
+            t = min(t, last);
             const int p = t >> 1;
-            if (b != id_b || p < id_first || p >= id_first + 64) {      // 64 page ids at a time, waited for here and not at every use
-                id_b = b; id_first = p;
+            if ((uint32_t)(p - id_first) >= 64u) {                // 64 page ids at a time, waited for here and not at every use
+                id_first = p;
                 id_lane = ids[min(p + lane, a.max_pages - 1)];
                 id_lane = id_lane >= 0 && id_lane < a.num_pages ? id_lane : -1;
                 asm volatile("" : "+v"(id_lane));
             }
-            return __builtin_amdgcn_readlane(id_lane, p - id_first);
+            const int page = __builtin_amdgcn_readlane(id_lane, p - id_first);
+            return Place{part0 + (uint64_t)(uint32_t)max(page, 0) * page_bytes, (uint32_t)(t & 1), page >= 0 ? s.len - t * 64 : 0};
         };
-        auto load_to = [&](Raw<D>& r, bool& on, int t) __attribute__((always_inline)) {
-            t = min(t, last);
-            const int page = page_at(t);
-            on = t * 64 + key < (page >= 0 ? s.len : 0);          // (keys behind the end: zeros, whatever the slots hold)
-            const unsigned char* part = part0 + (size_t)(uint32_t)max(page, 0) * page_bytes + (t & 1) * 64 * (D / 2);
-            const unsigned char* part_s = part - (t & 1) * (64 * (D / 2) - 64 * (D / 16));
+        auto load_at = [&](Raw<D>& r, bool& on, const Place& pl) __attribute__((always_inline)) {
+            on = key < pl.have;                                   // (keys behind the end: zeros, whatever the slots hold)
+            const unsigned char* codes = pl.page + (code_at + pl.odd * (uint32_t)(64 * (D / 2)));
+            const unsigned char* scales = pl.page + (scale_at + pl.odd * (uint32_t)(64 * (D / 16)));
             if constexpr (D == 128) {
-                const uint4v c = *reinterpret_cast<const uint4v*>(part + code_at);
+                const uint4v c = *reinterpret_cast<const uint4v*>(codes);
                 r.w[0] = c[0]; r.w[1] = c[1]; r.w[2] = c[2]; r.w[3] = c[3];
             } else {
-                const uint2v c = *reinterpret_cast<const uint2v*>(part + code_at);
+                const uint2v c = *reinterpret_cast<const uint2v*>(codes);
                 r.w[0] = c[0]; r.w[1] = c[1];
             }
-            r.sc = *reinterpret_cast<const uint32_t*>(part_s + scale_at);
+            r.sc = *reinterpret_cast<const uint32_t*>(scales);
         };
+        auto load_to = [&](Raw<D>& r, bool& on, int t) __attribute__((always_inline)) { load_at(r, on, place_of(t)); };
         auto load = [&](int t) __attribute__((always_inline)) { load_to(raw, raw_on, t); };
         // K: the 16 bytes of d = 16 i + 8 hf .. of a key in place 32 hf + key % 32 of operand (key / 32, i).  V: key after key.  A store serves eight lanes at
         // a time, the four pieces j of two keys, on 32 banks: the places of K's operands are turned by the piece, the 16-byte pieces of V's
@@ -708,7 +712,9 @@ __global__ __launch_bounds__(512, 2) void ragged_wide_kernel(const RaggedArgs a,
             for (int j = 0; j < 16; ++j) o[i][j] = 0.0f;
 
         // The products of a matrix phase in one run, each operand requested kAhead products before its own: a wave issues in order, and the trip to LDS
-        // is as long as four products.  First (t >= 0) O += V P of a tile, group of 16 keys by group, then S of the next.
+        // is as long as four products.  First O += V P of a tile, group of 16 keys by group, then S of the next.  The unpacking begins behind
+        // kUnpackAt products, a few instructions to each, so that what it waits for from memory has had its time (from product 2 on 1 % slower).
+        constexpr int kUnpackAt = D == 128 ? 8 : 4;
         constexpr int kAhead = 6, NV = 4 * NB, NK = 2 * ND;
         uint32_t k_base[4];
 #pragma unroll
@@ -721,6 +727,7 @@ __global__ __launch_bounds__(512, 2) void ragged_wide_kernel(const RaggedArgs a,
             for (int x = 0; x < 4; ++x) kb4[x] = k_base[x] + (uint32_t)(buf_k * KB);
             half8 ring[kAhead];
             Unpack up;
+            Place next_at;
             auto operand = [&](int n) __attribute__((always_inline)) {
                 if (n < NV) {
                     const uint32_t at = vb[(n % NB) >> 1] + (uint32_t)((n / NB) * 16 * RS + 64 * (n % NB));
@@ -745,8 +752,9 @@ __global__ __launch_bounds__(512, 2) void ragged_wide_kernel(const RaggedArgs a,
                     sc[kb] = __builtin_amdgcn_mfma_f32_32x32x16_f16(ring[n % kAhead], qreg[i], sc[kb], 0, 0, 0);
                 }
                 if (n + kAhead < N) ring[n % kAhead] = operand(n + kAhead);
-                if (N0 == 0 && n >= 2 && n - 2 < D / 8) unpack_part(up, raw, raw_on, n - 2, buf_v, buf_k);
-                if (N0 == 0 && n == 2 + D / 8) load(next);
+                if (N0 == 0 && n >= kUnpackAt && n - kUnpackAt < D / 8) unpack_part(up, raw, raw_on, n - kUnpackAt, buf_v, buf_k);
+                if (N0 == 0 && n == 4) next_at = place_of(next);
+                if (N0 == 0 && n == kUnpackAt + D / 8) load_at(raw, raw_on, next_at);
             }
             __builtin_amdgcn_sched_barrier(0);
         };
