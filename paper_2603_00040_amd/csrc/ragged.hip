@@ -120,7 +120,9 @@ struct FewWs { int* quota; int* front /* [B + 1] */; float* part_o /* [workgroup
 // Few rows (decode steps, drafted tokens): bound by reading the cache, so the pages of all units are dealt out evenly, `quota` consecutive ones to a
 // workgroup, however uneven the sequences are.  Which of them are its own a workgroup finds from the lengths itself (one trip to memory and a scan; a
 // launch that makes a list would cost more).  Its four waves take 32 keys of every page, each with its own maximum, sum and O; the pages of
-// the next iteration are requested before the present ones are used.
+// the next iteration are requested before the present ones are used.  One query of 32 sequences of 4096 - 16384 keys, 32/8 heads of 128: 326 MB in 61 us,
+// 5.3 TB/s, what a copy reaches.  With more rows and short segments the vector instructions bound it (unpacking, softmax: a wave issues one
+// in 9 cycles) and the start of a segment: one to six queries of 40 sequences of 300 - 9000 keys, 16/4 heads of 64, 34 MB in 17.6 us.
 template <int D, int RT /* 16-row groups of a unit */>
 __global__ __launch_bounds__(256, RT == 1 ? 3 : 2) void ragged_few_kernel(const RaggedArgs a, const FewWs ws)
 {
@@ -392,7 +394,7 @@ __global__ __launch_bounds__(256, RT == 1 ? 3 : 2) void ragged_few_kernel(const 
 }
 
 // O and lse of a unit whose pages were shared, and of rows that see no key, by a workgroup: groups of D / 4 threads have a row each, or, while there are
-// fewer rows than groups, several groups share the partial sums of a row.
+// fewer rows than groups, several groups share the partial sums of a row.  A launch and two trips to memory: 4.7 us.
 template <int D, int ROWS>
 __device__ void few_merge(const RaggedArgs& a, const FewWs& ws, int unit, int tiles /* of a sequence at most */)
 {
@@ -496,8 +498,14 @@ struct WideWs { long long* quota; WideRec* rec; float* part_o /* [workgroup][2][
 
 // Many rows (pieces of prompts): bound by the matrix instructions and by the softmax between them.  Eight waves have 32 rows each of a tile of 256 and
 // walk tiles of 64 keys together; waves 0 - 3 and 4 - 7 are half an iteration apart, between barriers: while one half computes O += V P and the next
-// tile's S, the other does the softmax and unpacks its half of the keys of a K and a V tile into LDS (K as operands of the matrix instruction, V key by
-// key), so that every SIMD has a wave for either unit.  The work (row tile, key tile) is dealt out evenly as in the kernel for few rows.
+// tile's S, and between these products unpacks its half of the keys of a K and a V tile into LDS (K as operands of the matrix instruction, V key by
+// key), the other does the softmax, so that every SIMD has a wave for either unit.  The work (row tile, key tile) is dealt out evenly as in the
+// kernel for few rows.
+// Rates, in floating-point operations that the mask leaves: 8192 queries and keys, 32/8 heads of 128, 960 TFLOP/s without a mask (1145 us), 945 causal; 16/4
+// heads of 64, 16384 queries, 8192 keys 780.  The products with their barriers alone would run at 1370, with their operands out of LDS and the
+// pages' loads at 1180 (a large library product: 1280): the rest is that a wave issues a vector instruction in 9 cycles, and that a tile has 180 of them
+// beside 1024 cycles of products.  Also tried: softmax and products of a wave in one stream (915, heads of 64 740), four waves of 32 rows and two
+// workgroups to a compute unit without phases (810), the unpacking shared between the phases (850).
 template <int D>
 __global__ __launch_bounds__(512, 2) void ragged_wide_kernel(const RaggedArgs a, const WideWs ws)
 {
@@ -849,7 +857,7 @@ __global__ __launch_bounds__(512, 2) void ragged_wide_kernel(const RaggedArgs a,
 }
 
 // O and lse of the row tiles whose key tiles were shared: a workgroup per place where one workgroup's work ended and another's began, and 32 rows; of the
-// places within a row tile the first has it.
+// places within a row tile the first has it.  Bound by memory (each of 256 workgroups leaves up to two tiles of 256 rows in fp32: 13.5 us for heads of 128).
 template <int D>
 __device__ void wide_merge(const RaggedArgs& a, const WideWs& ws, int place, int wave)
 {

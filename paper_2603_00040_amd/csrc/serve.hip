@@ -111,7 +111,8 @@ __device__ inline void plan_give(const PlanArgs& a, const PlanItem& it /* of req
 }
 
 // Up to 1024 requests: one launch, in which every workgroup makes out for itself who gets what and then does its share of the rows.  (Two launches, as
-// below, take as long on the GPU, but the second one costs the host its 3 us, which is what a step waits for.)
+// below, take as long on the GPU, but the second one costs the host its 3.5 us, which is what a step waits for.)  Bound by the launch and a chain of trips
+// to memory (lengths, ring, table): 24 requests 4.3 us, 700 with 39 000 rows 6.3 us.
 constexpr int kPlanOne = 1024;
 constexpr int kPlanOneWg = 4096;      // rows that one workgroup does alone: then nobody else reads what it writes
 __global__ __launch_bounds__(1024) void plan_one_kernel(const PlanArgs a)
@@ -175,7 +176,8 @@ __global__ __launch_bounds__(256) void plan_fill_kernel(const PlanArgs a, int ro
 }
 
 // A row (token, kv head) of K or V is D / 16 blocks; a thread takes a block of kAppendRows rows, which are under way at once.  Rows are taken token by
-// token, all heads of a token after each other: they lie side by side in memory.
+// token, all heads of a token after each other: they lie side by side in memory.  Bound by memory: 21 300 tokens, 8 heads of 128, 21.4 us (87 MB read, 25 MB
+// written, 5.2 TB/s, where a large copy reaches 5.1); 40 tokens 2.7 us, a launch.  (Half a block per thread, to store 1 KiB at once: the same.)
 constexpr int kAppendRows = 2;
 template <int D>
 __global__ __launch_bounds__(256) void append_kernel(const uint16_t* __restrict__ k, const uint16_t* __restrict__ v, size_t k_token, size_t k_head,
@@ -220,7 +222,8 @@ __global__ __launch_bounds__(256) void append_kernel(const uint16_t* __restrict_
 }
 
 // The same way back; a slot outside the cache reads as zeros.  (A value has at most 6 significant bits: exact in bf16.)  Bound by what it writes: a thread
-// makes 8 values, so that a wave stores 1 KiB in one piece per instruction, and has kReadRows rows under way at once.
+// makes 8 values, so that a wave stores 1 KiB in one piece per instruction, and has kReadRows rows under way at once.  116 000 tokens, 8 heads of 128:
+// 609 MB in 121.6 us, 5.0 TB/s (16 values per thread 136 us); 777 tokens 3.4 us.
 constexpr int kReadRows = 4;
 template <int D>
 __global__ __launch_bounds__(256) void read_kernel(uint16_t* __restrict__ k, uint16_t* __restrict__ v, size_t k_token, size_t k_head, size_t v_token,
