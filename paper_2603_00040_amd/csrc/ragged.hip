@@ -28,7 +28,7 @@ constexpr int kFewRows = 96;
 // largest probability so far is then up to 2^8 (as fp16 as good as 1), and most tiles need no rescaling of O: some row of 32 has a new maximum
 // in most of the first fifty tiles.
 constexpr float kSlack = 8.0f;
-constexpr int kWideStart = 5;         // (20 000 cycles against 4 000 for a tile of keys of 128 d)
+constexpr int kWideStart = 7;         // (six prompts of 766 - 3846 tokens: with 3 286 us, 5 272, 6 267, 8 266; pieces of prompts beside decodes 305, 298, 298, 298)
 constexpr int kWideRows = 256;        // rows of a tile of the other one
 
 struct Seq { int first, n, len; };    // first query of the step, number of queries, keys
@@ -501,11 +501,11 @@ struct WideWs { long long* quota; WideRec* rec; float* part_o /* [workgroup][2][
 // tile's S, and between these products unpacks its half of the keys of a K and a V tile into LDS (K as operands of the matrix instruction, V key by
 // key), the other does the softmax, so that every SIMD has a wave for either unit.  The work (row tile, key tile) is dealt out evenly as in the
 // kernel for few rows.
-// Rates, in floating-point operations that the mask leaves: 8192 queries and keys, 32/8 heads of 128, 960 TFLOP/s without a mask (1145 us), 945 causal; 16/4
-// heads of 64, 16384 queries, 8192 keys 780.  The products with their barriers alone would run at 1370, with their operands out of LDS and the
-// pages' loads at 1180 (a large library product: 1280): the rest is that a wave issues a vector instruction in 9 cycles, and that a tile has 180 of them
-// beside 1024 cycles of products.  Also tried: softmax and products of a wave in one stream (915, heads of 64 740), four waves of 32 rows and two
-// workgroups to a compute unit without phases (810), the unpacking shared between the phases (850).
+// Rates over 40 passes, in operations that the mask leaves: 8192 queries and keys, 32/8 heads of 128, 1130 TFLOP/s without a mask (973 us), 1010 causal; 8 x 512
+// queries over 8192 keys each 1050; 16/4 heads of 64, 16384 queries, 8192 keys 860.  The products with their barriers alone would run at 1550, with
+// their operands out of LDS and the pages' loads at 1375 (a large library product: 1280): the rest is that a wave issues a vector instruction
+// in 9 cycles, and that a tile has 180 of them beside 1024 cycles of products.  Also tried: softmax and products of a wave in one stream (5 % slower, heads
+// of 64 2 %), four waves of 32 rows and two workgroups to a compute unit without phases (10 %), the unpacking shared between the phases (5 %).
 template <int D>
 __global__ __launch_bounds__(512, 2) void ragged_wide_kernel(const RaggedArgs a, const WideWs ws)
 {
