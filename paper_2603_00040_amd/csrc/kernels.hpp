@@ -90,6 +90,7 @@ struct RaggedArgs {
     float c;                                     // log2(e) times the factor of the scores
     uint16_t* o; size_t o_token, o_head;
     float* lse;                                  // [T, Hq], or null
+    int group; uint32_t group_mul; int group_shift;      // Hq / Hkv, and for dividing by it (launch_ragged)
 };
 size_t ragged_ws_bytes(int T, int B, int Hq, int Hkv, int max_q, int max_pages, int D);
 int launch_ragged(const RaggedArgs& a, int D, void* ws, hipStream_t st);

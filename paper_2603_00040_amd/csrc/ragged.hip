@@ -31,6 +31,14 @@ constexpr float kSlack = 8.0f;
 constexpr int kWideStart = 7;         // (six prompts of 766 - 3846 tokens: with 3 286 us, 5 272, 6 267, 8 266; pieces of prompts beside decodes 305, 298, 298, 298)
 constexpr int kWideRows = 256;        // rows of a tile of the other one
 
+// The query heads of a kv head, and whole division by their number: x / G = x mul >> 31 + shift with mul = ceil(2^(31 + shift) / G), 2^shift >= G, exact for
+// 0 <= x < 2^31 (x times what mul is too large by stays below 2^(31 + shift)).  Three instructions instead of the two dozen of a division, of
+// which the start of a row tile has six.
+struct Group { int n; uint32_t mul; int shift; __device__ operator int() const { return n; } };
+__device__ inline int operator/(int x, const Group& g) { return (int)(((uint64_t)(uint32_t)x * g.mul) >> (31 + g.shift)); }
+__device__ inline int operator%(int x, const Group& g) { return x - (x / g) * g.n; }
+__device__ inline Group group_of(const RaggedArgs& a) { return Group{a.group, a.group_mul, a.group_shift}; }
+
 struct Seq { int first, n, len; };    // first query of the step, number of queries, keys
 __device__ inline Seq seq_of(const RaggedArgs& a, int b)
 {
@@ -52,7 +60,7 @@ __device__ inline void keys_of(const RaggedArgs& a, const Seq& s, int ta, int tb
 template <int D> constexpr int kFewStart = D == 64 ? 3 : 2;      // (6 000 cycles, against 2 000 and 3 200 for a page)
 struct Few { int rows, tiles /* of ROWS rows */, first_page, pages, units /* of a tile */; };
 template <int D, int ROWS>
-__device__ inline Few few_of(const RaggedArgs& a, const Seq& s, int G)
+__device__ inline Few few_of(const RaggedArgs& a, const Seq& s, const Group& G)
 {
     const int rows = s.n * G;
     int lo, hi;
@@ -103,6 +111,18 @@ __device__ inline half8 values8(const Raw<D>& r, half2v sc, int s)
     return __builtin_bit_cast(half8, v);
 }
 
+// The largest magnitude of 8 N bf16 values: without their signs they are ordered as whole numbers are.
+template <int N>
+__device__ inline float largest_of(const uint4v (&x)[N])
+{
+    typedef unsigned short ushort2v __attribute__((ext_vector_type(2)));
+    ushort2v m = {0, 0};
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) m = __builtin_elementwise_max(m, __builtin_bit_cast(ushort2v, x[i][j] & 0x7FFF7FFFu));
+    return __uint_as_float((uint32_t)max(m[0], m[1]) << 16);
+}
 // The power of two that brings a row's largest magnitude to [2^14, 2^15), and its inverse (magnitudes below 2^-112 count as that).  The factor of the
 // scores times the inverse is kept a normal number: where it would be less, scores differ by less than 2^-90, but a masked one times 0 would be a NaN.
 constexpr float kLeastFactor = 0x1p-126f;
@@ -136,7 +156,7 @@ __global__ __launch_bounds__(256, RT == 1 ? 3 : 2) void ragged_few_kernel(const 
 
     const int tid = threadIdx.x, lane = tid & 63, cc = lane & 15, g = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int G = a.Hq / a.Hkv;
+    const Group G = group_of(a);
     unsigned char* stg = stage + wave * (32 * RS);
     // (the two 16-byte pieces of every 32 change places in keys 4 - 7 of 8: a store serves eight lanes, eight keys, at a time on 32 banks)
     const uint32_t tr_base = lds_addr_of(stg) + (uint32_t)((4 * g + (cc >> 2)) * RS + 8 * ((cc & 3) ^ (2 * (g & 1))));
@@ -231,12 +251,7 @@ __global__ __launch_bounds__(256, RT == 1 ? 3 : 2) void ragged_few_kernel(const 
         float c_row[RT];
 #pragma unroll
         for (int rt = 0; rt < RT; ++rt) {
-            float amax = 0.0f;
-#pragma unroll
-            for (int i = 0; i < NS; ++i)
-#pragma unroll
-                for (int j = 0; j < 4; ++j) amax = fmaxf(amax, fmaxf(fabsf(__uint_as_float(x[rt][i][j] << 16)), fabsf(__uint_as_float(x[rt][i][j] & 0xFFFF0000u))));
-            amax = lanes_max<16, 32>(amax);
+            const float amax = lanes_max<16, 32>(largest_of(x[rt]));
             float f, inv;
             row_factor(amax, f, inv);
 #pragma unroll
@@ -401,7 +416,8 @@ __device__ void few_merge(const RaggedArgs& a, const FewWs& ws, int unit, int ti
     constexpr int NG = 256 / (D / 4);
     __shared__ __align__(16) float acc[NG][D];
     __shared__ float ml[NG][2];
-    const int G = a.Hq / a.Hkv, tile = unit % tiles, b = unit / tiles / a.Hkv, h = unit / tiles % a.Hkv;
+    const Group G = group_of(a);
+    const int tile = unit % tiles, b = unit / tiles / a.Hkv, h = unit / tiles % a.Hkv;
     const int tid = threadIdx.x, grp = tid / (D / 4), d = tid % (D / 4) * 4;
     const int quota = *ws.quota, front = ws.front[b];             // (beside the lengths, not behind them)
     const Seq s = seq_of(a, b);
@@ -463,7 +479,7 @@ __device__ void few_merge(const RaggedArgs& a, const FewWs& ws, int unit, int ti
 // The units of work of the kernel for many rows: a tile of kWideRows rows and the tiles of 64 keys that it sees, for every kv head, sequence by sequence,
 // head by head, tile by tile.  What a row tile costs besides (its rows of Q, the first tiles of K and V, the result) counts as kWideStart
 // tiles of keys in front of its own.
-__device__ inline void wide_tile(const RaggedArgs& a, const Seq& s, int G, int tile, int& t0, int& nt)
+__device__ inline void wide_tile(const RaggedArgs& a, const Seq& s, const Group& G, int tile, int& t0, int& nt)
 {
     const int r0 = tile * kWideRows;
     int lo, hi;
@@ -473,7 +489,7 @@ __device__ inline void wide_tile(const RaggedArgs& a, const Seq& s, int G, int t
 }
 // The key tiles (for one head) of all row tiles of sequence b, a thread each: the lanes of a wave go over the row tiles of one of its sequences after
 // another.  0 where the kernel for few rows takes the sequence.
-__device__ inline long long wide_work(const RaggedArgs& a, int G, int b)
+__device__ inline long long wide_work(const RaggedArgs& a, const Group& G, int b)
 {
     const int lane = threadIdx.x & 63;
     Seq s{0, 0, 0};
@@ -519,7 +535,7 @@ __global__ __launch_bounds__(512, 2) void ragged_wide_kernel(const RaggedArgs a,
     const int tid = threadIdx.x, lane = tid & 63, col = lane & 31, half = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const bool late = wave >= 4;
-    const int G = a.Hq / a.Hkv;
+    const Group G = group_of(a);
 
     // this workgroup's key tiles [w, w_end) of all units', and where they begin
     long long all = 0, total, n_b = 0, upto_b = 0;
@@ -561,6 +577,19 @@ __global__ __launch_bounds__(512, 2) void ragged_wide_kernel(const RaggedArgs a,
         __builtin_amdgcn_s_barrier();
         __builtin_amdgcn_sched_barrier(0);
     };
+
+    // Rows of Q and O pass through a place of LDS of the wave's own (of the tiles', which nobody reads before a segment's first barrier and behind its last):
+    // in memory the wave takes rows whole, D / 8 lanes to each, where in registers a lane has a piece of every row (one row's 16 bytes
+    // beside the next row's: 32 lines of memory to every instruction; 1 % slower).  Behind a row, where it lies.
+    constexpr int RO = 2 * D + 16, LR = D / 8, RP = 64 / LR;       // bytes of a row, lanes to a row, rows at a time
+    static_assert(8 * 32 * RO <= 2 * KB + 2 * VB && 32 / RP == ND);
+    const uint32_t own_row = lds0 + (uint32_t)((wave * 32 + col) * RO), own_piece = lds0 + (uint32_t)((wave * 32 + lane / LR) * RO + 16 * (lane % LR));
+    const uint32_t own_where = lds0 + (uint32_t)((wave * 32 + lane / LR) * RO + 2 * D);
+    auto row_at = [&](int p) __attribute__((always_inline)) {      // of row RP p + lane / LR, as it was written behind it
+        const uint2v w = lds_read8_at(own_where + (uint32_t)(p * RP * RO));
+        return (size_t)(((unsigned long long)w[1] << 32) | w[0]);
+    };
+    auto write_where = [&](size_t at) __attribute__((always_inline)) { lds_write8_at(own_row + 2 * D, uint2v{(uint32_t)at, (uint32_t)(at >> 32)}); };
 
     int tile = -1, h = 0, off = 0, t0 = 0, nt = 0;                 // tile < 0: to be looked up
     int id_lane = 0, id_b = -1, id_first = 0;                      // lane i: the id of page id_first + i of sequence id_b, -1: outside the cache
@@ -678,9 +707,10 @@ __global__ __launch_bounds__(512, 2) void ragged_wide_kernel(const RaggedArgs a,
 
         // what a segment needs from memory first, asked for at once: Q, the first tile of V, the first two of K
         uint4v x[ND];
+        write_where((size_t)(s.first + tok) * a.q_token + (size_t)head * a.q_head);
+        __builtin_amdgcn_wave_barrier();
 #pragma unroll
-        for (int i = 0; i < ND; ++i)
-            x[i] = *reinterpret_cast<const uint4v*>(a.q + (size_t)(s.first + tok) * a.q_token + (size_t)head * a.q_head + 16 * i + 8 * half);
+        for (int i = 0; i < ND; ++i) x[i] = *reinterpret_cast<const uint4v*>(a.q + row_at(i) + 8 * (lane % LR));
         Raw<D> raw0, raw1;
         bool on0, on1;
         load_to(raw0, on0, first);
@@ -691,12 +721,12 @@ __global__ __launch_bounds__(512, 2) void ragged_wide_kernel(const RaggedArgs a,
         half8 qreg[ND];
         float c_row;
         {
-            float amax = 0.0f;
 #pragma unroll
-            for (int i = 0; i < ND; ++i)
+            for (int i = 0; i < ND; ++i) lds_write16_at(own_piece + (uint32_t)(i * RP * RO), x[i]);
+            __builtin_amdgcn_wave_barrier();
 #pragma unroll
-                for (int j = 0; j < 4; ++j) amax = fmaxf(amax, fmaxf(fabsf(__uint_as_float(x[i][j] << 16)), fabsf(__uint_as_float(x[i][j] & 0xFFFF0000u))));
-            amax = lanes_max<32, 32>(amax);
+            for (int i = 0; i < ND; ++i) x[i] = lds_read16_at(own_row + (uint32_t)(32 * i + 16 * half));
+            const float amax = lanes_max<32, 32>(largest_of(x));
             float f, inv;
             row_factor(amax, f, inv);
 #pragma unroll
@@ -825,15 +855,21 @@ __global__ __launch_bounds__(512, 2) void ragged_wide_kernel(const RaggedArgs a,
             l = lanes_sum<32, 32>(l);
             if (whole) {
                 const float inv = l != 0.0f ? 1.0f / l : 0.0f;
-                if (w0 + col < rows) {
-                    uint16_t* dst = a.o + (size_t)(s.first + tok) * a.o_token + (size_t)head * a.o_head;
 #pragma unroll
-                    for (int i = 0; i < NB; ++i)
+                for (int i = 0; i < NB; ++i)
 #pragma unroll
-                        for (int j = 0; j < 4; ++j)
-                            *reinterpret_cast<uint2v*>(dst + 32 * i + 8 * j + 4 * half) = uint2v{pack_bf16x2_cvt(o[i][4 * j] * inv, o[i][4 * j + 1] * inv), pack_bf16x2_cvt(o[i][4 * j + 2] * inv, o[i][4 * j + 3] * inv)};
-                    if (half == 0 && a.lse) a.lse[(size_t)(s.first + tok) * a.Hq + head] = l != 0.0f ? m * 0.6931471805599453f + logf(l) : -INFINITY;
+                    for (int j = 0; j < 4; ++j)
+                        lds_write8_at(own_row + (uint32_t)(64 * i + 16 * j + 8 * half), uint2v{pack_bf16x2_cvt(o[i][4 * j] * inv, o[i][4 * j + 1] * inv), pack_bf16x2_cvt(o[i][4 * j + 2] * inv, o[i][4 * j + 3] * inv)});
+                write_where((size_t)(s.first + tok) * a.o_token + (size_t)head * a.o_head);
+                __builtin_amdgcn_wave_barrier();
+#pragma unroll
+                for (int p = 0; p < ND; ++p) {
+                    const uint4v y = lds_read16_at(own_piece + (uint32_t)(p * RP * RO));
+                    const size_t to = row_at(p);
+                    if (w0 + p * RP + lane / LR < rows) *reinterpret_cast<uint4v*>(a.o + to + 8 * (lane % LR)) = y;
                 }
+                if (half == 0 && w0 + col < rows && a.lse) a.lse[(size_t)(s.first + tok) * a.Hq + head] = l != 0.0f ? m * 0.6931471805599453f + logf(l) : -INFINITY;
+                __builtin_amdgcn_wave_barrier();
             } else {
                 const size_t slot = ((size_t)blockIdx.x * 2 + (at == 0 ? 1 : 0)) * 8 + wave;
 #pragma unroll
@@ -867,7 +903,8 @@ __device__ void wide_merge(const RaggedArgs& a, const WideWs& ws, int place, int
     const WideRec r = ws.rec[place];
     if (quota == 0 || r.off <= kWideStart || r.off - quota > kWideStart) return;      // it begins there, or has begun two workgroups ago
     const Seq s = seq_of(a, r.b);
-    const int G = a.Hq / a.Hkv, rows = s.n * G, lane = threadIdx.x & 63, j = threadIdx.x >> 6;
+    const Group G = group_of(a);
+    const int rows = s.n * G, lane = threadIdx.x & 63, j = threadIdx.x >> 6;
     const int col = lane & 31, half = lane >> 5, row = r.tile * kWideRows + 32 * wave + col;
     if (r.tile * kWideRows + 32 * wave >= rows) return;
     const int n = 1 + (int)((r.nt - r.off + quota - 1) / quota);
@@ -907,7 +944,7 @@ __device__ void wide_merge(const RaggedArgs& a, const WideWs& ws, int place, int
 template <int D>
 __device__ void wide_empty(const RaggedArgs& a, int which, int n)
 {
-    const int G = a.Hq / a.Hkv;
+    const Group G = group_of(a);
     for (int b = which; b < a.B; b += n) {
         const Seq s = seq_of(a, b);
         const int rows = s.n * G;
@@ -1002,8 +1039,13 @@ size_t ragged_ws_bytes(int T, int B, int Hq, int Hkv, int max_q, int max_pages, 
     return carve_ragged(nullptr, plan_of(T, B, Hq, Hkv, max_q, max_pages, D, kChipCus), B, D).bytes;
 }
 
-int launch_ragged(const RaggedArgs& a, int D, void* ws, hipStream_t st)
+int launch_ragged(const RaggedArgs& args, int D, void* ws, hipStream_t st)
 {
+    RaggedArgs a = args;
+    a.group = a.Hq / a.Hkv;
+    a.group_shift = 0;
+    while ((1 << a.group_shift) < a.group) ++a.group_shift;       // (a.group <= 2^28)
+    a.group_mul = (uint32_t)(((1ull << (31 + a.group_shift)) + a.group - 1) / a.group);
     const RaggedPlan p = plan_of(a.T, a.B, a.Hq, a.Hkv, a.max_q, a.max_pages, D, kChipCus);
     const RaggedWs w = carve_ragged(ws, p, a.B, D);
     return D == 128 ? (p.few_groups == 1 ? launch_ragged_of<128, 1>(a, p, w, st) : launch_ragged_of<128, 2>(a, p, w, st))
