@@ -409,7 +409,7 @@ __global__ __launch_bounds__(256, RT == 1 ? 3 : 2) void ragged_few_kernel(const 
 }
 
 // O and lse of a unit whose pages were shared, and of rows that see no key, by a workgroup: groups of D / 4 threads have a row each, or, while there are
-// fewer rows than groups, several groups share the partial sums of a row.  A launch and two trips to memory: 4.7 us.
+// fewer rows than groups, several groups share the partial sums of a row.  A launch and two or three trips to memory: 4.7 us.
 template <int D, int ROWS>
 __device__ void few_merge(const RaggedArgs& a, const FewWs& ws, int unit, int tiles /* of a sequence at most */)
 {
@@ -438,22 +438,25 @@ __device__ void few_merge(const RaggedArgs& a, const FewWs& ws, int unit, int ti
         float M = -INFINITY, l = 0.0f;
         floatx4 v = {0.0f, 0.0f, 0.0f, 0.0f};
         if (on) {
-            for (int i0 = grp % per; i0 < n; i0 += 4 * per) {      // four at a time: one trip to memory
-                floatx4 po[4];
-                float pm[4], pl[4];
+            constexpr int K = 8;                                  // at a time: one trip to memory (4: 16 000 keys 16.1 instead of 14.5 us; 16: 64 sequences of 500 17.4 instead of 16.6)
+            for (int i0 = grp % per; i0 < n; i0 += K * per) {
+                floatx4 po[K];
+                float pm[K], pl[K];
 #pragma unroll
-                for (int k = 0; k < 4; ++k) {
+                for (int k = 0; k < K; ++k) {
                     const int i = min(i0 + k * per, n - 1);
                     const size_t at = ((size_t)(f + i) * 2 + (i == 0 ? 1 : 0)) * ROWS + r;
                     po[k] = *reinterpret_cast<const floatx4*>(ws.part_o + at * D + d);
                     pm[k] = i0 + k * per < n ? ws.part_ml[at * 2] : -INFINITY;
                     pl[k] = ws.part_ml[at * 2 + 1];
                 }
-                const float top = fmaxf(fmaxf(fmaxf(pm[0], pm[1]), fmaxf(pm[2], pm[3])), M), at = top == -INFINITY ? 0.0f : top;
-                const float al = __builtin_amdgcn_exp2f(M - at);
+                float top = M;
+#pragma unroll
+                for (int k = 0; k < K; ++k) top = fmaxf(top, pm[k]);
+                const float at = top == -INFINITY ? 0.0f : top, al = __builtin_amdgcn_exp2f(M - at);
                 M = top; l *= al; v *= al;
 #pragma unroll
-                for (int k = 0; k < 4; ++k) { const float x = __builtin_amdgcn_exp2f(pm[k] - at); l = fmaf(pl[k], x, l); v += po[k] * x; }
+                for (int k = 0; k < K; ++k) { const float x = __builtin_amdgcn_exp2f(pm[k] - at); l = fmaf(pl[k], x, l); v += po[k] * x; }
             }
         }
         if (per > 1) {                                            // (then one round is all)
@@ -517,8 +520,8 @@ struct WideWs { long long* quota; WideRec* rec; float* part_o /* [workgroup][2][
 // tile's S, and between these products unpacks its half of the keys of a K and a V tile into LDS (K as operands of the matrix instruction, V key by
 // key), the other does the softmax, so that every SIMD has a wave for either unit.  The work (row tile, key tile) is dealt out evenly as in the
 // kernel for few rows.
-// Rates over 40 passes, in operations that the mask leaves: 8192 queries and keys, 32/8 heads of 128, 1130 TFLOP/s without a mask (973 us), 1010 causal; 8 x 512
-// queries over 8192 keys each 1050; 16/4 heads of 64, 16384 queries, 8192 keys 860.  The products with their barriers alone would run at 1550, with
+// Rates over 40 passes, in operations that the mask leaves: 8192 queries and keys, 32/8 heads of 128, 1170 TFLOP/s without a mask (937 us), 1070 causal; 8 x 512
+// queries over 8192 keys each 1090; 16/4 heads of 64, 16384 queries, 8192 keys 890.  The products with their barriers alone would run at 1550, with
 // their operands out of LDS and the pages' loads at 1375 (a large library product: 1280): the rest is that a wave issues a vector instruction
 // in 9 cycles, and that a tile has 180 of them beside 1024 cycles of products.  Also tried: softmax and products of a wave in one stream (5 % slower, heads
 // of 64 2 %), four waves of 32 rows and two workgroups to a compute unit without phases (10 %), the unpacking shared between the phases (5 %).
