@@ -280,6 +280,28 @@ def test_strided_rows(aq, layout):
     run_attention(aq, [1], [200], 1, 1, 64, layout=layout, seed=3, tail=0)
 
 
+@pytest.mark.parametrize("layout", ["plain", "fused", "heads"])
+@pytest.mark.parametrize("Hq,Hkv,d", [(6, 2, 128), (10, 2, 64), (1, 1, 128), (7, 1, 64)])
+def test_strided_rows_of_long_pieces(aq, layout, Hq, Hkv, d):
+    """Row tiles that end inside a wave's rows, in a query's heads and at one row; nothing written between rows or behind them."""
+    for n, kv in (([301, 1, 97], [301, 40, 500]), ([257], [257])):
+        q, cu, cache, num_pages, table = attention_case(n, kv, Hq, Hkv, d, 11, tail=2)
+        T = q.shape[0]
+        whole = torch.full((T, Hq + 3, d), 7.0, dtype=torch.bfloat16, device="cuda")
+        o = whole[:, 1:Hq + 1] if layout == "fused" else torch.full((T, Hq, d), 7.0, dtype=torch.bfloat16, device="cuda")
+        if layout == "heads":
+            whole = torch.full((Hq, T + 5, d), 7.0, dtype=torch.bfloat16, device="cuda")
+            o = whole[:, 2:T + 2].transpose(0, 1)
+        lse = torch.full((T, Hq), 7.0, device="cuda")
+        aq.attnqat_fwd_kv4_ragged(_views(q.cuda(), layout), i32(cu), dev(cache.reshape(-1)), num_pages, dev(table), i32(kv), Hkv, True, max_q=max(n), out=(o, lse))
+        check_attention(o, lse, S.attend(q.double().numpy(), cu, cache, table, kv, Hkv, True, 0, 1.0 / np.sqrt(d)), (layout, n, Hq, Hkv, d))
+        assert bool((o[-2:] == 7.0).all()) and bool((lse[-2:] == 7.0).all())
+        if layout == "fused":
+            assert bool((whole[:, 0] == 7.0).all()) and bool((whole[:, Hq + 1:] == 7.0).all())
+        if layout == "heads":
+            assert bool((whole[:, :2] == 7.0).all()) and bool((whole[:, T + 2:] == 7.0).all())
+
+
 @pytest.mark.parametrize("scale", [0.01, 0.5])
 def test_scale(aq, scale):
     run_attention(aq, [1, 20], [200, 300], 4, 2, 64, scale=scale, seed=3, q_scale=0.25)
