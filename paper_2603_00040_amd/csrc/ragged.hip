@@ -28,7 +28,7 @@ constexpr int kFewRows = 96;
 // largest probability so far is then up to 2^8 (as fp16 as good as 1), and most tiles need no rescaling of O: some row of 32 has a new maximum
 // in most of the first fifty tiles.
 constexpr float kSlack = 8.0f;
-constexpr int kWideStart = 7;         // (six prompts of 766 - 3846 tokens: with 3 286 us, 5 272, 6 267, 8 266; pieces of prompts beside decodes 305, 298, 298, 298)
+constexpr int kWideStart = 5;         // (13 000 cycles against 3400; six prompts of 766 - 3846 tokens: with 4 253.6 us, 5 251.7, 6 255.0, 7 255.4)
 constexpr int kWideRows = 256;        // rows of a tile of the other one
 
 // The query heads of a kv head, and whole division by their number: x / G = x mul >> 31 + shift with mul = ceil(2^(31 + shift) / G), 2^shift >= G, exact for
@@ -142,7 +142,7 @@ struct FewWs { int* quota; int* front /* [B + 1] */; float* part_o /* [workgroup
 // launch that makes a list would cost more).  Its four waves take 32 keys of every page, each with its own maximum, sum and O; the pages of
 // the next iteration are requested before the present ones are used.  One query of 32 sequences of 4096 - 16384 keys, 32/8 heads of 128: 326 MB in 61 us,
 // 5.3 TB/s, what a copy reaches.  With more rows and short segments the vector instructions bound it (unpacking, softmax: a wave issues one
-// in 9 cycles) and the start of a segment: one to six queries of 40 sequences of 300 - 9000 keys, 16/4 heads of 64, 34 MB in 17.6 us.
+// in 9 cycles) and the start of a segment: one to six queries of 40 sequences of 300 - 9000 keys, 16/4 heads of 64, 34 MB in 16.9 us.
 template <int D, int RT /* 16-row groups of a unit */>
 __global__ __launch_bounds__(256, RT == 1 ? 3 : 2) void ragged_few_kernel(const RaggedArgs a, const FewWs ws)
 {
@@ -896,7 +896,7 @@ __global__ __launch_bounds__(512, 2) void ragged_wide_kernel(const RaggedArgs a,
 }
 
 // O and lse of the row tiles whose key tiles were shared: a workgroup per place where one workgroup's work ended and another's began, and 32 rows; of the
-// places within a row tile the first has it.  Bound by memory (each of 256 workgroups leaves up to two tiles of 256 rows in fp32: 13.5 us for heads of 128).
+// places within a row tile the first has it.  Bound by memory (each of 256 workgroups leaves up to two tiles of 256 rows in fp32: 14 us for heads of 128).
 template <int D>
 __device__ void wide_merge(const RaggedArgs& a, const WideWs& ws, int place, int wave)
 {
