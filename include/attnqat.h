@@ -441,8 +441,8 @@ int attnqat_debug_fwd_infer_paged(const void* q, int B, int Hq, int Hkv, int Lq,
  * attnqat_fwd_kv4_ragged: O = softmax(scale Q K^T + mask) V, K and V being the values that the pages hold: only the cache is in 4 bits.  Q is not
  * quantized, nor are the probabilities (which are rounded to fp16 for their product with V; scores, sums and O are fp32), as for a
  * model that was not trained for Alg. 1; attnqat_fwd_infer_paged is Alg. 1.  q [T,Hq,d]; sequence b has kv_lens[b] keys, the last of which belong to
- * its rows: row i of n sees keys 0 .. kv_lens[b] - n + i with causal != 0, of those the last `window` if window > 0 (causal only), and all keys with
- * causal = 0.  max_q: no sequence has more rows (of one that has, the first max_q are computed as if there were no others).  A row without a key gets o = 0, lse = -inf.  o [T,Hq,d] bf16; lse
+ * its rows: row i of n sees keys 0 .. kv_lens[b] - n + i with causal != 0, of those the last `window` if window > 0 (causal only; max_pages * 128 and
+ * more hide nothing), and all keys with causal = 0.  max_q: no sequence has more rows (of one that has, the first max_q are computed as if there were no others).  A row without a key gets o = 0, lse = -inf.  o [T,Hq,d] bf16; lse
  * [T,Hq] fp32 (natural log), may be NULL; rows behind cu_q[B] are left as they are.  o and lse must not lie over q.  scale > 0.
  * Positions of a page table entry outside [0, num_pages) read as zeros; positions from kv_lens[b] on are never used, whatever their slots
  * hold.  At most 2^28 rows of heads (T Hq) and 2^22 (sequence, kv head)s.  Workspace: attnqat_kv4_ragged_workspace_bytes(), 16-byte aligned.

@@ -1045,6 +1045,7 @@ size_t ragged_ws_bytes(int T, int B, int Hq, int Hkv, int max_q, int max_pages, 
 int launch_ragged(const RaggedArgs& args, int D, void* ws, hipStream_t st)
 {
     RaggedArgs a = args;
+    if (a.window >= a.max_pages * 128) a.window = 0;              // (hides nothing; below, positions less a window stay within 32 bits)
     a.group = a.Hq / a.Hkv;
     a.group_shift = 0;
     while ((1 << a.group_shift) < a.group) ++a.group_shift;       // (a.group <= 2^28)
