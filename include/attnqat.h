@@ -439,7 +439,8 @@ int attnqat_debug_fwd_infer_paged(const void* q, int B, int Hq, int Hkv, int Lq,
  * the cache.  k and v must not lie over each other.  (Both: at most 2^29 rows of heads, T Hkv.)
  *
  * attnqat_fwd_kv4_ragged: O = softmax(scale Q K^T + mask) V, K and V being the values that the pages hold: only the cache is in 4 bits.  Q is not
- * quantized, nor are the probabilities (which are rounded to fp16 for their product with V; scores, sums and O are fp32), as for a
+ * quantized, nor are the probabilities (which are rounded to fp16 for their product with V: by a relative 2^-12, below 2^-25 of the
+ * row's largest by 2^-36 of it; scores, sums and O are fp32, and rows whose scores reach 2^26 in magnitude may come out as NaN), as for a
  * model that was not trained for Alg. 1; attnqat_fwd_infer_paged is Alg. 1.  q [T,Hq,d]; sequence b has kv_lens[b] keys, the last of which belong to
  * its rows: row i of n sees keys 0 .. kv_lens[b] - n + i with causal != 0, of those the last `window` if window > 0 (causal only; max_pages * 128 and
  * more hide nothing), and all keys with causal = 0.  max_q: no sequence has more rows (of one that has, the first max_q are computed as if there were no others).  A row without a key gets o = 0, lse = -inf.  o [T,Hq,d] bf16; lse

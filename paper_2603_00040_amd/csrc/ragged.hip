@@ -8,8 +8,10 @@
 //
 // Numbers: a cached value has at most 6 significant bits and lies in [2^-10, 2688], exact in fp16.  A row of Q, bf16, is multiplied by the power of
 // two that brings its largest element to [2^14, 2^15) and is exact in fp16 but for elements 2^-28 of the largest and less, which lose
-// what lies below 2^-39 of the largest.  Scores, maxima, sums and O are fp32.  P is rounded to fp16 (11 bits, P <= 2^8, see kSlack) for the product with V: a
-// relative 2^-12 per probability, an eighth of what rounding the output to bf16 costs; the sum that divides O is of the unrounded ones.
+// what lies below 2^-39 of the largest.  Scores, maxima, sums and O are fp32.  P is rounded to fp16 for the product with V, scaled so that a row's largest is
+// at least 2^11 (kTop): by a relative 2^-12, an eighth of what rounding the output to bf16 costs, down to 2^-25 of the row's largest so far, and by 2^-36 of that
+// largest below (all of them together by less than 2^-16 of the largest |V|, for 2^20 keys).  The sum that divides O is of the unrounded ones.  Scores
+// times log2 e that reach 2^27 have no reference in fp32 that is near enough for that: P may leave fp16.
 #include "common.hpp"
 #include "kernels.hpp"
 #include "nvfp4.hpp"
@@ -24,10 +26,11 @@ namespace {
 // tiles of 256.  Few -> many, 16 sequences of 4096 keys, 8 kv heads of 128: 48 rows 56 against 78 us, 80 rows 76 against 79, 128 rows 84 against 87;
 // 4 of 16 000 keys: 40 rows 59 against 75, 120 rows 91 against 81.
 constexpr int kFewRows = 96;
-// The reference that a row's exponents are taken against, in powers of two, follows its running maximum only when that is more than this above it: a row's
-// largest probability so far is then up to 2^8 (as fp16 as good as 1), and most tiles need no rescaling of O: some row of 32 has a new maximum
-// in most of the first fifty tiles.
-constexpr float kSlack = 8.0f;
+// The reference that a row's exponents are taken against, in powers of two, is set where the row's largest probability becomes 2^kTop, and follows the running
+// maximum only when that would make it more than 2^kTopMost, half of what fp16 holds: most tiles need no rescaling of O, though some row of 32 has a
+// new maximum in most of the first fifty tiles.  The higher the one, the smaller the probabilities that keep all their bits; the nearer to the other, the more
+// often O is rescaled where scores spread widely (six prompts, four channels of K times 20: kTop 7 225 us, 9 226, 11 229; scores of deviation 1: even).
+constexpr float kTop = 11.0f, kTopMost = 15.0f;
 constexpr int kWideStart = 5;         // (13 000 cycles against 3400; six prompts of 766 - 3846 tokens: with 4 253.6 us, 5 251.7, 6 255.0, 7 255.4)
 constexpr int kWideRows = 256;        // rows of a tile of the other one
 
@@ -267,7 +270,7 @@ __global__ __launch_bounds__(256, RT == 1 ? 3 : 2) void ragged_few_kernel(const 
         const int see_first = a.window > 0 ? s.len - s.n + (r0 + rows - 1) / G - a.window + 1 : 0, see_last = a.causal ? min(s.len - s.n + r0 / G, s.len - 1) : s.len - 1;
 
         floatx4 o[RT][NDT];
-        float m[RT], l[RT];                                       // the maximum in units of the exponent of 2
+        float m[RT], l[RT];                                       // the reference (kTop)
 #pragma unroll
         for (int rt = 0; rt < RT; ++rt) {
             m[rt] = -INFINITY; l[rt] = 0.0f;
@@ -312,9 +315,9 @@ __global__ __launch_bounds__(256, RT == 1 ? 3 : 2) void ragged_few_kernel(const 
                 }
                 float mx = max_nc(max_nc(max_nc(sc[rt][0][0], sc[rt][0][1]), max_nc(sc[rt][0][2], sc[rt][0][3])),
                                   max_nc(max_nc(sc[rt][1][0], sc[rt][1][1]), max_nc(sc[rt][1][2], sc[rt][1][3])));
-                mx = lanes_max<16, 32>(mx) * c_row[rt];
-                if (__builtin_amdgcn_ballot_w64(mx > m[rt] + kSlack) != 0) {
-                    const float m_new = fmaxf(m[rt], mx), alpha = __builtin_amdgcn_exp2f(m[rt] - (m_new == -INFINITY ? 0.0f : m_new));
+                mx = lanes_max<16, 32>(mx);
+                if (__builtin_amdgcn_ballot_w64(fmaf(mx, c_row[rt], -m[rt]) > kTopMost) != 0) {
+                    const float m_new = fmaxf(m[rt], fmaf(mx, c_row[rt], -kTop)), alpha = __builtin_amdgcn_exp2f(m[rt] - (m_new == -INFINITY ? 0.0f : m_new));
                     m[rt] = m_new;
                     l[rt] *= alpha;
 #pragma unroll
@@ -745,7 +748,7 @@ __global__ __launch_bounds__(512, 2) void ragged_wide_kernel(const RaggedArgs a,
         unpack(raw0, on0, 0, 0);
         if (!is_v) unpack(raw1, on1, 1, 0);
         floatx16 o[NB], sc[2];
-        float m = -INFINITY, l = 0.0f;                             // the maximum in units of the exponent of 2
+        float m = -INFINITY, l = 0.0f;                             // the reference (kTop)
         half8 pt[4];
 #pragma unroll
         for (int i = 0; i < NB; ++i)
@@ -814,9 +817,9 @@ __global__ __launch_bounds__(512, 2) void ragged_wide_kernel(const RaggedArgs a,
             for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
                 for (int j = 0; j < 16; ++j) mx = max_nc(mx, sc[kb][j]);
-            mx = lanes_max<32, 32>(mx) * c_row;
-            if (__builtin_amdgcn_ballot_w64(mx > m + kSlack) != 0) {
-                const float m_new = fmaxf(m, mx), alpha = __builtin_amdgcn_exp2f(m - (m_new == -INFINITY ? 0.0f : m_new));
+            mx = lanes_max<32, 32>(mx);
+            if (__builtin_amdgcn_ballot_w64(fmaf(mx, c_row, -m) > kTopMost) != 0) {
+                const float m_new = fmaxf(m, fmaf(mx, c_row, -kTop)), alpha = __builtin_amdgcn_exp2f(m - (m_new == -INFINITY ? 0.0f : m_new));
                 m = m_new;
                 l *= alpha;
 #pragma unroll
