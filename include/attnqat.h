@@ -415,12 +415,13 @@ int attnqat_debug_fwd_infer_paged(const void* q, int B, int Hq, int Hkv, int Lq,
  *
  * attnqat_page_plan makes page table, slots and positions of a step.  Request b has kv_lens[b] positions and wants new_lens[b] (device int32 [B]):
  * more (the step's new positions), as many, or fewer (drafted tokens taken back, 0: a request that has ended).  Pages that it needs come out of
- * the ring free_pages (device int32 [num_free_slots], at least as many places as the cache has pages that the ring may come to hold):
+ * the ring free_pages (device int32 [num_free_slots]; as many places as the cache has pages are always enough):
  * free_state[0] is the place of the first free page, free_state[1] their number, and they follow each other around the ring.  Pages that a request no
- * longer needs go behind them, in the order of the requests, and may be taken from the next call on.  page_table (device int32
+ * longer needs go behind them, in the order of the requests, into places that no page has that was free before, and may be taken from the next call on.  page_table (device int32
  * [B, max_pages]) gets the new pages; its other entries stay as they are (those of pages given back, too).
  * A request is refused, and keeps what it had, if it wants more than max_pages * 128 positions, if its new positions do not end within
- * the first T of the step, or if the pages that requests 0 .. b ask for are more than were free.
+ * the first T of the step, if the pages that requests 0 .. b ask for are more than were free, or if it gives back pages and those that requests
+ * 0 .. b give back do not all find a place.
  * kv_lens_out[b]      new_lens[b], or kv_lens[b] where the request was refused (may be kv_lens itself)
  * cu_q[B+1]           sums of the new positions that requests ask for (also of refused ones, except those that want more than their row of the
  *                     page table holds), at most T

@@ -19,9 +19,10 @@ __device__ inline int pages_of(int positions) { return (positions + 127) >> 7; }
 
 // Who gets what, by a workgroup of 1024: of request b (a thread each) what the rest of the plan needs; sums of the requests in front in `in`, which moves on.
 // A request is served if it fits its row of the page table, its new positions end within the step's capacity T, and the pages asked for up to and
-// including it are free; pages given back by this step are for the next one.  The sums run over refused requests too, so that nobody
+// including it are free; pages given back by this step are for the next one, and go into places of the ring that no free page has (those of the free ones are
+// read by whoever takes them, at the same time): a request whose pages find no such place is refused.  The sums run over refused requests too, so that nobody
 // waits for a decision: refused for want of pages are then all that ask for any from the first such on, and the pages that are taken are a prefix
-// of those asked for.  (64 bits for the positions: what is asked for is not limited by T.)
+// of those asked for, as those that come back are of those given.  (64 bits for the positions: what is asked for is not limited by T.)
 struct PlanArgs {
     const int *kv_lens, *new_lens; int B;
     int* page_table; int max_pages;
@@ -30,13 +31,14 @@ struct PlanArgs {
     int *kv_out, *cu; long long* slots; int *positions, *state_out;
 };
 struct PlanSums { long long grown; int needed, given; };
+struct PlanDone { int taken, given, refused; };      // pages, pages, requests
 struct PlanRing { int head, count; };
 __device__ inline PlanRing plan_ring(const PlanArgs& a)
 {
     if (a.ring_size == 0) return PlanRing{0, 0};
     return PlanRing{min(max(a.ring_state[0], 0), a.ring_size - 1), min(max(a.ring_state[1], 0), a.ring_size)};
 }
-__device__ inline PlanItem plan_request(const PlanArgs& a, const PlanRing& r, int b, PlanSums& in, int& cu_end, int& kv_new, int& taken /* LDS */, int& refused /* LDS */,
+__device__ inline PlanItem plan_request(const PlanArgs& a, const PlanRing& r, int b, PlanSums& in, int& cu_end, int& kv_new, PlanDone& done /* LDS */,
                                         long long* red_l /* [16], LDS */, int* red_i /* [16], LDS */)
 {
     const bool on = b < a.B, ring = a.ring_size > 0;
@@ -53,19 +55,20 @@ __device__ inline PlanItem plan_request(const PlanArgs& a, const PlanRing& r, in
     in.needed += total;
     const int give_end = in.given + wg_scan<16>(give, red_i, total);
     in.given += total;
-    const bool ok = !bad && !late && (need == 0 || upto <= r.count);
+    const bool ok = !bad && !late && (need == 0 || upto <= r.count) && (give == 0 || give_end <= a.ring_size - r.count);
     cu_end = (int)min(end, (long long)a.T);
     kv_new = ok ? want : old;
-    if (on && need > 0 && ok) atomicMax(&taken, upto);
-    if (on && !ok) atomicAdd(&refused, 1);
-    return PlanItem{old, ok ? (ring ? (int)(((long long)r.head + upto - need) % a.ring_size) : 0) : -1, give, give_end - give};
+    if (on && need > 0 && ok) atomicMax(&done.taken, upto);
+    if (on && give > 0 && ok) atomicMax(&done.given, give_end);
+    if (on && !ok) atomicAdd(&done.refused, 1);
+    return PlanItem{old, ok ? (ring ? (int)(((long long)r.head + upto - need) % a.ring_size) : 0) : -1, ok ? give : 0, give_end - give};
 }
-__device__ inline void plan_state(const PlanArgs& a, const PlanRing& r, const PlanSums& in, int taken, int refused)
+__device__ inline void plan_state(const PlanArgs& a, const PlanRing& r, const PlanDone& done)
 {
     if (!a.state_out) return;
-    a.state_out[0] = a.ring_size > 0 ? (int)(((long long)r.head + taken) % a.ring_size) : 0;
-    a.state_out[1] = (int)min((long long)r.count - taken + in.given, (long long)a.ring_size);
-    a.state_out[2] = refused;
+    a.state_out[0] = a.ring_size > 0 ? (int)(((long long)r.head + done.taken) % a.ring_size) : 0;
+    a.state_out[1] = r.count - done.taken + done.given;           // (at most r.count + done.given, which the ring has places for)
+    a.state_out[2] = done.refused;
 }
 
 // The request of position t of the step: the last b with cu[b] <= t (t < cu[B]).
@@ -97,7 +100,7 @@ __device__ inline void plan_row(const PlanArgs& a, int t, int b, int pos, int ol
     a.positions[t] = b >= 0 ? pos : 0;
 }
 // Pages that 64 requests from b0 on give back, by a wave: its lanes over the pages of one request after another.  What is read of the ring and what is
-// written to it do not meet: free pages and pages given back together are no more than the ring has places.
+// written to it do not meet: free pages and pages given back together are no more than the ring has places (plan_request).
 __device__ inline void plan_give(const PlanArgs& a, const PlanItem& it /* of request b0 + lane */, int b0, int tail)
 {
     const int lane = threadIdx.x & 63;
@@ -118,18 +121,19 @@ constexpr int kPlanOneWg = 4096;      // rows that one workgroup does alone: the
 __global__ __launch_bounds__(1024) void plan_one_kernel(const PlanArgs a)
 {
     __shared__ long long red_l[16];
-    __shared__ int red_i[16], taken, refused, cu_s[kPlanOne + 1], old_s[kPlanOne], take_s[kPlanOne];
+    __shared__ int red_i[16], cu_s[kPlanOne + 1], old_s[kPlanOne], take_s[kPlanOne];
+    __shared__ PlanDone done;
     const int tid = threadIdx.x;
     const PlanRing r = plan_ring(a);
-    if (tid == 0) { taken = 0; refused = 0; cu_s[0] = 0; }
+    if (tid == 0) { done = PlanDone{0, 0, 0}; cu_s[0] = 0; }
     PlanSums in{0, 0, 0};
     int cu_end, kv_new;
-    const PlanItem it = plan_request(a, r, tid, in, cu_end, kv_new, taken, refused, red_l, red_i);
+    const PlanItem it = plan_request(a, r, tid, in, cu_end, kv_new, done, red_l, red_i);
     cu_s[tid + 1] = cu_end; old_s[tid] = it.old_len; take_s[tid] = it.take;
     __syncthreads();                                              // (every input but the ring and the table has been read: outputs may lie over them)
     if (blockIdx.x == 0) {
         if (tid < a.B) { a.kv_out[tid] = kv_new; a.cu[tid + 1] = cu_end; }
-        if (tid == 0) { a.cu[0] = 0; plan_state(a, r, in, taken, refused); }
+        if (tid == 0) { a.cu[0] = 0; plan_state(a, r, done); }
         if (a.ring_size > 0) plan_give(a, it, tid & ~63, (int)(((long long)r.head + r.count) % a.ring_size));
     }
     for (int t = (int)blockIdx.x * 1024 + tid; t < a.T; t += (int)gridDim.x * 1024) {
@@ -143,20 +147,21 @@ __global__ __launch_bounds__(1024) void plan_one_kernel(const PlanArgs a)
 __global__ __launch_bounds__(1024) void plan_scan_kernel(const PlanArgs a, PlanHead* __restrict__ hd, PlanItem* __restrict__ items)
 {
     __shared__ long long red_l[16];
-    __shared__ int red_i[16], taken, refused;
+    __shared__ int red_i[16];
+    __shared__ PlanDone done;
     const int tid = threadIdx.x;
     const PlanRing r = plan_ring(a);
-    if (tid == 0) { taken = 0; refused = 0; a.cu[0] = 0; }
+    if (tid == 0) { done = PlanDone{0, 0, 0}; a.cu[0] = 0; }
     PlanSums in{0, 0, 0};
     for (int b0 = 0; b0 < a.B; b0 += 1024) {
         int cu_end, kv_new;
-        const PlanItem it = plan_request(a, r, b0 + tid, in, cu_end, kv_new, taken, refused, red_l, red_i);
+        const PlanItem it = plan_request(a, r, b0 + tid, in, cu_end, kv_new, done, red_l, red_i);
         if (b0 + tid < a.B) { a.cu[b0 + tid + 1] = cu_end; a.kv_out[b0 + tid] = kv_new; items[b0 + tid] = it; }
     }
     __syncthreads();
     if (tid == 0) {
         hd->tail = a.ring_size > 0 ? (int)(((long long)r.head + r.count) % a.ring_size) : 0;
-        plan_state(a, r, in, taken, refused);
+        plan_state(a, r, done);
     }
 }
 __global__ __launch_bounds__(256) void plan_fill_kernel(const PlanArgs a, int row_wgs, const PlanHead* __restrict__ hd, const PlanItem* __restrict__ items)

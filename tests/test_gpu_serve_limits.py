@@ -1,9 +1,10 @@
 """Serving steps at the ends of their ranges."""
 import numpy as np
 import pytest
+import torch
 
 from tests import serve_util as S
-from tests.test_gpu_serve import check_attention, dev, i32, run_attention
+from tests.test_gpu_serve import _plan_case, check_attention, dev, i32, run_attention
 
 pytestmark = pytest.mark.gpu
 
@@ -50,3 +51,35 @@ def test_a_first_key_that_draws_the_attention(aq, B, n, kv, Hq, Hkv, d, noise, g
     cu = n * np.arange(B + 1)
     o, lse = aq.attnqat_fwd_kv4_ragged(q.cuda(), i32(cu), dev(cache.reshape(-1)), cache.shape[0], dev(table), i32([kv] * B), Hkv, True, max_q=n)
     check_attention(o, lse, S.attend(q.double().numpy(), cu, cache, table, [kv] * B, Hkv, True, 0, d ** -0.5), (B, n, d, noise, gap))
+
+
+@pytest.mark.parametrize("B,most,places,in_place", [(2, 3, 4, True), (60, 6, 150, False), (60, 6, 150, True), (900, 4, 700, False), (900, 4, 700, True), (1500, 3, 1000, True)])
+def test_plan_with_a_ring_that_pages_given_back_do_not_fit(aq, B, most, places, in_place):
+    """Pages come back into places that none of the free ones has; requests whose pages find none keep theirs and count as refused."""
+    rng = np.random.default_rng(B)
+    if B == 2:                                                   # one takes two of four free pages, the other has two to give: they would go where those are read
+        old, want, table, T = np.array([0, 384]), np.array([256, 100]), np.array([[-1, -1, -1], [10, 11, 12]], np.int32), 300
+        ring, state = np.arange(4, dtype=np.int32), np.array([3, 4])
+    else:
+        old, want, table, _, _, T = _plan_case(B, rng, most, 200, 1.0)
+        ring, state = np.arange(10_000, 10_000 + places, dtype=np.int32), np.array([places - 5, places - 20])
+    room, refused, kept = places - state[1], 0, want.copy()
+    back = 0
+    for b in range(B):                                           # the plan of requests that do not ask to give back what finds no place
+        give = S.pages(int(old[b])) - S.pages(int(max(want[b], 0)))
+        if give > 0:
+            back += give
+            if back > room:
+                kept[b], refused = old[b], refused + 1
+    assert refused > 0
+    t_ref, r_ref = table.copy(), ring.copy()
+    ref = S.plan(old, kept, t_ref, r_ref, state, T)
+    ref[4][2] += refused
+    lens, st, t_dev, r_dev = i32(old), i32(list(state) + [0]), dev(table), dev(ring)
+    out = None
+    if in_place:
+        out = (lens, torch.empty(B + 1, dtype=torch.int32, device="cuda"), torch.empty(T, dtype=torch.int64, device="cuda"), torch.empty(T, dtype=torch.int32, device="cuda"), st)
+    got = aq.attnqat_page_plan(lens, i32(want), t_dev, T, free=(r_dev, st), out=out)
+    for name, g, r in zip(("kv_lens", "cu_q", "slots", "positions", "free_state"), got, ref):
+        assert np.array_equal(g.cpu().numpy(), r), name
+    assert np.array_equal(t_dev.cpu().numpy(), t_ref) and np.array_equal(r_dev.cpu().numpy(), r_ref)
