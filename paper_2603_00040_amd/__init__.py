@@ -383,8 +383,14 @@ def attnqat_kv_cache_read(cache, slots, Hkv: int, d: int, num_pages=None, out=No
     return k, v
 
 
+def _within_int(x):
+    """The nearest number that the library's int holds: ctypes would take the low 32 bits.  (For numbers that are limits: more rows than there are, a window
+    beyond every length, anything below 1.)"""
+    return max(-1, min(int(x), 0x7FFFFFFF))
+
+
 def kv4_ragged_workspace_bytes(T: int, B: int, Hq: int, Hkv: int, max_q: int, max_pages: int, d: int) -> int:
-    return lib().attnqat_kv4_ragged_workspace_bytes(T, B, Hq, Hkv, max_q, max_pages, d)
+    return lib().attnqat_kv4_ragged_workspace_bytes(T, B, Hq, Hkv, _within_int(max_q), max_pages, d)
 
 
 def attnqat_fwd_kv4_ragged(q, cu_q, cache, num_pages, page_table, kv_lens, Hkv: int, causal: bool, max_q=None, window: int = 0, scale=None,
@@ -409,12 +415,12 @@ def attnqat_fwd_kv4_ragged(q, cu_q, cache, num_pages, page_table, kv_lens, Hkv: 
     (qt, qh, q1), (ot, oh, o1) = q.stride(), o.stride()
     if not q1 == o1 == 1 and q.numel() > 0:
         _serve_refuse([], [("q", q, shape), ("out[0]", o, shape)])
-    max_q = max(T, 1) if max_q is None else int(max_q)
+    max_q, window = max(T, 1) if max_q is None else _within_int(max_q), _within_int(window)
     if workspace is None:
         workspace = torch.empty(max(kv4_ragged_workspace_bytes(T, B, Hq, Hkv, max_q, most, d), 1), dtype=_U8, device=q.device)
     elif workspace.get_device() != dev:
         raise AttnQatError("workspace must be on the device of the other tensors")
-    rc = (_lib or lib()).attnqat_fwd_kv4_ragged(q.data_ptr(), qt, qh, cu_q.data_ptr(), T, max_q, B, Hq, Hkv, d, int(causal), int(window), d ** -0.5 if scale is None else scale, BF16,
+    rc = (_lib or lib()).attnqat_fwd_kv4_ragged(q.data_ptr(), qt, qh, cu_q.data_ptr(), T, max_q, B, Hq, Hkv, d, 1 if causal else 0, window, d ** -0.5 if scale is None else scale, BF16,
                                                 cache.data_ptr(), _serve_pages(cache, num_pages, Hkv, d), page_table.data_ptr(), most, kv_lens.data_ptr(),
                                                 o.data_ptr(), ot, oh, None if lse is None else lse.data_ptr(), workspace.data_ptr(), workspace.nbytes, _stream_on(dev))
     if rc:

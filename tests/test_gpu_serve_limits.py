@@ -4,7 +4,7 @@ import pytest
 import torch
 
 from tests import serve_util as S
-from tests.test_gpu_serve import _plan_case, check_attention, dev, i32, run_attention
+from tests.test_gpu_serve import _plan_case, attention_case, check_attention, dev, i32, run_attention
 
 pytestmark = pytest.mark.gpu
 
@@ -20,6 +20,19 @@ def aq():
 def test_windows_with_more_queries_than_keys(aq, d, window):
     """Few rows and many; what lies before a sequence's first position is behind no window, however large."""
     run_attention(aq, [10, 3, 1, 40, 200, 7], [4, 0, 1, 0, 150, 300], 4, 2, d, window=window, seed=8)
+
+
+@pytest.mark.parametrize("kw", [dict(max_q=(1 << 32) + 1), dict(max_q=1 << 31), dict(window=(1 << 32) + 5), dict(window=1 << 31)])
+def test_numbers_beyond_32_bits_are_not_cut(aq, kw):
+    q, cu, cache, num_pages, table = attention_case([5, 60], [300, 200], 4, 2, 64, 1, tail=0)
+    args = (q.cuda(), i32(cu), dev(cache.reshape(-1)), num_pages, dev(table), i32([300, 200]), 2, True)
+    o, lse = aq.attnqat_fwd_kv4_ragged(*args)
+    out = torch.full_like(o, 5.0), torch.full_like(lse, 5.0)
+    aq.attnqat_fwd_kv4_ragged(*args, **kw, out=out)
+    assert torch.equal(out[0], o) and torch.equal(out[1], lse)
+    for kw in (dict(max_q=1 - (1 << 32)), dict(window=5 - (1 << 32))):
+        with pytest.raises(aq.AttnQatError):
+            aq.attnqat_fwd_kv4_ragged(*args, **kw)
 
 
 def _cache_with_a_first_key(kv, gap, noise, Hkv, d, rng):
