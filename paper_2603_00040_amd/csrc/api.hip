@@ -688,7 +688,7 @@ int attnqat_fwd_kv4_ragged(const void* q, int64_t q_token_stride, int64_t q_head
     int rc = ragged_dims(T, B, Hq, Hkv, max_q, max_pages, d);
     if (rc) return rc;
     if (dtype != ATTNQAT_BF16) return ATTNQAT_EDTYPE;
-    if (num_pages < 1 || window < 0 || (window > 0 && !causal) || !(scale > 0.0f) || !(scale < INFINITY)) return ATTNQAT_EINVAL;
+    if (num_pages < 1 || window < 0 || (window > 0 && !causal) || !(scale > 0.0f) || !(scale * 1.4426950408889634f < INFINITY)) return ATTNQAT_EINVAL;
     if (T == 0) return ATTNQAT_OK;
     if (!q || !cu_q || !cache || !page_table || !kv_lens || !o || ((uintptr_t)cache & 15)) return ATTNQAT_EINVAL;
     Rows qr, out;
