@@ -338,8 +338,8 @@ def attnqat_page_plan(kv_lens, new_lens, page_table, capacity: int, free=None, w
         pr, ps, po = ring.data_ptr(), state.data_ptr(), state_out.data_ptr()
     if workspace is None:
         workspace = torch.empty(max(page_plan_workspace_bytes(B), 1), dtype=_U8, device=kv_lens.device)
-    elif workspace.get_device() != dev:
-        raise AttnQatError("workspace must be on the device of the other tensors")
+    elif workspace.get_device() != dev or not workspace.is_contiguous():
+        raise AttnQatError("workspace must be contiguous, on the device of the other tensors")
     rc = (_lib or lib()).attnqat_page_plan(kv_lens.data_ptr(), new_lens.data_ptr(), B, page_table.data_ptr(), most, pr, places, ps, T, lens.data_ptr(), cu.data_ptr(),
                                            slots.data_ptr(), positions.data_ptr(), po, workspace.data_ptr(), workspace.nbytes, _stream_on(dev))
     if rc:
@@ -418,8 +418,8 @@ def attnqat_fwd_kv4_ragged(q, cu_q, cache, num_pages, page_table, kv_lens, Hkv: 
     max_q, window = max(T, 1) if max_q is None else _within_int(max_q), _within_int(window)
     if workspace is None:
         workspace = torch.empty(max(kv4_ragged_workspace_bytes(T, B, Hq, Hkv, max_q, most, d), 1), dtype=_U8, device=q.device)
-    elif workspace.get_device() != dev:
-        raise AttnQatError("workspace must be on the device of the other tensors")
+    elif workspace.get_device() != dev or not workspace.is_contiguous():
+        raise AttnQatError("workspace must be contiguous, on the device of the other tensors")
     rc = (_lib or lib()).attnqat_fwd_kv4_ragged(q.data_ptr(), qt, qh, cu_q.data_ptr(), T, max_q, B, Hq, Hkv, d, 1 if causal else 0, window, d ** -0.5 if scale is None else scale, BF16,
                                                 cache.data_ptr(), _serve_pages(cache, num_pages, Hkv, d), page_table.data_ptr(), most, kv_lens.data_ptr(),
                                                 o.data_ptr(), ot, oh, None if lse is None else lse.data_ptr(), workspace.data_ptr(), workspace.nbytes, _stream_on(dev))

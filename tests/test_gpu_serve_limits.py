@@ -35,6 +35,16 @@ def test_numbers_beyond_32_bits_are_not_cut(aq, kw):
             aq.attnqat_fwd_kv4_ragged(*args, **kw)
 
 
+def test_a_workspace_with_gaps_is_refused(aq):
+    """What lies between its bytes is not the call's."""
+    q, cu, cache, num_pages, table = attention_case([1, 2], [30, 20], 4, 2, 64, 1, tail=0)
+    wide = torch.zeros((1 << 20, 2), dtype=torch.uint8, device="cuda")
+    with pytest.raises(aq.AttnQatError):
+        aq.attnqat_fwd_kv4_ragged(q.cuda(), i32(cu), dev(cache.reshape(-1)), num_pages, dev(table), i32([30, 20]), 2, True, workspace=wide[:, 0])
+    with pytest.raises(aq.AttnQatError):
+        aq.attnqat_page_plan(i32([1, 2]), i32([1, 3]), i32([[0], [1]]), 4, workspace=wide[:, 0])
+
+
 def _cache_with_a_first_key(kv, gap, noise, Hkv, d, rng):
     """One sequence: the first key's score lies `gap` above the others' for a query of ones times gap / sqrt(d), and its value is zero; the others' values
     are 1 and 1.5, their keys zero or (noise) random."""
