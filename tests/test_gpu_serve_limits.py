@@ -35,6 +35,22 @@ def test_numbers_beyond_32_bits_are_not_cut(aq, kw):
             aq.attnqat_fwd_kv4_ragged(*args, **kw)
 
 
+@pytest.mark.parametrize("n,kv,max_q", [([5, 2], [300, 20], 3), ([150, 40, 1], [400, 40, 9], 100), ([150, 97, 3], [150, 500, 9], 96), ([130, 300], [90, 700], 7)])
+@pytest.mark.parametrize("G,causal", [(1, True), (2, True), (1, False)])
+def test_sequences_cut_by_max_q(aq, n, kv, max_q, G, causal):
+    """The first max_q rows of a sequence as if there were no others, the rest left alone."""
+    q, cu, cache, num_pages, table = attention_case(n, kv, 2 * G, 2, 64, 1, tail=2)
+    o, lse = torch.full(q.shape, 5.0, dtype=torch.bfloat16, device="cuda"), torch.full(q.shape[:2], 5.0, device="cuda")
+    aq.attnqat_fwd_kv4_ragged(q.cuda(), i32(cu), dev(cache.reshape(-1)), num_pages, dev(table), i32(kv), 2, causal, max_q=max_q, out=(o, lse))
+    m = np.minimum(n, max_q)
+    rows = np.concatenate([cu[b] + np.arange(m[b]) for b in range(len(n))])
+    ref = S.attend(q.double().numpy()[rows], np.concatenate([[0], np.cumsum(m)]), cache, table, kv, 2, causal, 0, 1.0 / 8.0)
+    at = torch.from_numpy(rows).cuda()
+    check_attention(o[at], lse[at], ref)
+    o[at], lse[at] = 5.0, 5.0
+    assert bool((o == 5.0).all()) and bool((lse == 5.0).all())
+
+
 def test_a_workspace_with_gaps_is_refused(aq):
     """What lies between its bytes is not the call's."""
     q, cu, cache, num_pages, table = attention_case([1, 2], [30, 20], 4, 2, 64, 1, tail=0)
