@@ -73,6 +73,24 @@ __device__ inline Few few_of(const RaggedArgs& a, const Seq& s, const Group& G)
 }
 __device__ inline int few_units(const Few& u) { return u.tiles * u.units; }      // of a head
 __device__ inline Seq uniform_seq(const Seq& s) { return Seq{uniform(s.first), uniform(s.n), uniform(s.len)}; }
+// The first sequence from b on that has work for a kernel (has(s)), and its index: a wave asks 64 at a time, since a step's places that are idle, or the other
+// kernel's, may be thousands (three prompts far apart among 4096 idle places: one after the other 770 us, so 224).  a.B: there is none.
+template <class Has>
+__device__ inline Seq next_seq(const RaggedArgs& a, int& b, const Has& has)
+{
+    const int lane = threadIdx.x & 63;
+    for (; b < a.B; b += 64) {
+        const Seq s = b + lane < a.B ? seq_of(a, b + lane) : Seq{0, 0, 0};
+        const unsigned long long hit = __builtin_amdgcn_ballot_w64(has(s));
+        if (hit != 0) {
+            const int src = (int)__builtin_ctzll(hit);
+            b += src;
+            return Seq{__builtin_amdgcn_readlane(s.first, src), __builtin_amdgcn_readlane(s.n, src), __builtin_amdgcn_readlane(s.len, src)};
+        }
+    }
+    b = a.B;
+    return Seq{0, 0, 0};
+}
 
 // Codes and scale bytes of D / 4 values of one key: lane (key cc of 16, group g) holds d = (D/4) g .. + D/4 - 1.  (The scale bytes as the dword that they
 // lie in: of a narrower load the compiler makes the widening an instruction of its own, which waits for the load wherever it puts it.)
@@ -401,12 +419,12 @@ __global__ __launch_bounds__(256, RT == 1 ? 3 : 2) void ragged_few_kernel(const 
         // on to the next head, sequence (there is one while w < w_end; a sequence of the other kernel, or without a key, has no units)
         off = 0;
         if (++ht == a.Hkv * u.tiles) {
+            if (w >= w_end) return;
             ht = 0;
-            do {
-                if (++b >= a.B) return;
-                s = uniform_seq(seq_of(a, b));
-                u = few_of<D, ROWS>(a, s, G);
-            } while (w < w_end && u.units == 0);
+            ++b;
+            s = next_seq(a, b, [&](const Seq& x) { return few_of<D, ROWS>(a, x, G).units > 0; });
+            if (b >= a.B) return;                                 // (lengths that change under the launch)
+            u = few_of<D, ROWS>(a, s, G);
         }
     }
 }
@@ -599,21 +617,22 @@ __global__ __launch_bounds__(512, 2) void ragged_wide_kernel(const RaggedArgs a,
 
     int tile = -1, h = 0, off = 0, t0 = 0, nt = 0;                 // tile < 0: to be looked up
     int id_lane = 0, id_b = -1, id_first = 0;                      // lane i: the id of page id_first + i of sequence id_b, -1: outside the cache
-    Seq s{0, 0, 0};
+    Seq s = uniform_seq(seq_of(a, b));
     while (w < w_end) {
         if (tile < 0) {
             // the row tile of a sequence's work that w lies in
-            if (b >= a.B) return;
-            s = uniform_seq(seq_of(a, b));
+            if (per == 0) {                                       // (of many rows and a key: the last row sees one)
+                s = next_seq(a, b, [&](const Seq& x) { return x.n * G > kFewRows && x.len > 0; });
+                if (b >= a.B) return;                             // (lengths that change under the launch)
+            }
             const int tiles = (s.n * G + kWideRows - 1) / kWideRows;
-            if (per == 0 && s.n * G > kFewRows) {
+            if (per == 0) {
                 for (int r0 = 0; r0 < tiles; r0 += 64) {
                     int x0, n = 0;
                     if (r0 + lane < tiles) wide_tile(a, s, G, r0 + lane, x0, n);
                     per += lane_total(n);                         // (64 row tiles of at most 2^14 key tiles)
                 }
             }
-            if (per == 0) { ++b; continue; }                      // (a sequence of the other kernel, or without a key)
             const long long in_seq = w - front * a.Hkv;
             h = (int)(in_seq / per);
             long long rem = in_seq % per;
@@ -946,26 +965,32 @@ __device__ void wide_merge(const RaggedArgs& a, const WideWs& ws, int place, int
     }
     if (j == 0 && half == 0 && a.lse) a.lse[(size_t)(s.first + tok) * a.Hq + head] = l != 0.0f ? M * 0.6931471805599453f + logf(l) : -INFINITY;
 }
-// O = 0, lse = -inf for row tiles, of sequences with many rows, that see no key: they are nobody's work.  One of n workgroups.
+// O = 0, lse = -inf for row tiles, of sequences with many rows, that see no key: they are nobody's work.  One of n workgroups, which has every n-th sequence
+// and asks for the lengths of 64 of them at once.
 template <int D>
 __device__ void wide_empty(const RaggedArgs& a, int which, int n)
 {
     const Group G = group_of(a);
-    for (int b = which; b < a.B; b += n) {
-        const Seq s = seq_of(a, b);
-        const int rows = s.n * G;
-        if (rows <= kFewRows) continue;
-        for (int tile = 0; tile * kWideRows < rows; ++tile) {
-            int t0, nt;
-            wide_tile(a, s, G, tile, t0, nt);
-            if (nt > 0) break;                                    // (the ones behind it see keys as well)
-            const int r1 = min((tile + 1) * kWideRows, rows);
-            for (int h = 0; h < a.Hkv; ++h)
-                for (int e = threadIdx.x; e < (r1 - tile * kWideRows) * (D / 8); e += 256) {
-                    const int row = tile * kWideRows + e / (D / 8), d = e % (D / 8) * 8, head = h * G + row % G;
-                    *reinterpret_cast<uint4v*>(a.o + (size_t)(s.first + row / G) * a.o_token + (size_t)head * a.o_head + d) = uint4v{0u, 0u, 0u, 0u};
-                    if (d == 0 && a.lse) a.lse[(size_t)(s.first + row / G) * a.Hq + head] = -INFINITY;
-                }
+    const int lane = threadIdx.x & 63;
+    for (int b0 = which; b0 < a.B; b0 += 64 * n) {
+        const Seq mine = b0 + lane * n < a.B ? seq_of(a, b0 + lane * n) : Seq{0, 0, 0};
+        int t0, nt = 1;
+        if (mine.n * G > kFewRows) wide_tile(a, mine, G, 0, t0, nt);
+        for (unsigned long long left = __builtin_amdgcn_ballot_w64(nt == 0); left != 0; left &= left - 1) {
+            const int src = (int)__builtin_ctzll(left);
+            const Seq s{__builtin_amdgcn_readlane(mine.first, src), __builtin_amdgcn_readlane(mine.n, src), __builtin_amdgcn_readlane(mine.len, src)};
+            const int rows = s.n * G;
+            for (int tile = 0; tile * kWideRows < rows; ++tile) {
+                wide_tile(a, s, G, tile, t0, nt);
+                if (nt > 0) break;                                // (the ones behind it see keys as well)
+                const int r1 = min((tile + 1) * kWideRows, rows);
+                for (int h = 0; h < a.Hkv; ++h)
+                    for (int e = threadIdx.x; e < (r1 - tile * kWideRows) * (D / 8); e += 256) {
+                        const int row = tile * kWideRows + e / (D / 8), d = e % (D / 8) * 8, head = h * G + row % G;
+                        *reinterpret_cast<uint4v*>(a.o + (size_t)(s.first + row / G) * a.o_token + (size_t)head * a.o_head + d) = uint4v{0u, 0u, 0u, 0u};
+                        if (d == 0 && a.lse) a.lse[(size_t)(s.first + row / G) * a.Hq + head] = -INFINITY;
+                    }
+            }
         }
     }
 }

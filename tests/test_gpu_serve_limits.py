@@ -51,6 +51,50 @@ def test_sequences_cut_by_max_q(aq, n, kv, max_q, G, causal):
     assert bool((o == 5.0).all()) and bool((lse == 5.0).all())
 
 
+@pytest.mark.parametrize("n", [1, 3, 150])
+@pytest.mark.parametrize("Hkv", [1, 3])
+def test_sequences_far_apart(aq, n, Hkv):
+    """Idle places, places of the other kernel and places without a key between sequences whose heads and pages do not divide evenly: each finds the next."""
+    for B, at in ((700, (0, 65, 66, 130, 400, 699)), (1300, (3, 640, 1299)), (129, (0, 64, 128))):
+        ns, kv = [0] * B, [0] * B
+        for i, b in enumerate(at):
+            ns[b], kv[b] = n, 200 + 77 * i
+        for b in (1, 70, B - 2):                                  # of the other kernel, and with nothing to see
+            ns[b], kv[b] = 120 if n == 1 else 1, 150
+        ns[2], kv[2] = 110, 0
+        run_attention(aq, ns, kv, 2 * Hkv, Hkv, 64, seed=B)
+
+
+def test_idle_places_are_passed_by_in_no_time(aq):
+    """Three prompts far apart among idle places of a step against the three alone.  One look at the lengths per place would be eight times their time; asked
+    for 64 at once it is less than twice, most of it the sums over the lengths that every workgroup makes."""
+    rng = np.random.default_rng(1)
+    Hq, Hkv, d = 32, 8, 128
+    kv, n = [3900, 4000, 4100], 700
+    cache = dev(S.random_cache(33, Hkv, d, rng).reshape(-1))
+    q = torch.randn(3 * n, Hq, d, device="cuda").bfloat16()
+    times, outs = [], []
+    for B in (3, 8192):
+        lens, ns = np.zeros(B, int), np.zeros(B, int)
+        lens[[0, B // 2, B - 1]], ns[[0, B // 2, B - 1]] = kv, n
+        table = i32(np.tile(np.arange(33), (B, 1)))
+        args = (q, i32(np.concatenate([[0], np.cumsum(ns)])), cache, 33, table, i32(lens), Hkv, True)
+        ws = torch.empty(aq.kv4_ragged_workspace_bytes(3 * n, B, Hq, Hkv, n, 33, d), dtype=torch.uint8, device="cuda")
+        t = []
+        for _ in range(6):
+            start, end = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+            start.record()
+            for _ in range(4):
+                out = aq.attnqat_fwd_kv4_ragged(*args, max_q=n, workspace=ws)
+            end.record()
+            end.synchronize()
+            t.append(start.elapsed_time(end))
+        times.append(min(t))
+        outs.append(out)
+    assert torch.equal(outs[0][0], outs[1][0]) and torch.equal(outs[0][1], outs[1][1])
+    assert times[1] < 4 * times[0], times
+
+
 def test_a_workspace_with_gaps_is_refused(aq):
     """What lies between its bytes is not the call's."""
     q, cu, cache, num_pages, table = attention_case([1, 2], [30, 20], 4, 2, 64, 1, tail=0)
