@@ -27,10 +27,12 @@ namespace {
 // 4 of 16 000 keys: 40 rows 59 against 75, 120 rows 91 against 81.
 constexpr int kFewRows = 96;
 // The reference that a row's exponents are taken against, in powers of two, is set where the row's largest probability becomes 2^kTop, and follows the running
-// maximum only when that would make it more than 2^kTopMost, half of what fp16 holds: most tiles need no rescaling of O, though some row of 32 has a
+// maximum only when that would make it more than 2^kTopMost, just below what fp16 holds: most tiles need no rescaling of O, though some row of 32 has a
 // new maximum in most of the first fifty tiles.  The higher the one, the smaller the probabilities that keep all their bits; the nearer to the other, the more
-// often O is rescaled where scores spread widely (six prompts, four channels of K times 20: kTop 7 225 us, 9 226, 11 229; scores of deviation 1: even).
-constexpr float kTop = 11.0f, kTopMost = 15.0f;
+// often O is rescaled where scores spread widely (six prompts, four channels of K times 20, kTopMost 15: kTop 7 225 us, 9 226, 11 229; scores of deviation 1: even).
+constexpr float kTop = 11.0f, kTopMost = 15.9f;
+// The score up to which that holds (no score beyond, whatever is rounded here): a tile's largest is compared as it comes out of the product.
+__device__ inline float score_up_to(float m, float c_row) { return fmaf(fabsf(m), -0x1p-20f, m + (kTopMost - 0x1p-10f)) * __builtin_amdgcn_rcpf(c_row); }
 constexpr int kWideStart = 5;         // (13 000 cycles against 3400; six prompts of 766 - 3846 tokens: with 4 253.6 us, 5 251.7, 6 255.0, 7 255.4)
 constexpr int kWideRows = 256;        // rows of a tile of the other one
 
@@ -288,10 +290,10 @@ __global__ __launch_bounds__(256, RT == 1 ? 3 : 2) void ragged_few_kernel(const 
         const int see_first = a.window > 0 ? s.len - s.n + (r0 + rows - 1) / G - a.window + 1 : 0, see_last = a.causal ? min(s.len - s.n + r0 / G, s.len - 1) : s.len - 1;
 
         floatx4 o[RT][NDT];
-        float m[RT], l[RT];                                       // the reference (kTop)
+        float m[RT], up_to[RT], l[RT];                                       // the reference (kTop)
 #pragma unroll
         for (int rt = 0; rt < RT; ++rt) {
-            m[rt] = -INFINITY; l[rt] = 0.0f;
+            m[rt] = up_to[rt] = -INFINITY; l[rt] = 0.0f;
 #pragma unroll
             for (int dt = 0; dt < NDT; ++dt) o[rt][dt] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
         }
@@ -334,9 +336,10 @@ __global__ __launch_bounds__(256, RT == 1 ? 3 : 2) void ragged_few_kernel(const 
                 float mx = max_nc(max_nc(max_nc(sc[rt][0][0], sc[rt][0][1]), max_nc(sc[rt][0][2], sc[rt][0][3])),
                                   max_nc(max_nc(sc[rt][1][0], sc[rt][1][1]), max_nc(sc[rt][1][2], sc[rt][1][3])));
                 mx = lanes_max<16, 32>(mx);
-                if (__builtin_amdgcn_ballot_w64(fmaf(mx, c_row[rt], -m[rt]) > kTopMost) != 0) {
+                if (__builtin_amdgcn_ballot_w64(mx > up_to[rt]) != 0) {
                     const float m_new = fmaxf(m[rt], fmaf(mx, c_row[rt], -kTop)), alpha = __builtin_amdgcn_exp2f(m[rt] - (m_new == -INFINITY ? 0.0f : m_new));
                     m[rt] = m_new;
+                    up_to[rt] = score_up_to(m_new, c_row[rt]);
                     l[rt] *= alpha;
 #pragma unroll
                     for (int dt = 0; dt < NDT; ++dt) o[rt][dt] *= alpha;
@@ -767,7 +770,7 @@ __global__ __launch_bounds__(512, 2) void ragged_wide_kernel(const RaggedArgs a,
         unpack(raw0, on0, 0, 0);
         if (!is_v) unpack(raw1, on1, 1, 0);
         floatx16 o[NB], sc[2];
-        float m = -INFINITY, l = 0.0f;                             // the reference (kTop)
+        float m = -INFINITY, up_to = -INFINITY, l = 0.0f;                             // the reference (kTop)
         half8 pt[4];
 #pragma unroll
         for (int i = 0; i < NB; ++i)
@@ -837,9 +840,10 @@ __global__ __launch_bounds__(512, 2) void ragged_wide_kernel(const RaggedArgs a,
 #pragma unroll
                 for (int j = 0; j < 16; ++j) mx = max_nc(mx, sc[kb][j]);
             mx = lanes_max<32, 32>(mx);
-            if (__builtin_amdgcn_ballot_w64(fmaf(mx, c_row, -m) > kTopMost) != 0) {
+            if (__builtin_amdgcn_ballot_w64(mx > up_to) != 0) {
                 const float m_new = fmaxf(m, fmaf(mx, c_row, -kTop)), alpha = __builtin_amdgcn_exp2f(m - (m_new == -INFINITY ? 0.0f : m_new));
                 m = m_new;
+                up_to = score_up_to(m_new, c_row);
                 l *= alpha;
 #pragma unroll
                 for (int i = 0; i < NB; ++i) o[i] *= alpha;
