@@ -444,7 +444,8 @@ int attnqat_debug_fwd_infer_paged(const void* q, int B, int Hq, int Hkv, int Lq,
  * row's largest by 2^-36 of it; scores, sums and O are fp32, and rows whose scores reach 2^26 in magnitude may come out as NaN), as for a
  * model that was not trained for Alg. 1; attnqat_fwd_infer_paged is Alg. 1.  q [T,Hq,d]; sequence b has kv_lens[b] keys, the last of which belong to
  * its rows: row i of n sees keys 0 .. kv_lens[b] - n + i with causal != 0, of those the last `window` if window > 0 (causal only; max_pages * 128 and
- * more hide nothing), and all keys with causal = 0.  max_q: no sequence has more rows (of one that has, the first max_q are computed as if there were no others).  A row without a key gets o = 0, lse = -inf.  o [T,Hq,d] bf16; lse
+ * more hide nothing), and all keys with causal = 0.  max_q: no sequence has more rows (of one that has, the first max_q are computed as if there were no others); the
+ * kernels are chosen by it, so a decode step should say 1 and not T.  A row without a key gets o = 0, lse = -inf.  o [T,Hq,d] bf16; lse
  * [T,Hq] fp32 (natural log), may be NULL; rows behind cu_q[B] are left as they are.  o and lse must not lie over q.  scale > 0, and scale log2 e
  * a finite fp32 number.
  * Positions of a page table entry outside [0, num_pages) read as zeros; positions from kv_lens[b] on are never used, whatever their slots

@@ -306,7 +306,7 @@ def attnqat_page_plan(kv_lens, new_lens, page_table, capacity: int, free=None, w
     """Page table, slots and positions of a serving step.  kv_lens, new_lens int32 [B]: positions that the requests have and want;
     page_table int32 [B,max_pages], updated in place; ``capacity`` the most new positions of the step; ``free`` = (free_pages int32 [places],
     free_state int32 [>= 2]: place of the first free page, number of free pages), a ring from which pages are taken and to which they are given
-    back (updated in place), or None for a table that is complete already.  Returns (kv_lens int32 [B], cu_q int32 [B+1], slots int64 [capacity],
+    back (updated in place; as many places as the cache has pages are always enough), or None for a table that is complete already.  Returns (kv_lens int32 [B], cu_q int32 [B+1], slots int64 [capacity],
     positions int32 [capacity], free_state int32 [3]: first free place, free pages, refused requests, or None without ``free``).  ``out``: those
     five; the first and the last may be kv_lens and a free_state of 3."""
     B, T, dev = kv_lens.numel(), int(capacity), kv_lens.get_device()
@@ -397,7 +397,8 @@ def attnqat_fwd_kv4_ragged(q, cu_q, cache, num_pages, page_table, kv_lens, Hkv: 
                            workspace=None, out=None):
     """Attention over an NVFP4 KV cache, Q and the probabilities not quantized, of sequences with different numbers of queries.  q [T,Hq,d] bf16 (any stride
     per row and head), rows cu_q[b] .. cu_q[b+1]-1 (int32 [B+1]) being the last positions of sequence b, which has kv_lens[b] keys (int32 [B]) in the
-    pages page_table[b] (int32 [B,max_pages]).  ``max_q``: the most rows of a sequence (default T); ``window`` (causal only): a row sees that many keys at
+    pages page_table[b] (int32 [B,max_pages]).  ``max_q``: the most rows of a sequence (default T; the
+    kernels are chosen by it, and a decode step that does not say 1 pays for those of many rows); ``window`` (causal only): a row sees that many keys at
     most, its own position included; ``scale``: default 1/sqrt(d).  Returns (o bf16 [T,Hq,d], lse fp32 [T,Hq]); ``out``: those two (lse may be None)."""
     shape, dev, B = q.shape, q.get_device(), kv_lens.numel()
     if len(shape) != 3 or page_table.dim() != 2:

@@ -24,7 +24,7 @@ namespace {
 
 // Most rows of a (sequence, kv head) that the kernel for few rows takes, in tiles of 16 or 32 that read the keys each for itself; more go to the one that has
 // tiles of 256.  Few -> many, 16 sequences of 4096 keys, 8 kv heads of 128: 48 rows 56 against 78 us, 80 rows 76 against 79, 128 rows 84 against 87;
-// 4 of 16 000 keys: 40 rows 59 against 75, 120 rows 91 against 81.
+// 4 of 16 000 keys: 40 rows 59 against 75, 120 rows 91 against 81.  (Not measured where a window leaves fewer keys to see.)
 constexpr int kFewRows = 96;
 // The reference that a row's exponents are taken against, in powers of two, is set where the row's largest probability becomes 2^kTop, and follows the running
 // maximum only when that would make it more than 2^kTopMost, just below what fp16 holds: most tiles need no rescaling of O, though some row of 32 has a
@@ -33,7 +33,9 @@ constexpr int kFewRows = 96;
 constexpr float kTop = 11.0f, kTopMost = 15.9f;
 // The score up to which that holds (no score beyond, whatever is rounded here): a tile's largest is compared as it comes out of the product.
 __device__ inline float score_up_to(float m, float c_row) { return fmaf(fabsf(m), -0x1p-20f, m + (kTopMost - 0x1p-10f)) * __builtin_amdgcn_rcpf(c_row); }
-constexpr int kWideStart = 5;         // (13 000 cycles against 3400; six prompts of 766 - 3846 tokens: with 4 253.6 us, 5 251.7, 6 255.0, 7 255.4)
+// What the start and the end of a row tile weigh in tiles of keys: 13 000 cycles against 3200 (heads of 64: 2600), and a piece of a row tile that ends a
+// workgroup's work is joined later.  (Six prompts of 766 - 3846 tokens, heads of 128: with 4 253.6 us, 5 251.7, 6 255.0, 7 255.4.)
+constexpr int kWideStart = 5;
 constexpr int kWideRows = 256;        // rows of a tile of the other one
 
 // The query heads of a kv head, and whole division by their number: x / G = x mul >> 31 + shift with mul = ceil(2^(31 + shift) / G), 2^shift >= G, exact for
@@ -165,7 +167,7 @@ struct FewWs { int* quota; int* front /* [B + 1] */; float* part_o /* [workgroup
 // launch that makes a list would cost more).  Its four waves take 32 keys of every page, each with its own maximum, sum and O; the pages of
 // the next iteration are requested before the present ones are used.  One query of 32 sequences of 4096 - 16384 keys, 32/8 heads of 128: 326 MB in 61 us,
 // 5.3 TB/s, what a copy reaches.  With more rows and short segments the vector instructions bound it (unpacking, softmax: a wave issues one
-// in 9 cycles) and the start of a segment: one to six queries of 40 sequences of 300 - 9000 keys, 16/4 heads of 64, 34 MB in 16.9 us.
+// in 9 cycles) and the start of a segment: one to six queries of 40 sequences of 300 - 9000 keys, 16/4 heads of 64, 34 MB in 16.7 us.
 template <int D, int RT /* 16-row groups of a unit */>
 __global__ __launch_bounds__(256, RT == 1 ? 3 : 2) void ragged_few_kernel(const RaggedArgs a, const FewWs ws)
 {
@@ -544,10 +546,11 @@ struct WideWs { long long* quota; WideRec* rec; float* part_o /* [workgroup][2][
 // tile's S, and between these products unpacks its half of the keys of a K and a V tile into LDS (K as operands of the matrix instruction, V key by
 // key), the other does the softmax, so that every SIMD has a wave for either unit.  The work (row tile, key tile) is dealt out evenly as in the
 // kernel for few rows.
-// Rates over 40 passes, in operations that the mask leaves: 8192 queries and keys, 32/8 heads of 128, 1170 TFLOP/s without a mask (937 us), 1070 causal; 8 x 512
-// queries over 8192 keys each 1090; 16/4 heads of 64, 16384 queries, 8192 keys 890.  The products with their barriers alone would run at 1550, with
-// their operands out of LDS and the pages' loads at 1375 (a large library product: 1280): the rest is that a wave issues a vector instruction
-// in 9 cycles, and that a tile has 180 of them beside 1024 cycles of products.  Also tried: softmax and products of a wave in one stream (5 % slower, heads
+// Rates over 20 passes and more, in operations that the mask leaves: 8192 queries and keys, 32/8 heads of 128, 1110 TFLOP/s without a mask (988 us), 1030 causal;
+// 8 x 512 queries over 8192 keys each 1040; 16/4 heads of 64, 16384 queries and keys, 870.  The products with their barriers alone would run at 1550, with
+// their operands out of LDS and the pages' loads at 1375 (a large library product: 1280).  A wave's phases of a tile, in cycles: heads of 128 vector 1350 and
+// 180 of waiting, matrix 1590 (1024 of products) and 75; heads of 64 vector 1165 and 70, matrix 1070 (512) and 310: the matrix phase bounds the one, the
+// vector phase the other.  Also tried: softmax and products of a wave in one stream (5 % slower, heads
 // of 64 2 %), four waves of 32 rows and two workgroups to a compute unit without phases (10 %), the unpacking shared between the phases (5 %).
 template <int D>
 __global__ __launch_bounds__(512, 2) void ragged_wide_kernel(const RaggedArgs a, const WideWs ws)

@@ -181,8 +181,8 @@ __global__ __launch_bounds__(256) void plan_fill_kernel(const PlanArgs a, int ro
 }
 
 // A row (token, kv head) of K or V is D / 16 blocks; a thread takes a block of kAppendRows rows, which are under way at once.  Rows are taken token by
-// token, all heads of a token after each other: they lie side by side in memory.  Bound by memory: 21 300 tokens, 8 heads of 128, 21.4 us (87 MB read, 25 MB
-// written, 5.2 TB/s, where a large copy reaches 5.1); 40 tokens 2.7 us, a launch.  (Half a block per thread, to store 1 KiB at once: the same.)
+// token, all heads of a token after each other: they lie side by side in memory.  Bound by memory: 21 300 tokens, 8 heads of 128, 87 MB read, 25 MB
+// written: 26.7 us, 4.2 TB/s, of rows that no cache holds, 21.3 us again on the same ones; 40 tokens 2.6 us, a launch.  (Half a block per thread, to store 1 KiB at once: the same.)
 constexpr int kAppendRows = 2;
 template <int D>
 __global__ __launch_bounds__(256) void append_kernel(const uint16_t* __restrict__ k, const uint16_t* __restrict__ v, size_t k_token, size_t k_head,
