@@ -16,6 +16,10 @@
  *   attnqat_kv_cache_*, attnqat_fwd_infer_mx_paged       an FP4 KV cache in pages and the forward over it
  *   attnqat_page_plan, attnqat_kv_cache_append, attnqat_kv_cache_read, attnqat_fwd_kv4_ragged
  *                                       a serving step of sequences with different numbers of new positions, over an NVFP4 cache
+ *   attnqat_kv_summarize, attnqat_kv_select, attnqat_fwd_kv4_sparse
+ *                                       the same step over a choice of pages for every query
+ *   attnqat_rope_fwd, attnqat_rope_bwd, attnqat_kv_cache_append_rope
+ *                                       rotary positions in one to four axes, in training and on the way into the cache
  *   attnqat_fwd_infer_mx_sparse                          block-sparse attention
  *
  * Conventions shared by every entry point
@@ -466,6 +470,82 @@ int attnqat_fwd_kv4_ragged(const void* q, int64_t q_token_stride, int64_t q_head
                            const void* cache, int num_pages, const int* page_table, int max_pages, const int* kv_lens,
                            void* o, int64_t o_token_stride, int64_t o_head_stride, float* lse,
                            void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Rotary positions.  A rotary table says how a head's values turn: pair i of `pairs` by the angle p freq[i], p the position in axis axis[i] (time, height
+ * and width of a video's token, say) and freq[i] radians per position: (a, b) -> (a cos - b sin, a sin + b cos).  layout ATTNQAT_ROPE_PAIRED: pair i is
+ * elements 2i and 2i+1; ATTNQAT_ROPE_HALVES: elements i and i + pairs (pairs a multiple of 8: ATTNQAT_ESHAPE otherwise).  1 <= pairs <= d / 2, 1 to
+ * ATTNQAT_ROPE_MAX_AXES axes, finite frequencies: ATTNQAT_EINVAL otherwise; elements from 2 pairs on stay as they are, bit for bit.  The table is HOST
+ * memory and read during the call.  Angles are exact to 2^-32 turns and |p| 2^-52 times the frequency, however far the position; turned values are
+ * computed in fp32 and rounded once, to bf16.
+ *
+ * attnqat_rope_fwd turns q [B,Hq,L,d] and k [B,Hkv,L,d] into q_out and k_out: what attnqat_fwd and its kind take, where these are contiguous.  All four have d
+ * innermost and any stride per batch, head and token (in elements, multiples of 8; pointers 16-byte aligned), such as the views of one projection's
+ * output.  positions (device int32): entry [b * positions_batch + l * axes + a] is the position of token l of batch b in axis a (positions_batch 0: the
+ * same for every batch).  Hkv = 0: k is left out.  An output may be its own input (the same pointer and strides); beyond that outputs share no element
+ * with anything.  B L <= 2^28.
+ * attnqat_rope_bwd is its gradient: from those of q_out and k_out (any strides) to those of q and k (any strides), the same turn the other way.
+ *
+ * attnqat_kv_cache_append_rope is attnqat_kv_cache_append with q and k turned on the way: row t of k is turned by positions[t * axes + a], rounded to bf16
+ * and quantized into its slot (the bits of attnqat_rope_fwd followed by attnqat_kv_cache_append), v as there, and row t of q [T,Hq,d] goes
+ * turned to q_out, also where its slot is outside the cache.  q_out may be q (the same pointer and strides).  Hq = 0: no q.
+ */
+#define ATTNQAT_ROPE_PAIRED         0
+#define ATTNQAT_ROPE_HALVES         1
+#define ATTNQAT_ROPE_MAX_AXES       4
+typedef struct attnqat_rope {
+    int pairs, axes, layout, reserved;
+    double freq[64];
+    uint8_t axis[64];
+} attnqat_rope;
+int attnqat_rope_fwd(const void* q, int64_t q_batch_stride, int64_t q_head_stride, int64_t q_token_stride,
+                     const void* k, int64_t k_batch_stride, int64_t k_head_stride, int64_t k_token_stride,
+                     int B, int Hq, int Hkv, int L, int d, int dtype, const int* positions, int64_t positions_batch, const attnqat_rope* rope,
+                     void* q_out, int64_t qo_batch_stride, int64_t qo_head_stride, int64_t qo_token_stride,
+                     void* k_out, int64_t ko_batch_stride, int64_t ko_head_stride, int64_t ko_token_stride, void* stream);
+int attnqat_rope_bwd(const void* dq_out, int64_t qo_batch_stride, int64_t qo_head_stride, int64_t qo_token_stride,
+                     const void* dk_out, int64_t ko_batch_stride, int64_t ko_head_stride, int64_t ko_token_stride,
+                     int B, int Hq, int Hkv, int L, int d, int dtype, const int* positions, int64_t positions_batch, const attnqat_rope* rope,
+                     void* dq, int64_t q_batch_stride, int64_t q_head_stride, int64_t q_token_stride,
+                     void* dk, int64_t k_batch_stride, int64_t k_head_stride, int64_t k_token_stride, void* stream);
+int attnqat_kv_cache_append_rope(const void* q, int64_t q_token_stride, int64_t q_head_stride, const void* k, int64_t k_token_stride, int64_t k_head_stride,
+                                 const void* v, int64_t v_token_stride, int64_t v_head_stride, int T, int Hq, int Hkv, int d, int dtype,
+                                 const int* positions, const attnqat_rope* rope, void* cache, int num_pages, const int64_t* slots,
+                                 void* q_out, int64_t qo_token_stride, int64_t qo_head_stride, void* stream);
+
+/*
+ * A serving step whose queries attend to a choice of their sequence's pages (arguments not described here: as for attnqat_fwd_kv4_ragged, always causal).
+ *
+ * attnqat_kv_summarize keeps the mean of the keys of every page.  For every row t whose slot is the last of a page (slots[t] % 128 == 127, inside the cache), once
+ * its page is complete, so behind attnqat_kv_cache_append of the same slots: per kv head S_c = sum of the 128 keys' values of channel c; with
+ * max |S_c| 2^10 in [2^(b-1), 2^b), e = b - 7 (-7 where all are 0): codes RNE(S_c 2^(10-e)), at most 127 in magnitude, and scale 2^(e-17), so that
+ * code * scale is the mean of the keys.  Summary: num_pages * attnqat_kv_summary_page_bytes(Hkv, d) bytes, 16-byte aligned, page by page, per head
+ * d int8 codes, the scale (fp32) and 12 bytes that nobody reads.  Pages that are not complete need no entry: they are never compared.  (Slots made by the
+ * caller, page * 128 + 127, summarize the pages of a cache filled in another way.)
+ *
+ * attnqat_kv_select chooses, for row t at position p of its sequence and every kv head, n_blocks of the pages 0 .. p / 128 (all of them where there are no more):
+ * the first `first`, the last `last` (>= 1: the row's own page among them) and of the rest those of the highest score, the lower page where scores are
+ * equal.  The score of a page is the largest over the query heads of the group of (q8 . code), times the page's scale, q8 = RNE(q 2^(6-x)) limited to
+ * +-127, 2^x <= largest |q| of the group < 2^(x+1): whole numbers and a power of two, so that the choice is the same however it is computed.
+ * A page whose table entry lies outside the cache scores 0.  blocks int32 [T,Hkv,n_blocks]: page numbers of the sequence, ascending, -1 behind them; rows
+ * behind cu_q[B] are left as they are.  q: the rows that attention takes (turned).  first + last <= n_blocks <= 1024.  max_q: the most rows of a
+ * sequence, by which the work is laid out; less than the truth costs time and changes nothing.
+ *
+ * attnqat_fwd_kv4_sparse is attnqat_fwd_kv4_ragged (causal, no window) over those of a row's keys that lie in its pages: blocks as above, or
+ * any other choice; entries that are negative or behind the row's own page are passed over, the same page twice counts once, and a row without a key gets o = 0,
+ * lse = -inf.  Rows that stand side by side share what they read, so they cost less where their pages are the same.  Sums are taken in an order that follows from
+ * the sizes alone: the same bits every time.  blocks, o and lse lie over nothing else.  Workspace: attnqat_kv4_sparse_workspace_bytes(), 16-byte aligned.
+ * Both: T Hq <= 2^28, T Hkv ceil(Hq / Hkv / 16) <= 2^23.
+ */
+size_t attnqat_kv_summary_page_bytes(int Hkv, int d);
+int attnqat_kv_summarize(const void* cache, int num_pages, const int64_t* slots, int T, int Hkv, int d, void* summary, void* stream);
+int attnqat_kv_select(const void* q, int64_t q_token_stride, int64_t q_head_stride, const int* cu_q, int T, int max_q, int B, int Hq, int Hkv, int d, int dtype,
+                      const void* summary, int num_pages, const int* page_table, int max_pages, const int* kv_lens,
+                      int n_blocks, int first, int last, int* blocks, void* stream);
+size_t attnqat_kv4_sparse_workspace_bytes(int T, int Hq, int Hkv, int max_q, int n_blocks, int d);
+int attnqat_fwd_kv4_sparse(const void* q, int64_t q_token_stride, int64_t q_head_stride, const int* cu_q, int T, int max_q, int B, int Hq, int Hkv, int d, float scale, int dtype,
+                           const void* cache, int num_pages, const int* page_table, int max_pages, const int* kv_lens, const int* blocks, int n_blocks,
+                           void* o, int64_t o_token_stride, int64_t o_head_stride, float* lse, void* workspace, size_t workspace_bytes, void* stream);
 
 /*
  * Block-sparse attention (Sec. 5: the paper's datacenter inference kernel supports it): attnqat_fwd_infer_mx with a

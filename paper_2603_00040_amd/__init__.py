@@ -58,6 +58,14 @@ _SIGNATURES = {
     "attnqat_kv4_ragged_workspace_bytes": (_sz, [_i, _i, _i, _i, _i, _i, _i]),
     "attnqat_fwd_kv4_ragged": (_i, [_vp, _ll, _ll, _vp, _i, _i, _i, _i, _i, _i, _i, _i, _f, _i, _vp, _i, _vp, _i, _vp, _vp, _ll, _ll, _vp,
                                     _vp, _sz, _vp]),
+    "attnqat_rope_fwd": (_i, [_vp, _ll, _ll, _ll] * 2 + [_i] * 6 + [_vp, _ll, _vp] + [_vp, _ll, _ll, _ll] * 2 + [_vp]),
+    "attnqat_rope_bwd": (_i, [_vp, _ll, _ll, _ll] * 2 + [_i] * 6 + [_vp, _ll, _vp] + [_vp, _ll, _ll, _ll] * 2 + [_vp]),
+    "attnqat_kv_cache_append_rope": (_i, [_vp, _ll, _ll] * 3 + [_i] * 5 + [_vp, _vp, _vp, _i, _vp] + [_vp, _ll, _ll, _vp]),
+    "attnqat_kv_summary_page_bytes": (_sz, [_i, _i]),
+    "attnqat_kv_summarize": (_i, [_vp, _i, _vp, _i, _i, _i, _vp, _vp]),
+    "attnqat_kv_select": (_i, [_vp, _ll, _ll, _vp] + [_i] * 7 + [_vp, _i, _vp, _i, _vp] + [_i] * 3 + [_vp, _vp]),
+    "attnqat_kv4_sparse_workspace_bytes": (_sz, [_i] * 6),
+    "attnqat_fwd_kv4_sparse": (_i, [_vp, _ll, _ll, _vp] + [_i] * 6 + [_f, _i, _vp, _i, _vp, _i, _vp, _vp, _i, _vp, _ll, _ll, _vp, _vp, _sz, _vp]),
     "attnqat_fwd_infer_mx_sparse": (_i, [_vp, _vp, _vp, _i, _i, _i, _i, _i, _i, _i, _vp, _vp, _vp, _vp, _sz, _vp]),
     "attnqat_fwd_mx": (_i, [_vp, _vp, _vp, _i, _i, _i, _i, _i, _i, _i, _vp, _vp, _vp, _vp, _sz, _vp]),
     "attnqat_bwd_mx": (_i, [_vp, _vp, _vp, _vp, _vp, _vp, _i, _i, _i, _i, _i, _i, _i,
@@ -423,6 +431,198 @@ def attnqat_fwd_kv4_ragged(q, cu_q, cache, num_pages, page_table, kv_lens, Hkv: 
         raise AttnQatError("workspace must be contiguous, on the device of the other tensors")
     rc = (_lib or lib()).attnqat_fwd_kv4_ragged(q.data_ptr(), qt, qh, cu_q.data_ptr(), T, max_q, B, Hq, Hkv, d, 1 if causal else 0, window, d ** -0.5 if scale is None else scale, BF16,
                                                 cache.data_ptr(), _serve_pages(cache, num_pages, Hkv, d), page_table.data_ptr(), most, kv_lens.data_ptr(),
+                                                o.data_ptr(), ot, oh, None if lse is None else lse.data_ptr(), workspace.data_ptr(), workspace.nbytes, _stream_on(dev))
+    if rc:
+        _check(rc)
+    return o, lse
+
+
+ROPE_PAIRED, ROPE_HALVES = 0, 1
+
+
+class Rope(ctypes.Structure):
+    """How the values of a head turn with their positions (host memory; made by ``rope_table``)."""
+    _fields_ = [("pairs", ctypes.c_int), ("axes", ctypes.c_int), ("layout", ctypes.c_int), ("reserved", ctypes.c_int),
+                ("freq", ctypes.c_double * 64), ("axis", ctypes.c_uint8 * 64)]
+
+
+def rope_table(dims, theta: float = 10000.0, layout: str = "paired", freqs=None, axis=None) -> Rope:
+    """A table of rotary positions, to be kept by the program.  ``dims``: how many values of a head turn with each axis, e.g. (128,) or, for time, height and
+    width, (44, 42, 42): pair i of an axis of n values turns by theta^(-2i/n) radians per position.  ``layout``: "paired" (elements 2i, 2i+1) or
+    "halves" (i and i + half the turned values).  ``freqs`` and ``axis``: radians per position and axis of every pair where they follow another rule
+    (then ``dims`` only says how many axes and values there are)."""
+    dims = tuple(int(n) for n in dims)
+    if layout not in ("paired", "halves"):
+        raise AttnQatError("layout must be 'paired' or 'halves'")
+    if not 1 <= len(dims) <= 4 or any(n < 0 or n % 2 for n in dims) or not 2 <= sum(dims) <= 128:
+        raise AttnQatError("dims must be one to four even numbers, of 2 to 128 values together")
+    pairs = sum(dims) // 2
+    if freqs is None:
+        freqs = [float(theta) ** (-2.0 * i / n) for n in dims for i in range(n // 2)]
+    if axis is None:
+        axis = [a for a, n in enumerate(dims) for _ in range(n // 2)]
+    freqs, axis = [float(f) for f in freqs], [int(a) for a in axis]
+    if len(freqs) != pairs or len(axis) != pairs or any(not 0 <= a < len(dims) for a in axis):
+        raise AttnQatError(f"freqs and axis must have an entry for each of the {pairs} pairs, axis below {len(dims)}")
+    return Rope(pairs, len(dims), ROPE_HALVES if layout == "halves" else ROPE_PAIRED, 0, (ctypes.c_double * 64)(*freqs), (ctypes.c_uint8 * 64)(*axis))
+
+
+def _heads(name, t, shape, dev):
+    """Strides per batch, head and token of a bf16 CUDA tensor [B,heads,L,d]."""
+    if not (t.dim() == 4 and t.dtype is _BF and t.get_device() == dev == _current_device() and t.shape == shape and (t.stride(3) == 1 or t.numel() == 0)):
+        raise AttnQatError(f"{name} must be a bf16 tensor {tuple(shape)} on the current device (cuda:{_current_device()}), d innermost")
+    return t.stride()[:3]
+
+
+def _rope_call(name, q, k, positions, rope, out):
+    if q.dim() != 4 or (k is not None and k.dim() != 4):
+        raise AttnQatError("q and k must be [B,heads,L,d]")
+    B, Hq, L, d = q.shape
+    dev, Hkv = q.get_device(), 0 if k is None else k.shape[1]
+    if not isinstance(rope, Rope):
+        raise AttnQatError("rope must be a table made by rope_table")
+    if not (positions.dtype is _I32 and positions.get_device() == dev and positions.is_contiguous() and positions.shape in ((L, rope.axes), (B, L, rope.axes))):
+        raise AttnQatError(f"positions must be a contiguous int32 tensor [{L},{rope.axes}] or [{B},{L},{rope.axes}] on the device of q")
+    if out is None:
+        out = (torch.empty((B, Hq, L, d), dtype=_BF, device=q.device), None if k is None else torch.empty((B, Hkv, L, d), dtype=_BF, device=q.device))
+    none = (None, 0, 0, 0)
+    args = []
+    for what, t, o, h in (("q", q, out[0], Hq), ("k", k, out[1], Hkv)):
+        if t is None:
+            args.append((none, none))
+        else:
+            args.append(((t.data_ptr(), *_heads(what, t, (B, h, L, d), dev)), (o.data_ptr(), *_heads("out", o, (B, h, L, d), dev))))
+    rc = getattr(_lib or lib(), name)(*args[0][0], *args[1][0], B, Hq, Hkv, L, d, BF16, positions.data_ptr(), L * rope.axes if positions.dim() == 3 else 0, ctypes.addressof(rope),
+                                      *args[0][1], *args[1][1], _stream_on(dev))
+    if rc:
+        _check(rc)
+    return out[0], out[1]
+
+
+def attnqat_rope_fwd(q, k, positions, rope, out=None):
+    """Rotary positions of q [B,Hq,L,d] and k [B,Hkv,L,d] (bf16, any stride per batch, head and token, d innermost; k may be None).  positions int32 [L,axes], or
+    [B,L,axes]; ``rope``: ``rope_table``.  Returns (q, k), contiguous: what attnqat_fwd takes; ``out``: those two, of any strides, each of which may be its input."""
+    return _rope_call("attnqat_rope_fwd", q, k, positions, rope, out)
+
+
+def attnqat_rope_bwd(dq, dk, positions, rope, out=None):
+    """Gradient of attnqat_rope_fwd: from dq [B,Hq,L,d] and dk [B,Hkv,L,d] of its outputs to those of its inputs.  Arguments as there; ``out`` may be views of one
+    projection's gradient."""
+    return _rope_call("attnqat_rope_bwd", dq, dk, positions, rope, out)
+
+
+def attnqat_kv_cache_append_rope(q, k, v, positions, rope, cache, slots, num_pages=None, out=None):
+    """attnqat_kv_cache_append with rotary positions on the way: k turned, rounded to bf16 and quantized, v as it is, and q [T,Hq,d] (or None) turned.  positions
+    int32 [T,axes], or [T] with one axis; ``rope``: ``rope_table``.  Returns the turned q, bf16 [T,Hq,d]; ``out``: that, of any stride per row and head, or q itself."""
+    shape, dev = k.shape, k.get_device()
+    if not isinstance(rope, Rope):
+        raise AttnQatError("rope must be a table made by rope_table")
+    if not (len(shape) == 3 and v.shape == shape and k.dtype is v.dtype is _BF and slots.dtype is _I64 and slots.shape == shape[:1] and cache.dtype is _U8
+            and positions.dtype is _I32 and positions.is_contiguous() and (positions.shape == (shape[0], rope.axes) or (rope.axes == 1 and positions.shape == shape[:1]))
+            and dev == _current_device() == v.get_device() == cache.get_device() == slots.get_device() == positions.get_device() and cache.is_contiguous() and slots.is_contiguous()):
+        _serve_refuse([("slots", slots, tuple(shape[:1]), _I64), ("positions", positions, (shape[0], rope.axes), _I32)], [("k", k, shape), ("v", v, shape)], cache)
+    T, Hkv, d = shape
+    (kt, kh, k1), (vt, vh, v1) = k.stride(), v.stride()
+    if not k1 == v1 == 1 and k.numel() > 0:
+        _serve_refuse([], [("k", k, shape), ("v", v, shape)])
+    Hq, qp, qt, qh, op, ot, oh = 0, None, 0, 0, None, 0, 0
+    if q is not None:
+        if q.dim() != 3:
+            raise AttnQatError("q must be [T,Hq,d]")
+        Hq = q.shape[1]
+        if out is None:
+            out = torch.empty((T, Hq, d), dtype=_BF, device=q.device)
+        (qt, qh, q1), want = q.stride(), (T, Hq, d)
+        if not (q.shape == out.shape == want and q.dtype is out.dtype is _BF and dev == q.get_device() == out.get_device() and (q1 == out.stride(2) == 1 or q.numel() == 0)):
+            _serve_refuse([], [("q", q, want), ("out", out, want)])
+        ot, oh, _ = out.stride()
+        qp, op = q.data_ptr(), out.data_ptr()
+    rc = (_lib or lib()).attnqat_kv_cache_append_rope(qp, qt, qh, k.data_ptr(), kt, kh, v.data_ptr(), vt, vh, T, Hq, Hkv, d, BF16, positions.data_ptr(), ctypes.addressof(rope),
+                                                      cache.data_ptr(), _serve_pages(cache, num_pages, Hkv, d), slots.data_ptr(), op, ot, oh, _stream_on(dev))
+    if rc:
+        _check(rc)
+    return out if q is not None else None
+
+
+def kv_summary_page_bytes(Hkv: int, d: int) -> int:
+    return lib().attnqat_kv_summary_page_bytes(Hkv, d)
+
+
+def _summary_pages(summary, pages, Hkv, d):
+    if summary.numel() < pages * Hkv * (d + 16):
+        raise AttnQatError(f"summary has no room for {pages} pages")
+
+
+def attnqat_kv_summarize(cache, slots, summary, Hkv: int, d: int, num_pages=None):
+    """The means of the keys of every page whose last position is among ``slots`` (int64 [T], those that have just been appended), in 8 bits, into ``summary``
+    (uint8 CUDA tensor of num_pages * kv_summary_page_bytes(Hkv, d) bytes)."""
+    dev = slots.get_device()
+    if not (slots.dtype is _I64 and slots.dim() == 1 and cache.dtype is summary.dtype is _U8 and dev == _current_device() == cache.get_device() == summary.get_device()
+            and cache.is_contiguous() and summary.is_contiguous() and slots.is_contiguous()):
+        _serve_refuse([("slots", slots, (slots.numel(),), _I64), ("summary", summary, (summary.numel(),), _U8)], (), cache)
+    pages = _serve_pages(cache, num_pages, Hkv, d)
+    _summary_pages(summary, pages, Hkv, d)
+    rc = (_lib or lib()).attnqat_kv_summarize(cache.data_ptr(), pages, slots.data_ptr(), slots.numel(), Hkv, d, summary.data_ptr(), _stream_on(dev))
+    if rc:
+        _check(rc)
+
+
+def attnqat_kv_select(q, cu_q, summary, num_pages: int, page_table, kv_lens, Hkv: int, n_blocks: int, first: int = 1, last: int = 1, max_q=None, out=None):
+    """The pages that every row attends to: its sequence's ``first`` first ones, ``last`` last ones (its own among them), and those whose keys' mean
+    (``attnqat_kv_summarize``) gives the highest score, ``n_blocks`` at most.  q (turned), cu_q, page_table, kv_lens, max_q: as for attnqat_fwd_kv4_ragged.  Returns
+    int32 [T,Hkv,n_blocks]: page numbers of the sequence, ascending, -1 behind them; ``out``: that."""
+    shape, dev, B = q.shape, q.get_device(), kv_lens.numel()
+    if len(shape) != 3 or page_table.dim() != 2:
+        raise AttnQatError("q must be [T,Hq,d] and page_table [B,max_pages]")
+    T, Hq, d = shape
+    most, want = page_table.shape[1], (T, Hkv, n_blocks)
+    if out is None:
+        out = torch.empty((T, max(Hkv, 0), max(n_blocks, 0)), dtype=_I32, device=q.device)
+    (qt, qh, q1) = q.stride()
+    if not (q.dtype is _BF and (q1 == 1 or q.numel() == 0) and kv_lens.dtype is cu_q.dtype is page_table.dtype is out.dtype is _I32 and summary.dtype is _U8 and out.shape == want
+            and kv_lens.shape == (B,) and cu_q.shape == (B + 1,) and page_table.shape[0] == B
+            and dev == _current_device() == cu_q.get_device() == summary.get_device() == page_table.get_device() == kv_lens.get_device() == out.get_device()
+            and summary.is_contiguous() and cu_q.is_contiguous() and page_table.is_contiguous() and kv_lens.is_contiguous() and out.is_contiguous()):
+        _serve_refuse([("kv_lens", kv_lens, (B,), _I32), ("cu_q", cu_q, (B + 1,), _I32), ("page_table", page_table, (B, most), _I32), ("out", out, want, _I32),
+                       ("summary", summary, (summary.numel(),), _U8)], [("q", q, shape)])
+    _summary_pages(summary, num_pages, Hkv, d)
+    rc = (_lib or lib()).attnqat_kv_select(q.data_ptr(), qt, qh, cu_q.data_ptr(), T, max(T, 1) if max_q is None else _within_int(max_q), B, Hq, Hkv, d, BF16, summary.data_ptr(),
+                                           num_pages, page_table.data_ptr(), most, kv_lens.data_ptr(), n_blocks, first, last, out.data_ptr(), _stream_on(dev))
+    if rc:
+        _check(rc)
+    return out
+
+
+def kv4_sparse_workspace_bytes(T: int, Hq: int, Hkv: int, max_q: int, n_blocks: int, d: int) -> int:
+    return lib().attnqat_kv4_sparse_workspace_bytes(T, Hq, Hkv, _within_int(max_q), n_blocks, d)
+
+
+def attnqat_fwd_kv4_sparse(q, cu_q, cache, num_pages, page_table, kv_lens, Hkv: int, blocks, max_q=None, scale=None, workspace=None, out=None):
+    """attnqat_fwd_kv4_ragged (causal) over a choice of pages: row t of kv head h sees those of its keys that lie in pages ``blocks[t,h]`` of its sequence (int32
+    [T,Hkv,n_blocks], from attnqat_kv_select or any other; entries outside the row's pages are passed over).  Other arguments, and (o, lse), as there."""
+    shape, dev, B = q.shape, q.get_device(), kv_lens.numel()
+    if len(shape) != 3 or page_table.dim() != 2 or blocks.dim() != 3:
+        raise AttnQatError("q must be [T,Hq,d], page_table [B,max_pages] and blocks [T,Hkv,n_blocks]")
+    T, Hq, d = shape
+    most, n_blocks = page_table.shape[1], blocks.shape[2]
+    o, lse = out if out is not None else (torch.empty(shape, dtype=_BF, device=q.device), torch.empty((T, Hq), dtype=_F32, device=q.device))
+    if not (q.dtype is o.dtype is _BF and o.shape == shape and kv_lens.dtype is cu_q.dtype is page_table.dtype is blocks.dtype is _I32 and cache.dtype is _U8
+            and kv_lens.shape == (B,) and cu_q.shape == (B + 1,) and page_table.shape[0] == B and blocks.shape[:2] == (T, Hkv)
+            and dev == _current_device() == o.get_device() == cu_q.get_device() == cache.get_device() == page_table.get_device() == kv_lens.get_device() == blocks.get_device()
+            and cache.is_contiguous() and cu_q.is_contiguous() and page_table.is_contiguous() and kv_lens.is_contiguous() and blocks.is_contiguous()
+            and (lse is None or (lse.dtype is _F32 and lse.shape == (T, Hq) and lse.get_device() == dev and lse.is_contiguous()))):
+        _serve_refuse([("kv_lens", kv_lens, (B,), _I32), ("cu_q", cu_q, (B + 1,), _I32), ("page_table", page_table, (B, most), _I32), ("blocks", blocks, (T, Hkv, n_blocks), _I32)]
+                      + ([] if lse is None else [("out[1]", lse, (T, Hq), _F32)]), [("q", q, shape), ("out[0]", o, shape)], cache)
+    (qt, qh, q1), (ot, oh, o1) = q.stride(), o.stride()
+    if not q1 == o1 == 1 and q.numel() > 0:
+        _serve_refuse([], [("q", q, shape), ("out[0]", o, shape)])
+    max_q = max(T, 1) if max_q is None else _within_int(max_q)
+    if workspace is None:
+        workspace = torch.empty(max(kv4_sparse_workspace_bytes(T, Hq, Hkv, max_q, n_blocks, d), 1), dtype=_U8, device=q.device)
+    elif workspace.get_device() != dev or not workspace.is_contiguous():
+        raise AttnQatError("workspace must be contiguous, on the device of the other tensors")
+    rc = (_lib or lib()).attnqat_fwd_kv4_sparse(q.data_ptr(), qt, qh, cu_q.data_ptr(), T, max_q, B, Hq, Hkv, d, d ** -0.5 if scale is None else scale, BF16, cache.data_ptr(),
+                                                _serve_pages(cache, num_pages, Hkv, d), page_table.data_ptr(), most, kv_lens.data_ptr(), blocks.data_ptr(), n_blocks,
                                                 o.data_ptr(), ot, oh, None if lse is None else lse.data_ptr(), workspace.data_ptr(), workspace.nbytes, _stream_on(dev))
     if rc:
         _check(rc)

@@ -4,6 +4,7 @@
 #include "kernels.hpp"
 
 #include <atomic>
+#include <cmath>
 #include <mutex>
 
 using namespace aq;
@@ -702,6 +703,259 @@ int attnqat_fwd_kv4_ragged(const void* q, int64_t q_token_stride, int64_t q_head
                        B, Hq, Hkv, causal != 0, window, scale * 1.4426950408889634f, (uint16_t*)o, out.token, out.head, lse};
     if (launch_ragged(a, d, workspace, st)) return ATTNQAT_ELAUNCH;
     prof_mark("fwd_kv4_ragged", st);
+    return ATTNQAT_OK;
+}
+
+namespace {
+// Elements of a strided tensor, to tell whether two of them share any: levels from the widest stride in, then `row` bytes side by side.  (Views of one buffer
+// lie between each other: their addresses overlap though their elements do not.)
+struct View { uintptr_t p; int levels; int64_t n[3], stride[3] /* bytes */, row; };
+View view_of(const void* p, int64_t n0, int64_t s0, int64_t n1, int64_t s1, int64_t n2, int64_t s2, int d)
+{
+    View v{(uintptr_t)p, 0, {}, {}, 2 * (int64_t)d};
+    const int64_t n[3] = {n0, n1, n2}, st[3] = {2 * s0, 2 * s1, 2 * s2};
+    for (int i = 0; i < 3; ++i)
+        if (n[i] > 1 && st[i] > 0) {
+            int at = v.levels++;
+            for (; at > 0 && v.stride[at - 1] < st[i]; --at) { v.n[at] = v.n[at - 1]; v.stride[at] = v.stride[at - 1]; }
+            v.n[at] = n[i]; v.stride[at] = st[i];
+        }
+    return v;
+}
+int64_t view_extent(const View& v, int from)
+{
+    int64_t e = v.row;
+    for (int i = from; i < v.levels; ++i) e += (v.n[i] - 1) * v.stride[i];
+    return e;
+}
+// Whether a (at 0) and b (at `at` bytes) may share an element, by their levels from `level` on.  Strides that differ count as sharing.
+bool views_share(const View& a, const View& b, int64_t at, int level)
+{
+    if (at >= view_extent(a, level) || -at >= view_extent(b, level)) return false;
+    if (level >= a.levels || level >= b.levels || a.stride[level] != b.stride[level]) return true;
+    const int64_t s = a.stride[level];
+    if (view_extent(a, level + 1) > s || view_extent(b, level + 1) > s) return true;
+    const int64_t d = ((at % s) + s) % s;
+    return views_share(a, b, d, level + 1) || views_share(a, b, d - s, level + 1);
+}
+bool share(const View& a, const View& b) { return views_share(a, b, (int64_t)(b.p - a.p), 0); }
+bool same(const View& a, const View& b)
+{
+    if (a.p != b.p || a.levels != b.levels) return false;
+    for (int i = 0; i < a.levels; ++i) if (a.n[i] != b.n[i] || a.stride[i] != b.stride[i]) return false;
+    return true;
+}
+bool view_overlaps(const View& v, const void* p, size_t n) { return overlap((const void*)v.p, (size_t)view_extent(v, 0), p, n); }
+// No element twice.
+bool rows_apart(const View& v)
+{
+    for (int i = 0; i < v.levels; ++i) if (v.stride[i] < view_extent(v, i + 1)) return false;
+    return true;
+}
+
+// The table that the kernels take.  A frequency of f radians per position is f / 2 pi turns; whole turns change nothing.
+int rope_of(const attnqat_rope* rope, int d, bool back, RopeTable& r)
+{
+    if (!rope || rope->pairs < 1 || rope->pairs > d / 2 || rope->axes < 1 || rope->axes > kRopeAxes) return ATTNQAT_EINVAL;
+    if (rope->layout != ATTNQAT_ROPE_PAIRED && rope->layout != ATTNQAT_ROPE_HALVES) return ATTNQAT_EINVAL;
+    if (rope->layout == ATTNQAT_ROPE_HALVES && rope->pairs % 8 != 0) return ATTNQAT_ESHAPE;
+    r = RopeTable{};
+    r.pairs = rope->pairs; r.axes = rope->axes;
+    for (int i = 0; i < rope->pairs; ++i) {
+        if (!std::isfinite(rope->freq[i]) || rope->axis[i] >= rope->axes) return ATTNQAT_EINVAL;
+        const long double turns = (long double)rope->freq[i] / 6.283185307179586476925286766559005768L, part = turns - floorl(turns);
+        const long double x = part * 18446744073709551616.0L;
+        const uint64_t f = x >= 18446744073709551615.0L ? 0 : (uint64_t)x;
+        r.freq[i] = back ? 0 - f : f;
+        r.axis[i >> 4] |= (uint32_t)rope->axis[i] << (2 * (i & 15));
+    }
+    return ATTNQAT_OK;
+}
+
+// A tensor [B, heads, L, d] of any strides (in elements): false where the kernels could not address it.
+bool tensor_of(const void* p, int64_t batch, int64_t head, int64_t token, int B, int heads, int L, int d, View& v)
+{
+    if (!p || ((uintptr_t)p & 15)) return false;
+    const int64_t n[3] = {B, heads, L}, st[3] = {batch, head, token};
+    for (int i = 0; i < 3; ++i)
+        if (n[i] > 1 && (st[i] < 0 || st[i] % 8 != 0 || st[i] > (1ll << 46) / n[i])) return false;
+    v = view_of(p, B, batch, heads, head, L, token, d);
+    return true;
+}
+
+int rope_common(const void* const (&src)[2], const int64_t (&ss)[2][3], void* const (&dst)[2], const int64_t (&ds)[2][3], const int (&heads)[2], int B, int L, int d, int dtype,
+                const int* positions, int64_t pos_batch, const attnqat_rope* rope, bool back, void* stream)
+{
+    if (B < 1 || L < 0 || heads[0] < 1 || heads[1] < 0) return ATTNQAT_EINVAL;
+    if (dtype != ATTNQAT_BF16) return ATTNQAT_EDTYPE;
+    if ((d != 64 && d != 128) || heads[0] > 65535 || heads[1] > 65535 || (long long)B * L > (1 << 28)) return ATTNQAT_ESHAPE;
+    RopeTable r;
+    int rc = rope_of(rope, d, back, r);
+    if (rc || L == 0) return rc;
+    if (!positions || ((uintptr_t)positions & 3) || pos_batch < 0 || pos_batch > (1ll << 46)) return ATTNQAT_EINVAL;
+    if (B == 1) pos_batch = 0;
+    const size_t np = 4 * ((size_t)(B - 1) * pos_batch + (size_t)L * r.axes);
+    RopeArgs a{};
+    View in[2], out[2];
+    const int n = heads[1] > 0 ? 2 : 1;
+    for (int i = 0; i < n; ++i) {
+        if (!tensor_of(src[i], ss[i][0], ss[i][1], ss[i][2], B, heads[i], L, d, in[i]) || !tensor_of(dst[i], ds[i][0], ds[i][1], ds[i][2], B, heads[i], L, d, out[i])) return ATTNQAT_EINVAL;
+        const int64_t cnt[3] = {B, heads[i], L};
+        for (int j = 0; j < 3; ++j) if (cnt[j] > 1 && ds[i][j] < d) return ATTNQAT_EINVAL;
+        if (!rows_apart(out[i]) || view_overlaps(out[i], positions, np)) return ATTNQAT_EINVAL;
+        a.t[i] = RopeTensor{(const uint16_t*)src[i], (size_t)(B > 1 ? ss[i][0] : 0), (size_t)(heads[i] > 1 ? ss[i][1] : 0), (size_t)(L > 1 ? ss[i][2] : 0),
+                            (uint16_t*)dst[i], (size_t)(B > 1 ? ds[i][0] : 0), (size_t)(heads[i] > 1 ? ds[i][1] : 0), (size_t)(L > 1 ? ds[i][2] : 0), heads[i]};
+    }
+    for (int o = 0; o < n; ++o) {
+        for (int i = 0; i < n; ++i)
+            if (share(out[o], in[i]) && !(o == i && same(out[o], in[i]))) return ATTNQAT_EINVAL;      // (in place: a thread reads what it writes)
+        if (o == 1 && share(out[0], out[1])) return ATTNQAT_EINVAL;
+    }
+    a.B = B; a.L = L; a.positions = positions; a.pos_batch = (size_t)pos_batch;
+    hipStream_t st = (hipStream_t)stream;
+    prof_begin(st);
+    if (launch_rope(a, r, d, rope->layout == ATTNQAT_ROPE_HALVES, st)) return ATTNQAT_ELAUNCH;
+    prof_mark(back ? "rope_bwd" : "rope_fwd", st);
+    return ATTNQAT_OK;
+}
+}  // namespace
+
+int attnqat_rope_fwd(const void* q, int64_t q_batch, int64_t q_head, int64_t q_token, const void* k, int64_t k_batch, int64_t k_head, int64_t k_token,
+                     int B, int Hq, int Hkv, int L, int d, int dtype, const int* positions, int64_t positions_batch, const attnqat_rope* rope,
+                     void* q_out, int64_t qo_batch, int64_t qo_head, int64_t qo_token, void* k_out, int64_t ko_batch, int64_t ko_head, int64_t ko_token, void* stream)
+{
+    return rope_common({q, k}, {{q_batch, q_head, q_token}, {k_batch, k_head, k_token}}, {q_out, k_out}, {{qo_batch, qo_head, qo_token}, {ko_batch, ko_head, ko_token}},
+                       {Hq, Hkv}, B, L, d, dtype, positions, positions_batch, rope, false, stream);
+}
+
+int attnqat_rope_bwd(const void* dq_out, int64_t qo_batch, int64_t qo_head, int64_t qo_token, const void* dk_out, int64_t ko_batch, int64_t ko_head, int64_t ko_token,
+                     int B, int Hq, int Hkv, int L, int d, int dtype, const int* positions, int64_t positions_batch, const attnqat_rope* rope,
+                     void* dq, int64_t q_batch, int64_t q_head, int64_t q_token, void* dk, int64_t k_batch, int64_t k_head, int64_t k_token, void* stream)
+{
+    return rope_common({dq_out, dk_out}, {{qo_batch, qo_head, qo_token}, {ko_batch, ko_head, ko_token}}, {dq, dk}, {{q_batch, q_head, q_token}, {k_batch, k_head, k_token}},
+                       {Hq, Hkv}, B, L, d, dtype, positions, positions_batch, rope, true, stream);
+}
+
+int attnqat_kv_cache_append_rope(const void* q, int64_t q_token_stride, int64_t q_head_stride, const void* k, int64_t k_token_stride, int64_t k_head_stride,
+                                 const void* v, int64_t v_token_stride, int64_t v_head_stride, int T, int Hq, int Hkv, int d, int dtype,
+                                 const int* positions, const attnqat_rope* rope, void* cache, int num_pages, const int64_t* slots,
+                                 void* q_out, int64_t qo_token_stride, int64_t qo_head_stride, void* stream)
+{
+    AppendRopeArgs a{};
+    if (Hq < 0) return ATTNQAT_EINVAL;
+    if ((long long)(T > 0 ? T : 0) * Hq > kMaxServeRows || Hq > 65535 || Hkv > 65535) return ATTNQAT_ESHAPE;
+    int rc = rows_common(k, k_token_stride, k_head_stride, v, v_token_stride, v_head_stride, T, Hkv, d, dtype, cache, num_pages, slots, false, a.k, a.v);
+    if (rc) return rc;
+    RopeTable r;
+    rc = rope_of(rope, d, false, r);
+    if (rc || T == 0) return rc;
+    if (!positions || ((uintptr_t)positions & 3)) return ATTNQAT_EINVAL;
+    if (Hq > 0) {
+        if (!q || !q_out || !rows_of(q, q_token_stride, q_head_stride, T, Hq, d, false, a.q) || !rows_of(q_out, qo_token_stride, qo_head_stride, T, Hq, d, true, a.q_out)) return ATTNQAT_EINVAL;
+        auto view = [&](const Rows& x, int heads) { return view_of(x.p, 1, 0, heads, (int64_t)x.head, T, (int64_t)x.token, d); };
+        const View out = view(a.q_out, Hq), in = view(a.q, Hq);
+        if ((share(out, in) && !same(out, in)) || share(out, view(a.k, Hkv)) || share(out, view(a.v, Hkv))) return ATTNQAT_EINVAL;
+        if (view_overlaps(out, cache, (size_t)num_pages * nvfp4_page_bytes(Hkv, d)) || view_overlaps(out, slots, (size_t)T * 8) || view_overlaps(out, positions, (size_t)T * r.axes * 4))
+            return ATTNQAT_EINVAL;
+    }
+    a.T = T; a.Hq = Hq; a.Hkv = Hkv; a.positions = positions; a.cache = (unsigned char*)cache; a.num_pages = num_pages; a.slots = (const long long*)slots;
+    hipStream_t st = (hipStream_t)stream;
+    prof_begin(st);
+    if (launch_append_rope(a, r, d, rope->layout == ATTNQAT_ROPE_HALVES, st)) return ATTNQAT_ELAUNCH;
+    prof_mark("kv_cache_append_rope", st);
+    return ATTNQAT_OK;
+}
+
+size_t attnqat_kv_summary_page_bytes(int Hkv, int d) { return Hkv < 1 || (d != 64 && d != 128) ? 0 : (size_t)Hkv * (d + kSummaryTail); }
+
+int attnqat_kv_summarize(const void* cache, int num_pages, const int64_t* slots, int T, int Hkv, int d, void* summary, void* stream)
+{
+    if (T < 0 || Hkv < 1 || num_pages < 1) return ATTNQAT_EINVAL;
+    if ((d != 64 && d != 128) || T > kMaxServeRows || Hkv > 65535) return ATTNQAT_ESHAPE;
+    if (T == 0) return ATTNQAT_OK;
+    if (!cache || !slots || !summary || ((uintptr_t)cache & 15) || ((uintptr_t)slots & 7) || ((uintptr_t)summary & 15)) return ATTNQAT_EINVAL;
+    const size_t ns = (size_t)num_pages * attnqat_kv_summary_page_bytes(Hkv, d);
+    if (overlap(summary, ns, cache, (size_t)num_pages * nvfp4_page_bytes(Hkv, d)) || overlap(summary, ns, slots, (size_t)T * 8)) return ATTNQAT_EINVAL;
+    hipStream_t st = (hipStream_t)stream;
+    prof_begin(st);
+    if (launch_summarize(cache, num_pages, Hkv, d, (const long long*)slots, T, summary, st)) return ATTNQAT_ELAUNCH;
+    prof_mark("kv_summarize", st);
+    return ATTNQAT_OK;
+}
+
+namespace {
+int sparse_dims(int T, int Hq, int Hkv, int max_q, int n_blocks, int d)
+{
+    if (T < 0 || Hq < 1 || Hkv < 1 || max_q < 1 || n_blocks < 1) return ATTNQAT_EINVAL;
+    if ((d != 64 && d != 128) || Hq % Hkv != 0 || n_blocks > kMaxBlocks || (long long)T * Hq > (1 << 28)) return ATTNQAT_ESHAPE;
+    if ((long long)T * Hkv * ((Hq / Hkv + 15) / 16) > (1 << 23)) return ATTNQAT_ESHAPE;               // (a workgroup each at most)
+    return ATTNQAT_OK;
+}
+int step_of(const void* q, int64_t q_token, int64_t q_head, const int* cu_q, int T, int B, int Hq, int Hkv, int d, int dtype, int num_pages, const int* table, int max_pages,
+            const int* kv_lens, StepArgs& s)
+{
+    if (dtype != ATTNQAT_BF16) return ATTNQAT_EDTYPE;
+    if (B < 1 || num_pages < 1 || max_pages < 1) return ATTNQAT_EINVAL;
+    if (B > kMaxServeBatch || max_pages > kMaxServePages) return ATTNQAT_ESHAPE;
+    if (T == 0) return ATTNQAT_OK;
+    Rows r;
+    if (!q || !cu_q || !table || !kv_lens || !rows_of(q, q_token, q_head, T, Hq, d, false, r)) return ATTNQAT_EINVAL;
+    s = StepArgs{(const uint16_t*)q, r.token, r.head, cu_q, T, B, Hq, Hkv, table, max_pages, num_pages, kv_lens};
+    return ATTNQAT_OK;
+}
+}  // namespace
+
+int attnqat_kv_select(const void* q, int64_t q_token_stride, int64_t q_head_stride, const int* cu_q, int T, int max_q, int B, int Hq, int Hkv, int d, int dtype,
+                      const void* summary, int num_pages, const int* page_table, int max_pages, const int* kv_lens,
+                      int n_blocks, int first, int last, int* blocks, void* stream)
+{
+    SelectArgs a{};
+    int rc = sparse_dims(T, Hq, Hkv, max_q, n_blocks, d);
+    if (rc) return rc;
+    rc = step_of(q, q_token_stride, q_head_stride, cu_q, T, B, Hq, Hkv, d, dtype, num_pages, page_table, max_pages, kv_lens, a.s);
+    if (rc) return rc;
+    if (first < 0 || last < 1 || first > n_blocks - last || last > n_blocks) return ATTNQAT_EINVAL;
+    if (T == 0) return ATTNQAT_OK;
+    if (!summary || !blocks || ((uintptr_t)summary & 15) || ((uintptr_t)blocks & 3)) return ATTNQAT_EINVAL;
+    const size_t nb = (size_t)T * Hkv * n_blocks * 4;
+    if (overlap(blocks, nb, q, rows_extent(Rows{const_cast<void*>(q), a.s.q_token, a.s.q_head}, T, Hq, d)) || overlap(blocks, nb, summary, (size_t)num_pages * attnqat_kv_summary_page_bytes(Hkv, d))
+        || overlap(blocks, nb, page_table, (size_t)B * max_pages * 4) || overlap(blocks, nb, cu_q, (size_t)B * 4 + 4) || overlap(blocks, nb, kv_lens, (size_t)B * 4)) return ATTNQAT_EINVAL;
+    a.summary = (const unsigned char*)summary; a.blocks = blocks; a.n_blocks = n_blocks; a.first = first; a.last = last;
+    hipStream_t st = (hipStream_t)stream;
+    prof_begin(st);
+    if (launch_select(a, max_q, d, st)) return ATTNQAT_ELAUNCH;
+    prof_mark("kv_select", st);
+    return ATTNQAT_OK;
+}
+
+size_t attnqat_kv4_sparse_workspace_bytes(int T, int Hq, int Hkv, int max_q, int n_blocks, int d)
+{
+    return sparse_dims(T, Hq, Hkv, max_q, n_blocks, d) ? 0 : sparse_ws_bytes(T, Hq, Hkv, max_q, n_blocks, d);
+}
+
+int attnqat_fwd_kv4_sparse(const void* q, int64_t q_token_stride, int64_t q_head_stride, const int* cu_q, int T, int max_q, int B, int Hq, int Hkv, int d, float scale, int dtype,
+                           const void* cache, int num_pages, const int* page_table, int max_pages, const int* kv_lens, const int* blocks, int n_blocks,
+                           void* o, int64_t o_token_stride, int64_t o_head_stride, float* lse, void* workspace, size_t workspace_bytes, void* stream)
+{
+    SparseArgs a{};
+    int rc = sparse_dims(T, Hq, Hkv, max_q, n_blocks, d);
+    if (rc) return rc;
+    rc = step_of(q, q_token_stride, q_head_stride, cu_q, T, B, Hq, Hkv, d, dtype, num_pages, page_table, max_pages, kv_lens, a.s);
+    if (rc) return rc;
+    if (!(scale > 0.0f) || !(scale * 1.4426950408889634f < INFINITY)) return ATTNQAT_EINVAL;
+    if (T == 0) return ATTNQAT_OK;
+    Rows out;
+    if (!cache || ((uintptr_t)cache & 15) || !blocks || ((uintptr_t)blocks & 3) || !o || !rows_of(o, o_token_stride, o_head_stride, T, Hq, d, true, out)) return ATTNQAT_EINVAL;
+    const size_t nq = rows_extent(Rows{const_cast<void*>(q), a.s.q_token, a.s.q_head}, T, Hq, d), no = rows_extent(out, T, Hq, d), nl = (size_t)T * Hq * 4, nb = (size_t)T * Hkv * n_blocks * 4;
+    if (overlap(q, nq, o, no) || overlap(blocks, nb, o, no)) return ATTNQAT_EINVAL;
+    if (lse && (overlap(q, nq, lse, nl) || overlap(o, no, lse, nl) || overlap(blocks, nb, lse, nl))) return ATTNQAT_EINVAL;
+    if (!workspace || ((uintptr_t)workspace & 15) || workspace_bytes < sparse_ws_bytes(T, Hq, Hkv, max_q, n_blocks, d)) return ATTNQAT_EWORKSPACE;
+    a.cache = (const unsigned char*)cache; a.blocks = blocks; a.n_blocks = n_blocks; a.c = scale * 1.4426950408889634f;
+    a.o = (uint16_t*)o; a.o_token = out.token; a.o_head = out.head; a.lse = lse;
+    hipStream_t st = (hipStream_t)stream;
+    prof_begin(st);
+    if (launch_sparse(a, max_q, d, workspace, st)) return ATTNQAT_ELAUNCH;
+    prof_mark("fwd_kv4_sparse", st);
     return ATTNQAT_OK;
 }
 

@@ -80,6 +80,17 @@ struct Rows { void* p; size_t token, head; };
 int launch_kv_append(const Rows& k, const Rows& v, int T, int Hkv, int D, void* cache, int num_pages, const long long* slots, hipStream_t st);
 int launch_kv_read(const Rows& k, const Rows& v, int T, int Hkv, int D, const void* cache, int num_pages, const long long* slots, hipStream_t st);
 
+// Rotary positions (rope.hip).  freq: the pairs' frequencies in turns per position, as fractions of 2^64 (of the opposite sign for the way back); axis: two
+// bits per pair.  Strides in elements; no heads: the tensor is left out.
+constexpr int kRopeAxes = 4;
+struct RopeTable { uint64_t freq[64]; uint32_t axis[4]; int pairs, axes; };
+struct RopeTensor { const uint16_t* src; size_t src_batch, src_head, src_token; uint16_t* dst; size_t dst_batch, dst_head, dst_token; int heads; };
+struct RopeArgs { RopeTensor t[2]; int B, L; const int* positions; size_t pos_batch; };
+int launch_rope(const RopeArgs& a, const RopeTable& r, int D, bool halves /* partners half the turned part apart, not neighbours */, hipStream_t st);
+// launch_kv_append with Q and K turned on the way: Q [T, Hq, D] to q_out (Hq = 0: none).
+struct AppendRopeArgs { Rows q, k, v, q_out; int T, Hq, Hkv; const int* positions; unsigned char* cache; int num_pages; const long long* slots; };
+int launch_append_rope(const AppendRopeArgs& a, const RopeTable& r, int D, bool halves, hipStream_t st);
+
 // Attention over the NVFP4 pages without any further quantization, sequence b with the queries cu_q[b] .. cu_q[b + 1] - 1 of T (ragged.hip).
 struct RaggedArgs {
     const uint16_t* q; size_t q_token, q_head;
@@ -94,6 +105,27 @@ struct RaggedArgs {
 };
 size_t ragged_ws_bytes(int T, int B, int Hq, int Hkv, int max_q, int max_pages, int D);
 int launch_ragged(const RaggedArgs& a, int D, void* ws, hipStream_t st);
+
+// Attention over chosen pages of the NVFP4 cache (sparse.hip).  The means of the keys of complete pages, [num_pages][Hkv][D codes, scale, 12 bytes]; the
+// choice of pages for every (row, kv head), [T, Hkv, n_blocks]; and attention of the rows over theirs.
+constexpr int kSummaryTail = 16;                 // bytes of a page's head behind the D codes
+constexpr int kMaxBlocks = 1024;                 // most pages of a row
+int launch_summarize(const void* cache, int num_pages, int Hkv, int D, const long long* slots, int T, void* summary, hipStream_t st);
+struct StepArgs {
+    const uint16_t* q; size_t q_token, q_head;
+    const int* cu_q; int T, B, Hq, Hkv;
+    const int* table; int max_pages, num_pages; const int* kv_lens;
+};
+struct SelectArgs { StepArgs s; const unsigned char* summary; int* blocks; int n_blocks, first, last; };
+int launch_select(const SelectArgs& a, int max_q, int D, hipStream_t st);
+struct SparseArgs {
+    StepArgs s;
+    const unsigned char* cache; const int* blocks; int n_blocks;
+    float c;                                     // log2(e) times the factor of the scores
+    uint16_t* o; size_t o_token, o_head; float* lse /* [T, Hq], or null */;
+};
+size_t sparse_ws_bytes(int T, int Hq, int Hkv, int max_q, int n_blocks, int D);
+int launch_sparse(const SparseArgs& a, int max_q, int D, void* ws, hipStream_t st);
 
 // Alg. 1 for decode steps over the NVFP4 pages: at most decode_max_rows() query rows per (sequence, kv head), i.e.
 // (Hq / Hkv) * Lq of them; q [B*Hkv, (Hq/Hkv)*Lq, D] (the rows of a kv group are neighbours in [B,Hq,Lq,d]); qh: scratch for

@@ -1,0 +1,580 @@
+// Attention over a choice of the pages of the NVFP4 KV cache: for every query and kv head the first pages, the last ones and those whose keys, by their mean,
+// look most like what the query asks for (attnqat_kv_summarize, attnqat_kv_select, attnqat_fwd_kv4_sparse).
+//
+// The choice is made of whole numbers and powers of two, so that it does not depend on the order of sums: means in 8 bits with a power of two per (page, head),
+// the queries of a kv head's group in 8 bits with one power of two between them (which no comparison needs), products in int32.
+#include "common.hpp"
+#include "kernels.hpp"
+#include "kv4.hpp"
+
+namespace aq {
+
+namespace {
+
+typedef int intx4 __attribute__((ext_vector_type(4)));
+
+// ---------------------------------------------------------------------------------------------- means of the keys of a page
+// A cached value is a multiple of 2^-10 below 2^12, the sum S of a page's 128 a whole number of 2^-10 below 2^29: exact in int32, in any order (a thread's own two keys
+// in fp32, where they fit).  With the largest |S| of a head in [2^(b-1), 2^b) the codes are S 2^-e, e = b - 7, rounded to nearest even, at most 127 in
+// magnitude, and the mean is code 2^(e-17).
+struct OpAddInt { __device__ __forceinline__ float operator()(float a, float b) const { return __uint_as_float(__float_as_uint(a) + __float_as_uint(b)); } };
+
+template <int D>
+__global__ __launch_bounds__(256) void summarize_kernel(const unsigned char* __restrict__ cache, int num_pages, int Hkv, const long long* __restrict__ slots, int T, int rows_per,
+                                                        unsigned char* __restrict__ summary)
+{
+    constexpr int NCH = D / 32, KEYS = 256 / NCH;                 // threads to a key (32 values each), keys at a time
+    __shared__ int part[4][D];
+    __shared__ int top;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, ch = tid % NCH, kk = tid / NCH, h = blockIdx.y;
+    const int r_end = min(((int)blockIdx.x + 1) * rows_per, T);
+    for (int r0 = (int)blockIdx.x * rows_per; r0 < r_end; r0 += 64) {
+        const long long slot = r0 + lane < r_end ? slots[r0 + lane] : -1;
+        const bool ends = slot >= 0 && slot < (long long)num_pages * 128 && (slot & 127) == 127;
+        const int page_lane = (int)(slot >> 7);
+        for (unsigned long long left = __builtin_amdgcn_ballot_w64(ends); left != 0; left &= left - 1) {
+            const int page = __builtin_amdgcn_readlane(page_lane, (int)__builtin_ctzll(left));
+            const unsigned char* k = cache + ((size_t)page * Hkv + h) * nvfp4_page_head_bytes(D);
+            if (tid == 0) top = 0;
+            float acc[32];
+#pragma unroll
+            for (int i = 0; i < 32; ++i) acc[i] = 0.0f;
+#pragma unroll
+            for (int p = 0; p < 128 / KEYS; ++p) {
+                const int key = p * KEYS + kk;
+                const uint4v c = *reinterpret_cast<const uint4v*>(k + key * (D / 2) + 16 * ch);
+                const uint32_t sc = *reinterpret_cast<const uint16_t*>(k + 128 * (D / 2) + key * (D / 16) + 2 * ch);
+                typedef float float2v __attribute__((ext_vector_type(2)));
+                const float s0 = __builtin_amdgcn_cvt_scalef32_f32_fp8(sc, 1.0f, 0), s1 = __builtin_amdgcn_cvt_scalef32_f32_fp8(sc, 1.0f, 1);
+#pragma unroll
+                for (int w = 0; w < 4; ++w) {
+                    const float s = w < 2 ? s0 : s1;
+#define AQ_ADD2(J) { const float2v v = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c[w], 1.0f, J); acc[8 * w + 2 * J] = fmaf(v[0], s, acc[8 * w + 2 * J]); acc[8 * w + 2 * J + 1] = fmaf(v[1], s, acc[8 * w + 2 * J + 1]); }
+                    AQ_ADD2(0) AQ_ADD2(1) AQ_ADD2(2) AQ_ADD2(3)
+#undef AQ_ADD2
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < 32; ++i) {
+                const float x = xor_tree<NCH, 32>(__uint_as_float((uint32_t)(int)(acc[i] * 1024.0f)), OpAddInt{});
+                if (lane < NCH) part[wave][32 * ch + i] = (int)__float_as_uint(x);
+            }
+            __syncthreads();
+            int sum = 0;
+            if (tid < D) {
+                sum = part[0][tid] + part[1][tid] + part[2][tid] + part[3][tid];
+                atomicMax(&top, abs(sum));
+            }
+            __syncthreads();
+            const int e = (top > 0 ? 32 - __builtin_clz((unsigned)top) : 0) - 7;
+            int code;
+            if (e <= 0) code = sum * (1 << -e);
+            else {
+                code = sum >> e;
+                const int rest = sum - (code << e), half = 1 << (e - 1);
+                code += rest > half || (rest == half && (code & 1)) ? 1 : 0;
+            }
+            uint32_t w = (uint32_t)min(max(code, -127), 127) & 0xFFu;
+            w |= lane_down<1>(w) << 8;
+            w |= lane_down<2>(w) << 16;
+            unsigned char* dst = summary + ((size_t)page * Hkv + h) * (D + kSummaryTail);
+            if (tid < D && (tid & 3) == 0) *reinterpret_cast<uint32_t*>(dst + tid) = w;
+            if (tid == 0) *reinterpret_cast<float*>(dst + D) = __uint_as_float((uint32_t)(e + 110) << 23);
+            __syncthreads();                                      // (top and part have been read)
+        }
+    }
+}
+
+// ---------------------------------------------------------------------------------------------- what a workgroup's tokens are
+// Sequence (-1: of none) and position (below 0: before the first key) of tokens t0 .. t0 + nt - 1, nt <= 16.
+__device__ inline void find_tokens(const StepArgs& a, int t0, int nt, int* seq, int* pos)
+{
+    const int tid = threadIdx.x;
+    if (tid < 16) { seq[tid] = -1; pos[tid] = -1; }
+    __syncthreads();
+    for (int b = tid; b < a.B; b += 256) {
+        const int s = min(max(a.cu_q[b], 0), a.T), e = min(max(a.cu_q[b + 1], s), a.T);
+        const int len = max(0, min(a.kv_lens[b], a.max_pages * 128));
+        for (int t = max(s, t0); t < min(e, t0 + nt); ++t) { seq[t - t0] = b; pos[t - t0] = max(len - e + t, -1); }
+    }
+    __syncthreads();
+}
+
+// ---------------------------------------------------------------------------------------------- the choice
+// Order of floats as of unsigned numbers.
+__device__ inline uint32_t ordered(float x) { const uint32_t u = __float_as_uint(x); return (u >> 31) ? ~u : (u | 0x80000000u); }
+
+// 16 rows of the matrix instruction are the query heads of a kv head's group, padded to GP by heads that are there, for 16 / GP tokens, against 16 pages at a
+// time.  Scores stay in LDS; a wave then finds the threshold of a token's best ones bit by bit.
+template <int D, int GP>
+__global__ __launch_bounds__(256) void select_kernel(const SelectArgs a, int nt /* tokens of a workgroup */, int tiles)
+{
+    constexpr int NS = D / 64;
+    extern __shared__ uint32_t keys[];                            // [nt][max_pages]
+    __shared__ int seq[16], pos[16];
+    const StepArgs& s = a.s;
+    const int tid = threadIdx.x, lane = tid & 63, cc = lane & 15, g = lane >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int G = s.Hq / s.Hkv, subs = (G + 15) / 16, S = s.max_pages;
+    int h, tile;
+    head_tile_of_block((int)blockIdx.x, s.Hkv, tiles, h, tile);
+    const int t0 = tile * nt;
+    find_tokens(s, t0, nt, seq, pos);
+
+    // one power of two for the group: brings its largest magnitude to [64, 128) (magnitudes below 2^-121 count as that)
+    const int t = min(t0 + min(cc / GP, nt - 1), s.T - 1);
+    auto row = [&](int sub, uint4v (&x)[2 * NS]) __attribute__((always_inline)) {
+        const uint16_t* q = s.q + (size_t)t * s.q_token + (size_t)(h * G + min(16 * sub + cc % GP, G - 1)) * s.q_head + 16 * g;
+#pragma unroll
+        for (int i = 0; i < 2 * NS; ++i) x[i] = *reinterpret_cast<const uint4v*>(q + 64 * (i >> 1) + 8 * (i & 1));
+    };
+    float amax = 0.0f;
+    uint4v x[2 * NS];
+    for (int sub = 0; sub < subs; ++sub) { row(sub, x); amax = fmaxf(amax, largest_of(x)); }
+    amax = lanes_max<16, 32>(amax);
+    if constexpr (GP >= 2) amax = lanes_max<1, GP / 2>(amax);
+    const float f = __uint_as_float((260u - max(__float_as_uint(amax) >> 23, 6u)) << 23);
+
+    for (int sub = 0; sub < subs; ++sub) {
+        if (subs > 1) row(sub, x);
+        intx4 q8[NS];
+#pragma unroll
+        for (int i = 0; i < NS; ++i)
+#pragma unroll
+            for (int w = 0; w < 4; ++w) {
+                uint32_t r = 0;
+#pragma unroll
+                for (int j = 0; j < 2; ++j) {
+                    const uint32_t p = x[2 * i + (w >> 1)][2 * (w & 1) + j];
+                    // (1.5 2^23 added: rounded to nearest even, in two's complement in the low bits)
+                    const uint32_t lo = __float_as_uint(__builtin_amdgcn_fmed3f(__uint_as_float(p << 16) * f, -127.0f, 127.0f) + 12582912.0f) & 0xFFu;
+                    const uint32_t hi = __float_as_uint(__builtin_amdgcn_fmed3f(__uint_as_float(p & 0xFFFF0000u) * f, -127.0f, 127.0f) + 12582912.0f) & 0xFFu;
+                    r |= (lo | hi << 8) << (16 * j);
+                }
+                q8[i][w] = (int)r;
+            }
+        for (int i0 = 0, i1; i0 < nt; i0 = i1) {                  // tokens of one sequence
+            const int b = uniform(seq[i0]);
+            int hi = 0;                                           // behind the last page that competes
+            for (i1 = i0; i1 < nt && uniform(seq[i1]) == b; ++i1) {
+                const int own = uniform(pos[i1]) >> 7;
+                if (own + 1 > a.n_blocks) hi = max(hi, own + 1 - a.last);
+            }
+            if (b < 0) continue;
+            for (int j0 = (a.first & ~15) + 16 * wave; j0 < hi; j0 += 64) {
+                const int j = j0 + cc, id = s.table[(size_t)b * s.max_pages + min(j, s.max_pages - 1)];
+                const bool live = id >= 0 && id < s.num_pages;
+                const unsigned char* rec = a.summary + ((size_t)(live ? id : 0) * s.Hkv + h) * (D + kSummaryTail);
+                intx4 acc = {0, 0, 0, 0};
+#pragma unroll
+                for (int i = 0; i < NS; ++i) acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(q8[i], *reinterpret_cast<const intx4*>(rec + 64 * i + 16 * g), acc, 0, 0, 0);
+                const float scale = live ? *reinterpret_cast<const float*>(rec + D) : 0.0f;
+                // rows 4 g .. 4 g + 3 of page j: the largest of a token's heads
+                auto put = [&](int token, int v) __attribute__((always_inline)) {
+                    if (token < i0 || token >= i1 || j >= hi) return;
+                    const uint32_t key = ordered(fmaf((float)v, scale, 0.0f));
+                    uint32_t* p = keys + token * S + j;
+                    *p = sub == 0 ? key : max(*p, key);
+                };
+                if constexpr (GP == 1) { put(4 * g, acc[0]); put(4 * g + 1, acc[1]); put(4 * g + 2, acc[2]); put(4 * g + 3, acc[3]); }
+                else if constexpr (GP == 2) { put(2 * g, max(acc[0], acc[1])); put(2 * g + 1, max(acc[2], acc[3])); }
+                else {
+                    int m = max(max(acc[0], acc[1]), max(acc[2], acc[3]));
+                    if constexpr (GP >= 8) { const auto r = __builtin_amdgcn_permlane16_swap((uint32_t)m, (uint32_t)m, false, false); m = max((int)r[0], (int)r[1]); }
+                    if constexpr (GP >= 16) { const auto r = __builtin_amdgcn_permlane32_swap((uint32_t)m, (uint32_t)m, false, false); m = max((int)r[0], (int)r[1]); }
+                    if (GP == 4 || (GP == 8 && (g & 1) == 0) || g == 0) put(4 * g / GP, m);
+                }
+            }
+        }
+    }
+    __syncthreads();
+
+    for (int i = wave; i < nt; i += 4) {
+        if (uniform(seq[i]) < 0) continue;
+        const int own = uniform(pos[i]) >> 7, nb = own + 1;       // (position -1: page -1)
+        int* out = a.blocks + ((size_t)(t0 + i) * s.Hkv + h) * a.n_blocks;
+        if (nb <= a.n_blocks) {
+            for (int j = lane; j < a.n_blocks; j += 64) out[j] = j < nb ? j : -1;
+            continue;
+        }
+        const int lo = a.first, hi = nb - a.last, m = a.n_blocks - a.first - a.last;       // hi - lo > m
+        const uint32_t* key = keys + i * S;
+        // the m-th largest score, and how many of its equals are taken, from the front
+        uint32_t limit = 0xFFFFFFFFu;
+        int ties = 0;
+        if (m > 0) {
+            limit = 0;
+            for (int bit = 31; bit >= 0; --bit) {
+                const uint32_t cand = limit | (1u << bit);
+                int n = 0;
+                for (int j = lo + lane; j < hi; j += 64) n += key[j] >= cand ? 1 : 0;
+                if (lane_total(n) >= m) limit = cand;
+            }
+            int above = 0;
+            for (int j = lo + lane; j < hi; j += 64) above += key[j] > limit ? 1 : 0;
+            ties = m - lane_total(above);
+        }
+        int at = 0;
+        for (int j0 = 0; j0 < nb; j0 += 64) {
+            const int j = j0 + lane;
+            const bool comp = j >= lo && j < hi;
+            const uint32_t k = comp ? key[j] : 0u;
+            const unsigned long long eq = __builtin_amdgcn_ballot_w64(comp && k == limit && m > 0), below = (1ull << lane) - 1;
+            const bool take = j < nb && (!comp || (m > 0 && (k > limit || (k == limit && (int)__builtin_popcountll(eq & below) < ties))));
+            ties -= min(ties, (int)__builtin_popcountll(eq));
+            const unsigned long long all = __builtin_amdgcn_ballot_w64(take);
+            if (take) out[at + (int)__builtin_popcountll(all & below)] = j;
+            at += (int)__builtin_popcountll(all);
+        }
+    }
+}
+
+// ---------------------------------------------------------------------------------------------- attention
+constexpr int kEntries = 2048;        // (token, page)s of a workgroup at most
+
+// 16 rows: the G query heads of a kv head for nt tokens (rows = token * G + head of the group), or 16 of more heads for one token.  Their pages are taken together, each
+// once, whichever of the tokens asked for it (the others' rows are masked); split over `splits` workgroups where there are few rows.
+struct SparsePlan { int nt, subs, tiles, splits; };
+struct SparseWs { float *part_o /* [unit][split][16][D] */, *part_ml /* [unit][split][16][2]: maximum, sum; a sum below 0: not a row of any sequence */; };
+
+template <int D>
+__global__ __launch_bounds__(256, 3) void sparse_kernel(const SparseArgs a, const SparsePlan p, const SparseWs ws)
+{
+    constexpr int NS = D / 32, NDT = D / 16;
+    constexpr int SETS = D == 64 ? 3 : 2;
+    constexpr int RS = 2 * D + 32;                                // bytes per key of the V tile
+    constexpr size_t VOFF = (size_t)128 * (D / 2 + D / 16);
+    __shared__ __align__(16) unsigned char stage[4 * 32 * RS];     // first which tokens ask for a page, 16 bits each; then per wave V of 32 keys; at the end the waves' sums
+    __shared__ uint32_t ents[kEntries];                           // page of the sequence, and the tokens that ask for it << 16
+    __shared__ float ml[2][4][16];
+    __shared__ int seq[16], pos[16], red[4];
+    const StepArgs& s = a.s;
+    const int tid = threadIdx.x, lane = tid & 63, cc = lane & 15, g = lane >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int G = s.Hq / s.Hkv;
+    int h, rest;
+    head_tile_of_block((int)blockIdx.x, s.Hkv, p.tiles * p.subs * p.splits, h, rest);
+    const int split = rest % p.splits, sub = rest / p.splits % p.subs, tile = rest / p.splits / p.subs;
+    const int t0 = tile * p.nt, rows = p.subs > 1 ? min(16, G - 16 * sub) : p.nt * G;
+    find_tokens(s, t0, p.nt, seq, pos);
+
+    // the pages that any of the tokens asks for, sequence by sequence
+    int total = 0;
+    uint32_t* tab = reinterpret_cast<uint32_t*>(stage);
+    static_assert(sizeof(stage) >= 8192 * 2);
+    for (int i0 = 0, i1; i0 < p.nt; i0 = i1) {
+        const int b = uniform(seq[i0]);
+        int nb = 0;
+        for (i1 = i0; i1 < p.nt && uniform(seq[i1]) == b; ++i1) nb = max(nb, (uniform(pos[i1]) >> 7) + 1);
+        if (b < 0 || nb == 0) continue;
+        const int words = (nb + 1) / 2;
+        for (int w = tid; w < words; w += 256) tab[w] = 0;
+        __syncthreads();
+        for (int x = tid; x < (i1 - i0) * a.n_blocks; x += 256) {
+            const int i = i0 + x / a.n_blocks, blk = a.blocks[((size_t)(t0 + i) * s.Hkv + h) * a.n_blocks + x % a.n_blocks];
+            if (blk >= 0 && blk <= (pos[i] >> 7)) atomicOr(&tab[blk >> 1], 1u << (i + 16 * (blk & 1)));
+        }
+        __syncthreads();
+        for (int w0 = 0; w0 < words; w0 += 256) {
+            const uint32_t w = w0 + tid < words ? tab[w0 + tid] : 0u;
+            const int n = ((w & 0xFFFFu) != 0) + ((w >> 16) != 0);
+            int all;
+            int at = total + wg_scan<4>(n, red, all) - n;
+            if (w & 0xFFFFu) ents[at++] = 2 * (w0 + tid) | w << 16;
+            if (w >> 16) ents[at] = (2 * (w0 + tid) + 1) | (w & 0xFFFF0000u);
+            total += all;
+        }
+        __syncthreads();
+    }
+    const int e0 = (int)((long long)total * split / p.splits), cnt = (int)((long long)total * (split + 1) / p.splits) - e0;
+
+    // this lane's row: its token, head and last key
+    const int r = min(cc, rows - 1), tok = p.subs > 1 ? 0 : r / G, head = h * G + (p.subs > 1 ? 16 * sub + r : r % G);
+    const int k_last = pos[tok];
+    const uint32_t row_bit = 1u << (16 + tok);
+    uint32_t everyone = 0;                                        // the tokens that there are, and the last key that all of them see
+    int see_last = 0x7FFFFFFF;
+    for (int i = 0; i < p.nt; ++i)
+        if (uniform(seq[i]) >= 0) { everyone |= 1u << (16 + i); see_last = min(see_last, uniform(pos[i])); }
+
+    floatx4 o[NDT];
+    float m = -INFINITY, up_to = -INFINITY, l = 0.0f;
+#pragma unroll
+    for (int dt = 0; dt < NDT; ++dt) o[dt] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
+    if (cnt > 0) {
+        unsigned char* stg = stage + wave * (32 * RS);
+        // (the two 16-byte pieces of every 32 change places in keys 4 - 7 of 8: a store serves eight lanes, eight keys, at a time on 32 banks)
+        const uint32_t tr_base = lds_addr_of(stg) + (uint32_t)((4 * g + (cc >> 2)) * RS + 8 * ((cc & 3) ^ (2 * (g & 1))));
+        int ent_lane = 0, id_lane = 0, end_lane = 0, id_end = 0;  // of entry id_end - 64 + lane: itself, its page, the last key that any of its tokens sees
+        auto ids = [&](int i0) __attribute__((always_inline)) {
+            ent_lane = (int)ents[e0 + min(i0 + lane, cnt - 1)];
+            const int last = 15 - __builtin_clz((uint32_t)ent_lane), b = seq[last];      // (tokens of one sequence follow each other: the last sees most)
+            end_lane = pos[last];
+            id_lane = s.table[(size_t)b * s.max_pages + (ent_lane & 0xFFFF)];
+            asm volatile("" : "+v"(id_lane));                     // (waited for here and not at every use)
+            id_end = i0 + 64;
+        };
+        ids(0);
+        uint4v x[NS];
+        {
+            const uint16_t* q = s.q + (size_t)min(t0 + tok, s.T - 1) * s.q_token + (size_t)head * s.q_head + (D / 4) * g;
+#pragma unroll
+            for (int i = 0; i < NS; ++i) x[i] = *reinterpret_cast<const uint4v*>(q + 8 * i);
+        }
+        struct Tile { Raw<D> k[2], v[2]; bool live; uint32_t ent; int end; };
+        auto load = [&](Tile& t, int i) __attribute__((always_inline)) {
+            if (i >= id_end) ids(id_end);
+            const int page = __builtin_amdgcn_readlane(id_lane, i - (id_end - 64));
+            t.ent = (uint32_t)__builtin_amdgcn_readlane(ent_lane, i - (id_end - 64));
+            t.end = __builtin_amdgcn_readlane(end_lane, i - (id_end - 64));
+            t.live = page >= 0 && page < s.num_pages;
+            const unsigned char* part = a.cache + ((size_t)(t.live ? page : 0) * s.Hkv + h) * (2 * VOFF);
+#pragma unroll
+            for (int blk = 0; blk < 2; ++blk) t.k[blk] = load_raw<D>(part, 32 * wave + 16 * blk + cc, g);
+#pragma unroll
+            for (int blk = 0; blk < 2; ++blk) t.v[blk] = load_raw<D>(part + VOFF, 32 * wave + 16 * blk + cc, g);
+        };
+        Tile t[SETS];
+#pragma unroll
+        for (int i = 0; i + 1 < SETS; ++i) load(t[i], min(i, cnt - 1));
+
+        // Q: row cc, d = (D/4) g + 8 s .. + 7
+        half8 qreg[NS];
+        float c_row;
+        {
+            const float amax = lanes_max<16, 32>(largest_of(x));
+            float f, inv;
+            row_factor(amax, f, inv);
+#pragma unroll
+            for (int i = 0; i < NS; ++i)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    qreg[i][2 * j]     = (half_t)(__uint_as_float(x[i][j] << 16) * f);
+                    qreg[i][2 * j + 1] = (half_t)(__uint_as_float(x[i][j] & 0xFFFF0000u) * f);
+                }
+            c_row = fmaxf(a.c * inv, kLeastFactor);
+        }
+        auto step = [&](const Tile& t) __attribute__((always_inline)) {
+            const int kt = (int)(t.ent & 0xFFFFu) * 128 + 32 * wave;
+            const bool masked = (t.ent & 0xFFFF0000u) != everyone || kt + 31 > see_last;
+            floatx4 sc[2];
+#pragma unroll
+            for (int blk = 0; blk < 2; ++blk) {
+                const half2v ks = scales_of<D>(t.k[blk], g, t.live);
+                sc[blk] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+                for (int j = 0; j < NS; ++j) sc[blk] = __builtin_amdgcn_mfma_f32_16x16x32_f16(values8<D>(t.k[blk], ks, j), qreg[j], sc[blk], 0, 0, 0);
+            }
+            // V through LDS: written key by key, read back with four keys of one d in a lane
+            __builtin_amdgcn_wave_barrier();
+#pragma unroll
+            for (int blk = 0; blk < 2; ++blk) {
+                const half2v vs = scales_of<D>(t.v[blk], g, t.live && kt + 16 * blk + cc <= t.end);
+#pragma unroll
+                for (int j = 0; j < NS; ++j) *reinterpret_cast<half8*>(stg + (16 * blk + cc) * RS + (D / 2) * g + 16 * (j ^ ((cc >> 2) & 1))) = values8<D>(t.v[blk], vs, j);
+            }
+            __builtin_amdgcn_wave_barrier();
+            if (masked) {
+                const int last = (t.ent & row_bit) ? k_last : -1;
+#pragma unroll
+                for (int j = 0; j < 8; ++j)
+                    if (kt + 16 * (j >> 2) + 4 * g + (j & 3) > last) sc[j >> 2][j & 3] = -INFINITY;
+            }
+            float mx = max_nc(max_nc(max_nc(sc[0][0], sc[0][1]), max_nc(sc[0][2], sc[0][3])), max_nc(max_nc(sc[1][0], sc[1][1]), max_nc(sc[1][2], sc[1][3])));
+            mx = lanes_max<16, 32>(mx);
+            if (__builtin_amdgcn_ballot_w64(mx > up_to) != 0) {
+                const float m_new = fmaxf(m, fmaf(mx, c_row, -kTop)), alpha = __builtin_amdgcn_exp2f(m - (m_new == -INFINITY ? 0.0f : m_new));
+                m = m_new;
+                up_to = score_up_to(m_new, c_row);
+                l *= alpha;
+#pragma unroll
+                for (int dt = 0; dt < NDT; ++dt) o[dt] *= alpha;
+            }
+            const float m_at = m == -INFINITY ? 0.0f : m;
+            float add = 0.0f;
+            half8 pt;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const float x = __builtin_amdgcn_exp2f(fmaf(sc[j >> 2][j & 3], c_row, -m_at));
+                add += x;
+                pt[j] = (half_t)x;
+            }
+            l += add;
+#pragma unroll
+            for (int dt = 0; dt < NDT; ++dt) {
+                const uint2v u = lds_read_tr16_at(tr_base + 32 * dt), w = lds_read_tr16_at(tr_base + 32 * dt + 16 * RS);
+                const uint4v av = {u[0], u[1], w[0], w[1]};
+                o[dt] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(half8, av), pt, o[dt], 0, 0, 0);
+            }
+        };
+        for (int i = 0; i < cnt; i += SETS) {
+#pragma unroll
+            for (int x = 0; x < SETS; ++x) {
+                if (x > 0 && i + x >= cnt) break;
+                load(t[(x + SETS - 1) % SETS], min(i + x + SETS - 1, cnt - 1));
+                step(t[x]);
+            }
+        }
+    }
+
+    // the four waves' sums, in units of their common maximum
+    constexpr int SS = D + 4;                                     // floats per row of the sums (16 rows are written side by side)
+    static_assert(4 * 16 * SS * 4 <= sizeof(stage));
+    float* sums = reinterpret_cast<float*>(stage);
+    l = lanes_sum<16, 32>(l);
+    if (g == 0) { ml[0][wave][cc] = m; ml[1][wave][cc] = l; }
+    __syncthreads();
+    const float top = fmaxf(fmaxf(ml[0][0][cc], ml[0][1][cc]), fmaxf(ml[0][2][cc], ml[0][3][cc])), f = __builtin_amdgcn_exp2f(m - (top == -INFINITY ? 0.0f : top));
+#pragma unroll
+    for (int dt = 0; dt < NDT; ++dt) *reinterpret_cast<floatx4*>(sums + (wave * 16 + cc) * SS + 16 * dt + 4 * g) = o[dt] * f;
+    __syncthreads();
+    const size_t slot = (((size_t)tile * s.Hkv + h) * p.subs + sub) * p.splits + split;
+    for (int e = tid; e < rows * (D / 4); e += 256) {
+        const int q = e / (D / 4), d = e % (D / 4) * 4, tk = p.subs > 1 ? 0 : q / G, hd = h * G + (p.subs > 1 ? 16 * sub + q : q % G);
+        const bool on = seq[tk] >= 0;
+        const float tp = fmaxf(fmaxf(ml[0][0][q], ml[0][1][q]), fmaxf(ml[0][2][q], ml[0][3][q])), at = tp == -INFINITY ? 0.0f : tp;
+        float lt = 0.0f;
+        floatx4 v = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+        for (int x = 0; x < 4; ++x) {
+            lt += ml[1][x][q] * __builtin_amdgcn_exp2f(ml[0][x][q] - at);
+            v += *reinterpret_cast<const floatx4*>(sums + (x * 16 + q) * SS + d);
+        }
+        if (p.splits > 1) {
+            *reinterpret_cast<floatx4*>(ws.part_o + (slot * 16 + q) * D + d) = v;
+            if (d == 0) { ws.part_ml[(slot * 16 + q) * 2] = tp; ws.part_ml[(slot * 16 + q) * 2 + 1] = on ? lt : -1.0f; }
+        } else if (on) {
+            v *= lt != 0.0f ? 1.0f / lt : 0.0f;
+            const uint2v y = {pack_bf16x2_cvt(v[0], v[1]), pack_bf16x2_cvt(v[2], v[3])};
+            *reinterpret_cast<uint2v*>(a.o + (size_t)(t0 + tk) * a.o_token + (size_t)hd * a.o_head + d) = y;
+            if (d == 0 && a.lse) a.lse[(size_t)(t0 + tk) * s.Hq + hd] = lt != 0.0f ? tp * 0.6931471805599453f + logf(lt) : -INFINITY;
+        }
+    }
+}
+
+// O and lse of rows whose pages were split: D / 4 threads to a row.
+template <int D>
+__global__ __launch_bounds__(256) void sparse_merge_kernel(const SparseArgs a, const SparsePlan p, const SparseWs ws)
+{
+    constexpr int nt = D / 4;
+    const StepArgs& s = a.s;
+    const long long x = (long long)blockIdx.x * (256 / nt) + threadIdx.x / nt;
+    const int d = threadIdx.x % nt * 4, t = (int)(x / s.Hq), hd = (int)(x % s.Hq), G = s.Hq / s.Hkv, h = hd / G, gh = hd % G;
+    if (t >= s.T) return;
+    const int sub = p.subs > 1 ? gh / 16 : 0, row = p.subs > 1 ? gh % 16 : t % p.nt * G + gh;
+    const size_t slot0 = (((size_t)(t / p.nt) * s.Hkv + h) * p.subs + sub) * p.splits;
+    float M = -INFINITY, l = 0.0f;
+    floatx4 v = {0.0f, 0.0f, 0.0f, 0.0f};
+    constexpr int K = 8;                                          // at a time: one trip to memory
+    for (int i0 = 0; i0 < p.splits; i0 += K) {
+        floatx4 po[K];
+        float pm[K], pl[K];
+#pragma unroll
+        for (int k = 0; k < K; ++k) {
+            const size_t at = (slot0 + min(i0 + k, p.splits - 1)) * 16 + row;
+            po[k] = *reinterpret_cast<const floatx4*>(ws.part_o + at * D + d);
+            pm[k] = ws.part_ml[at * 2];
+            pl[k] = ws.part_ml[at * 2 + 1];
+        }
+        if (pl[0] < 0.0f) return;                                 // (no sequence's row)
+        float top = M;
+#pragma unroll
+        for (int k = 0; k < K; ++k) { if (i0 + k >= p.splits) pm[k] = -INFINITY; top = fmaxf(top, pm[k]); }
+        const float at = top == -INFINITY ? 0.0f : top, al = __builtin_amdgcn_exp2f(M - at);
+        M = top; l *= al; v *= al;
+#pragma unroll
+        for (int k = 0; k < K; ++k) { const float f = __builtin_amdgcn_exp2f(pm[k] - at); l = fmaf(pl[k], f, l); v += po[k] * f; }
+    }
+    v *= l != 0.0f ? 1.0f / l : 0.0f;
+    *reinterpret_cast<uint2v*>(a.o + (size_t)t * a.o_token + (size_t)hd * a.o_head + d) = uint2v{pack_bf16x2_cvt(v[0], v[1]), pack_bf16x2_cvt(v[2], v[3])};
+    if (d == 0 && a.lse) a.lse[(size_t)t * s.Hq + hd] = l != 0.0f ? M * 0.6931471805599453f + logf(l) : -INFINITY;
+}
+
+inline SparsePlan sparse_plan(int T, int Hq, int Hkv, int max_q, int n_blocks, int cus)
+{
+    const int G = Hq / Hkv;
+    SparsePlan p;
+    p.subs = (G + 15) / 16;
+    p.nt = p.subs > 1 ? 1 : 16 / G;
+    if (p.nt > max_q) p.nt = max_q;
+    if (p.nt > kEntries / n_blocks) p.nt = kEntries / n_blocks;
+    p.tiles = (T + p.nt - 1) / p.nt;
+    const long long units = (long long)p.tiles * Hkv * p.subs, wgs = 3ll * cus;
+    long long splits = units > 0 ? wgs / units : 1;
+    if (splits > n_blocks) splits = n_blocks;
+    p.splits = splits < 2 ? 1 : (int)splits;
+    return p;
+}
+inline SparseWs carve_sparse(void* ws, const SparsePlan& p, int Hkv, int D, size_t& bytes)
+{
+    const size_t rows = p.splits > 1 ? (size_t)p.tiles * Hkv * p.subs * p.splits * 16 : 0;
+    bytes = rows * (D + 2) * 4 + 256;
+    return SparseWs{(float*)ws, (float*)ws + rows * D};
+}
+template <int D>
+int launch_sparse_of(const SparseArgs& a, const SparsePlan& p, const SparseWs& w, hipStream_t st)
+{
+    hipLaunchKernelGGL((sparse_kernel<D>), dim3((unsigned)p.tiles * a.s.Hkv * p.subs * p.splits), dim3(256), 0, st, a, p, w);
+    if (hipGetLastError() != hipSuccess) return -1;
+    if (p.splits > 1) {
+        const int per = 256 / (D / 4);
+        hipLaunchKernelGGL((sparse_merge_kernel<D>), dim3((unsigned)(((long long)a.s.T * a.s.Hq + per - 1) / per)), dim3(256), 0, st, a, p, w);
+    }
+    return hipGetLastError() == hipSuccess ? 0 : -1;
+}
+template <int D, int GP>
+int launch_select_of(const SelectArgs& a, int nt, hipStream_t st)
+{
+    const int tiles = (a.s.T + nt - 1) / nt;
+    hipLaunchKernelGGL((select_kernel<D, GP>), dim3((unsigned)tiles * a.s.Hkv), dim3(256), (size_t)nt * a.s.max_pages * 4, st, a, nt, tiles);
+    return hipGetLastError() == hipSuccess ? 0 : -1;
+}
+template <int D>
+int launch_select_d(const SelectArgs& a, int max_q, hipStream_t st)
+{
+    const int G = a.s.Hq / a.s.Hkv;
+    int gp = 1;
+    while (gp < G && gp < 16) gp *= 2;
+    int nt = 16 / gp;
+    if (nt > max_q) nt = max_q;
+    const int room = 12288 / a.s.max_pages;                       // tokens whose scores fit 48 KiB of LDS
+    if (nt > room) nt = room > 1 ? room : 1;                      // (one token of 8192 pages: 32 KiB)
+    switch (gp) {
+        case 1: return launch_select_of<D, 1>(a, nt, st);
+        case 2: return launch_select_of<D, 2>(a, nt, st);
+        case 4: return launch_select_of<D, 4>(a, nt, st);
+        case 8: return launch_select_of<D, 8>(a, nt, st);
+        default: return launch_select_of<D, 16>(a, nt, st);
+    }
+}
+
+}  // namespace
+
+int launch_summarize(const void* cache, int num_pages, int Hkv, int D, const long long* slots, int T, void* summary, hipStream_t st)
+{
+    // rows of a workgroup: a page is complete at most once in 128 rows of a prompt, but every row of a step of single tokens may complete one
+    const int rows = T > 8192 ? 128 : 16;
+    const dim3 grid((T + rows - 1) / rows, Hkv);
+    if (D == 128) hipLaunchKernelGGL((summarize_kernel<128>), grid, dim3(256), 0, st, (const unsigned char*)cache, num_pages, Hkv, slots, T, rows, (unsigned char*)summary);
+    else          hipLaunchKernelGGL((summarize_kernel<64>), grid, dim3(256), 0, st, (const unsigned char*)cache, num_pages, Hkv, slots, T, rows, (unsigned char*)summary);
+    return hipGetLastError() == hipSuccess ? 0 : -1;
+}
+
+int launch_select(const SelectArgs& a, int max_q, int D, hipStream_t st) { return D == 128 ? launch_select_d<128>(a, max_q, st) : launch_select_d<64>(a, max_q, st); }
+
+size_t sparse_ws_bytes(int T, int Hq, int Hkv, int max_q, int n_blocks, int D)
+{
+    size_t bytes;
+    carve_sparse(nullptr, sparse_plan(T, Hq, Hkv, max_q, n_blocks, kChipCus), Hkv, D, bytes);
+    return bytes;
+}
+
+int launch_sparse(const SparseArgs& a, int max_q, int D, void* ws, hipStream_t st)
+{
+    size_t bytes;
+    const SparsePlan p = sparse_plan(a.s.T, a.s.Hq, a.s.Hkv, max_q, a.n_blocks, kChipCus);
+    const SparseWs w = carve_sparse(ws, p, a.s.Hkv, D, bytes);
+    return D == 128 ? launch_sparse_of<128>(a, p, w, st) : launch_sparse_of<64>(a, p, w, st);
+}
+
+}  // namespace aq
