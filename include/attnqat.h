@@ -475,9 +475,11 @@ int attnqat_fwd_kv4_ragged(const void* q, int64_t q_token_stride, int64_t q_head
  * Rotary positions.  A rotary table says how a head's values turn: pair i of `pairs` by the angle p freq[i], p the position in axis axis[i] (time, height
  * and width of a video's token, say) and freq[i] radians per position: (a, b) -> (a cos - b sin, a sin + b cos).  layout ATTNQAT_ROPE_PAIRED: pair i is
  * elements 2i and 2i+1; ATTNQAT_ROPE_HALVES: elements i and i + pairs (pairs a multiple of 8: ATTNQAT_ESHAPE otherwise).  1 <= pairs <= d / 2, 1 to
- * ATTNQAT_ROPE_MAX_AXES axes, finite frequencies: ATTNQAT_EINVAL otherwise; elements from 2 pairs on stay as they are, bit for bit.  The table is HOST
- * memory and read during the call.  Angles are exact to 2^-32 turns and |p| 2^-52 times the frequency, however far the position; turned values are
- * computed in fp32 and rounded once, to bf16.
+ * ATTNQAT_ROPE_MAX_AXES axes: ATTNQAT_EINVAL otherwise; elements from 2 pairs on stay as they are, bit for bit.  Angles are exact to 2^-32 turns and
+ * |p| 2^-52 times the frequency, however far the position; turned values are computed in fp32 and rounded once, to bf16.
+ *
+ * attnqat_rope_table fills a table, HOST memory that the program keeps and the calls below read while they run, from `pairs` (at most 64) finite frequencies
+ * and axes.  In it a frequency is a fraction of a turn per position, times 2^64 (whole turns change nothing), and an axis two bits, sixteen pairs to a word.
  *
  * attnqat_rope_fwd turns q [B,Hq,L,d] and k [B,Hkv,L,d] into q_out and k_out: what attnqat_fwd and its kind take, where these are contiguous.  All four have d
  * innermost and any stride per batch, head and token (in elements, multiples of 8; pointers 16-byte aligned), such as the views of one projection's
@@ -495,9 +497,10 @@ int attnqat_fwd_kv4_ragged(const void* q, int64_t q_token_stride, int64_t q_head
 #define ATTNQAT_ROPE_MAX_AXES       4
 typedef struct attnqat_rope {
     int pairs, axes, layout, reserved;
-    double freq[64];
-    uint8_t axis[64];
+    uint64_t turns[64];
+    uint32_t axis[4];
 } attnqat_rope;
+int attnqat_rope_table(attnqat_rope* rope, int pairs, int axes, int layout, const double* freq, const uint8_t* axis);
 int attnqat_rope_fwd(const void* q, int64_t q_batch_stride, int64_t q_head_stride, int64_t q_token_stride,
                      const void* k, int64_t k_batch_stride, int64_t k_head_stride, int64_t k_token_stride,
                      int B, int Hq, int Hkv, int L, int d, int dtype, const int* positions, int64_t positions_batch, const attnqat_rope* rope,

@@ -58,6 +58,7 @@ _SIGNATURES = {
     "attnqat_kv4_ragged_workspace_bytes": (_sz, [_i, _i, _i, _i, _i, _i, _i]),
     "attnqat_fwd_kv4_ragged": (_i, [_vp, _ll, _ll, _vp, _i, _i, _i, _i, _i, _i, _i, _i, _f, _i, _vp, _i, _vp, _i, _vp, _vp, _ll, _ll, _vp,
                                     _vp, _sz, _vp]),
+    "attnqat_rope_table": (_i, [_vp, _i, _i, _i, _vp, _vp]),
     "attnqat_rope_fwd": (_i, [_vp, _ll, _ll, _ll] * 2 + [_i] * 6 + [_vp, _ll, _vp] + [_vp, _ll, _ll, _ll] * 2 + [_vp]),
     "attnqat_rope_bwd": (_i, [_vp, _ll, _ll, _ll] * 2 + [_i] * 6 + [_vp, _ll, _vp] + [_vp, _ll, _ll, _ll] * 2 + [_vp]),
     "attnqat_kv_cache_append_rope": (_i, [_vp, _ll, _ll] * 3 + [_i] * 5 + [_vp, _vp, _vp, _i, _vp] + [_vp, _ll, _ll, _vp]),
@@ -443,7 +444,7 @@ ROPE_PAIRED, ROPE_HALVES = 0, 1
 class Rope(ctypes.Structure):
     """How the values of a head turn with their positions (host memory; made by ``rope_table``)."""
     _fields_ = [("pairs", ctypes.c_int), ("axes", ctypes.c_int), ("layout", ctypes.c_int), ("reserved", ctypes.c_int),
-                ("freq", ctypes.c_double * 64), ("axis", ctypes.c_uint8 * 64)]
+                ("turns", ctypes.c_uint64 * 64), ("axis", ctypes.c_uint32 * 4)]
 
 
 def rope_table(dims, theta: float = 10000.0, layout: str = "paired", freqs=None, axis=None) -> Rope:
@@ -464,51 +465,68 @@ def rope_table(dims, theta: float = 10000.0, layout: str = "paired", freqs=None,
     freqs, axis = [float(f) for f in freqs], [int(a) for a in axis]
     if len(freqs) != pairs or len(axis) != pairs or any(not 0 <= a < len(dims) for a in axis):
         raise AttnQatError(f"freqs and axis must have an entry for each of the {pairs} pairs, axis below {len(dims)}")
-    return Rope(pairs, len(dims), ROPE_HALVES if layout == "halves" else ROPE_PAIRED, 0, (ctypes.c_double * 64)(*freqs), (ctypes.c_uint8 * 64)(*axis))
+    rope = Rope()
+    _check(lib().attnqat_rope_table(ctypes.addressof(rope), pairs, len(dims), ROPE_HALVES if layout == "halves" else ROPE_PAIRED, (ctypes.c_double * pairs)(*freqs), (ctypes.c_uint8 * pairs)(*axis)))
+    rope.address = ctypes.addressof(rope)
+    return rope
 
 
-def _heads(name, t, shape, dev):
-    """Strides per batch, head and token of a bf16 CUDA tensor [B,heads,L,d]."""
-    if not (t.dim() == 4 and t.dtype is _BF and t.get_device() == dev == _current_device() and t.shape == shape and (t.stride(3) == 1 or t.numel() == 0)):
-        raise AttnQatError(f"{name} must be a bf16 tensor {tuple(shape)} on the current device (cuda:{_current_device()}), d innermost")
-    return t.stride()[:3]
-
-
-def _rope_call(name, q, k, positions, rope, out):
-    if q.dim() != 4 or (k is not None and k.dim() != 4):
-        raise AttnQatError("q and k must be [B,heads,L,d]")
-    B, Hq, L, d = q.shape
-    dev, Hkv = q.get_device(), 0 if k is None else k.shape[1]
+def _rope_refuse(q, k, positions, rope, out):
+    """Names what is not as it should be."""
     if not isinstance(rope, Rope):
         raise AttnQatError("rope must be a table made by rope_table")
-    if not (positions.dtype is _I32 and positions.get_device() == dev and positions.is_contiguous() and positions.shape in ((L, rope.axes), (B, L, rope.axes))):
-        raise AttnQatError(f"positions must be a contiguous int32 tensor [{L},{rope.axes}] or [{B},{L},{rope.axes}] on the device of q")
+    if q.dim() != 4 or (k is not None and k.dim() != 4):
+        raise AttnQatError("q and k must be [B,heads,L,d]")
+    (B, _, L, d), dev = q.shape, q.get_device()
+    if not (positions.dtype is _I32 and positions.is_cuda and positions.is_contiguous() and positions.shape in ((L, rope.axes), (B, L, rope.axes))):
+        raise AttnQatError(f"positions must be a contiguous int32 CUDA tensor [{L},{rope.axes}] or [{B},{L},{rope.axes}]")
+    for name, t, o in (("q", q, out[0]), ("k", k, out[1])):
+        for x in () if t is None else (t, o):
+            if not (x is not None and x.is_cuda and x.dtype is _BF and x.shape == (B, t.shape[1], L, d) and (x.stride(3) == 1 or x.numel() == 0)):
+                raise AttnQatError(f"{name} and its output must be bf16 CUDA tensors {(B, t.shape[1], L, d)}, d innermost")
+    raise AttnQatError(f"all tensors must be on the current device (cuda:{_current_device()})")
+
+
+def _rope_call(f, q, k, positions, rope, out):
     if out is None:
-        out = (torch.empty((B, Hq, L, d), dtype=_BF, device=q.device), None if k is None else torch.empty((B, Hkv, L, d), dtype=_BF, device=q.device))
-    none = (None, 0, 0, 0)
-    args = []
-    for what, t, o, h in (("q", q, out[0], Hq), ("k", k, out[1], Hkv)):
-        if t is None:
-            args.append((none, none))
-        else:
-            args.append(((t.data_ptr(), *_heads(what, t, (B, h, L, d), dev)), (o.data_ptr(), *_heads("out", o, (B, h, L, d), dev))))
-    rc = getattr(_lib or lib(), name)(*args[0][0], *args[1][0], B, Hq, Hkv, L, d, BF16, positions.data_ptr(), L * rope.axes if positions.dim() == 3 else 0, ctypes.addressof(rope),
-                                      *args[0][1], *args[1][1], _stream_on(dev))
+        out = (torch.empty(q.shape, dtype=_BF, device=q.device), None if k is None else torch.empty(k.shape, dtype=_BF, device=q.device))
+    qo, ko = out
+    dev, shape, at = q.get_device(), q.shape, positions.shape
+    if not (type(rope) is Rope and len(shape) == 4 and q.dtype is qo.dtype is _BF and positions.dtype is _I32 and qo.shape == shape and positions.is_contiguous()
+            and dev == _current_device() == qo.get_device() == positions.get_device()):
+        _rope_refuse(q, k, positions, rope, out)
+    B, Hq, L, d = shape
+    axes = rope.axes
+    (qb, qh, qt, q1), (ob, oh, ot, o1) = q.stride(), qo.stride()
+    if not (q1 == o1 == 1 or q.numel() == 0) or not (at == (L, axes) or at == (B, L, axes)):
+        _rope_refuse(q, k, positions, rope, out)
+    if k is None:
+        Hkv, kp, kb, kh, kt, kop, kob, koh, kot = 0, None, 0, 0, 0, None, 0, 0, 0
+    else:
+        ks = k.shape
+        if not (len(ks) == 4 and ko is not None and ko.shape == ks and k.dtype is ko.dtype is _BF and ks[0] == B and ks[2:] == shape[2:] and dev == k.get_device() == ko.get_device()):
+            _rope_refuse(q, k, positions, rope, out)
+        (kb, kh, kt, k1), (kob, koh, kot, ko1) = k.stride(), ko.stride()
+        if not (k1 == ko1 == 1 or k.numel() == 0):
+            _rope_refuse(q, k, positions, rope, out)
+        Hkv, kp, kop = ks[1], k.data_ptr(), ko.data_ptr()
+    rc = f(q.data_ptr(), qb, qh, qt, kp, kb, kh, kt, B, Hq, Hkv, L, d, BF16, positions.data_ptr(), L * axes if len(at) == 3 else 0, rope.address,
+           qo.data_ptr(), ob, oh, ot, kop, kob, koh, kot, _stream_on(dev))
     if rc:
         _check(rc)
-    return out[0], out[1]
+    return out
 
 
 def attnqat_rope_fwd(q, k, positions, rope, out=None):
     """Rotary positions of q [B,Hq,L,d] and k [B,Hkv,L,d] (bf16, any stride per batch, head and token, d innermost; k may be None).  positions int32 [L,axes], or
     [B,L,axes]; ``rope``: ``rope_table``.  Returns (q, k), contiguous: what attnqat_fwd takes; ``out``: those two, of any strides, each of which may be its input."""
-    return _rope_call("attnqat_rope_fwd", q, k, positions, rope, out)
+    return _rope_call((_lib or lib()).attnqat_rope_fwd, q, k, positions, rope, out)
 
 
 def attnqat_rope_bwd(dq, dk, positions, rope, out=None):
     """Gradient of attnqat_rope_fwd: from dq [B,Hq,L,d] and dk [B,Hkv,L,d] of its outputs to those of its inputs.  Arguments as there; ``out`` may be views of one
     projection's gradient."""
-    return _rope_call("attnqat_rope_bwd", dq, dk, positions, rope, out)
+    return _rope_call((_lib or lib()).attnqat_rope_bwd, dq, dk, positions, rope, out)
 
 
 def attnqat_kv_cache_append_rope(q, k, v, positions, rope, cache, slots, num_pages=None, out=None):
@@ -537,7 +555,7 @@ def attnqat_kv_cache_append_rope(q, k, v, positions, rope, cache, slots, num_pag
             _serve_refuse([], [("q", q, want), ("out", out, want)])
         ot, oh, _ = out.stride()
         qp, op = q.data_ptr(), out.data_ptr()
-    rc = (_lib or lib()).attnqat_kv_cache_append_rope(qp, qt, qh, k.data_ptr(), kt, kh, v.data_ptr(), vt, vh, T, Hq, Hkv, d, BF16, positions.data_ptr(), ctypes.addressof(rope),
+    rc = (_lib or lib()).attnqat_kv_cache_append_rope(qp, qt, qh, k.data_ptr(), kt, kh, v.data_ptr(), vt, vh, T, Hq, Hkv, d, BF16, positions.data_ptr(), rope.address,
                                                       cache.data_ptr(), _serve_pages(cache, num_pages, Hkv, d), slots.data_ptr(), op, ot, oh, _stream_on(dev))
     if rc:
         _check(rc)

@@ -753,22 +753,20 @@ bool rows_apart(const View& v)
     return true;
 }
 
-// The table that the kernels take.  A frequency of f radians per position is f / 2 pi turns; whole turns change nothing.
+int rope_sizes(int pairs, int axes, int layout, int most)
+{
+    if (pairs < 1 || pairs > most || axes < 1 || axes > kRopeAxes || (layout != ATTNQAT_ROPE_PAIRED && layout != ATTNQAT_ROPE_HALVES)) return ATTNQAT_EINVAL;
+    return layout == ATTNQAT_ROPE_HALVES && pairs % 8 != 0 ? ATTNQAT_ESHAPE : ATTNQAT_OK;
+}
+// The table as the kernels take it; `back`: turns the other way.
 int rope_of(const attnqat_rope* rope, int d, bool back, RopeTable& r)
 {
-    if (!rope || rope->pairs < 1 || rope->pairs > d / 2 || rope->axes < 1 || rope->axes > kRopeAxes) return ATTNQAT_EINVAL;
-    if (rope->layout != ATTNQAT_ROPE_PAIRED && rope->layout != ATTNQAT_ROPE_HALVES) return ATTNQAT_EINVAL;
-    if (rope->layout == ATTNQAT_ROPE_HALVES && rope->pairs % 8 != 0) return ATTNQAT_ESHAPE;
-    r = RopeTable{};
+    if (!rope) return ATTNQAT_EINVAL;
+    const int rc = rope_sizes(rope->pairs, rope->axes, rope->layout, d / 2);
+    if (rc) return rc;
     r.pairs = rope->pairs; r.axes = rope->axes;
-    for (int i = 0; i < rope->pairs; ++i) {
-        if (!std::isfinite(rope->freq[i]) || rope->axis[i] >= rope->axes) return ATTNQAT_EINVAL;
-        const long double turns = (long double)rope->freq[i] / 6.283185307179586476925286766559005768L, part = turns - floorl(turns);
-        const long double x = part * 18446744073709551616.0L;
-        const uint64_t f = x >= 18446744073709551615.0L ? 0 : (uint64_t)x;
-        r.freq[i] = back ? 0 - f : f;
-        r.axis[i >> 4] |= (uint32_t)rope->axis[i] << (2 * (i & 15));
-    }
+    for (int i = 0; i < 64; ++i) r.freq[i] = back ? 0 - rope->turns[i] : rope->turns[i];
+    for (int i = 0; i < 4; ++i) r.axis[i] = rope->axis[i];
     return ATTNQAT_OK;
 }
 
@@ -819,6 +817,23 @@ int rope_common(const void* const (&src)[2], const int64_t (&ss)[2][3], void* co
     return ATTNQAT_OK;
 }
 }  // namespace
+
+int attnqat_rope_table(attnqat_rope* rope, int pairs, int axes, int layout, const double* freq, const uint8_t* axis)
+{
+    if (!rope || !freq || !axis) return ATTNQAT_EINVAL;
+    const int rc = rope_sizes(pairs, axes, layout, 64);
+    if (rc) return rc;
+    attnqat_rope r{};
+    r.pairs = pairs; r.axes = axes; r.layout = layout;
+    for (int i = 0; i < pairs; ++i) {
+        if (!std::isfinite(freq[i]) || axis[i] >= axes) return ATTNQAT_EINVAL;
+        const long double turns = (long double)freq[i] / 6.283185307179586476925286766559005768L, x = (turns - floorl(turns)) * 18446744073709551616.0L;
+        r.turns[i] = x >= 18446744073709551615.0L ? 0 : (uint64_t)x;
+        r.axis[i >> 4] |= (uint32_t)axis[i] << (2 * (i & 15));
+    }
+    *rope = r;
+    return ATTNQAT_OK;
+}
 
 int attnqat_rope_fwd(const void* q, int64_t q_batch, int64_t q_head, int64_t q_token, const void* k, int64_t k_batch, int64_t k_head, int64_t k_token,
                      int B, int Hq, int Hkv, int L, int d, int dtype, const int* positions, int64_t positions_batch, const attnqat_rope* rope,

@@ -119,9 +119,9 @@ __global__ __launch_bounds__(256) void append_rope_kernel(const AppendRopeArgs a
 {
     constexpr int nt = D / 16, nb = D / 16, RS = 2 * D + 16;
     __shared__ __align__(16) unsigned char rows[HALVES ? 256 / nt * RS : 16];
-    const int chunk = threadIdx.x % nt, t = (int)blockIdx.x * (256 / nt) + threadIdx.x / nt;
     const int qg = (a.Hq + kRopeHeads - 1) / kRopeHeads, kg = (a.Hkv + kRopeHeads - 1) / kRopeHeads;
-    const int g = (int)blockIdx.y, role = g < qg ? 0 : g < qg + kg ? 1 : 2, h0 = (g - (role == 0 ? 0 : role == 1 ? qg : qg + kg)) * kRopeHeads;
+    const int chunk = threadIdx.x % nt, t = (int)(blockIdx.x / (unsigned)(qg + 2 * kg)) * (256 / nt) + threadIdx.x / nt;
+    const int g = (int)(blockIdx.x % (unsigned)(qg + 2 * kg)), role = g < qg ? 0 : g < qg + kg ? 1 : 2, h0 = (g - (role == 0 ? 0 : role == 1 ? qg : qg + kg)) * kRopeHeads;
     const Rows& in = role == 0 ? a.q : role == 1 ? a.k : a.v;
     const int heads = role == 0 ? a.Hq : a.Hkv;
     const int tc = min(t, a.T - 1);                               // (whole waves stay: they share LDS rows and lanes)
@@ -206,7 +206,8 @@ int launch_rope(const RopeArgs& a, const RopeTable& r, int D, bool halves, hipSt
 int launch_append_rope(const AppendRopeArgs& a, const RopeTable& r, int D, bool halves, hipStream_t st)
 {
     const int per = 256 / (D / 16);
-    const dim3 grid((a.T + per - 1) / per, groups_of(a.Hq) + 2 * groups_of(a.Hkv));
+    // (all heads of a group of tokens one after another: they lie side by side in memory)
+    const dim3 grid((unsigned)((a.T + per - 1) / per) * (groups_of(a.Hq) + 2 * groups_of(a.Hkv)));
     if (D == 128) {
         if (halves) hipLaunchKernelGGL((append_rope_kernel<128, true>), grid, dim3(256), 0, st, a, r);
         else        hipLaunchKernelGGL((append_rope_kernel<128, false>), grid, dim3(256), 0, st, a, r);

@@ -14,73 +14,100 @@ namespace {
 typedef int intx4 __attribute__((ext_vector_type(4)));
 
 // ---------------------------------------------------------------------------------------------- means of the keys of a page
-// A cached value is a multiple of 2^-10 below 2^12, the sum S of a page's 128 a whole number of 2^-10 below 2^29: exact in int32, in any order (a thread's own two keys
-// in fp32, where they fit).  With the largest |S| of a head in [2^(b-1), 2^b) the codes are S 2^-e, e = b - 7, rounded to nearest even, at most 127 in
+// A cached value is a multiple of 2^-10 below 2^12, the sum S of a page's 128 a whole number of 2^-10 below 2^29: exact in int32, in any order (up to six in fp32,
+// where they fit).  With the largest |S| of a head in [2^(b-1), 2^b) the codes are S 2^-e, e = b - 7, rounded to nearest even, at most 127 in
 // magnitude, and the mean is code 2^(e-17).
-struct OpAddInt { __device__ __forceinline__ float operator()(float a, float b) const { return __uint_as_float(__float_as_uint(a) + __float_as_uint(b)); } };
+//
+// A wave takes a (page, head), whole: a lane has 32 channels of 16 (D = 64: 32) bytes' keys, eight (four) of them, and sums over lanes halve what a lane holds at every
+// step.
+__device__ __forceinline__ uint32_t other_of_8(uint32_t x) { return __builtin_amdgcn_update_dpp(0u, x, 0x128, 0xF, 0xF, true); }                 // of lane ^ 8: row_ror 8
+__device__ __forceinline__ uint32_t other_of_4(uint32_t x)
+{
+    const uint32_t a = __builtin_amdgcn_update_dpp(x, x, 0x104, 0xF, 0x5, false);                                                               // row_shl 4 into quads 0 and 2
+    return __builtin_amdgcn_update_dpp(a, x, 0x114, 0xF, 0xA, false);                                                                            // row_shr 4 into quads 1 and 3
+}
+__device__ __forceinline__ uint32_t other_of_2(uint32_t x) { return __builtin_amdgcn_update_dpp(0u, x, 0x4E, 0xF, 0xF, true); }                  // quad_perm 2,3,0,1
 
 template <int D>
-__global__ __launch_bounds__(256) void summarize_kernel(const unsigned char* __restrict__ cache, int num_pages, int Hkv, const long long* __restrict__ slots, int T, int rows_per,
+__global__ __launch_bounds__(256) void summarize_kernel(const unsigned char* __restrict__ cache, int num_pages, int Hkv, const long long* __restrict__ slots, int T, int rows_per /* <= 128 */,
                                                         unsigned char* __restrict__ summary)
 {
-    constexpr int NCH = D / 32, KEYS = 256 / NCH;                 // threads to a key (32 values each), keys at a time
-    __shared__ int part[4][D];
-    __shared__ int top;
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, ch = tid % NCH, kk = tid / NCH, h = blockIdx.y;
-    const int r_end = min(((int)blockIdx.x + 1) * rows_per, T);
-    for (int r0 = (int)blockIdx.x * rows_per; r0 < r_end; r0 += 64) {
-        const long long slot = r0 + lane < r_end ? slots[r0 + lane] : -1;
-        const bool ends = slot >= 0 && slot < (long long)num_pages * 128 && (slot & 127) == 127;
-        const int page_lane = (int)(slot >> 7);
+    constexpr int NCH = D / 32, KEYS = 64 / NCH;                  // lanes to a key (32 values each), keys at a time
+    const int lane = threadIdx.x & 63, ch = lane % NCH, kk = lane / NCH;
+    const int h = (int)blockIdx.y * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    if (h >= Hkv) return;
+    const int r0 = (int)blockIdx.x * rows_per, r_end = min(r0 + rows_per, T);
+    long long slot[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) slot[i] = slots[min(r0 + 64 * i + lane, T - 1)];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const bool ends = r0 + 64 * i + lane < r_end && slot[i] >= 0 && slot[i] < (long long)num_pages * 128 && (slot[i] & 127) == 127;
+        const int page_lane = (int)(slot[i] >> 7);
         for (unsigned long long left = __builtin_amdgcn_ballot_w64(ends); left != 0; left &= left - 1) {
             const int page = __builtin_amdgcn_readlane(page_lane, (int)__builtin_ctzll(left));
             const unsigned char* k = cache + ((size_t)page * Hkv + h) * nvfp4_page_head_bytes(D);
-            if (tid == 0) top = 0;
-            float acc[32];
-#pragma unroll
-            for (int i = 0; i < 32; ++i) acc[i] = 0.0f;
+            uint4v c[128 / KEYS];
+            uint32_t sc[128 / KEYS];
 #pragma unroll
             for (int p = 0; p < 128 / KEYS; ++p) {
                 const int key = p * KEYS + kk;
-                const uint4v c = *reinterpret_cast<const uint4v*>(k + key * (D / 2) + 16 * ch);
-                const uint32_t sc = *reinterpret_cast<const uint16_t*>(k + 128 * (D / 2) + key * (D / 16) + 2 * ch);
-                typedef float float2v __attribute__((ext_vector_type(2)));
-                const float s0 = __builtin_amdgcn_cvt_scalef32_f32_fp8(sc, 1.0f, 0), s1 = __builtin_amdgcn_cvt_scalef32_f32_fp8(sc, 1.0f, 1);
+                c[p] = *reinterpret_cast<const uint4v*>(k + key * (D / 2) + 16 * ch);
+                sc[p] = *reinterpret_cast<const uint16_t*>(k + 128 * (D / 2) + key * (D / 16) + 2 * ch);
+            }
+            int sum[32];
 #pragma unroll
-                for (int w = 0; w < 4; ++w) {
-                    const float s = w < 2 ? s0 : s1;
-#define AQ_ADD2(J) { const float2v v = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c[w], 1.0f, J); acc[8 * w + 2 * J] = fmaf(v[0], s, acc[8 * w + 2 * J]); acc[8 * w + 2 * J + 1] = fmaf(v[1], s, acc[8 * w + 2 * J + 1]); }
-                    AQ_ADD2(0) AQ_ADD2(1) AQ_ADD2(2) AQ_ADD2(3)
+            for (int q = 0; q < 32 / KEYS; ++q) {                 // four keys at a time in fp32
+                float acc[32];
+#pragma unroll
+                for (int p = 4 * q; p < 4 * q + 4; ++p) {
+                    typedef float float2v __attribute__((ext_vector_type(2)));
+                    const float s0 = __builtin_amdgcn_cvt_scalef32_f32_fp8(sc[p], 1024.0f, 0), s1 = __builtin_amdgcn_cvt_scalef32_f32_fp8(sc[p], 1024.0f, 1);
+#pragma unroll
+                    for (int w = 0; w < 4; ++w) {
+                        const float s = w < 2 ? s0 : s1;
+#define AQ_ADD2(J) { const float2v v = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c[p][w], 1.0f, J); float &a = acc[8 * w + 2 * J], &b = acc[8 * w + 2 * J + 1]; \
+                     a = p == 4 * q ? v[0] * s : fmaf(v[0], s, a); b = p == 4 * q ? v[1] * s : fmaf(v[1], s, b); }
+                        AQ_ADD2(0) AQ_ADD2(1) AQ_ADD2(2) AQ_ADD2(3)
 #undef AQ_ADD2
+                    }
                 }
-            }
 #pragma unroll
-            for (int i = 0; i < 32; ++i) {
-                const float x = xor_tree<NCH, 32>(__uint_as_float((uint32_t)(int)(acc[i] * 1024.0f)), OpAddInt{});
-                if (lane < NCH) part[wave][32 * ch + i] = (int)__float_as_uint(x);
+                for (int j = 0; j < 32; ++j) sum[j] = q == 0 ? (int)acc[j] : sum[j] + (int)acc[j];
             }
-            __syncthreads();
-            int sum = 0;
-            if (tid < D) {
-                sum = part[0][tid] + part[1][tid] + part[2][tid] + part[3][tid];
-                atomicMax(&top, abs(sum));
+            // over lanes ^ 32, ^ 16, ^ 8, ^ 4 (^ 2): the lane whose bit is 0 keeps the lower half of what both hold
+#pragma unroll
+            for (int j = 0; j < 16; ++j) { const auto r = __builtin_amdgcn_permlane32_swap((uint32_t)sum[j], (uint32_t)sum[j + 16], false, false); sum[j] = (int)(r[0] + r[1]); }
+#pragma unroll
+            for (int j = 0; j < 8; ++j) { const auto r = __builtin_amdgcn_permlane16_swap((uint32_t)sum[j], (uint32_t)sum[j + 8], false, false); sum[j] = (int)(r[0] + r[1]); }
+#define AQ_HALVE(N, BIT, OTHER) _Pragma("unroll") for (int j = 0; j < N; ++j) { const int keep = (lane & BIT) ? sum[j + N] : sum[j], send = (lane & BIT) ? sum[j] : sum[j + N]; sum[j] = keep + (int)OTHER((uint32_t)send); }
+            AQ_HALVE(4, 8, other_of_8)
+            AQ_HALVE(2, 4, other_of_4)
+            int d = 32 * ch + 16 * ((lane >> 5) & 1) + 8 * ((lane >> 4) & 1) + 4 * ((lane >> 3) & 1) + 2 * ((lane >> 2) & 1);
+            constexpr int N = D == 64 ? 1 : 2;                    // sums that a lane is left with: channels d ..
+            if constexpr (D == 64) { AQ_HALVE(1, 2, other_of_2) d += (lane >> 1) & 1; }
+#undef AQ_HALVE
+            // (the exponent of the largest as a float, rounded towards zero: below 2^29 and a whole number)
+            int most = abs(sum[0]);
+            if (N == 2) most = max(most, abs(sum[1]));
+            for (int w = 1; w < 64; w <<= 1) most = max(most, __shfl_xor(most, w));
+            const int e = (most > 0 ? 32 - __builtin_clz((unsigned)most) : 0) - 7;
+            uint32_t code[N];
+#pragma unroll
+            for (int j = 0; j < N; ++j) {
+                int x;
+                if (e <= 0) x = sum[j] * (1 << -e);
+                else {
+                    x = sum[j] >> e;
+                    const int rest = sum[j] - (x << e), half = 1 << (e - 1);
+                    x += rest > half || (rest == half && (x & 1)) ? 1 : 0;
+                }
+                code[j] = (uint32_t)min(max(x, -127), 127) & 0xFFu;
             }
-            __syncthreads();
-            const int e = (top > 0 ? 32 - __builtin_clz((unsigned)top) : 0) - 7;
-            int code;
-            if (e <= 0) code = sum * (1 << -e);
-            else {
-                code = sum >> e;
-                const int rest = sum - (code << e), half = 1 << (e - 1);
-                code += rest > half || (rest == half && (code & 1)) ? 1 : 0;
-            }
-            uint32_t w = (uint32_t)min(max(code, -127), 127) & 0xFFu;
-            w |= lane_down<1>(w) << 8;
-            w |= lane_down<2>(w) << 16;
             unsigned char* dst = summary + ((size_t)page * Hkv + h) * (D + kSummaryTail);
-            if (tid < D && (tid & 3) == 0) *reinterpret_cast<uint32_t*>(dst + tid) = w;
-            if (tid == 0) *reinterpret_cast<float*>(dst + D) = __uint_as_float((uint32_t)(e + 110) << 23);
-            __syncthreads();                                      // (top and part have been read)
+            if constexpr (N == 2) *reinterpret_cast<uint16_t*>(dst + d) = (uint16_t)(code[0] | code[1] << 8);
+            else dst[d] = (unsigned char)code[0];
+            if (lane == 0) *reinterpret_cast<float*>(dst + D) = __uint_as_float((uint32_t)(e + 110) << 23);
         }
     }
 }
@@ -92,7 +119,7 @@ __device__ inline void find_tokens(const StepArgs& a, int t0, int nt, int* seq, 
     const int tid = threadIdx.x;
     if (tid < 16) { seq[tid] = -1; pos[tid] = -1; }
     __syncthreads();
-    for (int b = tid; b < a.B; b += 256) {
+    for (int b = tid; b < a.B; b += blockDim.x) {
         const int s = min(max(a.cu_q[b], 0), a.T), e = min(max(a.cu_q[b + 1], s), a.T);
         const int len = max(0, min(a.kv_lens[b], a.max_pages * 128));
         for (int t = max(s, t0); t < min(e, t0 + nt); ++t) { seq[t - t0] = b; pos[t - t0] = max(len - e + t, -1); }
@@ -104,10 +131,43 @@ __device__ inline void find_tokens(const StepArgs& a, int t0, int nt, int* seq, 
 // Order of floats as of unsigned numbers.
 __device__ inline uint32_t ordered(float x) { const uint32_t u = __float_as_uint(x); return (u >> 31) ? ~u : (u | 0x80000000u); }
 
+// The m best of n scores (0 < m < n; scores from `key` on, in LDS): the m-th largest, found bit by bit from the front until a limit has exactly m scores at or above it, and how many
+// that are equal to it are taken, lowest first.  By a wave, with its scores in R registers (64 R of them at most; R = 0: read from LDS every time).
+struct Limit { uint32_t at; int ties; };
+template <int R>
+__device__ inline Limit limit_of(const uint32_t* key, int n, int m)
+{
+    const int lane = threadIdx.x & 63;
+    uint32_t k[R > 0 ? R : 1];
+    if constexpr (R > 0) {
+#pragma unroll
+        for (int r = 0; r < R; ++r) k[r] = 64 * r + lane < n ? key[64 * r + lane] : 0u;
+    }
+    auto count = [&](uint32_t from) __attribute__((always_inline)) {      // scores >= from > 0
+        int c = 0;
+        if constexpr (R > 0) {
+#pragma unroll
+            for (int r = 0; r < R; ++r) c += (int)__builtin_popcountll(__builtin_amdgcn_ballot_w64(k[r] >= from));
+        } else {
+            for (int j = lane; j < n; j += 64) c += key[j] >= from ? 1 : 0;
+            c = lane_total(c);
+        }
+        return c;
+    };
+    uint32_t limit = 0;
+    for (int bit = 31; bit >= 0; --bit) {
+        const uint32_t cand = limit | (1u << bit);
+        const int c = count(cand);
+        if (c >= m) limit = cand;
+        if (c == m) return Limit{limit, m};
+    }
+    return Limit{limit, m - (limit == 0xFFFFFFFFu ? 0 : count(limit + 1))};
+}
+
 // 16 rows of the matrix instruction are the query heads of a kv head's group, padded to GP by heads that are there, for 16 / GP tokens, against 16 pages at a
-// time.  Scores stay in LDS; a wave then finds the threshold of a token's best ones bit by bit.
+// time.  Scores stay in LDS; then a wave has a token.
 template <int D, int GP>
-__global__ __launch_bounds__(256) void select_kernel(const SelectArgs a, int nt /* tokens of a workgroup */, int tiles)
+__global__ __launch_bounds__(1024) void select_kernel(const SelectArgs a, int nt /* tokens of a workgroup */, int tiles)
 {
     constexpr int NS = D / 64;
     extern __shared__ uint32_t keys[];                            // [nt][max_pages]
@@ -115,7 +175,7 @@ __global__ __launch_bounds__(256) void select_kernel(const SelectArgs a, int nt 
     const StepArgs& s = a.s;
     const int tid = threadIdx.x, lane = tid & 63, cc = lane & 15, g = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int G = s.Hq / s.Hkv, subs = (G + 15) / 16, S = s.max_pages;
+    const int G = s.Hq / s.Hkv, subs = (G + 15) / 16, S = s.max_pages, waves = (int)blockDim.x >> 6;
     int h, tile;
     head_tile_of_block((int)blockIdx.x, s.Hkv, tiles, h, tile);
     const int t0 = tile * nt;
@@ -161,14 +221,30 @@ __global__ __launch_bounds__(256) void select_kernel(const SelectArgs a, int nt 
                 if (own + 1 > a.n_blocks) hi = max(hi, own + 1 - a.last);
             }
             if (b < 0) continue;
-            for (int j0 = (a.first & ~15) + 16 * wave; j0 < hi; j0 += 64) {
-                const int j = j0 + cc, id = s.table[(size_t)b * s.max_pages + min(j, s.max_pages - 1)];
-                const bool live = id >= 0 && id < s.num_pages;
-                const unsigned char* rec = a.summary + ((size_t)(live ? id : 0) * s.Hkv + h) * (D + kSummaryTail);
+            constexpr int U = 4;                                  // sixteens of pages under way at once
+            for (int j1 = (a.first & ~15) + 16 * wave; j1 < hi; j1 += 16 * U * waves) {
+              int id[U];
+              intx4 k8[U][NS];
+              float scales[U];
+#pragma unroll
+              for (int u = 0; u < U; ++u) id[u] = s.table[(size_t)b * s.max_pages + min(j1 + 16 * u * waves + cc, s.max_pages - 1)];
+#pragma unroll
+              for (int u = 0; u < U; ++u) {
+                const bool live = id[u] >= 0 && id[u] < s.num_pages;
+                const unsigned char* rec = a.summary + ((size_t)(live ? id[u] : 0) * s.Hkv + h) * (D + kSummaryTail);
+#pragma unroll
+                for (int i = 0; i < NS; ++i) k8[u][i] = *reinterpret_cast<const intx4*>(rec + 64 * i + 16 * g);
+                scales[u] = *reinterpret_cast<const float*>(rec + D);
+                if (!live) scales[u] = 0.0f;
+              }
+#pragma unroll
+              for (int u = 0; u < U; ++u) {
+                const int j = j1 + 16 * u * waves + cc;
+                if (j - cc >= hi) break;
+                const float scale = scales[u];
                 intx4 acc = {0, 0, 0, 0};
 #pragma unroll
-                for (int i = 0; i < NS; ++i) acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(q8[i], *reinterpret_cast<const intx4*>(rec + 64 * i + 16 * g), acc, 0, 0, 0);
-                const float scale = live ? *reinterpret_cast<const float*>(rec + D) : 0.0f;
+                for (int i = 0; i < NS; ++i) acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(q8[i], k8[u][i], acc, 0, 0, 0);
                 // rows 4 g .. 4 g + 3 of page j: the largest of a token's heads
                 auto put = [&](int token, int v) __attribute__((always_inline)) {
                     if (token < i0 || token >= i1 || j >= hi) return;
@@ -184,12 +260,13 @@ __global__ __launch_bounds__(256) void select_kernel(const SelectArgs a, int nt 
                     if constexpr (GP >= 16) { const auto r = __builtin_amdgcn_permlane32_swap((uint32_t)m, (uint32_t)m, false, false); m = max((int)r[0], (int)r[1]); }
                     if (GP == 4 || (GP == 8 && (g & 1) == 0) || g == 0) put(4 * g / GP, m);
                 }
+              }
             }
         }
     }
     __syncthreads();
 
-    for (int i = wave; i < nt; i += 4) {
+    for (int i = wave; i < nt; i += waves) {
         if (uniform(seq[i]) < 0) continue;
         const int own = uniform(pos[i]) >> 7, nb = own + 1;       // (position -1: page -1)
         int* out = a.blocks + ((size_t)(t0 + i) * s.Hkv + h) * a.n_blocks;
@@ -197,33 +274,21 @@ __global__ __launch_bounds__(256) void select_kernel(const SelectArgs a, int nt 
             for (int j = lane; j < a.n_blocks; j += 64) out[j] = j < nb ? j : -1;
             continue;
         }
-        const int lo = a.first, hi = nb - a.last, m = a.n_blocks - a.first - a.last;       // hi - lo > m
-        const uint32_t* key = keys + i * S;
-        // the m-th largest score, and how many of its equals are taken, from the front
-        uint32_t limit = 0xFFFFFFFFu;
-        int ties = 0;
-        if (m > 0) {
-            limit = 0;
-            for (int bit = 31; bit >= 0; --bit) {
-                const uint32_t cand = limit | (1u << bit);
-                int n = 0;
-                for (int j = lo + lane; j < hi; j += 64) n += key[j] >= cand ? 1 : 0;
-                if (lane_total(n) >= m) limit = cand;
-            }
-            int above = 0;
-            for (int j = lo + lane; j < hi; j += 64) above += key[j] > limit ? 1 : 0;
-            ties = m - lane_total(above);
-        }
-        int at = 0;
-        for (int j0 = 0; j0 < nb; j0 += 64) {
+        for (int j = lane; j < a.first; j += 64) out[j] = j;
+        for (int j = lane; j < a.last; j += 64) out[a.n_blocks - a.last + j] = nb - a.last + j;
+        const int n = nb - a.first - a.last, m = a.n_blocks - a.first - a.last;            // n > m
+        if (m == 0) continue;
+        const uint32_t* key = keys + i * S + a.first;
+        const Limit l = n <= 64 ? limit_of<1>(key, n, m) : n <= 256 ? limit_of<4>(key, n, m) : n <= 512 ? limit_of<8>(key, n, m) : n <= 1024 ? limit_of<16>(key, n, m) : limit_of<0>(key, n, m);
+        int at = a.first, ties = l.ties;
+        for (int j0 = 0; j0 < n; j0 += 64) {
             const int j = j0 + lane;
-            const bool comp = j >= lo && j < hi;
-            const uint32_t k = comp ? key[j] : 0u;
-            const unsigned long long eq = __builtin_amdgcn_ballot_w64(comp && k == limit && m > 0), below = (1ull << lane) - 1;
-            const bool take = j < nb && (!comp || (m > 0 && (k > limit || (k == limit && (int)__builtin_popcountll(eq & below) < ties))));
+            const uint32_t k = key[min(j, n - 1)];
+            const unsigned long long eq = __builtin_amdgcn_ballot_w64(j < n && k == l.at), below = (1ull << lane) - 1;
+            const bool take = j < n && (k > l.at || (k == l.at && (int)__builtin_popcountll(eq & below) < ties));
             ties -= min(ties, (int)__builtin_popcountll(eq));
             const unsigned long long all = __builtin_amdgcn_ballot_w64(take);
-            if (take) out[at + (int)__builtin_popcountll(all & below)] = j;
+            if (take) out[at + (int)__builtin_popcountll(all & below)] = a.first + j;
             at += (int)__builtin_popcountll(all);
         }
     }
@@ -452,39 +517,52 @@ __global__ __launch_bounds__(256, 3) void sparse_kernel(const SparseArgs a, cons
     }
 }
 
-// O and lse of rows whose pages were split: D / 4 threads to a row.
+// O and lse of rows whose pages were split: `per` groups of D / 4 threads share a row, so that its partial sums take one trip to memory.
 template <int D>
-__global__ __launch_bounds__(256) void sparse_merge_kernel(const SparseArgs a, const SparsePlan p, const SparseWs ws)
+__global__ __launch_bounds__(256) void sparse_merge_kernel(const SparseArgs a, const SparsePlan p, const SparseWs ws, int per)
 {
-    constexpr int nt = D / 4;
+    constexpr int nt = D / 4, NG = 256 / nt, K = 8;               // partial sums of a group at a time
+    __shared__ __align__(16) float acc[NG][D];
+    __shared__ float ml[NG][2];
     const StepArgs& s = a.s;
-    const long long x = (long long)blockIdx.x * (256 / nt) + threadIdx.x / nt;
-    const int d = threadIdx.x % nt * 4, t = (int)(x / s.Hq), hd = (int)(x % s.Hq), G = s.Hq / s.Hkv, h = hd / G, gh = hd % G;
-    if (t >= s.T) return;
+    const int grp = threadIdx.x / nt, d = threadIdx.x % nt * 4, G = s.Hq / s.Hkv;
+    const long long x = (long long)blockIdx.x * (NG / per) + grp / per;
+    const int t = (int)min(x / s.Hq, (long long)s.T - 1), hd = (int)(x % s.Hq), h = hd / G, gh = hd % G;
     const int sub = p.subs > 1 ? gh / 16 : 0, row = p.subs > 1 ? gh % 16 : t % p.nt * G + gh;
     const size_t slot0 = (((size_t)(t / p.nt) * s.Hkv + h) * p.subs + sub) * p.splits;
     float M = -INFINITY, l = 0.0f;
     floatx4 v = {0.0f, 0.0f, 0.0f, 0.0f};
-    constexpr int K = 8;                                          // at a time: one trip to memory
-    for (int i0 = 0; i0 < p.splits; i0 += K) {
+    bool on = x < (long long)s.T * s.Hq;
+    for (int i0 = grp % per; i0 < p.splits; i0 += K * per) {
         floatx4 po[K];
         float pm[K], pl[K];
 #pragma unroll
         for (int k = 0; k < K; ++k) {
-            const size_t at = (slot0 + min(i0 + k, p.splits - 1)) * 16 + row;
+            const size_t at = (slot0 + min(i0 + k * per, p.splits - 1)) * 16 + row;
             po[k] = *reinterpret_cast<const floatx4*>(ws.part_o + at * D + d);
             pm[k] = ws.part_ml[at * 2];
             pl[k] = ws.part_ml[at * 2 + 1];
         }
-        if (pl[0] < 0.0f) return;                                 // (no sequence's row)
+        if (pl[0] < 0.0f) on = false;                             // (no sequence's row)
         float top = M;
 #pragma unroll
-        for (int k = 0; k < K; ++k) { if (i0 + k >= p.splits) pm[k] = -INFINITY; top = fmaxf(top, pm[k]); }
+        for (int k = 0; k < K; ++k) { if (i0 + k * per >= p.splits) pm[k] = -INFINITY; top = fmaxf(top, pm[k]); }
         const float at = top == -INFINITY ? 0.0f : top, al = __builtin_amdgcn_exp2f(M - at);
         M = top; l *= al; v *= al;
 #pragma unroll
         for (int k = 0; k < K; ++k) { const float f = __builtin_amdgcn_exp2f(pm[k] - at); l = fmaf(pl[k], f, l); v += po[k] * f; }
     }
+    if (per > 1) {
+        *reinterpret_cast<floatx4*>(&acc[grp][d]) = v;
+        if (d == 0) { ml[grp][0] = M; ml[grp][1] = l; }
+        __syncthreads();
+        if (grp % per != 0) return;
+        M = -INFINITY; l = 0.0f; v = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
+        for (int k = 0; k < per; ++k) M = fmaxf(M, ml[grp + k][0]);
+        const float at = M == -INFINITY ? 0.0f : M;
+        for (int k = 0; k < per; ++k) { const float f = __builtin_amdgcn_exp2f(ml[grp + k][0] - at); l = fmaf(ml[grp + k][1], f, l); v += *reinterpret_cast<const floatx4*>(&acc[grp + k][d]) * f; }
+    }
+    if (!on) return;
     v *= l != 0.0f ? 1.0f / l : 0.0f;
     *reinterpret_cast<uint2v*>(a.o + (size_t)t * a.o_token + (size_t)hd * a.o_head + d) = uint2v{pack_bf16x2_cvt(v[0], v[1]), pack_bf16x2_cvt(v[2], v[3])};
     if (d == 0 && a.lse) a.lse[(size_t)t * s.Hq + hd] = l != 0.0f ? M * 0.6931471805599453f + logf(l) : -INFINITY;
@@ -517,8 +595,11 @@ int launch_sparse_of(const SparseArgs& a, const SparsePlan& p, const SparseWs& w
     hipLaunchKernelGGL((sparse_kernel<D>), dim3((unsigned)p.tiles * a.s.Hkv * p.subs * p.splits), dim3(256), 0, st, a, p, w);
     if (hipGetLastError() != hipSuccess) return -1;
     if (p.splits > 1) {
-        const int per = 256 / (D / 4);
-        hipLaunchKernelGGL((sparse_merge_kernel<D>), dim3((unsigned)(((long long)a.s.T * a.s.Hq + per - 1) / per)), dim3(256), 0, st, a, p, w);
+        const int groups = 256 / (D / 4);
+        int per = 1;
+        while (per < groups && per * 8 < p.splits) per *= 2;
+        const int rows = groups / per;
+        hipLaunchKernelGGL((sparse_merge_kernel<D>), dim3((unsigned)(((long long)a.s.T * a.s.Hq + rows - 1) / rows)), dim3(256), 0, st, a, p, w, per);
     }
     return hipGetLastError() == hipSuccess ? 0 : -1;
 }
@@ -526,7 +607,11 @@ template <int D, int GP>
 int launch_select_of(const SelectArgs& a, int nt, hipStream_t st)
 {
     const int tiles = (a.s.T + nt - 1) / nt;
-    hipLaunchKernelGGL((select_kernel<D, GP>), dim3((unsigned)tiles * a.s.Hkv), dim3(256), (size_t)nt * a.s.max_pages * 4, st, a, nt, tiles);
+    // few workgroups: more waves each, for the way to memory; not more than there are sixteens of pages
+    const unsigned wgs = (unsigned)tiles * a.s.Hkv;
+    int waves = wgs <= 256 ? 16 : wgs <= 512 ? 8 : 4;
+    while (waves > 4 && waves * 16 > a.s.max_pages) waves /= 2;
+    hipLaunchKernelGGL((select_kernel<D, GP>), dim3(wgs), dim3(64 * waves), (size_t)nt * a.s.max_pages * 4, st, a, nt, tiles);
     return hipGetLastError() == hipSuccess ? 0 : -1;
 }
 template <int D>
@@ -554,7 +639,7 @@ int launch_summarize(const void* cache, int num_pages, int Hkv, int D, const lon
 {
     // rows of a workgroup: a page is complete at most once in 128 rows of a prompt, but every row of a step of single tokens may complete one
     const int rows = T > 8192 ? 128 : 16;
-    const dim3 grid((T + rows - 1) / rows, Hkv);
+    const dim3 grid((T + rows - 1) / rows, (Hkv + 3) / 4);
     if (D == 128) hipLaunchKernelGGL((summarize_kernel<128>), grid, dim3(256), 0, st, (const unsigned char*)cache, num_pages, Hkv, slots, T, rows, (unsigned char*)summary);
     else          hipLaunchKernelGGL((summarize_kernel<64>), grid, dim3(256), 0, st, (const unsigned char*)cache, num_pages, Hkv, slots, T, rows, (unsigned char*)summary);
     return hipGetLastError() == hipSuccess ? 0 : -1;

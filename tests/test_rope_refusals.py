@@ -1,15 +1,18 @@
 """What the entry points of rotary positions refuse, by status and before anything is enqueued (no GPU is touched: the pointers are numbers)."""
 import ctypes
+import math
+from fractions import Fraction
 
 import pytest
 
 import paper_2603_00040_amd as aq
 
 P = 1 << 24
+PI2 = 2 * Fraction("3.14159265358979323846264338327950288419716939937510582097494459")
 
 
-def _rope(pairs=32, axes=1, layout=0, freq=1.0, axis=0):
-    return aq.Rope(pairs, axes, layout, 0, (ctypes.c_double * 64)(*[freq] * 64), (ctypes.c_uint8 * 64)(*[axis] * 64))
+def _rope(pairs=32, axes=1, layout=0):
+    return aq.Rope(pairs, axes, layout, 0, (ctypes.c_uint64 * 64)(*[1 << 60] * 64))
 
 
 def _call(back=False, **kw):
@@ -29,7 +32,7 @@ def _call(back=False, **kw):
     (dict(pos_batch=-1), aq.EINVAL), (dict(qs=(8192, 60, 512)), aq.EINVAL), (dict(qs=(-8192, 64, 512)), aq.EINVAL), (dict(qs=(1 << 60, 64, 512)), aq.EINVAL),
     (dict(qos=(4096, 1024, 32)), aq.EINVAL), (dict(qos=(4096, 512, 64)), aq.EINVAL), (dict(qos=(0, 1024, 64)), aq.EINVAL), (dict(qos=(4096, 1024, 0)), aq.EINVAL),
     (dict(rope=_rope(pairs=0)), aq.EINVAL), (dict(rope=_rope(pairs=33)), aq.EINVAL), (dict(rope=_rope(axes=0)), aq.EINVAL), (dict(rope=_rope(axes=5)), aq.EINVAL),
-    (dict(rope=_rope(layout=2)), aq.EINVAL), (dict(rope=_rope(axis=1)), aq.EINVAL), (dict(rope=_rope(freq=float("nan"))), aq.EINVAL), (dict(rope=_rope(freq=float("inf"))), aq.EINVAL),
+    (dict(rope=_rope(layout=2)), aq.EINVAL),
     (dict(rope=_rope(pairs=12, layout=1)), aq.ESHAPE),
     # outputs over inputs, positions and each other
     (dict(qo=P), aq.EINVAL), (dict(qo=P + 512, qos=(8192, 64, 512)), aq.EINVAL), (dict(qo=P + 128, qos=(8192, 64, 512)), aq.EINVAL), (dict(ko=P, kos=(8192, 64, 512)), aq.EINVAL),
@@ -77,5 +80,30 @@ def test_tables_that_are_none(kw):
 
 
 def test_a_table():
-    r = aq.rope_table((4, 0, 2), theta=100.0, layout="halves")
-    assert (r.pairs, r.axes, r.layout) == (3, 3, aq.ROPE_HALVES) and list(r.freq[:3]) == [1.0, 0.1, 1.0] and list(r.axis[:3]) == [0, 0, 2]
+    r = aq.rope_table((4, 0, 2), theta=100.0)
+    assert (r.pairs, r.axes, r.layout) == (3, 3, aq.ROPE_PAIRED) and r.axis[0] == 2 << 4
+    for i, f in enumerate((1.0, 0.1, 1.0)):                        # (a frequency is within half a step of 53 bits)
+        assert abs(r.turns[i] / 2.0 ** 64 - f / (2 * math.pi)) <= 2.0 ** -53
+
+
+@pytest.mark.parametrize("f,turns", [(0.0, 0), (2 * math.pi, 0), (math.pi, 1 << 63), (-math.pi / 2, 3 << 62), (1e6, None), (-1e-30, None), (1e-12, None)])
+def test_turns_of_a_frequency(f, turns):
+    r = aq.rope_table((2,), freqs=[f])
+    want = (Fraction(f) / PI2 % 1) * (1 << 64)
+    assert abs((r.turns[0] - want + (1 << 63)) % (1 << 64) - (1 << 63)) <= 2 + abs(f) * 2.0      # (the quotient has 64 bits)
+    if turns is not None:                                          # (pi of 53 bits)
+        assert abs((r.turns[0] - turns + (1 << 63)) % (1 << 64) - (1 << 63)) <= 1 << 12
+
+
+def _table(**kw):
+    a = dict(rope=aq.Rope(), pairs=8, axes=2, layout=1, freq=[1.0] * 8, axis=[0, 1] * 4)
+    a.update(kw)
+    return aq.lib().attnqat_rope_table(None if a["rope"] is None else ctypes.addressof(a["rope"]), a["pairs"], a["axes"], a["layout"],
+                                       None if a["freq"] is None else (ctypes.c_double * 65)(*a["freq"]), None if a["axis"] is None else (ctypes.c_uint8 * 65)(*a["axis"]))
+
+
+@pytest.mark.parametrize("kw,code", [(dict(), aq.OK), (dict(rope=None), aq.EINVAL), (dict(freq=None), aq.EINVAL), (dict(axis=None), aq.EINVAL), (dict(pairs=0), aq.EINVAL), (dict(pairs=65), aq.EINVAL),
+                                     (dict(axes=0), aq.EINVAL), (dict(axes=5), aq.EINVAL), (dict(layout=2), aq.EINVAL), (dict(axis=[0, 2]), aq.EINVAL), (dict(freq=[1.0, float("nan")]), aq.EINVAL),
+                                     (dict(freq=[float("inf")]), aq.EINVAL), (dict(pairs=4), aq.ESHAPE), (dict(pairs=4, layout=0), aq.OK)])
+def test_table_of_the_library(kw, code):
+    assert _table(**kw) == code
