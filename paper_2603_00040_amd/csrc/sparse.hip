@@ -131,18 +131,23 @@ __device__ inline void find_tokens(const StepArgs& a, int t0, int nt, int* seq, 
 // Order of floats as of unsigned numbers.
 __device__ inline uint32_t ordered(float x) { const uint32_t u = __float_as_uint(x); return (u >> 31) ? ~u : (u | 0x80000000u); }
 
-// The m best of n scores (0 < m < n; scores from `key` on, in LDS): the m-th largest, found bit by bit from the front until a limit has exactly m scores at or above it, and how many
-// that are equal to it are taken, lowest first.  By a wave, with its scores in R registers (64 R of them at most; R = 0: read from LDS every time).
-struct Limit { uint32_t at; int ties; };
+// The m best of n scores (0 < m < n; scores from `key` on, in LDS), lowest first among equals, to out as page numbers first + index, ascending.  By a wave, with its scores
+// in R registers (64 R of them at most; R = 0: read from LDS every time).  The m-th largest lies not far below the largest (scores are floats: half of it is 2^23 away):
+// steps down from that double until there are m scores, and the last step is halved until a limit has exactly m at or above it, or is the m-th largest
+// itself, which others equal.
 template <int R>
-__device__ inline Limit limit_of(const uint32_t* key, int n, int m)
+__device__ inline void best_of(const uint32_t* key, int n, int m, int first, int* out)
 {
     const int lane = threadIdx.x & 63;
     uint32_t k[R > 0 ? R : 1];
+    uint32_t top = 0;
     if constexpr (R > 0) {
 #pragma unroll
-        for (int r = 0; r < R; ++r) k[r] = 64 * r + lane < n ? key[64 * r + lane] : 0u;
-    }
+        for (int r = 0; r < R; ++r) { k[r] = 64 * r + lane < n ? key[64 * r + lane] : 0u; top = max(top, k[r]); }
+    } else
+        for (int j = lane; j < n; j += 64) top = max(top, key[j]);
+    for (int w = 1; w < 64; w <<= 1) top = max(top, (uint32_t)__shfl_xor((int)top, w));
+    top = (uint32_t)uniform((int)top);
     auto count = [&](uint32_t from) __attribute__((always_inline)) {      // scores >= from > 0
         int c = 0;
         if constexpr (R > 0) {
@@ -154,14 +159,39 @@ __device__ inline Limit limit_of(const uint32_t* key, int n, int m)
         }
         return c;
     };
-    uint32_t limit = 0;
-    for (int bit = 31; bit >= 0; --bit) {
-        const uint32_t cand = limit | (1u << bit);
-        const int c = count(cand);
-        if (c >= m) limit = cand;
-        if (c == m) return Limit{limit, m};
+    // at: at least m scores; over: fewer (behind the largest none; 2^32 is 0 here)
+    uint32_t at = 1, over = top + 1;
+    int c = n;
+    for (uint32_t step = 1u << 22; step < top; step <<= 1) {
+        c = count(top - step);
+        if (c >= m) { at = top - step; break; }
+        over = top - step;
+        if (step >> 31) break;
     }
-    return Limit{limit, m - (limit == 0xFFFFFFFFu ? 0 : count(limit + 1))};
+    if (c < m) c = n;                                             // (at = 1)
+    while (c != m && over - at > 1) {
+        const uint32_t mid = at + (over - at) / 2;
+        const int x = count(mid);
+        if (x >= m) { at = mid; c = x; } else over = mid;
+    }
+    int ties = c == m ? n : m - (at == top ? 0 : count(at + 1)); // of those equal to the limit
+    auto emit = [&](uint32_t x, int j0) __attribute__((always_inline)) {
+        const unsigned long long below = (1ull << lane) - 1;
+        bool take = x >= at;
+        if (ties < n) {
+            const unsigned long long eq = __builtin_amdgcn_ballot_w64(x == at);
+            take = x > at || (x == at && (int)__builtin_popcountll(eq & below) < ties);
+            ties -= min(ties, (int)__builtin_popcountll(eq));
+        }
+        const unsigned long long all = __builtin_amdgcn_ballot_w64(take);
+        if (take) out[(int)__builtin_popcountll(all & below)] = first + j0 + lane;
+        out += (int)__builtin_popcountll(all);
+    };
+    if constexpr (R > 0) {
+#pragma unroll
+        for (int r = 0; r < R; ++r) if (64 * r < n) emit(k[r], 64 * r);
+    } else
+        for (int j0 = 0; j0 < n; j0 += 64) emit(j0 + lane < n ? key[j0 + lane] : 0u, j0);
 }
 
 // 16 rows of the matrix instruction are the query heads of a kv head's group, padded to GP by heads that are there, for 16 / GP tokens, against 16 pages at a
@@ -169,8 +199,10 @@ __device__ inline Limit limit_of(const uint32_t* key, int n, int m)
 template <int D, int GP>
 __global__ __launch_bounds__(1024) void select_kernel(const SelectArgs a, int nt /* tokens of a workgroup */, int tiles)
 {
-    constexpr int NS = D / 64;
+    constexpr int NS = D / 64, NC = D / 8;                        // steps of the contraction, eights of a row
     extern __shared__ uint32_t keys[];                            // [nt][max_pages]
+    __shared__ __align__(16) unsigned char q8s[16][D];
+    __shared__ uint32_t amax_s[16];
     __shared__ int seq[16], pos[16];
     const StepArgs& s = a.s;
     const int tid = threadIdx.x, lane = tid & 63, cc = lane & 15, g = lane >> 4;
@@ -179,96 +211,103 @@ __global__ __launch_bounds__(1024) void select_kernel(const SelectArgs a, int nt
     int h, tile;
     head_tile_of_block((int)blockIdx.x, s.Hkv, tiles, h, tile);
     const int t0 = tile * nt;
-    find_tokens(s, t0, nt, seq, pos);
 
-    // one power of two for the group: brings its largest magnitude to [64, 128) (magnitudes below 2^-121 count as that)
-    const int t = min(t0 + min(cc / GP, nt - 1), s.T - 1);
-    auto row = [&](int sub, uint4v (&x)[2 * NS]) __attribute__((always_inline)) {
-        const uint16_t* q = s.q + (size_t)t * s.q_token + (size_t)(h * G + min(16 * sub + cc % GP, G - 1)) * s.q_head + 16 * g;
-#pragma unroll
-        for (int i = 0; i < 2 * NS; ++i) x[i] = *reinterpret_cast<const uint4v*>(q + 64 * (i >> 1) + 8 * (i & 1));
+    // Q in 8 bits, eight values to a thread of the first four (D = 64: two) waves: one power of two for a token's group brings its largest magnitude to
+    // [64, 128) (magnitudes below 2^-121 count as that)
+    const int qrow = tid / NC, qtok = min(qrow / GP, nt - 1);
+    const bool has_q = qrow < 16;
+    uint4v x[1];
+    auto load_q = [&](int sub) __attribute__((always_inline)) {
+        x[0] = *reinterpret_cast<const uint4v*>(s.q + (size_t)min(t0 + qtok, s.T - 1) * s.q_token + (size_t)(h * G + min(16 * sub + qrow % GP, G - 1)) * s.q_head + 8 * (tid % NC));
     };
-    float amax = 0.0f;
-    uint4v x[2 * NS];
-    for (int sub = 0; sub < subs; ++sub) { row(sub, x); amax = fmaxf(amax, largest_of(x)); }
-    amax = lanes_max<16, 32>(amax);
-    if constexpr (GP >= 2) amax = lanes_max<1, GP / 2>(amax);
-    const float f = __uint_as_float((260u - max(__float_as_uint(amax) >> 23, 6u)) << 23);
+    if (tid < 16) amax_s[tid] = 0;
+    if (has_q) load_q(0);
+    find_tokens(s, t0, nt, seq, pos);                             // (two barriers)
+    for (int sub = 0; sub < subs; ++sub) {
+        if (!has_q) break;
+        if (sub > 0) load_q(sub);
+        atomicMax(&amax_s[qtok], __float_as_uint(largest_of(x)));
+    }
+    const int seq_lane = seq[cc], pos_lane = pos[cc];
 
     for (int sub = 0; sub < subs; ++sub) {
-        if (subs > 1) row(sub, x);
+        __syncthreads();                                          // (amax_s is whole; q8s has been read)
+        if (has_q) {
+            if (subs > 1) load_q(sub);
+            const float f = __uint_as_float((260u - max(amax_s[qtok] >> 23, 6u)) << 23);
+            uint2v r;
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                uint32_t v[4];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const uint32_t p = x[0][2 * i + (j >> 1)];
+                    // (1.5 2^23 added: rounded to nearest even, in two's complement in the low bits)
+                    v[j] = __float_as_uint(__builtin_amdgcn_fmed3f(__uint_as_float((j & 1) ? p & 0xFFFF0000u : p << 16) * f, -127.0f, 127.0f) + 12582912.0f);
+                }
+                r[i] = __builtin_amdgcn_perm(__builtin_amdgcn_perm(v[3], v[2], 0x0C0C0400u), __builtin_amdgcn_perm(v[1], v[0], 0x0C0C0400u), 0x05040100u);
+            }
+            *reinterpret_cast<uint2v*>(&q8s[qrow][8 * (tid % NC)]) = r;
+        }
+        __syncthreads();
         intx4 q8[NS];
 #pragma unroll
-        for (int i = 0; i < NS; ++i)
-#pragma unroll
-            for (int w = 0; w < 4; ++w) {
-                uint32_t r = 0;
-#pragma unroll
-                for (int j = 0; j < 2; ++j) {
-                    const uint32_t p = x[2 * i + (w >> 1)][2 * (w & 1) + j];
-                    // (1.5 2^23 added: rounded to nearest even, in two's complement in the low bits)
-                    const uint32_t lo = __float_as_uint(__builtin_amdgcn_fmed3f(__uint_as_float(p << 16) * f, -127.0f, 127.0f) + 12582912.0f) & 0xFFu;
-                    const uint32_t hi = __float_as_uint(__builtin_amdgcn_fmed3f(__uint_as_float(p & 0xFFFF0000u) * f, -127.0f, 127.0f) + 12582912.0f) & 0xFFu;
-                    r |= (lo | hi << 8) << (16 * j);
-                }
-                q8[i][w] = (int)r;
-            }
+        for (int i = 0; i < NS; ++i) q8[i] = *reinterpret_cast<const intx4*>(&q8s[cc][64 * i + 16 * g]);
         for (int i0 = 0, i1; i0 < nt; i0 = i1) {                  // tokens of one sequence
-            const int b = uniform(seq[i0]);
+            const int b = __builtin_amdgcn_readlane(seq_lane, i0);
             int hi = 0;                                           // behind the last page that competes
-            for (i1 = i0; i1 < nt && uniform(seq[i1]) == b; ++i1) {
-                const int own = uniform(pos[i1]) >> 7;
+            for (i1 = i0; i1 < nt && __builtin_amdgcn_readlane(seq_lane, i1) == b; ++i1) {
+                const int own = __builtin_amdgcn_readlane(pos_lane, i1) >> 7;
                 if (own + 1 > a.n_blocks) hi = max(hi, own + 1 - a.last);
             }
             if (b < 0) continue;
             constexpr int U = 4;                                  // sixteens of pages under way at once
             for (int j1 = (a.first & ~15) + 16 * wave; j1 < hi; j1 += 16 * U * waves) {
-              int id[U];
-              intx4 k8[U][NS];
-              float scales[U];
+                int id[U];
+                intx4 k8[U][NS];
+                float scales[U];
 #pragma unroll
-              for (int u = 0; u < U; ++u) id[u] = s.table[(size_t)b * s.max_pages + min(j1 + 16 * u * waves + cc, s.max_pages - 1)];
+                for (int u = 0; u < U; ++u) id[u] = s.table[(size_t)b * s.max_pages + min(j1 + 16 * u * waves + cc, s.max_pages - 1)];
 #pragma unroll
-              for (int u = 0; u < U; ++u) {
-                const bool live = id[u] >= 0 && id[u] < s.num_pages;
-                const unsigned char* rec = a.summary + ((size_t)(live ? id[u] : 0) * s.Hkv + h) * (D + kSummaryTail);
+                for (int u = 0; u < U; ++u) {
+                    const bool live = id[u] >= 0 && id[u] < s.num_pages;
+                    const unsigned char* rec = a.summary + ((size_t)(live ? id[u] : 0) * s.Hkv + h) * (D + kSummaryTail);
 #pragma unroll
-                for (int i = 0; i < NS; ++i) k8[u][i] = *reinterpret_cast<const intx4*>(rec + 64 * i + 16 * g);
-                scales[u] = *reinterpret_cast<const float*>(rec + D);
-                if (!live) scales[u] = 0.0f;
-              }
-#pragma unroll
-              for (int u = 0; u < U; ++u) {
-                const int j = j1 + 16 * u * waves + cc;
-                if (j - cc >= hi) break;
-                const float scale = scales[u];
-                intx4 acc = {0, 0, 0, 0};
-#pragma unroll
-                for (int i = 0; i < NS; ++i) acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(q8[i], k8[u][i], acc, 0, 0, 0);
-                // rows 4 g .. 4 g + 3 of page j: the largest of a token's heads
-                auto put = [&](int token, int v) __attribute__((always_inline)) {
-                    if (token < i0 || token >= i1 || j >= hi) return;
-                    const uint32_t key = ordered(fmaf((float)v, scale, 0.0f));
-                    uint32_t* p = keys + token * S + j;
-                    *p = sub == 0 ? key : max(*p, key);
-                };
-                if constexpr (GP == 1) { put(4 * g, acc[0]); put(4 * g + 1, acc[1]); put(4 * g + 2, acc[2]); put(4 * g + 3, acc[3]); }
-                else if constexpr (GP == 2) { put(2 * g, max(acc[0], acc[1])); put(2 * g + 1, max(acc[2], acc[3])); }
-                else {
-                    int m = max(max(acc[0], acc[1]), max(acc[2], acc[3]));
-                    if constexpr (GP >= 8) { const auto r = __builtin_amdgcn_permlane16_swap((uint32_t)m, (uint32_t)m, false, false); m = max((int)r[0], (int)r[1]); }
-                    if constexpr (GP >= 16) { const auto r = __builtin_amdgcn_permlane32_swap((uint32_t)m, (uint32_t)m, false, false); m = max((int)r[0], (int)r[1]); }
-                    if (GP == 4 || (GP == 8 && (g & 1) == 0) || g == 0) put(4 * g / GP, m);
+                    for (int i = 0; i < NS; ++i) k8[u][i] = *reinterpret_cast<const intx4*>(rec + 64 * i + 16 * g);
+                    scales[u] = *reinterpret_cast<const float*>(rec + D);
+                    if (!live) scales[u] = 0.0f;
                 }
-              }
+#pragma unroll
+                for (int u = 0; u < U; ++u) {
+                    const int j = j1 + 16 * u * waves + cc;
+                    if (j - cc >= hi) break;
+                    intx4 acc = {0, 0, 0, 0};
+#pragma unroll
+                    for (int i = 0; i < NS; ++i) acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(q8[i], k8[u][i], acc, 0, 0, 0);
+                    // rows 4 g .. 4 g + 3 of page j: the largest of a token's heads
+                    auto put = [&](int token, int v) __attribute__((always_inline)) {
+                        if (token < i0 || token >= i1 || j >= hi) return;
+                        const uint32_t key = max(ordered(fmaf((float)v, scales[u], 0.0f)), 1u);
+                        uint32_t* p = keys + token * S + j;
+                        *p = sub == 0 ? key : max(*p, key);
+                    };
+                    if constexpr (GP == 1) { put(4 * g, acc[0]); put(4 * g + 1, acc[1]); put(4 * g + 2, acc[2]); put(4 * g + 3, acc[3]); }
+                    else if constexpr (GP == 2) { put(2 * g, max(acc[0], acc[1])); put(2 * g + 1, max(acc[2], acc[3])); }
+                    else {
+                        int m = max(max(acc[0], acc[1]), max(acc[2], acc[3]));
+                        if constexpr (GP >= 8) { const auto r = __builtin_amdgcn_permlane16_swap((uint32_t)m, (uint32_t)m, false, false); m = max((int)r[0], (int)r[1]); }
+                        if constexpr (GP >= 16) { const auto r = __builtin_amdgcn_permlane32_swap((uint32_t)m, (uint32_t)m, false, false); m = max((int)r[0], (int)r[1]); }
+                        if (GP == 4 || (GP == 8 && (g & 1) == 0) || g == 0) put(4 * g / GP, m);
+                    }
+                }
             }
         }
     }
     __syncthreads();
 
     for (int i = wave; i < nt; i += waves) {
-        if (uniform(seq[i]) < 0) continue;
-        const int own = uniform(pos[i]) >> 7, nb = own + 1;       // (position -1: page -1)
+        if (__builtin_amdgcn_readlane(seq_lane, i) < 0) continue;
+        const int nb = (__builtin_amdgcn_readlane(pos_lane, i) >> 7) + 1;                  // (position -1: no page)
         int* out = a.blocks + ((size_t)(t0 + i) * s.Hkv + h) * a.n_blocks;
         if (nb <= a.n_blocks) {
             for (int j = lane; j < a.n_blocks; j += 64) out[j] = j < nb ? j : -1;
@@ -279,18 +318,12 @@ __global__ __launch_bounds__(1024) void select_kernel(const SelectArgs a, int nt
         const int n = nb - a.first - a.last, m = a.n_blocks - a.first - a.last;            // n > m
         if (m == 0) continue;
         const uint32_t* key = keys + i * S + a.first;
-        const Limit l = n <= 64 ? limit_of<1>(key, n, m) : n <= 256 ? limit_of<4>(key, n, m) : n <= 512 ? limit_of<8>(key, n, m) : n <= 1024 ? limit_of<16>(key, n, m) : limit_of<0>(key, n, m);
-        int at = a.first, ties = l.ties;
-        for (int j0 = 0; j0 < n; j0 += 64) {
-            const int j = j0 + lane;
-            const uint32_t k = key[min(j, n - 1)];
-            const unsigned long long eq = __builtin_amdgcn_ballot_w64(j < n && k == l.at), below = (1ull << lane) - 1;
-            const bool take = j < n && (k > l.at || (k == l.at && (int)__builtin_popcountll(eq & below) < ties));
-            ties -= min(ties, (int)__builtin_popcountll(eq));
-            const unsigned long long all = __builtin_amdgcn_ballot_w64(take);
-            if (take) out[at + (int)__builtin_popcountll(all & below)] = a.first + j;
-            at += (int)__builtin_popcountll(all);
-        }
+        out += a.first;
+        if (n <= 64) best_of<1>(key, n, m, a.first, out);
+        else if (n <= 256) best_of<4>(key, n, m, a.first, out);
+        else if (n <= 512) best_of<8>(key, n, m, a.first, out);
+        else if (n <= 1024) best_of<16>(key, n, m, a.first, out);
+        else best_of<0>(key, n, m, a.first, out);
     }
 }
 
