@@ -113,13 +113,14 @@ __global__ __launch_bounds__(256) void summarize_kernel(const unsigned char* __r
 }
 
 // ---------------------------------------------------------------------------------------------- what a workgroup's tokens are
-// Sequence (-1: of none) and position (below 0: before the first key) of tokens t0 .. t0 + nt - 1, nt <= 16.
-__device__ inline void find_tokens(const StepArgs& a, int t0, int nt, int* seq, int* pos)
+// Sequence (-1: of none) and position (below 0: before the first key) of tokens t0 .. t0 + nt - 1 (entries behind them: none).
+template <int N>
+__device__ inline void find_tokens(const StepArgs& a, int t0, int nt, int (&seq)[N], int (&pos)[N])
 {
     const int tid = threadIdx.x;
-    if (tid < 16) { seq[tid] = -1; pos[tid] = -1; }
+    if (tid < N) { seq[tid] = -1; pos[tid] = -1; }
     __syncthreads();
-    for (int b = tid; b < a.B; b += blockDim.x) {
+    for (int b = tid; b < a.B; b += (int)blockDim.x) {
         const int s = min(max(a.cu_q[b], 0), a.T), e = min(max(a.cu_q[b + 1], s), a.T);
         const int len = max(0, min(a.kv_lens[b], a.max_pages * 128));
         for (int t = max(s, t0); t < min(e, t0 + nt); ++t) { seq[t - t0] = b; pos[t - t0] = max(len - e + t, -1); }
@@ -331,19 +332,123 @@ __global__ __launch_bounds__(1024) void select_kernel(const SelectArgs a, int nt
 constexpr int kEntries = 2048;        // (token, page)s of a workgroup at most
 
 // 16 rows: the G query heads of a kv head for nt tokens (rows = token * G + head of the group), or 16 of more heads for one token.  Their pages are taken together, each
-// once, whichever of the tokens asked for it (the others' rows are masked); split over `splits` workgroups where there are few rows.
+// once, whichever of the tokens asked for it; split over `splits` workgroups where there are few rows.
 struct SparsePlan { int nt, subs, tiles, splits; };
 struct SparseWs { float *part_o /* [unit][split][16][D] */, *part_ml /* [unit][split][16][2]: maximum, sum; a sum below 0: not a row of any sequence */; };
 
+// The pages that any of a workgroup's tokens asks for, each once, sequence by sequence: page of the sequence, and the tokens that ask for it << 16.  tab: `cap` words, 16 bits
+// for every page of a sequence, zeros as far as tab_words() says; sequences that do not fit it together take their turns.  first: the choice number threadIdx.x of the
+// tokens', asked for ahead.  Returns how many.
+__device__ inline int tab_words(const StepArgs& s, int nt, int cap) { return min(nt * ((s.max_pages + 1) / 2), cap); }
+__device__ inline int choice_of(const StepArgs& s, const int* __restrict__ blocks, int n_blocks, int h, int t0, int nt, int x)
+{
+    const int t = t0 + x / n_blocks;
+    return x < nt * n_blocks && t < s.T ? blocks[((size_t)t * s.Hkv + h) * n_blocks + x % n_blocks] : -1;
+}
+__device__ inline int pages_of_tokens(const StepArgs& s, const int* __restrict__ blocks, int n_blocks, int h, int t0, int nt, const int (&seq)[16], const int (&pos)[16], int first,
+                                      uint32_t* tab, int cap, uint32_t* ents, int* red)
+{
+    const int tid = threadIdx.x, seq_lane = seq[tid & 15], pos_lane = pos[tid & 15];
+    int total = 0;
+    for (int i0 = 0, i1; i0 < nt; i0 = i1) {
+        // where each token's sequence has its words, as many sequences as fit
+        int words = 0, base_lane = -1;
+        for (i1 = i0; i1 < nt;) {
+            const int b = __builtin_amdgcn_readlane(seq_lane, i1);
+            int nb = 0, j = i1;
+            for (; j < nt && __builtin_amdgcn_readlane(seq_lane, j) == b; ++j) nb = max(nb, (__builtin_amdgcn_readlane(pos_lane, j) >> 7) + 1);
+            const int w = b < 0 ? 0 : (nb + 1) / 2;
+            if (words + w > cap) break;                           // (one alone fits)
+            if (w > 0 && (tid & 15) >= i1 && (tid & 15) < j) base_lane = words;
+            words += w;
+            i1 = j;
+        }
+        if (i0 > 0) {
+            for (int w = tid; w < words; w += 256) tab[w] = 0;
+            __syncthreads();
+        }
+        for (int x = i0 * n_blocks + tid; x < i1 * n_blocks; x += 256) {
+            const int i = x / n_blocks, blk = x < 256 ? first : choice_of(s, blocks, n_blocks, h, t0, nt, x);
+            const int base = __shfl(base_lane, i), last = __shfl(pos_lane, i) >> 7;
+            if (base >= 0 && blk >= 0 && blk <= last) atomicOr(&tab[base + (blk >> 1)], 1u << (i + 16 * (blk & 1)));
+        }
+        __syncthreads();
+        for (int w0 = 0; w0 < words; w0 += 256) {
+            const uint32_t w = w0 + tid < words ? tab[w0 + tid] : 0u;
+            int base = 0;
+            for (int i = i0; i < i1; ++i) { const int x = __builtin_amdgcn_readlane(base_lane, i); if (w0 + tid >= x) base = max(base, x); }
+            const int page = 2 * (w0 + tid - base), n = ((w & 0xFFFFu) != 0) + ((w >> 16) != 0);
+            int all;
+            int at = total + wg_scan<4>(n, red, all) - n;
+            if (w & 0xFFFFu) ents[at++] = (uint32_t)page | w << 16;
+            if (w >> 16) ents[at] = (uint32_t)(page + 1) | (w & 0xFFFF0000u);
+            total += all;
+        }
+        __syncthreads();
+    }
+    return total;
+}
+
+// Those pages, from the first of `cnt` on: what a wave has of one, 32 keys of K and V, and the lists behind it, 64 entries at a time in the lanes.  Addresses are a
+// page's, in scalar registers, and a lane's offsets, made once.
+template <int D> struct PageTile { Raw<D> k[2], v[2]; uint32_t ent; int end; };
 template <int D>
-__global__ __launch_bounds__(256, 3) void sparse_kernel(const SparseArgs a, const SparsePlan p, const SparseWs ws)
+struct PageWalk {
+    const StepArgs& s; const unsigned char* cache /* of the head */; const uint32_t* ents; const int *seq, *pos; int cnt;
+    uint32_t codes, scales;           // this lane's offsets in a part of a page's head
+    int ent_lane, id_lane, end_lane, id_end;                      // of entry id_end - 64 + lane: itself, its page, the last key that any of its tokens sees
+    __device__ __forceinline__ void ids(int i0)
+    {
+        ent_lane = (int)ents[min(i0 + (int)(threadIdx.x & 63), cnt - 1)];
+        const int last = 15 - __builtin_clz((uint32_t)ent_lane), b = seq[last];            // (tokens of one sequence follow each other: the last sees most)
+        end_lane = pos[last];
+        id_lane = s.table[(size_t)b * s.max_pages + (ent_lane & 0xFFFF)];
+        asm volatile("" : "+v"(id_lane));                         // (waited for here and not at every use)
+        id_end = i0 + 64;
+    }
+    __device__ __forceinline__ void begin(int wave, int cc, int g)
+    {
+        codes = (uint32_t)((32 * wave + cc) * (D / 2) + (D / 8) * g);
+        scales = (uint32_t)(128 * (D / 2) + (32 * wave + cc) * (D / 16) + (D == 128 ? 4 * (g >> 1) : 0));
+        ids(0);
+    }
+    __device__ __forceinline__ Raw<D> raw(const unsigned char* part, uint32_t key) const
+    {
+        Raw<D> r;
+        if constexpr (D == 128) {
+            const uint4v c = *reinterpret_cast<const uint4v*>(part + key * (D / 2) + (size_t)codes);
+            r.w[0] = c[0]; r.w[1] = c[1]; r.w[2] = c[2]; r.w[3] = c[3];
+        } else {
+            const uint2v c = *reinterpret_cast<const uint2v*>(part + key * (D / 2) + (size_t)codes);
+            r.w[0] = c[0]; r.w[1] = c[1];
+        }
+        r.sc = *reinterpret_cast<const uint32_t*>(part + key * (D / 16) + (size_t)scales);
+        return r;
+    }
+    __device__ __forceinline__ void load(PageTile<D>& t, int i)
+    {
+        constexpr size_t HALF = (size_t)128 * (D / 2 + D / 16);
+        if (i >= id_end) ids(id_end);
+        const int at = i - (id_end - 64), page = __builtin_amdgcn_readlane(id_lane, at);
+        const bool live = page >= 0 && page < s.num_pages;
+        t.ent = (uint32_t)__builtin_amdgcn_readlane(ent_lane, at);
+        t.end = live ? __builtin_amdgcn_readlane(end_lane, at) : -1;                       // (V, and K below, are zeros from here on)
+        const unsigned char* part = cache + (size_t)(live ? page : 0) * s.Hkv * (2 * HALF);
+#pragma unroll
+        for (int blk = 0; blk < 2; ++blk) t.k[blk] = raw(part, 16 * blk);
+#pragma unroll
+        for (int blk = 0; blk < 2; ++blk) t.v[blk] = raw(part + HALF, 16 * blk);
+    }
+};
+
+template <int D>
+__global__ __launch_bounds__(256, 4) void sparse_kernel(const SparseArgs a, const SparsePlan p, const SparseWs ws)
 {
     constexpr int NS = D / 32, NDT = D / 16;
-    constexpr int SETS = D == 64 ? 3 : 2;
     constexpr int RS = 2 * D + 32;                                // bytes per key of the V tile
     constexpr size_t VOFF = (size_t)128 * (D / 2 + D / 16);
     __shared__ __align__(16) unsigned char stage[4 * 32 * RS];     // first which tokens ask for a page, 16 bits each; then per wave V of 32 keys; at the end the waves' sums
-    __shared__ uint32_t ents[kEntries];                           // page of the sequence, and the tokens that ask for it << 16
+    extern __shared__ uint32_t ents[];                            // page of the sequence, and the tokens that ask for it << 16
     __shared__ float ml[2][4][16];
     __shared__ int seq[16], pos[16], red[4];
     const StepArgs& s = a.s;
@@ -354,46 +459,29 @@ __global__ __launch_bounds__(256, 3) void sparse_kernel(const SparseArgs a, cons
     head_tile_of_block((int)blockIdx.x, s.Hkv, p.tiles * p.subs * p.splits, h, rest);
     const int split = rest % p.splits, sub = rest / p.splits % p.subs, tile = rest / p.splits / p.subs;
     const int t0 = tile * p.nt, rows = p.subs > 1 ? min(16, G - 16 * sub) : p.nt * G;
-    find_tokens(s, t0, p.nt, seq, pos);
 
-    // the pages that any of the tokens asks for, sequence by sequence
-    int total = 0;
-    uint32_t* tab = reinterpret_cast<uint32_t*>(stage);
-    static_assert(sizeof(stage) >= 8192 * 2);
-    for (int i0 = 0, i1; i0 < p.nt; i0 = i1) {
-        const int b = uniform(seq[i0]);
-        int nb = 0;
-        for (i1 = i0; i1 < p.nt && uniform(seq[i1]) == b; ++i1) nb = max(nb, (uniform(pos[i1]) >> 7) + 1);
-        if (b < 0 || nb == 0) continue;
-        const int words = (nb + 1) / 2;
-        for (int w = tid; w < words; w += 256) tab[w] = 0;
-        __syncthreads();
-        for (int x = tid; x < (i1 - i0) * a.n_blocks; x += 256) {
-            const int i = i0 + x / a.n_blocks, blk = a.blocks[((size_t)(t0 + i) * s.Hkv + h) * a.n_blocks + x % a.n_blocks];
-            if (blk >= 0 && blk <= (pos[i] >> 7)) atomicOr(&tab[blk >> 1], 1u << (i + 16 * (blk & 1)));
-        }
-        __syncthreads();
-        for (int w0 = 0; w0 < words; w0 += 256) {
-            const uint32_t w = w0 + tid < words ? tab[w0 + tid] : 0u;
-            const int n = ((w & 0xFFFFu) != 0) + ((w >> 16) != 0);
-            int all;
-            int at = total + wg_scan<4>(n, red, all) - n;
-            if (w & 0xFFFFu) ents[at++] = 2 * (w0 + tid) | w << 16;
-            if (w >> 16) ents[at] = (2 * (w0 + tid) + 1) | (w & 0xFFFF0000u);
-            total += all;
-        }
-        __syncthreads();
+    // this lane's row: its token and head
+    const int r = min(cc, rows - 1), tok = p.subs > 1 ? 0 : r / G, head = h * G + (p.subs > 1 ? 16 * sub + r : r % G);
+    uint4v x[NS];
+    {
+        const uint16_t* q = s.q + (size_t)min(t0 + tok, s.T - 1) * s.q_token + (size_t)head * s.q_head + (D / 4) * g;
+#pragma unroll
+        for (int i = 0; i < NS; ++i) x[i] = *reinterpret_cast<const uint4v*>(q + 8 * i);
     }
+    const int first = choice_of(s, a.blocks, a.n_blocks, h, t0, p.nt, tid);
+    constexpr int cap = sizeof(stage) / 4;
+    static_assert(cap >= 8192 / 2);
+    uint32_t* tab = reinterpret_cast<uint32_t*>(stage);
+    for (int w = tid; w < tab_words(s, p.nt, cap); w += 256) tab[w] = 0;
+    find_tokens(s, t0, p.nt, seq, pos);
+    const int total = pages_of_tokens(s, a.blocks, a.n_blocks, h, t0, p.nt, seq, pos, first, tab, cap, ents, red);
     const int e0 = (int)((long long)total * split / p.splits), cnt = (int)((long long)total * (split + 1) / p.splits) - e0;
 
-    // this lane's row: its token, head and last key
-    const int r = min(cc, rows - 1), tok = p.subs > 1 ? 0 : r / G, head = h * G + (p.subs > 1 ? 16 * sub + r : r % G);
     const int k_last = pos[tok];
     const uint32_t row_bit = 1u << (16 + tok);
-    uint32_t everyone = 0;                                        // the tokens that there are, and the last key that all of them see
-    int see_last = 0x7FFFFFFF;
+    int see_last = 0x7FFFFFFF;                                    // the last key that every token sees
     for (int i = 0; i < p.nt; ++i)
-        if (uniform(seq[i]) >= 0) { everyone |= 1u << (16 + i); see_last = min(see_last, uniform(pos[i])); }
+        if (uniform(seq[i]) >= 0) see_last = min(see_last, uniform(pos[i]));
 
     floatx4 o[NDT];
     float m = -INFINITY, up_to = -INFINITY, l = 0.0f;
@@ -403,38 +491,10 @@ __global__ __launch_bounds__(256, 3) void sparse_kernel(const SparseArgs a, cons
         unsigned char* stg = stage + wave * (32 * RS);
         // (the two 16-byte pieces of every 32 change places in keys 4 - 7 of 8: a store serves eight lanes, eight keys, at a time on 32 banks)
         const uint32_t tr_base = lds_addr_of(stg) + (uint32_t)((4 * g + (cc >> 2)) * RS + 8 * ((cc & 3) ^ (2 * (g & 1))));
-        int ent_lane = 0, id_lane = 0, end_lane = 0, id_end = 0;  // of entry id_end - 64 + lane: itself, its page, the last key that any of its tokens sees
-        auto ids = [&](int i0) __attribute__((always_inline)) {
-            ent_lane = (int)ents[e0 + min(i0 + lane, cnt - 1)];
-            const int last = 15 - __builtin_clz((uint32_t)ent_lane), b = seq[last];      // (tokens of one sequence follow each other: the last sees most)
-            end_lane = pos[last];
-            id_lane = s.table[(size_t)b * s.max_pages + (ent_lane & 0xFFFF)];
-            asm volatile("" : "+v"(id_lane));                     // (waited for here and not at every use)
-            id_end = i0 + 64;
-        };
-        ids(0);
-        uint4v x[NS];
-        {
-            const uint16_t* q = s.q + (size_t)min(t0 + tok, s.T - 1) * s.q_token + (size_t)head * s.q_head + (D / 4) * g;
-#pragma unroll
-            for (int i = 0; i < NS; ++i) x[i] = *reinterpret_cast<const uint4v*>(q + 8 * i);
-        }
-        struct Tile { Raw<D> k[2], v[2]; bool live; uint32_t ent; int end; };
-        auto load = [&](Tile& t, int i) __attribute__((always_inline)) {
-            if (i >= id_end) ids(id_end);
-            const int page = __builtin_amdgcn_readlane(id_lane, i - (id_end - 64));
-            t.ent = (uint32_t)__builtin_amdgcn_readlane(ent_lane, i - (id_end - 64));
-            t.end = __builtin_amdgcn_readlane(end_lane, i - (id_end - 64));
-            t.live = page >= 0 && page < s.num_pages;
-            const unsigned char* part = a.cache + ((size_t)(t.live ? page : 0) * s.Hkv + h) * (2 * VOFF);
-#pragma unroll
-            for (int blk = 0; blk < 2; ++blk) t.k[blk] = load_raw<D>(part, 32 * wave + 16 * blk + cc, g);
-#pragma unroll
-            for (int blk = 0; blk < 2; ++blk) t.v[blk] = load_raw<D>(part + VOFF, 32 * wave + 16 * blk + cc, g);
-        };
-        Tile t[SETS];
-#pragma unroll
-        for (int i = 0; i + 1 < SETS; ++i) load(t[i], min(i, cnt - 1));
+        PageWalk<D> walk{s, a.cache + (size_t)h * (2 * VOFF), ents + e0, seq, pos, cnt};
+        walk.begin(wave, cc, g);
+        PageTile<D> t;
+        walk.load(t, 0);
 
         // Q: row cc, d = (D/4) g + 8 s .. + 7
         half8 qreg[NS];
@@ -452,13 +512,21 @@ __global__ __launch_bounds__(256, 3) void sparse_kernel(const SparseArgs a, cons
                 }
             c_row = fmaxf(a.c * inv, kLeastFactor);
         }
-        auto step = [&](const Tile& t) __attribute__((always_inline)) {
-            const int kt = (int)(t.ent & 0xFFFFu) * 128 + 32 * wave;
-            const bool masked = (t.ent & 0xFFFF0000u) != everyone || kt + 31 > see_last;
+        for (int i = 0; i < cnt; ++i) {
+            const uint32_t ent = t.ent;
+            const int kt = (int)(ent & 0xFFFFu) * 128 + 32 * wave, end = t.end;
+            const bool member = (ent & row_bit) != 0;             // (rows that do not ask for the page: probabilities of 0, by a reference of infinity)
+            if (kt + 31 > end) {                                  // behind a sequence's end there may be anything, and a page outside the cache reads as zeros
+#pragma unroll
+                for (int blk = 0; blk < 2; ++blk) {
+                    if (kt + 16 * blk + cc > end) t.v[blk].sc = 0;
+                    if (end < 0) t.k[blk].sc = 0;
+                }
+            }
             floatx4 sc[2];
 #pragma unroll
             for (int blk = 0; blk < 2; ++blk) {
-                const half2v ks = scales_of<D>(t.k[blk], g, t.live);
+                const half2v ks = scales_of<D>(t.k[blk], g, true);
                 sc[blk] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
                 for (int j = 0; j < NS; ++j) sc[blk] = __builtin_amdgcn_mfma_f32_16x16x32_f16(values8<D>(t.k[blk], ks, j), qreg[j], sc[blk], 0, 0, 0);
@@ -467,19 +535,21 @@ __global__ __launch_bounds__(256, 3) void sparse_kernel(const SparseArgs a, cons
             __builtin_amdgcn_wave_barrier();
 #pragma unroll
             for (int blk = 0; blk < 2; ++blk) {
-                const half2v vs = scales_of<D>(t.v[blk], g, t.live && kt + 16 * blk + cc <= t.end);
+                const half2v vs = scales_of<D>(t.v[blk], g, true);
 #pragma unroll
                 for (int j = 0; j < NS; ++j) *reinterpret_cast<half8*>(stg + (16 * blk + cc) * RS + (D / 2) * g + 16 * (j ^ ((cc >> 2) & 1))) = values8<D>(t.v[blk], vs, j);
             }
             __builtin_amdgcn_wave_barrier();
-            if (masked) {
-                const int last = (t.ent & row_bit) ? k_last : -1;
+            walk.load(t, min(i + 1, cnt - 1));
+            if (kt + 31 > see_last) {
+                const int last = member ? k_last : -1;
 #pragma unroll
                 for (int j = 0; j < 8; ++j)
                     if (kt + 16 * (j >> 2) + 4 * g + (j & 3) > last) sc[j >> 2][j & 3] = -INFINITY;
             }
             float mx = max_nc(max_nc(max_nc(sc[0][0], sc[0][1]), max_nc(sc[0][2], sc[0][3])), max_nc(max_nc(sc[1][0], sc[1][1]), max_nc(sc[1][2], sc[1][3])));
             mx = lanes_max<16, 32>(mx);
+            mx = member ? mx : -INFINITY;
             if (__builtin_amdgcn_ballot_w64(mx > up_to) != 0) {
                 const float m_new = fmaxf(m, fmaf(mx, c_row, -kTop)), alpha = __builtin_amdgcn_exp2f(m - (m_new == -INFINITY ? 0.0f : m_new));
                 m = m_new;
@@ -488,7 +558,7 @@ __global__ __launch_bounds__(256, 3) void sparse_kernel(const SparseArgs a, cons
 #pragma unroll
                 for (int dt = 0; dt < NDT; ++dt) o[dt] *= alpha;
             }
-            const float m_at = m == -INFINITY ? 0.0f : m;
+            const float m_at = !member ? INFINITY : m == -INFINITY ? 0.0f : m;
             float add = 0.0f;
             half8 pt;
 #pragma unroll
@@ -503,14 +573,6 @@ __global__ __launch_bounds__(256, 3) void sparse_kernel(const SparseArgs a, cons
                 const uint2v u = lds_read_tr16_at(tr_base + 32 * dt), w = lds_read_tr16_at(tr_base + 32 * dt + 16 * RS);
                 const uint4v av = {u[0], u[1], w[0], w[1]};
                 o[dt] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(half8, av), pt, o[dt], 0, 0, 0);
-            }
-        };
-        for (int i = 0; i < cnt; i += SETS) {
-#pragma unroll
-            for (int x = 0; x < SETS; ++x) {
-                if (x > 0 && i + x >= cnt) break;
-                load(t[(x + SETS - 1) % SETS], min(i + x + SETS - 1, cnt - 1));
-                step(t[x]);
             }
         }
     }
@@ -610,9 +672,14 @@ inline SparsePlan sparse_plan(int T, int Hq, int Hkv, int max_q, int n_blocks, i
     if (p.nt > max_q) p.nt = max_q;
     if (p.nt > kEntries / n_blocks) p.nt = kEntries / n_blocks;
     p.tiles = (T + p.nt - 1) / p.nt;
-    const long long units = (long long)p.tiles * Hkv * p.subs, wgs = 3ll * cus;
-    long long splits = units > 0 ? wgs / units : 1;
-    if (splits > n_blocks) splits = n_blocks;
+    // as many workgroups as the chip holds, four to a unit; up to twice as many while each has 16 pages, since tiles differ
+    const long long units = (long long)p.tiles * Hkv * p.subs, most = (long long)p.nt * n_blocks, wgs = 4ll * cus;
+    long long splits = 1;
+    if (units > 0) {
+        splits = wgs / units;
+        if (splits < 2 * wgs / units && splits < most / 16) splits = 2 * wgs / units < most / 16 ? 2 * wgs / units : most / 16;
+        if (splits > most) splits = most;
+    }
     p.splits = splits < 2 ? 1 : (int)splits;
     return p;
 }
@@ -625,7 +692,8 @@ inline SparseWs carve_sparse(void* ws, const SparsePlan& p, int Hkv, int D, size
 template <int D>
 int launch_sparse_of(const SparseArgs& a, const SparsePlan& p, const SparseWs& w, hipStream_t st)
 {
-    hipLaunchKernelGGL((sparse_kernel<D>), dim3((unsigned)p.tiles * a.s.Hkv * p.subs * p.splits), dim3(256), 0, st, a, p, w);
+    const dim3 grid((unsigned)p.tiles * a.s.Hkv * p.subs * p.splits);
+    hipLaunchKernelGGL((sparse_kernel<D>), grid, dim3(256), 4u * p.nt * a.n_blocks, st, a, p, w);
     if (hipGetLastError() != hipSuccess) return -1;
     if (p.splits > 1) {
         const int groups = 256 / (D / 4);

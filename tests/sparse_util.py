@@ -66,8 +66,10 @@ def select(q, cu, codes, scale, table, kv_lens, Hkv, n_blocks, first, last, fill
     return out
 
 
-def attend(q, cu, cache, table, kv_lens, Hkv, blocks, scale):
-    """attnqat_fwd_kv4_sparse in 64 bits: (o, lse, weight) as serve_util.attend gives them."""
+def attend(q, cu, cache, table, kv_lens, Hkv, blocks, scale, spread=False):
+    """attnqat_fwd_kv4_sparse in 64 bits: (o, lse, weight) as serve_util.attend gives them.  spread: where scores spread widely, the weight counts the probabilities
+    below 2^-25 of a row's largest too.  In fp16, with the largest at 2^11 or more, they are rounded by half a step of 2^-24, 2^-36 of the largest, which
+    the sum that divides is at least: |error| <= 2^-36 sum |v|, 2^-25.5 sum |v| in terms of a weight that counts 2^-10.5."""
     T, Hq, d = q.shape
     G = Hq // Hkv
     o, wt, lse = np.full(q.shape, np.nan), np.full(q.shape, np.nan), np.full((T, Hq), np.nan)
@@ -92,6 +94,8 @@ def attend(q, cu, cache, table, kv_lens, Hkv, blocks, scale):
                 p = np.exp(s - top)
                 l = p.sum(1, keepdims=True)
                 o[t0 + i, hq], wt[t0 + i, hq], lse[t0 + i, hq] = p @ v[key, h] / l, p @ np.abs(v[key, h]) / l, (top + np.log(l))[:, 0]
+                if spread:
+                    wt[t0 + i, hq] += 2.0 ** -25.5 * np.abs(v[key, h]).sum(0)
     return o, lse, wt
 
 

@@ -174,7 +174,7 @@ def random_blocks(T, Hkv, n_blocks, most, rng):
     return blocks
 
 
-def run_sparse(aq, n, kv, Hq, Hkv, d, n_blocks, seed=0, tail=3, layout="plain", max_q=None, scale=None, q_scale=1.0, blocks=None):
+def run_sparse(aq, n, kv, Hq, Hkv, d, n_blocks, seed=0, tail=3, layout="plain", max_q=None, scale=None, q_scale=1.0, blocks=None, spread=False):
     q, cu, cache, num, table = attention_case(n, kv, Hq, Hkv, d, seed, tail, q_scale)
     T = q.shape[0]
     rng = np.random.default_rng(seed + 1)
@@ -182,7 +182,7 @@ def run_sparse(aq, n, kv, Hq, Hkv, d, n_blocks, seed=0, tail=3, layout="plain", 
         blocks = random_blocks(T, Hkv, n_blocks, max(S.pages(k) for k in kv), rng)
     o, lse = _views(torch.full((T, Hq, d), 5.0, dtype=torch.bfloat16, device="cuda"), layout), torch.full((T, Hq), 5.0, device="cuda")
     aq.attnqat_fwd_kv4_sparse(_views(q.cuda(), layout), i32(cu), dev(cache.reshape(-1)), num, dev(table), i32(kv), Hkv, dev(blocks), max_q=max_q or max(max(n), 1), scale=scale, out=(o, lse))
-    check_attention(o, lse, P.attend(q.double().numpy(), cu, cache, table, kv, Hkv, blocks, d ** -0.5 if scale is None else scale), (n, kv, Hq, Hkv, d))
+    check_attention(o, lse, P.attend(q.double().numpy(), cu, cache, table, kv, Hkv, blocks, d ** -0.5 if scale is None else scale, spread), (n, kv, Hq, Hkv, d))
     if tail:
         assert bool((o[-tail:] == 5.0).all()) and bool((lse[-tail:] == 5.0).all())
     return o, lse
@@ -206,6 +206,51 @@ def test_heads_of_a_group(aq, G):
 @pytest.mark.parametrize("max_q", [None, 1, 2])
 def test_ragged(aq, n, kv, Hq, Hkv, d, layout, max_q):
     run_sparse(aq, n, kv, Hq, Hkv, d, 5, seed=sum(n), layout=layout, max_q=max_q)
+
+
+@pytest.mark.parametrize("Hq,Hkv,d,T", [(32, 8, 128, 1050), (8, 8, 64, 1030), (16, 8, 128, 1040), (24, 8, 64, 1100), (40, 8, 128, 900), (64, 8, 64, 520), (72, 8, 128, 400), (128, 8, 128, 270),
+                                        (160, 8, 64, 150), (264, 8, 128, 130)])
+@pytest.mark.parametrize("kind", ["random", "alike", "all"])
+def test_many_rows(aq, Hq, Hkv, d, T, kind):
+    """Long pieces beside single tokens, sequences without rows and rows without a key, in one step; any choice of pages, nearly the same one for all rows, and every page."""
+    n, kv = [1, 0, T // 2, 3, 17, 0, T - T // 2 - 61, 40], [700, 50, T // 2 + 300, 2, 1900, 0, T - T // 2 - 61, 23]
+    q, cu, cache, num, table = attention_case(n, kv, Hq, Hkv, d, T, 0)
+    rng = np.random.default_rng(T)
+    most = max(S.pages(k) for k in kv)
+    blocks = random_blocks(T, Hkv, 5, most, rng)
+    if kind == "alike":
+        blocks[:] = np.where(rng.random(blocks.shape) < 0.9, np.array([0, 2, 1, 2, 3], np.int32), blocks)
+    elif kind == "all":
+        blocks = np.broadcast_to(np.arange(most, dtype=np.int32), (T, Hkv, most)).copy()
+    o, lse = run_sparse(aq, n, kv, Hq, Hkv, d, blocks.shape[2], seed=T, tail=0, blocks=blocks)
+    few = aq.attnqat_fwd_kv4_sparse(q.cuda(), i32(cu), dev(cache.reshape(-1)), num, dev(table), i32(kv), Hkv, dev(blocks), max_q=1)      # (by the kernel of few rows)
+    ref = P.attend(q.double().numpy(), cu, cache, table, kv, Hkv, blocks, d ** -0.5)
+    check_attention(*few, ref, "few")
+    again = run_sparse(aq, n, kv, Hq, Hkv, d, blocks.shape[2], seed=T, tail=0, blocks=blocks, layout="fused")
+    assert torch.equal(again[0], o) and torch.equal(again[1], lse)
+
+
+@pytest.mark.parametrize("q_scale", [0.0, 1e-30, 40.0])
+def test_many_rows_whose_scores_spread(aq, q_scale):
+    """References that stay, and that follow at almost every page."""
+    for d in (64, 128):
+        run_sparse(aq, [1100, 20], [3000, 700], 32, 8, d, 9, seed=3, q_scale=q_scale, scale=0.02 if q_scale > 1 else None, spread=True)
+
+
+def test_nan_stays_in_its_row_among_many(aq):
+    n, kv, G = [1030, 60], [1100, 400], 4
+    q, cu, cache, num, table = attention_case(n, kv, 8 * G, 8, 128, 1, tail=0)
+    blocks = dev(random_blocks(sum(n), 8, 4, 9, np.random.default_rng(1)))
+    args = (i32(cu), dev(cache.reshape(-1)), num, dev(table), i32(kv), 8, blocks)
+    qd = q.cuda()
+    o, lse = aq.attnqat_fwd_kv4_sparse(qd, *args, max_q=max(n))
+    qn = qd.clone()
+    at = int((lse[:, 9] > -1e30).nonzero()[500])
+    qn[at, 9, 17] = float("nan")
+    on, ln = aq.attnqat_fwd_kv4_sparse(qn, *args, max_q=max(n))
+    assert bool(on[at, 9].isnan().all()) and bool(ln[at, 9].isnan())
+    on[at, 9], ln[at, 9] = o[at, 9], lse[at, 9]
+    assert torch.equal(on, o) and torch.equal(ln, lse)
 
 
 @pytest.mark.parametrize("n,T", [(1, 1), (900, 900), (3000, 3000)])
