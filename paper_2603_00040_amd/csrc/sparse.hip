@@ -132,34 +132,13 @@ __device__ inline void find_tokens(const StepArgs& a, int t0, int nt, int (&seq)
 // Order of floats as of unsigned numbers.
 __device__ inline uint32_t ordered(float x) { const uint32_t u = __float_as_uint(x); return (u >> 31) ? ~u : (u | 0x80000000u); }
 
-// The m best of n scores (0 < m < n; scores from `key` on, in LDS), lowest first among equals, to out as page numbers first + index, ascending.  By a wave, with its scores
-// in R registers (64 R of them at most; R = 0: read from LDS every time).  The m-th largest lies not far below the largest (scores are floats: half of it is 2^23 away):
-// steps down from that double until there are m scores, and the last step is halved until a limit has exactly m at or above it, or is the m-th largest
-// itself, which others equal.
-template <int R>
-__device__ inline void best_of(const uint32_t* key, int n, int m, int first, int* out)
+// The limit that the m best of some scores lie at or above, of which `top` is the largest and count(x) says how many are x or more (x > 0).  It lies not far below the largest
+// (scores are floats: half of it is 2^23 away): steps down from that double until there are m scores, and the last step is halved until a limit has exactly m at or above it,
+// or is the m-th largest itself, which others equal: then ties of those are taken.
+struct Limit { uint32_t at; int ties; };
+template <class Count>
+__device__ __forceinline__ Limit limit_of(uint32_t top, int n, int m, const Count& count)
 {
-    const int lane = threadIdx.x & 63;
-    uint32_t k[R > 0 ? R : 1];
-    uint32_t top = 0;
-    if constexpr (R > 0) {
-#pragma unroll
-        for (int r = 0; r < R; ++r) { k[r] = 64 * r + lane < n ? key[64 * r + lane] : 0u; top = max(top, k[r]); }
-    } else
-        for (int j = lane; j < n; j += 64) top = max(top, key[j]);
-    for (int w = 1; w < 64; w <<= 1) top = max(top, (uint32_t)__shfl_xor((int)top, w));
-    top = (uint32_t)uniform((int)top);
-    auto count = [&](uint32_t from) __attribute__((always_inline)) {      // scores >= from > 0
-        int c = 0;
-        if constexpr (R > 0) {
-#pragma unroll
-            for (int r = 0; r < R; ++r) c += (int)__builtin_popcountll(__builtin_amdgcn_ballot_w64(k[r] >= from));
-        } else {
-            for (int j = lane; j < n; j += 64) c += key[j] >= from ? 1 : 0;
-            c = lane_total(c);
-        }
-        return c;
-    };
     // at: at least m scores; over: fewer (behind the largest none; 2^32 is 0 here)
     uint32_t at = 1, over = top + 1;
     int c = n;
@@ -175,24 +154,80 @@ __device__ inline void best_of(const uint32_t* key, int n, int m, int first, int
         const int x = count(mid);
         if (x >= m) { at = mid; c = x; } else over = mid;
     }
-    int ties = c == m ? n : m - (at == top ? 0 : count(at + 1)); // of those equal to the limit
-    auto emit = [&](uint32_t x, int j0) __attribute__((always_inline)) {
-        const unsigned long long below = (1ull << lane) - 1;
-        bool take = x >= at;
-        if (ties < n) {
-            const unsigned long long eq = __builtin_amdgcn_ballot_w64(x == at);
-            take = x > at || (x == at && (int)__builtin_popcountll(eq & below) < ties);
-            ties -= min(ties, (int)__builtin_popcountll(eq));
-        }
-        const unsigned long long all = __builtin_amdgcn_ballot_w64(take);
-        if (take) out[(int)__builtin_popcountll(all & below)] = first + j0 + lane;
-        out += (int)__builtin_popcountll(all);
-    };
+    return Limit{at, c == m ? n : m - (at == top ? 0 : count(at + 1))};
+}
+__device__ inline uint32_t wave_max(uint32_t x)
+{
+    for (int w = 1; w < 64; w <<= 1) x = max(x, (uint32_t)__shfl_xor((int)x, w));
+    return (uint32_t)uniform((int)x);
+}
+// Those of a wave's scores x (0: none) that are taken, to out as numbers, in the order of the lanes.
+__device__ __forceinline__ void emit(uint32_t x, int number, uint32_t at, int n, int& ties, int*& out)
+{
+    const unsigned long long below = (1ull << (threadIdx.x & 63)) - 1;
+    bool take = x >= at;
+    if (ties < n) {
+        const unsigned long long eq = __builtin_amdgcn_ballot_w64(x == at);
+        take = x > at || (x == at && (int)__builtin_popcountll(eq & below) < ties);
+        ties -= min(ties, (int)__builtin_popcountll(eq));
+    }
+    const unsigned long long all = __builtin_amdgcn_ballot_w64(take);
+    if (take) out[(int)__builtin_popcountll(all & below)] = number;
+    out += (int)__builtin_popcountll(all);
+}
+// The m best of n scores (0 < m < n; scores from `key` on, in LDS), lowest first among equals, to out as page numbers first + index, ascending.  By a wave, with its scores
+// in R registers (64 R of them at most; R = 0: read from LDS every time).  The m-th largest of the lanes' largest is no more than the m-th largest of all, and few
+// scores beyond the m are as large: these go on alone, one to a lane (best, which: 64 places of the wave's in LDS).
+template <int R>
+__device__ inline void best_of(const uint32_t* key, int n, int m, int first, int* out, uint32_t* best, uint16_t* which)
+{
+    const int lane = threadIdx.x & 63;
+    uint32_t k[R > 0 ? R : 1];
+    uint32_t mine = 0;
     if constexpr (R > 0) {
 #pragma unroll
-        for (int r = 0; r < R; ++r) if (64 * r < n) emit(k[r], 64 * r);
+        for (int r = 0; r < R; ++r) { k[r] = 64 * r + lane < n ? key[64 * r + lane] : 0u; mine = max(mine, k[r]); }
     } else
-        for (int j0 = 0; j0 < n; j0 += 64) emit(j0 + lane < n ? key[j0 + lane] : 0u, j0);
+        for (int j = lane; j < n; j += 64) mine = max(mine, key[j]);
+    const uint32_t top = wave_max(mine);
+    if constexpr (R > 1) {
+        if (m <= 64) {
+            const uint32_t from = limit_of(top, 64, m, [&](uint32_t x) __attribute__((always_inline)) { return (int)__builtin_popcountll(__builtin_amdgcn_ballot_w64(mine >= x)); }).at;
+            int c = 0;
+#pragma unroll
+            for (int r = 0; r < R; ++r) {
+                const unsigned long long in = __builtin_amdgcn_ballot_w64(k[r] >= from);
+                const int at = c + (int)__builtin_popcountll(in & ((1ull << lane) - 1));
+                if (k[r] >= from && at < 64) { best[at] = k[r]; which[at] = (uint16_t)(64 * r + lane); }
+                c += (int)__builtin_popcountll(in);
+            }
+            if (c <= 64) {
+                __builtin_amdgcn_wave_barrier();
+                const uint32_t x = lane < c ? best[lane] : 0u;
+                Limit l{from, c};
+                if (c > m) l = limit_of(top, c, m, [&](uint32_t f) __attribute__((always_inline)) { return (int)__builtin_popcountll(__builtin_amdgcn_ballot_w64(x >= f)); });
+                emit(x, first + which[lane], l.at, c, l.ties, out);
+                return;
+            }
+        }
+    }
+    const Limit l = limit_of(top, n, m, [&](uint32_t from) __attribute__((always_inline)) {
+        int c = 0;
+        if constexpr (R > 0) {
+#pragma unroll
+            for (int r = 0; r < R; ++r) c += (int)__builtin_popcountll(__builtin_amdgcn_ballot_w64(k[r] >= from));
+        } else {
+            for (int j = lane; j < n; j += 64) c += key[j] >= from ? 1 : 0;
+            c = lane_total(c);
+        }
+        return c;
+    });
+    int ties = l.ties;
+    if constexpr (R > 0) {
+#pragma unroll
+        for (int r = 0; r < R; ++r) if (64 * r < n) emit(k[r], first + 64 * r + lane, l.at, n, ties, out);
+    } else
+        for (int j0 = 0; j0 < n; j0 += 64) emit(j0 + lane < n ? key[j0 + lane] : 0u, first + j0 + lane, l.at, n, ties, out);
 }
 
 // 16 rows of the matrix instruction are the query heads of a kv head's group, padded to GP by heads that are there, for 16 / GP tokens, against 16 pages at a
@@ -203,7 +238,8 @@ __global__ __launch_bounds__(1024) void select_kernel(const SelectArgs a, int nt
     constexpr int NS = D / 64, NC = D / 8;                        // steps of the contraction, eights of a row
     extern __shared__ uint32_t keys[];                            // [nt][max_pages]
     __shared__ __align__(16) unsigned char q8s[16][D];
-    __shared__ uint32_t amax_s[16];
+    __shared__ uint32_t amax_s[16], best[16][64];
+    __shared__ uint16_t which[16][64];
     __shared__ int seq[16], pos[16];
     const StepArgs& s = a.s;
     const int tid = threadIdx.x, lane = tid & 63, cc = lane & 15, g = lane >> 4;
@@ -264,31 +300,32 @@ __global__ __launch_bounds__(1024) void select_kernel(const SelectArgs a, int nt
             if (b < 0) continue;
             constexpr int U = 4;                                  // sixteens of pages under way at once
             for (int j1 = (a.first & ~15) + 16 * wave; j1 < hi; j1 += 16 * U * waves) {
-                int id[U];
+                // (a lane asks for the id and the scale of a page of sixteen g, and hands them to the lanes that need them: the way to memory takes a load of one
+                // dword for sixteen pages as long as one of sixteen bytes)
+                const int mine = s.table[(size_t)b * s.max_pages + min(j1 + 16 * g * waves + cc, s.max_pages - 1)];
+                const bool live = mine >= 0 && mine < s.num_pages;
+                const int page = live ? mine : 0;
+                float scale_mine = *reinterpret_cast<const float*>(a.summary + ((size_t)page * s.Hkv + h) * (D + kSummaryTail) + D);
                 intx4 k8[U][NS];
-                float scales[U];
-#pragma unroll
-                for (int u = 0; u < U; ++u) id[u] = s.table[(size_t)b * s.max_pages + min(j1 + 16 * u * waves + cc, s.max_pages - 1)];
 #pragma unroll
                 for (int u = 0; u < U; ++u) {
-                    const bool live = id[u] >= 0 && id[u] < s.num_pages;
-                    const unsigned char* rec = a.summary + ((size_t)(live ? id[u] : 0) * s.Hkv + h) * (D + kSummaryTail);
+                    const unsigned char* rec = a.summary + ((size_t)__shfl(page, 16 * u + cc) * s.Hkv + h) * (D + kSummaryTail);
 #pragma unroll
                     for (int i = 0; i < NS; ++i) k8[u][i] = *reinterpret_cast<const intx4*>(rec + 64 * i + 16 * g);
-                    scales[u] = *reinterpret_cast<const float*>(rec + D);
-                    if (!live) scales[u] = 0.0f;
                 }
+                if (!live) scale_mine = 0.0f;
 #pragma unroll
                 for (int u = 0; u < U; ++u) {
                     const int j = j1 + 16 * u * waves + cc;
                     if (j - cc >= hi) break;
+                    const float scale = __shfl(scale_mine, 16 * u + cc);
                     intx4 acc = {0, 0, 0, 0};
 #pragma unroll
                     for (int i = 0; i < NS; ++i) acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(q8[i], k8[u][i], acc, 0, 0, 0);
                     // rows 4 g .. 4 g + 3 of page j: the largest of a token's heads
                     auto put = [&](int token, int v) __attribute__((always_inline)) {
                         if (token < i0 || token >= i1 || j >= hi) return;
-                        const uint32_t key = max(ordered(fmaf((float)v, scales[u], 0.0f)), 1u);
+                        const uint32_t key = max(ordered(fmaf((float)v, scale, 0.0f)), 1u);
                         uint32_t* p = keys + token * S + j;
                         *p = sub == 0 ? key : max(*p, key);
                     };
@@ -320,11 +357,11 @@ __global__ __launch_bounds__(1024) void select_kernel(const SelectArgs a, int nt
         if (m == 0) continue;
         const uint32_t* key = keys + i * S + a.first;
         out += a.first;
-        if (n <= 64) best_of<1>(key, n, m, a.first, out);
-        else if (n <= 256) best_of<4>(key, n, m, a.first, out);
-        else if (n <= 512) best_of<8>(key, n, m, a.first, out);
-        else if (n <= 1024) best_of<16>(key, n, m, a.first, out);
-        else best_of<0>(key, n, m, a.first, out);
+        if (n <= 64) best_of<1>(key, n, m, a.first, out, best[wave], which[wave]);
+        else if (n <= 256) best_of<4>(key, n, m, a.first, out, best[wave], which[wave]);
+        else if (n <= 512) best_of<8>(key, n, m, a.first, out, best[wave], which[wave]);
+        else if (n <= 1024) best_of<16>(key, n, m, a.first, out, best[wave], which[wave]);
+        else best_of<0>(key, n, m, a.first, out, best[wave], which[wave]);
     }
 }
 
