@@ -405,7 +405,7 @@ __device__ inline int pages_of_tokens(const StepArgs& s, const int* __restrict__
             __syncthreads();
         }
         for (int x = i0 * n_blocks + tid; x < i1 * n_blocks; x += 256) {
-            const int i = x / n_blocks, blk = x < 256 ? first : choice_of(s, blocks, n_blocks, h, t0, nt, x);
+            const int i = x / n_blocks, blk = x == tid ? first : choice_of(s, blocks, n_blocks, h, t0, nt, x);
             const int base = __shfl(base_lane, i), last = __shfl(pos_lane, i) >> 7;
             if (base >= 0 && blk >= 0 && blk <= last) atomicOr(&tab[base + (blk >> 1)], 1u << (i + 16 * (blk & 1)));
         }

@@ -223,7 +223,7 @@ def test_many_rows(aq, Hq, Hkv, d, T, kind):
     elif kind == "all":
         blocks = np.broadcast_to(np.arange(most, dtype=np.int32), (T, Hkv, most)).copy()
     o, lse = run_sparse(aq, n, kv, Hq, Hkv, d, blocks.shape[2], seed=T, tail=0, blocks=blocks)
-    few = aq.attnqat_fwd_kv4_sparse(q.cuda(), i32(cu), dev(cache.reshape(-1)), num, dev(table), i32(kv), Hkv, dev(blocks), max_q=1)      # (by the kernel of few rows)
+    few = aq.attnqat_fwd_kv4_sparse(q.cuda(), i32(cu), dev(cache.reshape(-1)), num, dev(table), i32(kv), Hkv, dev(blocks), max_q=1)      # (a token to a tile)
     ref = P.attend(q.double().numpy(), cu, cache, table, kv, Hkv, blocks, d ** -0.5)
     check_attention(*few, ref, "few")
     again = run_sparse(aq, n, kv, Hq, Hkv, d, blocks.shape[2], seed=T, tail=0, blocks=blocks, layout="fused")
@@ -263,6 +263,29 @@ def test_many_pages(aq):
     run_sparse(aq, [1, 5], [9000, 17001], 4, 1, 64, 300, seed=4)
     run_sparse(aq, [2], [140000], 2, 1, 64, 1024, seed=5)
     run_sparse(aq, [20], [140000], 1, 1, 128, 70, seed=6)
+
+
+@pytest.mark.parametrize("d,kv", [(64, [700000, 300, 690000, 1048576, 654321]), (128, [900000, 1048576, 800000, 1000, 1048500])])
+def test_long_sequences_that_share_a_tile(aq, d, kv):
+    """More pages than the tokens of a tile find room for together: few of them chosen, and a cache of few pages that the tables name many times."""
+    rng = np.random.default_rng(d)
+    num, n_blocks, n, T = 9, 40, 3, 3 * len(kv)
+    cache = S.random_cache(num, 1, d, rng)
+    table = rng.integers(0, num, (len(kv), 8192)).astype(np.int32)
+    q, cu = torch.randn(T, 1, d, generator=torch.Generator().manual_seed(d)).bfloat16(), np.arange(len(kv) + 1) * n
+    # the pages that may be chosen, and the same choice of a sequence that has no others
+    blocks, small = np.full((T, 1, n_blocks), -1, np.int32), np.full((T, 1, n_blocks), -1, np.int32)
+    short, lens = np.zeros((len(kv), 60), np.int32), []
+    for b, x in enumerate(kv):
+        last = (x - 1) // 128
+        some = np.unique(np.append(rng.integers(0, last + 1, 59), last))
+        short[b, :some.size] = table[b, some]
+        lens.append(x - 128 * (last + 1 - some.size))
+        for i in range(n * b, n * b + n):
+            at = rng.integers(0, some.size, n_blocks)
+            small[i, 0], blocks[i, 0] = at, some[at]
+    o, lse = aq.attnqat_fwd_kv4_sparse(q.cuda(), i32(cu), dev(cache.reshape(-1)), num, dev(table), i32(kv), 1, dev(blocks), max_q=16)
+    check_attention(o, lse, P.attend(q.double().numpy(), cu, cache, short, lens, 1, small, d ** -0.5), (d, kv))
 
 
 @pytest.mark.parametrize("q_scale,scale", [(1e-38, None), (1e30, 1e-31), (0.0, None), (1.0, 0.4), (1.0, 1e-44)])
