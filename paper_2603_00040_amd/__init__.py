@@ -467,7 +467,6 @@ def rope_table(dims, theta: float = 10000.0, layout: str = "paired", freqs=None,
         raise AttnQatError(f"freqs and axis must have an entry for each of the {pairs} pairs, axis below {len(dims)}")
     rope = Rope()
     _check(lib().attnqat_rope_table(ctypes.addressof(rope), pairs, len(dims), ROPE_HALVES if layout == "halves" else ROPE_PAIRED, (ctypes.c_double * pairs)(*freqs), (ctypes.c_uint8 * pairs)(*axis)))
-    rope.address = ctypes.addressof(rope)
     return rope
 
 
@@ -510,7 +509,7 @@ def _rope_call(f, q, k, positions, rope, out):
         if not (k1 == ko1 == 1 or k.numel() == 0):
             _rope_refuse(q, k, positions, rope, out)
         Hkv, kp, kop = ks[1], k.data_ptr(), ko.data_ptr()
-    rc = f(q.data_ptr(), qb, qh, qt, kp, kb, kh, kt, B, Hq, Hkv, L, d, BF16, positions.data_ptr(), L * axes if len(at) == 3 else 0, rope.address,
+    rc = f(q.data_ptr(), qb, qh, qt, kp, kb, kh, kt, B, Hq, Hkv, L, d, BF16, positions.data_ptr(), L * axes if len(at) == 3 else 0, ctypes.addressof(rope),
            qo.data_ptr(), ob, oh, ot, kop, kob, koh, kot, _stream_on(dev))
     if rc:
         _check(rc)
@@ -555,7 +554,7 @@ def attnqat_kv_cache_append_rope(q, k, v, positions, rope, cache, slots, num_pag
             _serve_refuse([], [("q", q, want), ("out", out, want)])
         ot, oh, _ = out.stride()
         qp, op = q.data_ptr(), out.data_ptr()
-    rc = (_lib or lib()).attnqat_kv_cache_append_rope(qp, qt, qh, k.data_ptr(), kt, kh, v.data_ptr(), vt, vh, T, Hq, Hkv, d, BF16, positions.data_ptr(), rope.address,
+    rc = (_lib or lib()).attnqat_kv_cache_append_rope(qp, qt, qh, k.data_ptr(), kt, kh, v.data_ptr(), vt, vh, T, Hq, Hkv, d, BF16, positions.data_ptr(), ctypes.addressof(rope),
                                                       cache.data_ptr(), _serve_pages(cache, num_pages, Hkv, d), slots.data_ptr(), op, ot, oh, _stream_on(dev))
     if rc:
         _check(rc)

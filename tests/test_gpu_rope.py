@@ -2,6 +2,9 @@
 
 Sine and cosine are off by at most 2^-23 + 2 pi 2^-32 < 2^-22.9 each, the two products and their sum by 2^-24 of the product's size each: together less than
 (|a| + |b|) 2^-21 for a pair (a, b); the one rounding to bf16 is a relative 2^-8."""
+import copy
+import pickle
+
 import numpy as np
 import pytest
 import torch
@@ -217,6 +220,18 @@ def test_append_takes_the_positions_of_a_plan(aq):
     check(qo, q, pos[:, None], freqs, axis, "halves")
     empty = torch.zeros(0, dtype=torch.int64, device="cuda")
     assert aq.attnqat_kv_cache_append_rope(q[:0], k[:0], v[:0], i32(pos[:0]), rope, cache, empty).shape == (0, 4, 64)
+
+
+def test_copied_tables(aq):
+    """A copy of a table, one that went through a pickle and one whose entries were put in by hand turn as the table itself does, the original gone or not."""
+    q, pos = S.bf16(np.random.default_rng(6).standard_normal((1, 3, 50, 64))).cuda(), i32(np.arange(50)[:, None] * 77)
+    want, _ = aq.attnqat_rope_fwd(q, None, pos, aq.rope_table((64,)))
+    first = aq.rope_table((64,))
+    by_hand = aq.Rope(first.pairs, first.axes, first.layout, 0, first.turns, first.axis)
+    for other in (copy.copy(first), copy.deepcopy(first), pickle.loads(pickle.dumps(first)), by_hand):
+        first = None
+        got, _ = aq.attnqat_rope_fwd(q, None, pos, other)
+        assert torch.equal(got, want)
 
 
 def test_binding_refuses(aq):
