@@ -478,6 +478,31 @@ struct PageWalk {
     }
 };
 
+// NaN scales among a wave's 32 keys of V (lane (cc, g) has those of keys cc and 16 + cc, as scales_of() gives them): the matrix instruction would carry them to every
+// row, a probability of 0 times NaN being NaN, so rows that see such a key get their NaN here, and the product zeros.  seen: how many of the keys, from the first on,
+// the lane's row sees.
+template <int D>
+__device__ __forceinline__ void nan_of_v(half2v (&vs)[2], floatx4 (&o)[D / 16], int seen)
+{
+    constexpr int H = D / 64;                                     // blocks of 16 of a lane
+    const uint32_t keys = seen >= 32 ? 0xFFFFFFFFu : (1u << max(seen, 0)) - 1u;
+    unsigned long long bad[2][H];
+#pragma unroll
+    for (int blk = 0; blk < 2; ++blk)
+#pragma unroll
+        for (int i = 0; i < H; ++i) {
+            const bool is = vs[blk][i] != vs[blk][i];
+            bad[blk][i] = __builtin_amdgcn_ballot_w64(is);
+            if (is) vs[blk][i] = (half_t)0.0f;
+        }
+#pragma unroll
+    for (int dt = 0; dt < D / 16; ++dt) {
+        const int sh = 16 * (dt / H), i = dt % H;
+        const uint32_t b = ((uint32_t)(bad[0][i] >> sh) & 0xFFFFu) | (uint32_t)(bad[1][i] >> sh) << 16;
+        if ((b & keys) != 0) o[dt] = floatx4{NAN, NAN, NAN, NAN};
+    }
+}
+
 template <int D>
 __global__ __launch_bounds__(256, 4) void sparse_kernel(const SparseArgs a, const SparsePlan p, const SparseWs ws)
 {
@@ -552,7 +577,7 @@ __global__ __launch_bounds__(256, 4) void sparse_kernel(const SparseArgs a, cons
         for (int i = 0; i < cnt; ++i) {
             const uint32_t ent = t.ent;
             const int kt = (int)(ent & 0xFFFFu) * 128 + 32 * wave, end = t.end;
-            const bool member = (ent & row_bit) != 0;             // (rows that do not ask for the page: probabilities of 0, by a reference of infinity)
+            const bool member = (ent & row_bit) != 0;
             if (kt + 31 > end) {                                  // behind a sequence's end there may be anything, and a page outside the cache reads as zeros
 #pragma unroll
                 for (int blk = 0; blk < 2; ++blk) {
@@ -570,12 +595,13 @@ __global__ __launch_bounds__(256, 4) void sparse_kernel(const SparseArgs a, cons
             }
             // V through LDS: written key by key, read back with four keys of one d in a lane
             __builtin_amdgcn_wave_barrier();
+            half2v vs[2] = {scales_of<D>(t.v[0], g, true), scales_of<D>(t.v[1], g, true)};
+            const float any_nan = __builtin_amdgcn_fdot2(vs[0], vs[1], 0.0f, false);       // (scales are NaN or finite)
+            if (__builtin_amdgcn_ballot_w64(any_nan != any_nan) != 0) nan_of_v<D>(vs, o, member ? k_last - kt + 1 : 0);
 #pragma unroll
-            for (int blk = 0; blk < 2; ++blk) {
-                const half2v vs = scales_of<D>(t.v[blk], g, true);
+            for (int blk = 0; blk < 2; ++blk)
 #pragma unroll
-                for (int j = 0; j < NS; ++j) *reinterpret_cast<half8*>(stg + (16 * blk + cc) * RS + (D / 2) * g + 16 * (j ^ ((cc >> 2) & 1))) = values8<D>(t.v[blk], vs, j);
-            }
+                for (int j = 0; j < NS; ++j) *reinterpret_cast<half8*>(stg + (16 * blk + cc) * RS + (D / 2) * g + 16 * (j ^ ((cc >> 2) & 1))) = values8<D>(t.v[blk], vs[blk], j);
             __builtin_amdgcn_wave_barrier();
             walk.load(t, min(i + 1, cnt - 1));
             if (kt + 31 > see_last) {
@@ -595,7 +621,7 @@ __global__ __launch_bounds__(256, 4) void sparse_kernel(const SparseArgs a, cons
 #pragma unroll
                 for (int dt = 0; dt < NDT; ++dt) o[dt] *= alpha;
             }
-            const float m_at = !member ? INFINITY : m == -INFINITY ? 0.0f : m;
+            const float m_at = m == -INFINITY ? 0.0f : m;
             float add = 0.0f;
             half8 pt;
 #pragma unroll
@@ -604,7 +630,12 @@ __global__ __launch_bounds__(256, 4) void sparse_kernel(const SparseArgs a, cons
                 add += x;
                 pt[j] = (half_t)x;
             }
-            l += add;
+            // (rows that do not ask for the page take nothing of it, whatever their scores are: another sequence's keys may be NaN)
+            l += member ? add : 0.0f;
+            uint4v pw = __builtin_bit_cast(uint4v, pt);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) pw[j] = member ? pw[j] : 0u;
+            pt = __builtin_bit_cast(half8, pw);
 #pragma unroll
             for (int dt = 0; dt < NDT; ++dt) {
                 const uint2v u = lds_read_tr16_at(tr_base + 32 * dt), w = lds_read_tr16_at(tr_base + 32 * dt + 16 * RS);

@@ -321,6 +321,56 @@ def test_nan_stays_in_its_row(aq):
         assert torch.equal(on, o) and torch.equal(ln, lse)
 
 
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("which", ["K", "V"])
+@pytest.mark.parametrize("G,max_q", [(1, 16), (4, 4), (2, 1), (17, 4)])
+def test_nan_in_the_cache_reaches_the_rows_that_see_it(aq, which, d, G, max_q):
+    """A NaN scale of one key: rows of other sequences, rows that did not choose its page and rows before it keep their bits; of V only its 16 channels turn to NaN."""
+    n, kv, Hkv = [1, 5, 1, 8, 1, 1], [500, 300, 380, 390, 700, 40], 2
+    q, cu, cache, num, table = attention_case(n, kv, G * Hkv, Hkv, d, 7, tail=0)
+    T = q.shape[0]
+    rng = np.random.default_rng(3)
+    blocks = np.stack([np.sort(rng.permutation(4)[:3]) for _ in range(T * Hkv)]).reshape(T, Hkv, 3).astype(np.int32)
+    run = lambda c: aq.attnqat_fwd_kv4_sparse(q.cuda(), i32(cu), dev(c.reshape(-1)), num, dev(table), i32(kv), Hkv, dev(blocks), max_q=max_q)  # noqa: E731
+    o, lse = run(cache)
+    assert not bool(o.isnan().any())
+    for b, key, block in ((1, 260, 0), (3, 386, d // 16 - 1), (3, 100, 2), (4, 17, 1), (4, 255, d // 16 - 1), (0, 499, 1)):
+        bad = cache.copy()
+        half = 64 * d + 128 * (d // 16)                            # codes and scales of K, then of V
+        row = bad.reshape(num, Hkv, 2 * half)[table[b, key // 128], 1]
+        row[(which == "V") * half + 64 * d + key % 128 * (d // 16) + block] = 0x7F
+        got, gl = run(bad)
+        sees = torch.zeros(T, dtype=torch.bool)
+        for i in range(n[b]):
+            sees[cu[b] + i] = key <= kv[b] - n[b] + i and key // 128 in blocks[cu[b] + i, 1]
+        hit = torch.zeros(o.shape, dtype=torch.bool)
+        hit[sees, G:, 16 * block if which == "V" else 0:16 * block + 16 if which == "V" else d] = True
+        assert torch.equal(got.isnan().cpu(), hit), (b, key)
+        hit = hit.cuda()
+        assert torch.equal(torch.where(hit, 0, got), torch.where(hit, 0, o)), (b, key)
+        if which == "V":
+            assert torch.equal(gl, lse)
+        else:
+            at = torch.zeros(lse.shape, dtype=torch.bool)
+            at[sees, G:] = True
+            assert torch.equal(gl.isnan().cpu(), at) and torch.equal(torch.where(at.cuda(), 0, gl), torch.where(at.cuda(), 0, lse))
+
+
+def test_nan_queries_without_a_page(aq):
+    """A row that chose nothing beside rows that did: 0 and -inf, whatever its query is."""
+    n, kv = [6, 1, 1], [400, 300, 200]
+    q, cu, cache, num, table = attention_case(n, kv, 8, 2, 128, 3, tail=0)
+    q[2], q[6, :4], q[7, 5] = float("nan"), float("inf"), float("-inf")
+    blocks = np.broadcast_to(np.array([0, 1], np.int32), (8, 2, 2)).copy()
+    blocks[2], blocks[6, 0], blocks[7] = -1, 99, -5
+    for max_q in (1, 4):
+        o, lse = aq.attnqat_fwd_kv4_sparse(q.cuda(), i32(cu), dev(cache.reshape(-1)), num, dev(table), i32(kv), 2, dev(blocks), max_q=max_q)
+        none = torch.zeros((8, 8), dtype=torch.bool, device="cuda")
+        none[2], none[6, :4], none[7] = True, True, True
+        assert bool((o[none] == 0).all()) and bool((lse[none] == float("-inf")).all())
+        assert not bool(o[~none].isnan().any()) and bool(lse[~none].isfinite().all())
+
+
 def test_pages_outside_the_cache_read_as_zeros(aq):
     q, cu, cache, num, table = attention_case([1, 20], [700, 300], 4, 2, 128, 2)
     table[0, 2], table[1, 0], table[0, 4] = -1, num, 1 << 30
