@@ -605,10 +605,9 @@ __global__ __launch_bounds__(256, 4) void sparse_kernel(const SparseArgs a, cons
             __builtin_amdgcn_wave_barrier();
             walk.load(t, min(i + 1, cnt - 1));
             if (kt + 31 > see_last) {
-                const int last = member ? k_last : -1;
 #pragma unroll
                 for (int j = 0; j < 8; ++j)
-                    if (kt + 16 * (j >> 2) + 4 * g + (j & 3) > last) sc[j >> 2][j & 3] = -INFINITY;
+                    if (kt + 16 * (j >> 2) + 4 * g + (j & 3) > k_last) sc[j >> 2][j & 3] = -INFINITY;
             }
             float mx = max_nc(max_nc(max_nc(sc[0][0], sc[0][1]), max_nc(sc[0][2], sc[0][3])), max_nc(max_nc(sc[1][0], sc[1][1]), max_nc(sc[1][2], sc[1][3])));
             mx = lanes_max<16, 32>(mx);
