@@ -370,7 +370,8 @@ constexpr int kEntries = 2048;        // (token, page)s of a workgroup at most
 
 // 16 rows: the G query heads of a kv head for nt tokens (rows = token * G + head of the group), or 16 of more heads for one token.  Their pages are taken together, each
 // once, whichever of the tokens asked for it; split over `splits` workgroups where there are few rows.
-struct SparsePlan { int nt, subs, tiles, splits; };
+struct SparsePlan { int nt, subs, tiles, splits, waves; };
+constexpr int sparse_stage(int D, int waves) { return waves * 32 * (2 * D + 32); }        // bytes of LDS beside the list of pages
 struct SparseWs { float *part_o /* [unit][split][16][D] */, *part_ml /* [unit][split][16][2]: maximum, sum; a sum below 0: not a row of any sequence */; };
 
 // The pages that any of a workgroup's tokens asks for, each once, sequence by sequence: page of the sequence, and the tokens that ask for it << 16.  tab: `cap` words, 16 bits
@@ -382,6 +383,7 @@ __device__ inline int choice_of(const StepArgs& s, const int* __restrict__ block
     const int t = t0 + x / n_blocks;
     return x < nt * n_blocks && t < s.T ? blocks[((size_t)t * s.Hkv + h) * n_blocks + x % n_blocks] : -1;
 }
+template <int NW>
 __device__ inline int pages_of_tokens(const StepArgs& s, const int* __restrict__ blocks, int n_blocks, int h, int t0, int nt, const int (&seq)[16], const int (&pos)[16], int first,
                                       uint32_t* tab, int cap, uint32_t* ents, int* red)
 {
@@ -401,22 +403,22 @@ __device__ inline int pages_of_tokens(const StepArgs& s, const int* __restrict__
             i1 = j;
         }
         if (i0 > 0) {
-            for (int w = tid; w < words; w += 256) tab[w] = 0;
+            for (int w = tid; w < words; w += 64 * NW) tab[w] = 0;
             __syncthreads();
         }
-        for (int x = i0 * n_blocks + tid; x < i1 * n_blocks; x += 256) {
+        for (int x = i0 * n_blocks + tid; x < i1 * n_blocks; x += 64 * NW) {
             const int i = x / n_blocks, blk = x == tid ? first : choice_of(s, blocks, n_blocks, h, t0, nt, x);
             const int base = __shfl(base_lane, i), last = __shfl(pos_lane, i) >> 7;
             if (base >= 0 && blk >= 0 && blk <= last) atomicOr(&tab[base + (blk >> 1)], 1u << (i + 16 * (blk & 1)));
         }
         __syncthreads();
-        for (int w0 = 0; w0 < words; w0 += 256) {
+        for (int w0 = 0; w0 < words; w0 += 64 * NW) {
             const uint32_t w = w0 + tid < words ? tab[w0 + tid] : 0u;
             int base = 0;
             for (int i = i0; i < i1; ++i) { const int x = __builtin_amdgcn_readlane(base_lane, i); if (w0 + tid >= x) base = max(base, x); }
             const int page = 2 * (w0 + tid - base), n = ((w & 0xFFFFu) != 0) + ((w >> 16) != 0);
             int all;
-            int at = total + wg_scan<4>(n, red, all) - n;
+            int at = total + wg_scan<NW>(n, red, all) - n;
             if (w & 0xFFFFu) ents[at++] = (uint32_t)page | w << 16;
             if (w >> 16) ents[at] = (uint32_t)(page + 1) | (w & 0xFFFF0000u);
             total += all;
@@ -503,16 +505,18 @@ __device__ __forceinline__ void nan_of_v(half2v (&vs)[2], floatx4 (&o)[D / 16], 
     }
 }
 
-template <int D>
-__global__ __launch_bounds__(256, 4) void sparse_kernel(const SparseArgs a, const SparsePlan p, const SparseWs ws)
+template <int D, int NW /* waves: 4, or 16 where a unit's pages are not split */>
+__global__ __launch_bounds__(64 * NW, 4) void sparse_kernel(const SparseArgs a, const SparsePlan p, const SparseWs ws)
 {
     constexpr int NS = D / 32, NDT = D / 16;
     constexpr int RS = 2 * D + 32;                                // bytes per key of the V tile
     constexpr size_t VOFF = (size_t)128 * (D / 2 + D / 16);
-    __shared__ __align__(16) unsigned char stage[4 * 32 * RS];     // first which tokens ask for a page, 16 bits each; then per wave V of 32 keys; at the end the waves' sums
-    extern __shared__ uint32_t ents[];                            // page of the sequence, and the tokens that ask for it << 16
-    __shared__ float ml[2][4][16];
-    __shared__ int seq[16], pos[16], red[4];
+    // first which tokens ask for a page, 16 bits each; then per wave V of 32 keys; at the end the waves' sums
+    extern __shared__ __align__(16) unsigned char stage[];
+    constexpr int kStage = sparse_stage(D, NW);
+    uint32_t* ents = reinterpret_cast<uint32_t*>(stage + kStage);  // page of the sequence, and the tokens that ask for it << 16
+    __shared__ float ml[2][NW][16];
+    __shared__ int seq[16], pos[16], red[NW];
     const StepArgs& s = a.s;
     const int tid = threadIdx.x, lane = tid & 63, cc = lane & 15, g = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -531,12 +535,12 @@ __global__ __launch_bounds__(256, 4) void sparse_kernel(const SparseArgs a, cons
         for (int i = 0; i < NS; ++i) x[i] = *reinterpret_cast<const uint4v*>(q + 8 * i);
     }
     const int first = choice_of(s, a.blocks, a.n_blocks, h, t0, p.nt, tid);
-    constexpr int cap = sizeof(stage) / 4;
+    constexpr int cap = sparse_stage(D, 4) / 4;
     static_assert(cap >= 8192 / 2);
     uint32_t* tab = reinterpret_cast<uint32_t*>(stage);
-    for (int w = tid; w < tab_words(s, p.nt, cap); w += 256) tab[w] = 0;
+    for (int w = tid; w < tab_words(s, p.nt, cap); w += 64 * NW) tab[w] = 0;
     find_tokens(s, t0, p.nt, seq, pos);
-    const int total = pages_of_tokens(s, a.blocks, a.n_blocks, h, t0, p.nt, seq, pos, first, tab, cap, ents, red);
+    const int total = pages_of_tokens<NW>(s, a.blocks, a.n_blocks, h, t0, p.nt, seq, pos, first, tab, cap, ents, red);
     const int e0 = (int)((long long)total * split / p.splits), cnt = (int)((long long)total * (split + 1) / p.splits) - e0;
 
     const int k_last = pos[tok];
@@ -549,14 +553,15 @@ __global__ __launch_bounds__(256, 4) void sparse_kernel(const SparseArgs a, cons
     float m = -INFINITY, up_to = -INFINITY, l = 0.0f;
 #pragma unroll
     for (int dt = 0; dt < NDT; ++dt) o[dt] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
-    if (cnt > 0) {
+    const int group = wave >> 2;                                  // of four waves: pages group, group + NW / 4 ..
+    if (group < cnt) {
         unsigned char* stg = stage + wave * (32 * RS);
         // (the two 16-byte pieces of every 32 change places in keys 4 - 7 of 8: a store serves eight lanes, eight keys, at a time on 32 banks)
         const uint32_t tr_base = lds_addr_of(stg) + (uint32_t)((4 * g + (cc >> 2)) * RS + 8 * ((cc & 3) ^ (2 * (g & 1))));
         PageWalk<D> walk{s, a.cache + (size_t)h * (2 * VOFF), ents + e0, seq, pos, cnt};
-        walk.begin(wave, cc, g);
+        walk.begin(wave & 3, cc, g);
         PageTile<D> t;
-        walk.load(t, 0);
+        walk.load(t, group);
 
         // Q: row cc, d = (D/4) g + 8 s .. + 7
         half8 qreg[NS];
@@ -574,9 +579,9 @@ __global__ __launch_bounds__(256, 4) void sparse_kernel(const SparseArgs a, cons
                 }
             c_row = fmaxf(a.c * inv, kLeastFactor);
         }
-        for (int i = 0; i < cnt; ++i) {
+        for (int i = group; i < cnt; i += NW / 4) {
             const uint32_t ent = t.ent;
-            const int kt = (int)(ent & 0xFFFFu) * 128 + 32 * wave, end = t.end;
+            const int kt = (int)(ent & 0xFFFFu) * 128 + 32 * (wave & 3), end = t.end;
             const bool member = (ent & row_bit) != 0;
             if (kt + 31 > end) {                                  // behind a sequence's end there may be anything, and a page outside the cache reads as zeros
 #pragma unroll
@@ -603,7 +608,7 @@ __global__ __launch_bounds__(256, 4) void sparse_kernel(const SparseArgs a, cons
 #pragma unroll
                 for (int j = 0; j < NS; ++j) *reinterpret_cast<half8*>(stg + (16 * blk + cc) * RS + (D / 2) * g + 16 * (j ^ ((cc >> 2) & 1))) = values8<D>(t.v[blk], vs[blk], j);
             __builtin_amdgcn_wave_barrier();
-            walk.load(t, min(i + 1, cnt - 1));
+            walk.load(t, min(i + NW / 4, cnt - 1));
             if (kt + 31 > see_last) {
 #pragma unroll
                 for (int j = 0; j < 8; ++j)
@@ -644,26 +649,32 @@ __global__ __launch_bounds__(256, 4) void sparse_kernel(const SparseArgs a, cons
         }
     }
 
-    // the four waves' sums, in units of their common maximum
+    // the waves' sums, in units of their common maximum
     constexpr int SS = D + 4;                                     // floats per row of the sums (16 rows are written side by side)
-    static_assert(4 * 16 * SS * 4 <= sizeof(stage));
+    static_assert(NW * 16 * SS * 4 <= kStage);
     float* sums = reinterpret_cast<float*>(stage);
     l = lanes_sum<16, 32>(l);
     if (g == 0) { ml[0][wave][cc] = m; ml[1][wave][cc] = l; }
     __syncthreads();
-    const float top = fmaxf(fmaxf(ml[0][0][cc], ml[0][1][cc]), fmaxf(ml[0][2][cc], ml[0][3][cc])), f = __builtin_amdgcn_exp2f(m - (top == -INFINITY ? 0.0f : top));
+    auto largest = [&](int row) __attribute__((always_inline)) {
+        float x = ml[0][0][row];
+#pragma unroll
+        for (int w = 1; w < NW; ++w) x = fmaxf(x, ml[0][w][row]);
+        return x;
+    };
+    const float top = largest(cc), f = __builtin_amdgcn_exp2f(m - (top == -INFINITY ? 0.0f : top));
 #pragma unroll
     for (int dt = 0; dt < NDT; ++dt) *reinterpret_cast<floatx4*>(sums + (wave * 16 + cc) * SS + 16 * dt + 4 * g) = o[dt] * f;
     __syncthreads();
     const size_t slot = (((size_t)tile * s.Hkv + h) * p.subs + sub) * p.splits + split;
-    for (int e = tid; e < rows * (D / 4); e += 256) {
+    for (int e = tid; e < rows * (D / 4); e += 64 * NW) {
         const int q = e / (D / 4), d = e % (D / 4) * 4, tk = p.subs > 1 ? 0 : q / G, hd = h * G + (p.subs > 1 ? 16 * sub + q : q % G);
         const bool on = seq[tk] >= 0;
-        const float tp = fmaxf(fmaxf(ml[0][0][q], ml[0][1][q]), fmaxf(ml[0][2][q], ml[0][3][q])), at = tp == -INFINITY ? 0.0f : tp;
+        const float tp = largest(q), at = tp == -INFINITY ? 0.0f : tp;
         float lt = 0.0f;
         floatx4 v = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-        for (int x = 0; x < 4; ++x) {
+        for (int x = 0; x < NW; ++x) {
             lt += ml[1][x][q] * __builtin_amdgcn_exp2f(ml[0][x][q] - at);
             v += *reinterpret_cast<const floatx4*>(sums + (x * 16 + q) * SS + d);
         }
@@ -739,8 +750,17 @@ inline SparsePlan sparse_plan(int T, int Hq, int Hkv, int max_q, int n_blocks, i
     if (p.nt > max_q) p.nt = max_q;
     if (p.nt > kEntries / n_blocks) p.nt = kEntries / n_blocks;
     p.tiles = (T + p.nt - 1) / p.nt;
-    // as many workgroups as the chip holds, four to a unit; up to twice as many while each has 16 pages, since tiles differ
     const long long units = (long long)p.tiles * Hkv * p.subs, most = (long long)p.nt * n_blocks, wgs = 4ll * cus;
+    p.waves = 4; p.splits = 1;
+    // Steps of single or drafted tokens, whose units are alike: where units of 16 or 8 waves just fill the chip, or there is little to read, waves share a unit's
+    // pages inside a workgroup, and nothing is joined afterwards (32 pages, heads of 128, with the choice: 256 units 47.5 us instead of 50.7, 512 76 instead of 82; 8 pages: 256 25.5
+    // instead of 28.7, 96 23.5 instead of 24.5).  Units that are not alike need smaller workgroups (steps of pieces and single tokens: 45 us instead of 53).
+    if (p.subs > 1 || max_q <= 16 / G) {
+        if (units <= cus && (8 * units >= 7ll * cus || most <= 8)) p.waves = 16;
+        else if (units <= 2ll * cus && 8 * units >= 14ll * cus) p.waves = 8;
+        if (p.waves > 4) return p;
+    }
+    // as many workgroups as the chip holds, four to a compute unit; up to twice as many while each has 16 pages, since tiles differ
     long long splits = 1;
     if (units > 0) {
         splits = wgs / units;
@@ -760,7 +780,16 @@ template <int D>
 int launch_sparse_of(const SparseArgs& a, const SparsePlan& p, const SparseWs& w, hipStream_t st)
 {
     const dim3 grid((unsigned)p.tiles * a.s.Hkv * p.subs * p.splits);
-    hipLaunchKernelGGL((sparse_kernel<D>), grid, dim3(256), 4u * p.nt * a.n_blocks, st, a, p, w);
+    const unsigned lds = sparse_stage(D, p.waves) + 4u * p.nt * a.n_blocks;
+    if (p.waves == 16) {
+        static unsigned long long done = 0;
+        if (!ensure_dynamic_lds((const void*)sparse_kernel<D, 16>, sparse_stage(D, 16) + 4 * kEntries, done)) return -1;
+        hipLaunchKernelGGL((sparse_kernel<D, 16>), grid, dim3(1024), lds, st, a, p, w);
+    } else if (p.waves == 8) {
+        static unsigned long long done = 0;
+        if (!ensure_dynamic_lds((const void*)sparse_kernel<D, 8>, sparse_stage(D, 8) + 4 * kEntries, done)) return -1;
+        hipLaunchKernelGGL((sparse_kernel<D, 8>), grid, dim3(512), lds, st, a, p, w);
+    } else hipLaunchKernelGGL((sparse_kernel<D, 4>), grid, dim3(256), lds, st, a, p, w);
     if (hipGetLastError() != hipSuccess) return -1;
     if (p.splits > 1) {
         const int groups = 256 / (D / 4);

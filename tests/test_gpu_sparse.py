@@ -259,6 +259,16 @@ def test_few_and_many_rows(aq, n, T):
     run_sparse(aq, [n], [max(n, 1500)], 4, 1, 64, 3, seed=n, tail=1)
 
 
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("B,n", [(32, 1), (29, 1), (32, 4), (64, 1), (58, 2), (57, 4)])
+@pytest.mark.parametrize("n_blocks", [2, 90])
+def test_steps_that_fill_the_chip(aq, d, B, n, n_blocks):
+    """Single and drafted tokens, as many as workgroups of 16 or 8 waves for a unit have room: long lists of pages beside sequences of nothing, one key and less than their rows."""
+    kv = [0, 1, 12000, 127, 128, 129, 11777] + [n + 61 * b for b in range(B - 7)]
+    kv[9] = max(n - 1, 1)
+    run_sparse(aq, [n] * B, kv, 32, 8, d, n_blocks, seed=B + n, tail=0 if n > 1 else 3)
+
+
 def test_many_pages(aq):
     run_sparse(aq, [1, 5], [9000, 17001], 4, 1, 64, 300, seed=4)
     run_sparse(aq, [2], [140000], 2, 1, 64, 1024, seed=5)

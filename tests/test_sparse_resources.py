@@ -12,7 +12,7 @@ pytestmark = pytest.mark.skipif(shutil.which("hipcc") is None, reason="hipcc not
 
 @pytest.mark.parametrize("src,pattern,count,waves", [
     ("rope.hip", r"\drope_kernel", 4, 5), ("rope.hip", r"append_rope_kernel", 4, 5), ("sparse.hip", r"summarize_kernel", 2, 3), ("sparse.hip", r"select_kernel", 10, 4),
-    ("sparse.hip", r"\dsparse_kernel", 2, 4), ("sparse.hip", r"sparse_merge_kernel", 2, 5)])
+    ("sparse.hip", r"\dsparse_kernel", 6, 4), ("sparse.hip", r"sparse_merge_kernel", 2, 5)])
 def test_no_scratch_and_occupancy(src, pattern, count, waves):
     hit = {k: v for k, v in _resources(src).items() if re.search(pattern, k)}
     assert len(hit) == count, sorted(hit)
