@@ -298,11 +298,11 @@ __global__ __launch_bounds__(1024) void select_kernel(const SelectArgs a, int nt
                 if (own + 1 > a.n_blocks) hi = max(hi, own + 1 - a.last);
             }
             if (b < 0) continue;
-            constexpr int U = 4;                                  // sixteens of pages under way at once
+            constexpr int U = 2;                                  // sixteens of pages under way at once
             for (int j1 = (a.first & ~15) + 16 * wave; j1 < hi; j1 += 16 * U * waves) {
                 // (a lane asks for the id and the scale of a page of sixteen g, and hands them to the lanes that need them: the way to memory takes a load of one
                 // dword for sixteen pages as long as one of sixteen bytes)
-                const int mine = s.table[(size_t)b * s.max_pages + min(j1 + 16 * g * waves + cc, s.max_pages - 1)];
+                const int mine = s.table[(size_t)b * s.max_pages + min(j1 + 16 * (g % U) * waves + cc, s.max_pages - 1)];
                 const bool live = mine >= 0 && mine < s.num_pages;
                 const int page = live ? mine : 0;
                 float scale_mine = *reinterpret_cast<const float*>(a.summary + ((size_t)page * s.Hkv + h) * (D + kSummaryTail) + D);
@@ -804,7 +804,8 @@ template <int D, int GP>
 int launch_select_of(const SelectArgs& a, int nt, hipStream_t st)
 {
     const int tiles = (a.s.T + nt - 1) / nt;
-    // few workgroups: more waves each, for the way to memory; not more than there are sixteens of pages
+    // few workgroups: more waves each, for the way to memory; not more than there are sixteens of pages (8 workgroups, 938 pages: 11.9 us with 16 waves, 12.8 with 4; 464, up to 204
+    // pages: 7.4 with 8, 7.9 with 4; 7504, up to 470 pages: 71 with 4, 151 with 16)
     const unsigned wgs = (unsigned)tiles * a.s.Hkv;
     int waves = wgs <= 256 ? 16 : wgs <= 512 ? 8 : 4;
     while (waves > 4 && waves * 16 > a.s.max_pages) waves /= 2;
