@@ -18,8 +18,10 @@ typedef int intx4 __attribute__((ext_vector_type(4)));
 // where they fit).  With the largest |S| of a head in [2^(b-1), 2^b) the codes are S 2^-e, e = b - 7, rounded to nearest even, at most 127 in
 // magnitude, and the mean is code 2^(e-17).
 //
-// A wave takes a (page, head), whole: a lane has 32 channels of 16 (D = 64: 32) bytes' keys, eight (four) of them, and sums over lanes halve what a lane holds at every
-// step.
+// A wave takes a (page, head), whole: a key's 32 channels lie with one lane, 16 (D = 64: 32) keys side by side, eight (four) times over, all loads under way at once; sums over
+// lanes halve what a lane holds at every step.  A workgroup has four heads of its rows' pages: their parts of a page lie one after another.  Bound by memory for long
+// prompts (5 prompts, 100 916 rows, 8 heads of 128, 59 MB of K: 14.4 us, 4.1 TB/s with the launch), by launch and two trips to memory for a step of decodes (600 rows, 8 of
+// them complete a page: 3.9 us).
 __device__ __forceinline__ uint32_t other_of_8(uint32_t x) { return __builtin_amdgcn_update_dpp(0u, x, 0x128, 0xF, 0xF, true); }                 // of lane ^ 8: row_ror 8
 __device__ __forceinline__ uint32_t other_of_4(uint32_t x)
 {
@@ -231,7 +233,9 @@ __device__ inline void best_of(const uint32_t* key, int n, int m, int first, int
 }
 
 // 16 rows of the matrix instruction are the query heads of a kv head's group, padded to GP by heads that are there, for 16 / GP tokens, against 16 pages at a
-// time.  Scores stay in LDS; then a wave has a token.
+// time.  Scores stay in LDS; then a wave has a token.  What bounds it: one token over 938 pages, 32/8 heads of 128, 11.9 us, trips to memory that wait for each other
+// (lengths, page ids, means) and the search, whose steps are chains of counts over a wave; 32 tokens of 63 - 375 pages 9.9 us; 3751 tokens over up to 470 pages 68 us, vector
+// instructions for 41 % of it.
 template <int D, int GP>
 __global__ __launch_bounds__(1024) void select_kernel(const SelectArgs a, int nt /* tokens of a workgroup */, int tiles)
 {
@@ -298,7 +302,7 @@ __global__ __launch_bounds__(1024) void select_kernel(const SelectArgs a, int nt
                 if (own + 1 > a.n_blocks) hi = max(hi, own + 1 - a.last);
             }
             if (b < 0) continue;
-            constexpr int U = 2;                                  // sixteens of pages under way at once
+            constexpr int U = 2;                                  // sixteens of pages under way at once (the 3751 tokens: 68 us; with one 79, with four 71)
             for (int j1 = (a.first & ~15) + 16 * wave; j1 < hi; j1 += 16 * U * waves) {
                 // (a lane asks for the id and the scale of a page of sixteen g, and hands them to the lanes that need them: the way to memory takes a load of one
                 // dword for sixteen pages as long as one of sixteen bytes)
@@ -357,6 +361,7 @@ __global__ __launch_bounds__(1024) void select_kernel(const SelectArgs a, int nt
         if (m == 0) continue;
         const uint32_t* key = keys + i * S + a.first;
         out += a.first;
+        // (scores in registers: one token over 938 pages 12 us, 22 with all of them read from LDS for every count)
         if (n <= 64) best_of<1>(key, n, m, a.first, out, best[wave], which[wave]);
         else if (n <= 256) best_of<4>(key, n, m, a.first, out, best[wave], which[wave]);
         else if (n <= 512) best_of<8>(key, n, m, a.first, out, best[wave], which[wave]);
@@ -369,7 +374,18 @@ __global__ __launch_bounds__(1024) void select_kernel(const SelectArgs a, int nt
 constexpr int kEntries = 2048;        // (token, page)s of a workgroup at most
 
 // 16 rows: the G query heads of a kv head for nt tokens (rows = token * G + head of the group), or 16 of more heads for one token.  Their pages are taken together, each
-// once, whichever of the tokens asked for it; split over `splits` workgroups where there are few rows.
+// once, whichever of the tokens asked for it; split over `splits` workgroups, or over groups of four waves of one workgroup, where there are few rows.
+//
+// Scores are computed transposed, S^T = K Q^T, so that a lane has one row, its maximum and sum are the lane's, and P^T is what O^T += V^T P^T takes.  K goes from memory into
+// registers, is unpacked (exact in fp16) and multiplied; V goes through LDS, written key by key and read transposed.  A wave has 32 keys of a page, four waves a page, and the next
+// page is on its way while one is worked on.  Q is exact in fp16 by a power of two per row; the probabilities are rounded to fp16, by a relative 2^-12 down to 2^-25 of
+// a row's largest, because that is the product's type; scores, sums and O are fp32.
+//
+// What bounds it.  One token, 32 pages, 32/8 heads of 128: 7.6 us and 4.8 to join, trips to memory one after another (choice, lengths, page ids, page).  32 tokens of 32 pages each
+// (157 MB): 36 us, 4.3 TB/s, from memory.  Pieces of three prompts, 3751 tokens of 24 pages each, 196 GFLOP: 1.08 ms, the vector instructions: they are busy for 82 % of
+// the time (matrix instructions 20 %), 245 for a wave's 32 keys, of which unpacking K and V, a conversion and a multiplication for two values, is 130; a wave's 16 rows cost as much with all
+// four tokens in a page as with one (four tokens visit 66 pages of 96 asked for).  Two sixteens of rows to a wave share the unpacking but leave three waves to a SIMD: 1.13 ms; four
+// and two: 1.17; rows of 16 or 32 tokens gathered page by page, P through LDS: 1.20 and 1.35; waves that score and waves that add: 1.22.
 struct SparsePlan { int nt, subs, tiles, splits, waves; };
 constexpr int sparse_stage(int D, int waves) { return waves * 32 * (2 * D + 32); }        // bytes of LDS beside the list of pages
 struct SparseWs { float *part_o /* [unit][split][16][D] */, *part_ml /* [unit][split][16][2]: maximum, sum; a sum below 0: not a row of any sequence */; };
@@ -690,7 +706,8 @@ __global__ __launch_bounds__(64 * NW, 4) void sparse_kernel(const SparseArgs a, 
     }
 }
 
-// O and lse of rows whose pages were split: `per` groups of D / 4 threads share a row, so that its partial sums take one trip to memory.
+// O and lse of rows whose pages were split: `per` groups of D / 4 threads share a row, so that its partial sums take one trip to memory.  Bound by launch and that trip: 4.8 us for 32
+// rows of 32 pieces as for 7408 rows of four.
 template <int D>
 __global__ __launch_bounds__(256) void sparse_merge_kernel(const SparseArgs a, const SparsePlan p, const SparseWs ws, int per)
 {
