@@ -490,7 +490,7 @@ int attnqat_fwd_kv4_ragged(const void* q, int64_t q_token_stride, int64_t q_head
  *
  * attnqat_kv_cache_append_rope is attnqat_kv_cache_append with q and k turned on the way: row t of k is turned by positions[t * axes + a], rounded to bf16
  * and quantized into its slot (the bits of attnqat_rope_fwd followed by attnqat_kv_cache_append), v as there, and row t of q [T,Hq,d] goes
- * turned to q_out, also where its slot is outside the cache.  q_out may be q (the same pointer and strides).  Hq = 0: no q.
+ * turned to q_out, also where its slot is outside the cache.  q_out may be q (the same pointer and strides).  Hq = 0: no q.  T (Hq + 2 Hkv + 9) <= 2^30.
  */
 #define ATTNQAT_ROPE_PAIRED         0
 #define ATTNQAT_ROPE_HALVES         1

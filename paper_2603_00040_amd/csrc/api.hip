@@ -858,7 +858,7 @@ int attnqat_kv_cache_append_rope(const void* q, int64_t q_token_stride, int64_t 
 {
     AppendRopeArgs a{};
     if (Hq < 0) return ATTNQAT_EINVAL;
-    if ((long long)(T > 0 ? T : 0) * Hq > kMaxServeRows || Hq > 65535 || Hkv > 65535) return ATTNQAT_ESHAPE;
+    if (Hq > 65535 || Hkv > 65535 || (long long)T * (Hq + 2ll * Hkv + 9) > (1 << 30)) return ATTNQAT_ESHAPE;      // (four heads and 32 tokens or more to 256 of the 2^32 threads of a launch)
     int rc = rows_common(k, k_token_stride, k_head_stride, v, v_token_stride, v_head_stride, T, Hkv, d, dtype, cache, num_pages, slots, false, a.k, a.v);
     if (rc) return rc;
     RopeTable r;

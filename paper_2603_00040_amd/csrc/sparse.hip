@@ -14,8 +14,8 @@ namespace {
 typedef int intx4 __attribute__((ext_vector_type(4)));
 
 // ---------------------------------------------------------------------------------------------- means of the keys of a page
-// A cached value is a multiple of 2^-10 below 2^12, the sum S of a page's 128 a whole number of 2^-10 below 2^29: exact in int32, in any order (up to six in fp32,
-// where they fit).  With the largest |S| of a head in [2^(b-1), 2^b) the codes are S 2^-e, e = b - 7, rounded to nearest even, at most 127 in
+// A cached value is a multiple of 2^-10 below 2^12, the sum S of a page's 128 a whole number of 2^-10 below 2^29: exact in int32, in any order (four of them in
+// fp32, where six would fit).  With the largest |S| of a head in [2^(b-1), 2^b) the codes are S 2^-e, e = b - 7, rounded to nearest even, at most 127 in
 // magnitude, and the mean is code 2^(e-17).
 //
 // A wave takes a (page, head), whole: a key's 32 channels lie with one lane, 16 (D = 64: 32) keys side by side, eight (four) times over, all loads under way at once; sums over
@@ -89,7 +89,6 @@ __global__ __launch_bounds__(256) void summarize_kernel(const unsigned char* __r
             constexpr int N = D == 64 ? 1 : 2;                    // sums that a lane is left with: channels d ..
             if constexpr (D == 64) { AQ_HALVE(1, 2, other_of_2) d += (lane >> 1) & 1; }
 #undef AQ_HALVE
-            // (the exponent of the largest as a float, rounded towards zero: below 2^29 and a whole number)
             int most = abs(sum[0]);
             if (N == 2) most = max(most, abs(sum[1]));
             for (int w = 1; w < 64; w <<= 1) most = max(most, __shfl_xor(most, w));

@@ -68,6 +68,13 @@ def test_append(kw, code):
     assert _append(**kw) == code
 
 
+def test_append_of_more_rows_than_a_launch_has_threads_for():
+    """One head, T small enough for T Hkv <= 2^29: the limit stands between."""
+    most = (1 << 30) // 12
+    assert _append(T=most + 1, Hq=1, Hkv=1) == aq.ESHAPE
+    assert _append(T=most, Hq=1, Hkv=1, slots=None) == aq.EINVAL
+
+
 def test_append_without_rows():
     assert _append(T=0) == aq.OK and _append(T=0, k=None, v=None, q=None, qo=None, slots=None, pos=None) == aq.OK
 
