@@ -370,6 +370,7 @@ __global__ __launch_bounds__(1024) void select_kernel(const SelectArgs a, int nt
 }
 
 // ---------------------------------------------------------------------------------------------- attention
+constexpr float kNoScore = -0x1p126f; // the reference of a row that has none yet: finite, so that differences of two are, and no score lies as low
 constexpr int kEntries = 2048;        // (token, page)s of a workgroup at most
 
 // 16 rows: the G query heads of a kv head for nt tokens (rows = token * G + head of the group), or 16 of more heads for one token.  Their pages are taken together, each
@@ -468,15 +469,17 @@ struct PageWalk {
     }
     __device__ __forceinline__ Raw<D> raw(const unsigned char* part, uint32_t key) const
     {
+        uint32_t codes = this->codes, scales = this->scales;
+        asm("" : "+v"(codes), "+v"(scales));                      // (32 bits beside a scalar address; widened in front of the loop they would be added to it by vector instructions)
         Raw<D> r;
         if constexpr (D == 128) {
-            const uint4v c = *reinterpret_cast<const uint4v*>(part + key * (D / 2) + (size_t)codes);
+            const uint4v c = *reinterpret_cast<const uint4v*>(part + key * (D / 2) + codes);
             r.w[0] = c[0]; r.w[1] = c[1]; r.w[2] = c[2]; r.w[3] = c[3];
         } else {
-            const uint2v c = *reinterpret_cast<const uint2v*>(part + key * (D / 2) + (size_t)codes);
+            const uint2v c = *reinterpret_cast<const uint2v*>(part + key * (D / 2) + codes);
             r.w[0] = c[0]; r.w[1] = c[1];
         }
-        r.sc = *reinterpret_cast<const uint32_t*>(part + key * (D / 16) + (size_t)scales);
+        r.sc = *reinterpret_cast<const uint32_t*>(part + key * (D / 16) + scales);
         return r;
     }
     __device__ __forceinline__ void load(PageTile<D>& t, int i)
@@ -488,10 +491,12 @@ struct PageWalk {
         t.ent = (uint32_t)__builtin_amdgcn_readlane(ent_lane, at);
         t.end = live ? __builtin_amdgcn_readlane(end_lane, at) : -1;                       // (V, and K below, are zeros from here on)
         const unsigned char* part = cache + (size_t)(live ? page : 0) * s.Hkv * (2 * HALF);
+        const unsigned char* values = part + HALF;
+        asm("" : "+s"(values));                                   // (the distance is more than a load adds)
 #pragma unroll
         for (int blk = 0; blk < 2; ++blk) t.k[blk] = raw(part, 16 * blk);
 #pragma unroll
-        for (int blk = 0; blk < 2; ++blk) t.v[blk] = raw(part + HALF, 16 * blk);
+        for (int blk = 0; blk < 2; ++blk) t.v[blk] = raw(values, 16 * blk);
     }
 };
 
@@ -565,7 +570,8 @@ __global__ __launch_bounds__(64 * NW, 4) void sparse_kernel(const SparseArgs a, 
         if (uniform(seq[i]) >= 0) see_last = min(see_last, uniform(pos[i]));
 
     floatx4 o[NDT];
-    float m = -INFINITY, up_to = -INFINITY, l = 0.0f;
+    float m = kNoScore, up_to = -INFINITY, l = 0.0f;
+    uint32_t asked = 0;                                           // tokens that asked for any page
 #pragma unroll
     for (int dt = 0; dt < NDT; ++dt) o[dt] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
     const int group = wave >> 2;                                  // of four waves: pages group, group + NW / 4 ..
@@ -605,19 +611,24 @@ __global__ __launch_bounds__(64 * NW, 4) void sparse_kernel(const SparseArgs a, 
                     if (end < 0) t.k[blk].sc = 0;
                 }
             }
+            asked |= ent;
             floatx4 sc[2];
+            const half2v ks[2] = {scales_of<D>(t.k[0], g, true), scales_of<D>(t.k[1], g, true)};
 #pragma unroll
             for (int blk = 0; blk < 2; ++blk) {
-                const half2v ks = scales_of<D>(t.k[blk], g, true);
                 sc[blk] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-                for (int j = 0; j < NS; ++j) sc[blk] = __builtin_amdgcn_mfma_f32_16x16x32_f16(values8<D>(t.k[blk], ks, j), qreg[j], sc[blk], 0, 0, 0);
+                for (int j = 0; j < NS; ++j) sc[blk] = __builtin_amdgcn_mfma_f32_16x16x32_f16(values8<D>(t.k[blk], ks[blk], j), qreg[j], sc[blk], 0, 0, 0);
             }
             // V through LDS: written key by key, read back with four keys of one d in a lane
             __builtin_amdgcn_wave_barrier();
             half2v vs[2] = {scales_of<D>(t.v[0], g, true), scales_of<D>(t.v[1], g, true)};
-            const float any_nan = __builtin_amdgcn_fdot2(vs[0], vs[1], 0.0f, false);       // (scales are NaN or finite)
-            if (__builtin_amdgcn_ballot_w64(any_nan != any_nan) != 0) nan_of_v<D>(vs, o, member ? k_last - kt + 1 : 0);
+            // (scales are NaN or finite.  Rows that do not ask for the page: another sequence's keys may be NaN)
+            const float any_nan = __builtin_amdgcn_fdot2(vs[0], vs[1], __builtin_amdgcn_fdot2(ks[0], ks[1], 0.0f, false), false);
+            if (__builtin_amdgcn_ballot_w64(any_nan != any_nan) != 0) {
+                nan_of_v<D>(vs, o, member ? k_last - kt + 1 : 0);
+                if (!member) sc[0] = sc[1] = floatx4{-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+            }
 #pragma unroll
             for (int blk = 0; blk < 2; ++blk)
 #pragma unroll
@@ -629,32 +640,30 @@ __global__ __launch_bounds__(64 * NW, 4) void sparse_kernel(const SparseArgs a, 
                 for (int j = 0; j < 8; ++j)
                     if (kt + 16 * (j >> 2) + 4 * g + (j & 3) > k_last) sc[j >> 2][j & 3] = -INFINITY;
             }
-            float mx = max_nc(max_nc(max_nc(sc[0][0], sc[0][1]), max_nc(sc[0][2], sc[0][3])), max_nc(max_nc(sc[1][0], sc[1][1]), max_nc(sc[1][2], sc[1][3])));
-            mx = lanes_max<16, 32>(mx);
+            float mx = max_nc(max_nc(sc[0][0], sc[0][1]), sc[0][2]);                       // (chains of three)
+            mx = max_nc(max_nc(mx, sc[0][3]), sc[1][0]);
+            mx = max_nc(max_nc(mx, sc[1][1]), sc[1][2]);
+            mx = max_nc(mx, sc[1][3]);
+            mx = xor_tree<16, 32>(mx, [](float a, float b) __attribute__((always_inline)) { return max_raw(a, b); });
             mx = member ? mx : -INFINITY;
             if (__builtin_amdgcn_ballot_w64(mx > up_to) != 0) {
-                const float m_new = fmaxf(m, fmaf(mx, c_row, -kTop)), alpha = __builtin_amdgcn_exp2f(m - (m_new == -INFINITY ? 0.0f : m_new));
+                const float m_new = fmaxf(m, fmaf(mx, c_row, -kTop)), alpha = __builtin_amdgcn_exp2f(m - m_new);
                 m = m_new;
                 up_to = score_up_to(m_new, c_row);
                 l *= alpha;
 #pragma unroll
                 for (int dt = 0; dt < NDT; ++dt) o[dt] *= alpha;
             }
-            const float m_at = m == -INFINITY ? 0.0f : m;
-            float add = 0.0f;
+            const float m_at = member ? m : INFINITY;             // (rows that do not ask for the page: probabilities of 0)
+            float add;
             half8 pt;
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
                 const float x = __builtin_amdgcn_exp2f(fmaf(sc[j >> 2][j & 3], c_row, -m_at));
-                add += x;
+                add = j == 0 ? x : add + x;
                 pt[j] = (half_t)x;
             }
-            // (rows that do not ask for the page take nothing of it, whatever their scores are: another sequence's keys may be NaN)
-            l += member ? add : 0.0f;
-            uint4v pw = __builtin_bit_cast(uint4v, pt);
-#pragma unroll
-            for (int j = 0; j < 4; ++j) pw[j] = member ? pw[j] : 0u;
-            pt = __builtin_bit_cast(half8, pw);
+            l += add;
 #pragma unroll
             for (int dt = 0; dt < NDT; ++dt) {
                 const uint2v u = lds_read_tr16_at(tr_base + 32 * dt), w = lds_read_tr16_at(tr_base + 32 * dt + 16 * RS);
@@ -664,6 +673,12 @@ __global__ __launch_bounds__(64 * NW, 4) void sparse_kernel(const SparseArgs a, 
         }
     }
 
+    // (a row that asked for nothing has nothing, whatever its query was)
+    if ((asked & row_bit) == 0) {
+        l = 0.0f;
+#pragma unroll
+        for (int dt = 0; dt < NDT; ++dt) o[dt] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
+    }
     // the waves' sums, in units of their common maximum
     constexpr int SS = D + 4;                                     // floats per row of the sums (16 rows are written side by side)
     static_assert(NW * 16 * SS * 4 <= kStage);
