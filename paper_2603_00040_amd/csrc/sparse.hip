@@ -382,10 +382,11 @@ constexpr int kEntries = 2048;        // (token, page)s of a workgroup at most
 // a row's largest, because that is the product's type; scores, sums and O are fp32.
 //
 // What bounds it.  One token, 32 pages, 32/8 heads of 128: 7.6 us and 4.8 to join, trips to memory one after another (choice, lengths, page ids, page).  32 tokens of 32 pages each
-// (157 MB): 36 us, 4.3 TB/s, from memory.  Pieces of three prompts, 3751 tokens of 24 pages each, 196 GFLOP: 1.08 ms, the vector instructions: they are busy for 82 % of
-// the time (matrix instructions 20 %), 245 for a wave's 32 keys, of which unpacking K and V, a conversion and a multiplication for two values, is 130; a wave's 16 rows cost as much with all
-// four tokens in a page as with one (four tokens visit 66 pages of 96 asked for).  Two sixteens of rows to a wave share the unpacking but leave three waves to a SIMD: 1.13 ms; four
-// and two: 1.17; rows of 16 or 32 tokens gathered page by page, P through LDS: 1.20 and 1.35; waves that score and waves that add: 1.22.
+// (157 MB): 36 us, 4.3 TB/s, from memory.  Pieces of three prompts, 3751 tokens of 24 pages each, 196 GFLOP: 1.04 ms, the vector instructions: they issue for 80 % of the time
+// (exponentials four times as long; matrix instructions 21 %, LDS 37 %), 226 for a wave's 32 keys, of which unpacking K and V, a conversion and a multiplication for two values,
+// is 136; a wave's 16 rows cost as much with all four tokens in a page as with one (four tokens visit 66 pages where they asked for 96).  Two sixteens of rows to a wave share the
+// unpacking but leave three waves to a SIMD: 5 % slower; four and two: 8 %; rows of 16 or 32 tokens gathered page by page, P through LDS: 6 and 19 %; waves that score and waves
+// that add, a barrier between them: 13 %.
 struct SparsePlan { int nt, subs, tiles, splits, waves; };
 constexpr int sparse_stage(int D, int waves) { return waves * 32 * (2 * D + 32); }        // bytes of LDS beside the list of pages
 struct SparseWs { float *part_o /* [unit][split][16][D] */, *part_ml /* [unit][split][16][2]: maximum, sum; a sum below 0: not a row of any sequence */; };
@@ -446,17 +447,18 @@ __device__ inline int pages_of_tokens(const StepArgs& s, const int* __restrict__
 
 // Those pages, from the first of `cnt` on: what a wave has of one, 32 keys of K and V, and the lists behind it, 64 entries at a time in the lanes.  Addresses are a
 // page's, in scalar registers, and a lane's offsets, made once.
-template <int D> struct PageTile { Raw<D> k[2], v[2]; uint32_t ent; int end; };
+template <int D> struct PageTile { Raw<D> k[2], v[2]; uint32_t ent; int end, all; };
 template <int D>
 struct PageWalk {
     const StepArgs& s; const unsigned char* cache /* of the head */; const uint32_t* ents; const int *seq, *pos; int cnt;
     uint32_t codes, scales;           // this lane's offsets in a part of a page's head
-    int ent_lane, id_lane, end_lane, id_end;                      // of entry id_end - 64 + lane: itself, its page, the last key that any of its tokens sees
+    int ent_lane, id_lane, end_lane, all_lane, id_end;            // of entry id_end - 64 + lane: itself, its page, the last key that any of its tokens sees, and that all of them see
     __device__ __forceinline__ void ids(int i0)
     {
         ent_lane = (int)ents[min(i0 + (int)(threadIdx.x & 63), cnt - 1)];
         const int last = 15 - __builtin_clz((uint32_t)ent_lane), b = seq[last];            // (tokens of one sequence follow each other: the last sees most)
         end_lane = pos[last];
+        all_lane = pos[__builtin_ctz((uint32_t)ent_lane >> 16)];
         id_lane = s.table[(size_t)b * s.max_pages + (ent_lane & 0xFFFF)];
         asm volatile("" : "+v"(id_lane));                         // (waited for here and not at every use)
         id_end = i0 + 64;
@@ -489,6 +491,7 @@ struct PageWalk {
         const int at = i - (id_end - 64), page = __builtin_amdgcn_readlane(id_lane, at);
         const bool live = page >= 0 && page < s.num_pages;
         t.ent = (uint32_t)__builtin_amdgcn_readlane(ent_lane, at);
+        t.all = __builtin_amdgcn_readlane(all_lane, at);
         t.end = live ? __builtin_amdgcn_readlane(end_lane, at) : -1;                       // (V, and K below, are zeros from here on)
         const unsigned char* part = cache + (size_t)(live ? page : 0) * s.Hkv * (2 * HALF);
         const unsigned char* values = part + HALF;
@@ -565,10 +568,6 @@ __global__ __launch_bounds__(64 * NW, 4) void sparse_kernel(const SparseArgs a, 
 
     const int k_last = pos[tok];
     const uint32_t row_bit = 1u << (16 + tok);
-    int see_last = 0x7FFFFFFF;                                    // the last key that every token sees
-    for (int i = 0; i < p.nt; ++i)
-        if (uniform(seq[i]) >= 0) see_last = min(see_last, uniform(pos[i]));
-
     floatx4 o[NDT];
     float m = kNoScore, up_to = -INFINITY, l = 0.0f;
     uint32_t asked = 0;                                           // tokens that asked for any page
@@ -602,7 +601,7 @@ __global__ __launch_bounds__(64 * NW, 4) void sparse_kernel(const SparseArgs a, 
         }
         for (int i = group; i < cnt; i += NW / 4) {
             const uint32_t ent = t.ent;
-            const int kt = (int)(ent & 0xFFFFu) * 128 + 32 * (wave & 3), end = t.end;
+            const int kt = (int)(ent & 0xFFFFu) * 128 + 32 * (wave & 3), end = t.end, all = t.all;
             const bool member = (ent & row_bit) != 0;
             if (kt + 31 > end) {                                  // behind a sequence's end there may be anything, and a page outside the cache reads as zeros
 #pragma unroll
@@ -635,7 +634,7 @@ __global__ __launch_bounds__(64 * NW, 4) void sparse_kernel(const SparseArgs a, 
                 for (int j = 0; j < NS; ++j) *reinterpret_cast<half8*>(stg + (16 * blk + cc) * RS + (D / 2) * g + 16 * (j ^ ((cc >> 2) & 1))) = values8<D>(t.v[blk], vs[blk], j);
             __builtin_amdgcn_wave_barrier();
             walk.load(t, min(i + NW / 4, cnt - 1));
-            if (kt + 31 > see_last) {
+            if (kt + 31 > all) {
 #pragma unroll
                 for (int j = 0; j < 8; ++j)
                     if (kt + 16 * (j >> 2) + 4 * g + (j & 3) > k_last) sc[j >> 2][j & 3] = -INFINITY;
