@@ -169,6 +169,48 @@ def test_another_stream_and_a_graph(aq):
         assert all(torch.equal(a, b) for a, b in zip(out, want))
 
 
+@pytest.mark.parametrize("d,dims,layout", [(128, (44, 42, 42), "paired"), (64, (64,), "halves")])
+def test_training_step(aq, d, dims, layout):
+    """Q and K of one projection turned, attention and its gradient, and from there to the projection's gradient; then the same in a captured graph, the inputs new at every replay."""
+    rng = np.random.default_rng(8)
+    B, L, Hq, Hkv = 2, 200, 4, 2
+    rope, freqs, axis = table(aq, dims, layout)
+    pos = grid(1, L, len(dims), rng, 40)[0]
+    pd = i32(pos)
+    qkv, do = S.bf16(rng.standard_normal((B, L, Hq + 2 * Hkv, d))).cuda(), S.bf16(rng.standard_normal((B, Hq, L, d))).cuda()
+    heads = lambda t, a, n: t[:, :, a:a + n].transpose(1, 2)  # noqa: E731
+    kept = {}
+
+    def step(grad):
+        q, k = aq.attnqat_rope_fwd(heads(qkv, 0, Hq), heads(qkv, Hq, Hkv), pd, rope)
+        v = heads(qkv, Hq + Hkv, Hkv).contiguous()
+        o, lse, o_hp = aq.attnqat_fwd(q, k, v, True)
+        dq, dk, dv = aq.attnqat_bwd(q, k, v, do, lse, o_hp, True)
+        aq.attnqat_rope_bwd(dq, dk, pd, rope, out=(heads(grad, 0, Hq), heads(grad, Hq, Hkv)))
+        heads(grad, Hq + Hkv, Hkv).copy_(dv)
+        kept.update(q=q, k=k, dq=dq, dk=dk, dv=dv, o=o)
+
+    grad = torch.full_like(qkv, 9.0)
+    step(grad)
+    rows = lambda t: t.transpose(1, 2)  # noqa: E731
+    for b in range(B):
+        check(rows(kept["q"])[b], qkv[b, :, :Hq], pos, freqs, axis, layout)
+        check(rows(kept["k"])[b], qkv[b, :, Hq:Hq + Hkv], pos, freqs, axis, layout)
+        check(grad[b, :, :Hq], rows(kept["dq"])[b], pos, freqs, axis, layout, -1.0)
+        check(grad[b, :, Hq:Hq + Hkv], rows(kept["dk"])[b], pos, freqs, axis, layout, -1.0)
+    assert torch.equal(grad[:, :, Hq + Hkv:], rows(kept["dv"]))
+    graph, out = torch.cuda.CUDAGraph(), torch.full_like(qkv, 9.0)
+    with torch.cuda.graph(graph):
+        step(out)
+    for i in range(4):
+        qkv.mul_(0.875)
+        pd.add_(i)
+        step(grad)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, grad), i
+
+
 def test_nothing_to_do(aq):
     rope, _, _ = table(aq, (64,), "paired")
     q = torch.zeros((2, 3, 0, 64), dtype=torch.bfloat16, device="cuda")
