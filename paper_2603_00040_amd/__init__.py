@@ -604,7 +604,7 @@ def attnqat_kv_select(q, cu_q, summary, num_pages: int, page_table, kv_lens, Hkv
                        ("summary", summary, (summary.numel(),), _U8)], [("q", q, shape)])
     _summary_pages(summary, num_pages, Hkv, d)
     rc = (_lib or lib()).attnqat_kv_select(q.data_ptr(), qt, qh, cu_q.data_ptr(), T, max(T, 1) if max_q is None else _within_int(max_q), B, Hq, Hkv, d, BF16, summary.data_ptr(),
-                                           num_pages, page_table.data_ptr(), most, kv_lens.data_ptr(), n_blocks, first, last, out.data_ptr(), _stream_on(dev))
+                                           num_pages, page_table.data_ptr(), most, kv_lens.data_ptr(), n_blocks, _within_int(first), _within_int(last), out.data_ptr(), _stream_on(dev))
     if rc:
         _check(rc)
     return out

@@ -584,7 +584,7 @@ def test_binding_refuses(aq):
     blocks = aq.attnqat_kv_select(**good)
     for kw in (dict(q=good["q"].float()), dict(q=good["q"].transpose(1, 2)), dict(q=q), dict(cu_q=i32([0, 1])), dict(kv_lens=good["kv_lens"].long()), dict(page_table=good["page_table"][:1]),
                dict(summary=summary[:-1]), dict(summary=summary.view(torch.int8)), dict(num_pages=num + 1), dict(num_pages=0), dict(Hkv=3), dict(n_blocks=0), dict(n_blocks=1025), dict(first=3),
-               dict(last=0), dict(first=-1), dict(out=blocks[:2]), dict(out=blocks.long()), dict(max_q=0)):
+               dict(last=0), dict(first=-1), dict(first=1 << 32), dict(last=(1 << 32) + 1), dict(out=blocks[:2]), dict(out=blocks.long()), dict(max_q=0)):
         with pytest.raises(aq.AttnQatError):
             aq.attnqat_kv_select(**{**good, **kw})
     good = dict(q=good["q"], cu_q=good["cu_q"], cache=dev(cache.reshape(-1)), num_pages=num, page_table=good["page_table"], kv_lens=good["kv_lens"], Hkv=2, blocks=blocks)
