@@ -134,33 +134,57 @@ __device__ inline void find_tokens(const StepArgs& a, int t0, int nt, int (&seq)
 __device__ inline uint32_t ordered(float x) { const uint32_t u = __float_as_uint(x); return (u >> 31) ? ~u : (u | 0x80000000u); }
 
 // The limit that the m best of some scores lie at or above, of which `top` is the largest and count(x) says how many are x or more (x > 0).  It lies not far below the largest
-// (scores are floats: half of it is 2^23 away): steps down from that double until there are m scores, and the last step is halved until a limit has exactly m at or above it,
-// or is the m-th largest itself, which others equal: then ties of those are taken.
+// (scores are floats: half of it is 2^23 away): steps down from that double until there are m scores, and the last step is quartered until a limit has exactly m at or above it,
+// or is the m-th largest itself, which others equal: then ties of those are taken.  SIDE: two or three limits are counted side by side, since a count waits for the one before
+// (the 3751 tokens below 70 us without, 67 with; where a count is many instructions, registers run out).
 struct Limit { uint32_t at; int ties; };
-template <class Count>
+template <bool SIDE, class Count>
 __device__ __forceinline__ Limit limit_of(uint32_t top, int n, int m, const Count& count)
 {
     // at: at least m scores; over: fewer (behind the largest none; 2^32 is 0 here)
     uint32_t at = 1, over = top + 1;
     int c = n;
-    for (uint32_t step = 1u << 22; step < top; step <<= 1) {
-        c = count(top - step);
-        if (c >= m) { at = top - step; break; }
-        over = top - step;
-        if (step >> 31) break;
+    for (uint32_t step = 1u << 22; step < top; step <<= SIDE ? 2 : 1) {
+        if constexpr (SIDE) {
+            const uint32_t far = step < top - step ? top - 2 * step : 1;
+            const int near = count(top - step), x = count(far);
+            if (near >= m) { at = top - step; c = near; break; }
+            over = top - step;
+            if (x >= m) { at = far; c = x; break; }
+            over = far;
+        } else {
+            const int x = count(top - step);
+            if (x >= m) { at = top - step; c = x; break; }
+            over = top - step;
+        }
+        if (step >> 30) break;
     }
-    if (c < m) c = n;                                             // (at = 1)
     while (c != m && over - at > 1) {
-        const uint32_t mid = at + (over - at) / 2;
-        const int x = count(mid);
-        if (x >= m) { at = mid; c = x; } else over = mid;
+        const uint32_t w = over - at, a2 = at + w / 2;
+        if constexpr (!SIDE) {
+            const int x = count(a2);
+            if (x >= m) { at = a2; c = x; } else over = a2;
+            continue;
+        }
+        const uint32_t a1 = at + w / 4, a3 = a2 + w / 4;
+        const int c1 = count(a1), c2 = count(a2), c3 = count(a3);
+        if (c3 >= m) { at = a3; c = c3; }
+        else if (c2 >= m) { at = a2; c = c2; over = a3; }
+        else if (c1 >= m) { at = a1; c = c1; over = a2; }
+        else over = a1;
     }
     return Limit{at, c == m ? n : m - (at == top ? 0 : count(at + 1))};
 }
 __device__ inline uint32_t wave_max(uint32_t x)
 {
-    for (int w = 1; w < 64; w <<= 1) x = max(x, (uint32_t)__shfl_xor((int)x, w));
-    return (uint32_t)uniform((int)x);
+    x = max(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x128, 0xF, 0xF, true));          // rows of 16, turned by 8, 4, 2, 1
+    x = max(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x124, 0xF, 0xF, true));
+    x = max(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x122, 0xF, 0xF, true));
+    x = max(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x121, 0xF, 0xF, true));
+    const auto a = __builtin_amdgcn_permlane16_swap(x, x, false, false);
+    x = max(a[0], a[1]);
+    const auto b = __builtin_amdgcn_permlane32_swap(x, x, false, false);
+    return (uint32_t)uniform((int)max(b[0], b[1]));
 }
 // Those of a wave's scores x (0: none) that are taken, to out as numbers, in the order of the lanes.
 __device__ __forceinline__ void emit(uint32_t x, int number, uint32_t at, int n, int& ties, int*& out)
@@ -193,7 +217,7 @@ __device__ inline void best_of(const uint32_t* key, int n, int m, int first, int
     const uint32_t top = wave_max(mine);
     if constexpr (R > 1) {
         if (m <= 64) {
-            const uint32_t from = limit_of(top, 64, m, [&](uint32_t x) __attribute__((always_inline)) { return (int)__builtin_popcountll(__builtin_amdgcn_ballot_w64(mine >= x)); }).at;
+            const uint32_t from = limit_of<true>(top, 64, m, [&](uint32_t x) __attribute__((always_inline)) { return (int)__builtin_popcountll(__builtin_amdgcn_ballot_w64(mine >= x)); }).at;
             int c = 0;
 #pragma unroll
             for (int r = 0; r < R; ++r) {
@@ -206,13 +230,13 @@ __device__ inline void best_of(const uint32_t* key, int n, int m, int first, int
                 __builtin_amdgcn_wave_barrier();
                 const uint32_t x = lane < c ? best[lane] : 0u;
                 Limit l{from, c};
-                if (c > m) l = limit_of(top, c, m, [&](uint32_t f) __attribute__((always_inline)) { return (int)__builtin_popcountll(__builtin_amdgcn_ballot_w64(x >= f)); });
+                if (c > m) l = limit_of<true>(top, c, m, [&](uint32_t f) __attribute__((always_inline)) { return (int)__builtin_popcountll(__builtin_amdgcn_ballot_w64(x >= f)); });
                 emit(x, first + which[lane], l.at, c, l.ties, out);
                 return;
             }
         }
     }
-    const Limit l = limit_of(top, n, m, [&](uint32_t from) __attribute__((always_inline)) {
+    const Limit l = limit_of<R == 1>(top, n, m, [&](uint32_t from) __attribute__((always_inline)) {
         int c = 0;
         if constexpr (R > 0) {
 #pragma unroll
@@ -232,9 +256,9 @@ __device__ inline void best_of(const uint32_t* key, int n, int m, int first, int
 }
 
 // 16 rows of the matrix instruction are the query heads of a kv head's group, padded to GP by heads that are there, for 16 / GP tokens, against 16 pages at a
-// time.  Scores stay in LDS; then a wave has a token.  What bounds it: one token over 938 pages, 32/8 heads of 128, 11.9 us, trips to memory that wait for each other
-// (lengths, page ids, means) and the search, whose steps are chains of counts over a wave; 32 tokens of 63 - 375 pages 9.9 us; 3751 tokens over up to 470 pages 68 us, vector
-// instructions for 41 % of it.
+// time.  Scores stay in LDS; then a wave has a token.  What bounds it: one token over 938 pages, 32/8 heads of 128, 11.6 us, trips to memory that wait for each other
+// (lengths, page ids, means) and the search, whose steps are chains of counts over a wave; 32 tokens of 63 - 375 pages 9.2 us; 3751 tokens over up to 470 pages 67 us, vector
+// instructions for 43 % of it.
 template <int D, int GP>
 __global__ __launch_bounds__(1024) void select_kernel(const SelectArgs a, int nt /* tokens of a workgroup */, int tiles)
 {
