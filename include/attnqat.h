@@ -537,7 +537,8 @@ int attnqat_kv_cache_append_rope(const void* q, int64_t q_token_stride, int64_t 
  * attnqat_fwd_kv4_sparse is attnqat_fwd_kv4_ragged (causal, no window) over those of a row's keys that lie in its pages: blocks as above, or
  * any other choice; entries that are negative or behind the row's own page are passed over, the same page twice counts once, and a row without a key gets o = 0,
  * lse = -inf.  Rows that stand side by side share what they read, so they cost less where their pages are the same.  A NaN of the cache reaches the rows that see
- * it and no others.  Sums are taken in an order that follows from the sizes alone: the same bits every time.  blocks, o and lse lie over nothing else.  Workspace: attnqat_kv4_sparse_workspace_bytes(), 16-byte aligned.
+ * it and no others.  Sums are taken in an order that follows from sizes, lengths and choice: the same bits every time.  blocks, o and lse lie over nothing else.
+ * Workspace: attnqat_kv4_sparse_workspace_bytes(), 16-byte aligned.
  * Both: T Hq <= 2^28, T Hkv ceil(Hq / Hkv / 16) <= 2^23.
  */
 size_t attnqat_kv_summary_page_bytes(int Hkv, int d);
