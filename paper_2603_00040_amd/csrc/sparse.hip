@@ -447,10 +447,13 @@ __device__ inline int pages_of_tokens(const StepArgs& s, const int* __restrict__
             for (int w = tid; w < words; w += 64 * NW) tab[w] = 0;
             __syncthreads();
         }
-        for (int x = i0 * n_blocks + tid; x < i1 * n_blocks; x += 64 * NW) {
-            const int i = x / n_blocks, blk = x == tid ? first : choice_of(s, blocks, n_blocks, h, t0, nt, x);
+        // (waves go round whole: a lane reads what the token's lane has, and one that has left a loop reads as 0)
+        for (int x0 = i0 * n_blocks + uniform(tid & ~63); x0 < i1 * n_blocks; x0 += 64 * NW) {
+            const int x = x0 + (tid & 63), i = min(x / n_blocks, 15);
             const int base = __shfl(base_lane, i), last = __shfl(pos_lane, i) >> 7;
-            if (base >= 0 && blk >= 0 && blk <= last) atomicOr(&tab[base + (blk >> 1)], 1u << (i + 16 * (blk & 1)));
+            if (x >= i1 * n_blocks || base < 0) continue;
+            const int blk = x == tid ? first : choice_of(s, blocks, n_blocks, h, t0, nt, x);
+            if (blk >= 0 && blk <= last) atomicOr(&tab[base + (blk >> 1)], 1u << (i + 16 * (blk & 1)));
         }
         __syncthreads();
         for (int w0 = 0; w0 < words; w0 += 64 * NW) {
