@@ -739,12 +739,6 @@ bool views_share(const View& a, const View& b, int64_t at, int level)
     return views_share(a, b, d, level + 1) || views_share(a, b, d - s, level + 1);
 }
 bool share(const View& a, const View& b) { return views_share(a, b, (int64_t)(b.p - a.p), 0); }
-bool same(const View& a, const View& b)
-{
-    if (a.p != b.p || a.levels != b.levels) return false;
-    for (int i = 0; i < a.levels; ++i) if (a.n[i] != b.n[i] || a.stride[i] != b.stride[i]) return false;
-    return true;
-}
 bool view_overlaps(const View& v, const void* p, size_t n) { return overlap((const void*)v.p, (size_t)view_extent(v, 0), p, n); }
 // No element twice.
 bool rows_apart(const View& v)
@@ -769,6 +763,10 @@ int rope_of(const attnqat_rope* rope, int d, bool back, RopeTable& r)
     for (int i = 0; i < 4; ++i) r.axis[i] = rope->axis[i];
     return ATTNQAT_OK;
 }
+
+// In place a thread reads what it writes, and nobody else does: the same element for every batch, head and token (strides of axes with one entry are 0 by now).
+bool in_place(const RopeTensor& t) { return t.src == t.dst && t.src_batch == t.dst_batch && t.src_head == t.dst_head && t.src_token == t.dst_token; }
+bool same_rows(const Rows& a, const Rows& b) { return a.p == b.p && a.token == b.token && a.head == b.head; }
 
 // A tensor [B, heads, L, d] of any strides (in elements): false where the kernels could not address it.
 bool tensor_of(const void* p, int64_t batch, int64_t head, int64_t token, int B, int heads, int L, int d, View& v)
@@ -806,7 +804,7 @@ int rope_common(const void* const (&src)[2], const int64_t (&ss)[2][3], void* co
     }
     for (int o = 0; o < n; ++o) {
         for (int i = 0; i < n; ++i)
-            if (share(out[o], in[i]) && !(o == i && same(out[o], in[i]))) return ATTNQAT_EINVAL;      // (in place: a thread reads what it writes)
+            if (share(out[o], in[i]) && !(o == i && in_place(a.t[i]))) return ATTNQAT_EINVAL;
         if (o == 1 && share(out[0], out[1])) return ATTNQAT_EINVAL;
     }
     a.B = B; a.L = L; a.positions = positions; a.pos_batch = (size_t)pos_batch;
@@ -869,7 +867,7 @@ int attnqat_kv_cache_append_rope(const void* q, int64_t q_token_stride, int64_t 
         if (!q || !q_out || !rows_of(q, q_token_stride, q_head_stride, T, Hq, d, false, a.q) || !rows_of(q_out, qo_token_stride, qo_head_stride, T, Hq, d, true, a.q_out)) return ATTNQAT_EINVAL;
         auto view = [&](const Rows& x, int heads) { return view_of(x.p, 1, 0, heads, (int64_t)x.head, T, (int64_t)x.token, d); };
         const View out = view(a.q_out, Hq), in = view(a.q, Hq);
-        if ((share(out, in) && !same(out, in)) || share(out, view(a.k, Hkv)) || share(out, view(a.v, Hkv))) return ATTNQAT_EINVAL;
+        if ((share(out, in) && !same_rows(a.q, a.q_out)) || share(out, view(a.k, Hkv)) || share(out, view(a.v, Hkv))) return ATTNQAT_EINVAL;
         if (view_overlaps(out, cache, (size_t)num_pages * nvfp4_page_bytes(Hkv, d)) || view_overlaps(out, slots, (size_t)T * 8) || view_overlaps(out, positions, (size_t)T * r.axes * 4))
             return ATTNQAT_EINVAL;
     }
