@@ -522,9 +522,9 @@ int attnqat_kv_cache_append_rope(const void* q, int64_t q_token_stride, int64_t 
  * attnqat_kv_summarize keeps the mean of the keys of every page.  For every row t whose slot is the last of a page (slots[t] % 128 == 127, inside the cache), once
  * its page is complete, so behind attnqat_kv_cache_append of the same slots: per kv head S_c = sum of the 128 keys' values of channel c; with
  * max |S_c| 2^10 in [2^(b-1), 2^b), e = b - 7 (-7 where all are 0): codes RNE(S_c 2^(10-e)), at most 127 in magnitude, and scale 2^(e-17), so that
- * code * scale is the mean of the keys.  Summary: num_pages * attnqat_kv_summary_page_bytes(Hkv, d) bytes, 16-byte aligned, page by page, per head
- * d int8 codes, the scale (fp32) and 12 bytes that nobody reads.  Pages that are not complete need no entry: they are never compared.  (Slots made by the
- * caller, page * 128 + 127, summarize the pages of a cache filled in another way.)
+ * code * scale is the mean of the keys.  Values of a block whose scale is NaN count as 0 here.  Summary: num_pages * attnqat_kv_summary_page_bytes(Hkv, d)
+ * bytes, 16-byte aligned, page by page, per head d int8 codes, the scale (fp32) and 12 bytes that nobody reads.  Pages that are not complete need no
+ * entry: they are never compared.  (Slots made by the caller, page * 128 + 127, summarize the pages of a cache filled in another way.)
  *
  * attnqat_kv_select chooses, for row t at position p of its sequence and every kv head, n_blocks of the pages 0 .. p / 128 (all of them where there are no more):
  * the first `first`, the last `last` (>= 1: the row's own page among them) and of the rest those of the highest score, the lower page where scores are

@@ -14,7 +14,7 @@ namespace {
 typedef int intx4 __attribute__((ext_vector_type(4)));
 
 // ---------------------------------------------------------------------------------------------- means of the keys of a page
-// A cached value is a multiple of 2^-10 below 2^12, the sum S of a page's 128 a whole number of 2^-10 below 2^29: exact in int32, in any order (four of them in
+// A cached value is a multiple of 2^-10 below 2^12 (one of a block whose scale is NaN counts as 0), the sum S of a page's 128 a whole number of 2^-10 below 2^29: exact in int32, in any order (four of them in
 // fp32, where six would fit).  With the largest |S| of a head in [2^(b-1), 2^b) the codes are S 2^-e, e = b - 7, rounded to nearest even, at most 127 in
 // magnitude, and the mean is code 2^(e-17).
 //
@@ -64,7 +64,8 @@ __global__ __launch_bounds__(256) void summarize_kernel(const unsigned char* __r
 #pragma unroll
                 for (int p = 4 * q; p < 4 * q + 4; ++p) {
                     typedef float float2v __attribute__((ext_vector_type(2)));
-                    const float s0 = __builtin_amdgcn_cvt_scalef32_f32_fp8(sc[p], 1024.0f, 0), s1 = __builtin_amdgcn_cvt_scalef32_f32_fp8(sc[p], 1024.0f, 1);
+                    auto scale_of = [](float s) __attribute__((always_inline)) { return s == s ? s : 0.0f; };                      // (a NaN has no whole number)
+                    const float s0 = scale_of(__builtin_amdgcn_cvt_scalef32_f32_fp8(sc[p], 1024.0f, 0)), s1 = scale_of(__builtin_amdgcn_cvt_scalef32_f32_fp8(sc[p], 1024.0f, 1));
 #pragma unroll
                     for (int w = 0; w < 4; ++w) {
                         const float s = w < 2 ? s0 : s1;
