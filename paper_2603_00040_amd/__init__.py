@@ -566,8 +566,8 @@ def kv_summary_page_bytes(Hkv: int, d: int) -> int:
 
 
 def _summary_pages(summary, pages, Hkv, d):
-    if summary.numel() < pages * Hkv * (d + 16):
-        raise AttnQatError(f"summary has no room for {pages} pages")
+    if pages < 1 or summary.numel() < pages * Hkv * (d + 16):
+        raise AttnQatError(f"summary has no room for {pages} pages (of 1 at least)")
 
 
 def attnqat_kv_summarize(cache, slots, summary, Hkv: int, d: int, num_pages=None):
