@@ -529,15 +529,18 @@ int attnqat_kv_cache_append_rope(const void* q, int64_t q_token_stride, int64_t 
  * attnqat_kv_select chooses, for row t at position p of its sequence and every kv head, n_blocks of the pages 0 .. p / 128 (all of them where there are no more):
  * the first `first`, the last `last` (>= 1: the row's own page among them) and of the rest those of the highest score, the lower page where scores are
  * equal.  The score of a page is the largest over the query heads of the group of (q8 . code), times the page's scale, q8 = RNE(q 2^(6-x)) limited to
- * +-127, 2^x <= largest |q| of the group < 2^(x+1): whole numbers and a power of two, so that the choice is the same however it is computed.
- * A page whose table entry lies outside the cache scores 0.  blocks int32 [T,Hkv,n_blocks]: page numbers of the sequence, ascending, -1 behind them; rows
- * behind cu_q[B] are left as they are.  q: the rows that attention takes (turned).  first + last <= n_blocks <= 1024.  max_q: the most rows of a
- * sequence, by which the work is laid out; less than the truth costs time and changes nothing.
+ * +-127, 2^x <= largest |q| of the group < 2^(x+1), x = -121 where it is less: whole numbers and a power of two, so that the choice is the same however it
+ * is computed.  (With a NaN or an infinity among the queries of a group it is some choice, the same every time.)  A page whose table entry lies outside
+ * the cache scores 0.  blocks int32 [T,Hkv,n_blocks]: page numbers of the sequence, ascending, -1 behind them; rows behind cu_q[B] are left as they are.
+ * q: the rows that attention takes (turned).  first + last <= n_blocks <= 1024.  max_q: the most rows of a sequence, by which the work is laid out;
+ * another number costs time (T in place of 1 for single tokens too) and the choice stays the same.
  *
  * attnqat_fwd_kv4_sparse is attnqat_fwd_kv4_ragged (causal, no window) over those of a row's keys that lie in its pages: blocks as above, or
  * any other choice; entries that are negative or behind the row's own page are passed over, the same page twice counts once, and a row without a key gets o = 0,
  * lse = -inf.  Rows that stand side by side share what they read, so they cost less where their pages are the same.  A NaN of the cache reaches the rows that see
- * it and no others.  Sums are taken in an order that follows from sizes, lengths and choice: the same bits every time.  blocks, o and lse lie over nothing else.
+ * it and no others.  Sums are taken in an order that follows from T, max_q, the heads, n_blocks, the lengths and the choices of rows that stand side by
+ * side: a call gives the same bits every time, while another max_q, or other neighbours of a row, may change the last bits of what it gives.  blocks, o and lse lie
+ * over nothing else.
  * Workspace: attnqat_kv4_sparse_workspace_bytes(), 16-byte aligned.
  * Both: T Hq <= 2^28, T Hkv ceil(Hq / Hkv / 16) <= 2^23.
  */

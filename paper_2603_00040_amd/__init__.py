@@ -586,8 +586,9 @@ def attnqat_kv_summarize(cache, slots, summary, Hkv: int, d: int, num_pages=None
 
 def attnqat_kv_select(q, cu_q, summary, num_pages: int, page_table, kv_lens, Hkv: int, n_blocks: int, first: int = 1, last: int = 1, max_q=None, out=None):
     """The pages that every row attends to: its sequence's ``first`` first ones, ``last`` last ones (its own among them), and those whose keys' mean
-    (``attnqat_kv_summarize``) gives the highest score, ``n_blocks`` at most.  q (turned), cu_q, page_table, kv_lens, max_q: as for attnqat_fwd_kv4_ragged.  Returns
-    int32 [T,Hkv,n_blocks]: page numbers of the sequence, ascending, -1 behind them; ``out``: that."""
+    (``attnqat_kv_summarize``) gives the highest score, ``n_blocks`` at most.  q (turned), cu_q, page_table, kv_lens: as for attnqat_fwd_kv4_ragged.  max_q: the most rows of a
+    sequence, by which the work is laid out (T where left out; the choice is the same with any).  A step of single tokens says 1.  Returns int32 [T,Hkv,n_blocks]: page numbers
+    of the sequence, ascending, -1 behind them; ``out``: that."""
     shape, dev, B = q.shape, q.get_device(), kv_lens.numel()
     if len(shape) != 3 or page_table.dim() != 2:
         raise AttnQatError("q must be [T,Hq,d] and page_table [B,max_pages]")
@@ -616,7 +617,11 @@ def kv4_sparse_workspace_bytes(T: int, Hq: int, Hkv: int, max_q: int, n_blocks: 
 
 def attnqat_fwd_kv4_sparse(q, cu_q, cache, num_pages, page_table, kv_lens, Hkv: int, blocks, max_q=None, scale=None, workspace=None, out=None):
     """attnqat_fwd_kv4_ragged (causal) over a choice of pages: row t of kv head h sees those of its keys that lie in pages ``blocks[t,h]`` of its sequence (int32
-    [T,Hkv,n_blocks], from attnqat_kv_select or any other; entries outside the row's pages are passed over).  Other arguments, and (o, lse), as there."""
+    [T,Hkv,n_blocks], from attnqat_kv_select or any other; entries outside the row's pages are passed over).  Other arguments, and (o, lse), as there.
+
+    max_q: the most rows of a sequence, the same number as for the workspace.  Where it is left out it is T, which is right and lays the work out for long pieces: rows of up to
+    16 * Hkv / Hq sequences share a workgroup, each going through the pages of all.  A step of single tokens says 1, one of drafted tokens their number.  The order of the sums
+    follows from it, and with that the last bits."""
     shape, dev, B = q.shape, q.get_device(), kv_lens.numel()
     if len(shape) != 3 or page_table.dim() != 2 or blocks.dim() != 3:
         raise AttnQatError("q must be [T,Hq,d], page_table [B,max_pages] and blocks [T,Hkv,n_blocks]")
