@@ -449,9 +449,10 @@ class Rope(ctypes.Structure):
 
 def rope_table(dims, theta: float = 10000.0, layout: str = "paired", freqs=None, axis=None) -> Rope:
     """A table of rotary positions, to be kept by the program.  ``dims``: how many values of a head turn with each axis, e.g. (128,) or, for time, height and
-    width, (44, 42, 42): pair i of an axis of n values turns by theta^(-2i/n) radians per position.  ``layout``: "paired" (elements 2i, 2i+1) or
-    "halves" (i and i + half the turned values).  ``freqs`` and ``axis``: radians per position and axis of every pair where they follow another rule
-    (then ``dims`` only says how many axes and values there are)."""
+    width, (44, 42, 42): pair i of an axis of n values turns by theta^(-2i/n) radians per position, from i = 0 in every axis, as video models have it.
+    ``layout``: "paired" (elements 2i, 2i+1) or "halves" (i and i + half the turned values).  ``freqs`` and ``axis``: radians per position and axis of every
+    pair where they follow another rule (of ``dims`` the number of axes and of values is left, and its sections where ``axis`` is not given).  A language model whose
+    axes share one ladder of frequencies over the head, cut into sections, has ``rope_table((32, 48, 48), layout="halves", freqs=[theta ** (-2.0 * i / 128) for i in range(64)])``."""
     dims = tuple(int(n) for n in dims)
     if layout not in ("paired", "halves"):
         raise AttnQatError("layout must be 'paired' or 'halves'")
