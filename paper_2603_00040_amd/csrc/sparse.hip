@@ -395,7 +395,7 @@ __global__ __launch_bounds__(1024) void select_kernel(const SelectArgs a, int nt
 }
 
 // ---------------------------------------------------------------------------------------------- attention
-constexpr float kNoScore = -0x1p126f; // the reference of a row that has none yet: finite, so that differences of two are, and no score lies as low
+constexpr float kNoScore = -0x1p126f; // the reference of a row that has none yet: finite, so that differences of two are, also of waves and pieces without a score; no score lies as low
 constexpr int kEntries = 2048;        // (token, page)s of a workgroup at most
 
 // 16 rows: the G query heads of a kv head for nt tokens (rows = token * G + head of the group), or 16 of more heads for one token.  Their pages are taken together, each
@@ -719,7 +719,7 @@ __global__ __launch_bounds__(64 * NW, 4) void sparse_kernel(const SparseArgs a, 
         for (int w = 1; w < NW; ++w) x = fmaxf(x, ml[0][w][row]);
         return x;
     };
-    const float top = largest(cc), f = __builtin_amdgcn_exp2f(m - (top == -INFINITY ? 0.0f : top));
+    const float top = largest(cc), f = __builtin_amdgcn_exp2f(m - top);
 #pragma unroll
     for (int dt = 0; dt < NDT; ++dt) *reinterpret_cast<floatx4*>(sums + (wave * 16 + cc) * SS + 16 * dt + 4 * g) = o[dt] * f;
     __syncthreads();
@@ -727,12 +727,12 @@ __global__ __launch_bounds__(64 * NW, 4) void sparse_kernel(const SparseArgs a, 
     for (int e = tid; e < rows * (D / 4); e += 64 * NW) {
         const int q = e / (D / 4), d = e % (D / 4) * 4, tk = p.subs > 1 ? 0 : q / G, hd = h * G + (p.subs > 1 ? 16 * sub + q : q % G);
         const bool on = seq[tk] >= 0;
-        const float tp = largest(q), at = tp == -INFINITY ? 0.0f : tp;
+        const float tp = largest(q);
         float lt = 0.0f;
         floatx4 v = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
         for (int x = 0; x < NW; ++x) {
-            lt += ml[1][x][q] * __builtin_amdgcn_exp2f(ml[0][x][q] - at);
+            lt += ml[1][x][q] * __builtin_amdgcn_exp2f(ml[0][x][q] - tp);
             v += *reinterpret_cast<const floatx4*>(sums + (x * 16 + q) * SS + d);
         }
         if (p.splits > 1) {
@@ -778,10 +778,10 @@ __global__ __launch_bounds__(256) void sparse_merge_kernel(const SparseArgs a, c
         float top = M;
 #pragma unroll
         for (int k = 0; k < K; ++k) { if (i0 + k * per >= p.splits) pm[k] = -INFINITY; top = fmaxf(top, pm[k]); }
-        const float at = top == -INFINITY ? 0.0f : top, al = __builtin_amdgcn_exp2f(M - at);
+        const float al = __builtin_amdgcn_exp2f(M - top);          // (every group has a piece: top is finite)
         M = top; l *= al; v *= al;
 #pragma unroll
-        for (int k = 0; k < K; ++k) { const float f = __builtin_amdgcn_exp2f(pm[k] - at); l = fmaf(pl[k], f, l); v += po[k] * f; }
+        for (int k = 0; k < K; ++k) { const float f = __builtin_amdgcn_exp2f(pm[k] - top); l = fmaf(pl[k], f, l); v += po[k] * f; }
     }
     if (per > 1) {
         *reinterpret_cast<floatx4*>(&acc[grp][d]) = v;
@@ -790,8 +790,7 @@ __global__ __launch_bounds__(256) void sparse_merge_kernel(const SparseArgs a, c
         if (grp % per != 0) return;
         M = -INFINITY; l = 0.0f; v = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
         for (int k = 0; k < per; ++k) M = fmaxf(M, ml[grp + k][0]);
-        const float at = M == -INFINITY ? 0.0f : M;
-        for (int k = 0; k < per; ++k) { const float f = __builtin_amdgcn_exp2f(ml[grp + k][0] - at); l = fmaf(ml[grp + k][1], f, l); v += *reinterpret_cast<const floatx4*>(&acc[grp + k][d]) * f; }
+        for (int k = 0; k < per; ++k) { const float f = __builtin_amdgcn_exp2f(ml[grp + k][0] - M); l = fmaf(ml[grp + k][1], f, l); v += *reinterpret_cast<const floatx4*>(&acc[grp + k][d]) * f; }
     }
     if (!on) return;
     v *= l != 0.0f ? 1.0f / l : 0.0f;
