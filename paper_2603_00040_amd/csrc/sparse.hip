@@ -20,7 +20,7 @@ typedef int intx4 __attribute__((ext_vector_type(4)));
 //
 // A wave takes a (page, head), whole: a key's 32 channels lie with one lane, 16 (D = 64: 32) keys side by side, eight (four) times over, all loads under way at once; sums over
 // lanes halve what a lane holds at every step.  A workgroup has four heads of its rows' pages: their parts of a page lie one after another.  Bound by memory for long
-// prompts (5 prompts, 100 916 rows, 8 heads of 128, 59 MB of K: 14.4 us, 4.1 TB/s with the launch), by launch and two trips to memory for a step of decodes (600 rows, 8 of
+// prompts (5 prompts, 100 916 rows, 8 heads of 128, 59 MB of K: 15.0 us, 4.0 TB/s with the launch), by launch and two trips to memory for a step of decodes (600 rows, 8 of
 // them complete a page: 3.9 us).
 __device__ __forceinline__ uint32_t other_of_8(uint32_t x) { return __builtin_amdgcn_update_dpp(0u, x, 0x128, 0xF, 0xF, true); }                 // of lane ^ 8: row_ror 8
 __device__ __forceinline__ uint32_t other_of_4(uint32_t x)
@@ -137,7 +137,7 @@ __device__ inline uint32_t ordered(float x) { const uint32_t u = __float_as_uint
 // The limit that the m best of some scores lie at or above, of which `top` is the largest and count(x) says how many are x or more (x > 0).  It lies not far below the largest
 // (scores are floats: half of it is 2^23 away): steps down from that double until there are m scores, and the last step is quartered until a limit has exactly m at or above it,
 // or is the m-th largest itself, which others equal: then ties of those are taken.  SIDE: two or three limits are counted side by side, since a count waits for the one before
-// (the 3751 tokens below 70 us without, 67 with; where a count is many instructions, registers run out).
+// (the 3751 tokens below 67.6 us without, 66 with; where a count is many instructions, registers run out).
 struct Limit { uint32_t at; int ties; };
 template <bool SIDE, class Count>
 __device__ __forceinline__ Limit limit_of(uint32_t top, int n, int m, const Count& count)
@@ -258,8 +258,8 @@ __device__ inline void best_of(const uint32_t* key, int n, int m, int first, int
 
 // 16 rows of the matrix instruction are the query heads of a kv head's group, padded to GP by heads that are there, for 16 / GP tokens, against 16 pages at a
 // time.  Scores stay in LDS; then a wave has a token.  What bounds it: one token over 938 pages, 32/8 heads of 128, 11.6 us, trips to memory that wait for each other
-// (lengths, page ids, means) and the search, whose steps are chains of counts over a wave; 32 tokens of 63 - 375 pages 9.2 us; 3751 tokens over up to 470 pages 67 us, vector
-// instructions for 43 % of it.
+// (lengths, page ids, means) and the search, whose steps are chains of counts over a wave; 32 tokens of 63 - 375 pages 9.2 us; 3751 tokens over up to 470 pages 66 us, vector
+// instructions for 33 % of it.
 template <int D, int GP>
 __global__ __launch_bounds__(1024) void select_kernel(const SelectArgs a, int nt /* tokens of a workgroup */, int tiles)
 {
@@ -326,7 +326,7 @@ __global__ __launch_bounds__(1024) void select_kernel(const SelectArgs a, int nt
                 if (own + 1 > a.n_blocks) hi = max(hi, own + 1 - a.last);
             }
             if (b < 0) continue;
-            constexpr int U = 2;                                  // sixteens of pages under way at once (the 3751 tokens: 68 us; with one 79, with four 71)
+            constexpr int U = 2;                                  // sixteens of pages under way at once (the 3751 tokens: 66 us; with one 79, with four 65, but 32 tokens 9.5 instead of 9.2)
             for (int j1 = (a.first & ~15) + 16 * wave; j1 < hi; j1 += 16 * U * waves) {
                 // (a lane asks for the id and the scale of a page of sixteen g, and hands them to the lanes that need them: the way to memory takes a load of one
                 // dword for sixteen pages as long as one of sixteen bytes)
@@ -385,7 +385,7 @@ __global__ __launch_bounds__(1024) void select_kernel(const SelectArgs a, int nt
         if (m == 0) continue;
         const uint32_t* key = keys + i * S + a.first;
         out += a.first;
-        // (scores in registers: one token over 938 pages 12 us, 22 with all of them read from LDS for every count)
+        // (scores in registers: one token over 938 pages 11.6 us, 23 with all of them read from LDS for every count; the 3751 tokens 66 and 78)
         if (n <= 64) best_of<1>(key, n, m, a.first, out, best[wave], which[wave]);
         else if (n <= 256) best_of<4>(key, n, m, a.first, out, best[wave], which[wave]);
         else if (n <= 512) best_of<8>(key, n, m, a.first, out, best[wave], which[wave]);
@@ -406,8 +406,8 @@ constexpr int kEntries = 2048;        // (token, page)s of a workgroup at most
 // page is on its way while one is worked on.  Q is exact in fp16 by a power of two per row; the probabilities are rounded to fp16, by a relative 2^-12 down to 2^-25 of
 // a row's largest, because that is the product's type; scores, sums and O are fp32.
 //
-// What bounds it.  One token, 32 pages, 32/8 heads of 128: 7.6 us and 4.8 to join, trips to memory one after another (choice, lengths, page ids, page).  32 tokens of 32 pages each
-// (157 MB): 36 us, 4.3 TB/s, from memory.  Pieces of three prompts, 3751 tokens of 24 pages each, 196 GFLOP: 1.04 ms, the vector instructions: they issue for 80 % of the time
+// What bounds it.  One token, 32 pages, 32/8 heads of 128: 7.5 us and 4.5 to join, trips to memory one after another (choice, lengths, page ids, page).  32 tokens of 32 pages each
+// (157 MB): 36 us, 4.3 TB/s, from memory.  Pieces of three prompts, 3751 tokens of 24 pages each, 196 GFLOP: 1.00 ms, the vector instructions: they issue for 81 % of the time
 // (exponentials four times as long; matrix instructions 21 %, LDS 37 %), 226 for a wave's 32 keys, of which unpacking K and V, a conversion and a multiplication for two values,
 // is 136; a wave's 16 rows cost as much with all four tokens in a page as with one (four tokens visit 66 pages where they asked for 96).  Two sixteens of rows to a wave share the
 // unpacking but leave three waves to a SIMD: 5 % slower; four and two: 8 %; rows of 16 or 32 tokens gathered page by page, P through LDS: 6 and 19 %; waves that score and waves
@@ -861,8 +861,8 @@ template <int D, int GP>
 int launch_select_of(const SelectArgs& a, int nt, hipStream_t st)
 {
     const int tiles = (a.s.T + nt - 1) / nt;
-    // few workgroups: more waves each, for the way to memory; not more than there are sixteens of pages (8 workgroups, 938 pages: 11.9 us with 16 waves, 12.8 with 4; 464, up to 204
-    // pages: 7.4 with 8, 7.9 with 4; 7504, up to 470 pages: 71 with 4, 151 with 16)
+    // few workgroups: more waves each, for the way to memory; not more than there are sixteens of pages (8 workgroups, 938 pages: 11.6 us with 16 waves, 13.6 with 4; 256, up to 375
+    // pages: 9.2 with 16, 10.1 with 4; 464, up to 204 pages: 7.2 with 8, 7.4 with 4; 7504, up to 470 pages: 66 with 4, 146 with 16)
     const unsigned wgs = (unsigned)tiles * a.s.Hkv;
     int waves = wgs <= 256 ? 16 : wgs <= 512 ? 8 : 4;
     while (waves > 4 && waves * 16 > a.s.max_pages) waves /= 2;
